@@ -71,7 +71,8 @@ typedef enum {
     SQN_ERR_UNSUPPORTED = 4     /* valid but not supported by this build        */
 } sqn_status;
 
-typedef enum { SQN_F32 = 0, SQN_F16 = 1 } sqn_dtype;
+/* SQN_BF16 (bfloat16) is taken by the calls on learned tables and layers. */
+typedef enum { SQN_F32 = 0, SQN_F16 = 1, SQN_BF16 = 2 } sqn_dtype;
 
 /* Opaque, library-owned device copy of the caches. */
 typedef struct sqn_caches sqn_caches;
@@ -365,6 +366,131 @@ size_t sqn_networks_device_bytes(const sqn_networks* nets);
 
 /* Free the networks; NULL is a no-op. */
 void sqn_destroy_networks(sqn_networks* nets);
+
+/* ---- learned tables and layers ---------------------------------------------
+ *
+ * Operators on what a program fits, updates and stores around the renderer:
+ * rows of a table fetched by index and the table's gradient, a layer's
+ * update orthogonalised, a layer held in 4-bit blocks and evaluated so.
+ * Every call is asynchronous on `stream`, allocates nothing, keeps nothing
+ * between calls and gives the same bits for the same arguments every time.
+ * Scratch is the caller's: the *_workspace functions say how many bytes
+ * (any alignment to 256 bytes; its contents need not be set and are left
+ * unspecified); it must stay valid until the stream has finished the call.
+ * Outputs must not overlap inputs except where stated. */
+
+/* A matrix in device memory: element (i, j) of `dtype` at data +
+ * (i row_stride + j) elements. */
+typedef struct {
+    void* data;
+    int64_t rows, cols;       /* 0 <= rows < 2^31, 1 <= cols <= 2^20           */
+    int64_t row_stride;       /* elements; >= cols for an output, >= 0 else    */
+    int32_t dtype;            /* sqn_dtype                                     */
+    int32_t reserved;         /* must be 0                                     */
+} sqn_matrix;
+
+typedef enum { SQN_I32 = 0, SQN_I64 = 1 } sqn_index_type;
+
+/* Rows of a table by index: out[t] = scale * table[ids[t]], the product in
+ * binary32 and rounded once to the table's dtype.  An index outside
+ * [0, table->rows) (a padding mark such as -1) gives a row of zeros.
+ *   ids:  device, n = out->rows indices of ids_type;
+ *   out:  [n][table->cols] of the table's dtype.
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
+sqn_status sqn_lookup(const sqn_matrix* table, const void* ids, int32_t ids_type, float scale,
+                      const sqn_matrix* out, void* stream);
+
+/* The gradient of sqn_lookup's table: with g[v] the sum of grad[t] over the t
+ * with ids[t] = v in binary32 (in an order that the indices alone fix),
+ *   table_grad[v] = scale * g[v]                       (accumulate = 0), or
+ *   table_grad[v] = table_grad[v] + scale * g[v]       (accumulate = 1; rows
+ *                   without an index are neither read nor written),
+ * rounded once to table_grad's dtype.  Indices outside [0, table_grad->rows)
+ * take part in nothing.
+ *   grad:       [n][cols], any dtype;  ids: n = grad->rows indices, n <= 2^30;
+ *   table_grad: [rows][cols], any dtype, rows >= 1;
+ *   workspace:  sqn_lookup_gradient_workspace(n, rows, cols) bytes.
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
+sqn_status sqn_lookup_gradient(const sqn_matrix* grad, const void* ids, int32_t ids_type, float scale,
+                               int32_t accumulate, const sqn_matrix* table_grad, void* workspace,
+                               size_t workspace_bytes, void* stream);
+size_t sqn_lookup_gradient_workspace(int64_t n_ids, int64_t rows, int64_t cols);
+
+/* A batch of matrices in device memory: element (b, i, j) at data +
+ * (b batch_stride + i row_stride + j col_stride) elements. */
+typedef struct {
+    void* data;
+    int32_t batch, rows, cols;   /* 0 <= batch <= 65535; 1 <= rows, cols <= 32768 */
+    int32_t dtype;               /* sqn_dtype                                     */
+    int64_t batch_stride, row_stride, col_stride;   /* >= 0; an output's elements */
+                                                    /* must lie apart             */
+} sqn_batch;
+
+/* Update matrices orthogonalised as the Muon optimiser does: for each matrix
+ * G of the batch
+ *   X <- G / (||G||_F + eps),
+ *   `steps` times  A = X X^T,  X <- a X + (b A + c A A) X,
+ * (on the transpose where G has more rows than columns, which is the same
+ * map), with (a, b, c) = coefficients: X's singular values go through
+ * s -> a s + b s^3 + c s^5 each step, near 1 in the end.  Sums are binary32.
+ * For a bfloat16 output the products take binary16 factors, the diagonals
+ * of A and b A + c A A kept apart in binary32 and X in 22 bits; for
+ * binary16 and binary32 outputs every factor has 22 bits.
+ *   coefficients: host, finite; refused where the steps could take a singular
+ *                 value past 2 or b s^2 + c s^4 past 16 in magnitude, the
+ *                 range the binary16 factors are scaled for;
+ *   eps:          finite, >= 0; a zero matrix stays zero (0 / 0 included);
+ *   steps:        0..64;
+ *   out:          the updates' batch, rows and cols; may be the updates' own
+ *                 memory if the layout is the same;
+ *   workspace:    sqn_orthogonalise_workspace bytes.
+ * A matrix with a NaN or an infinity comes out as NaN throughout; the others
+ * of the batch are not touched by it.
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
+sqn_status sqn_orthogonalise(const sqn_batch* updates, int32_t steps, const float coefficients[3], float eps,
+                             const sqn_batch* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t sqn_orthogonalise_workspace(int32_t batch, int32_t rows, int32_t cols, int32_t out_dtype);
+
+/* A matrix in 4-bit blocks (the OCP microscaling format MXFP4): each row is
+ * cut into blocks of 32 elements, the last one filled up with zeros; a block
+ * has one scale 2^(s - 127) with s its byte (E8M0) and 32 E2M1 elements
+ * (sign, magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6), two to a byte, the first in
+ * the low half.  Both arrays are contiguous. */
+typedef struct {
+    void* codes;              /* device, [rows][blocks][16] bytes, 16-byte aligned */
+    void* scales;             /* device, [rows][blocks] bytes                  */
+    int64_t rows, cols;       /* 0 <= rows < 2^31, 1 <= cols <= 2^20;          */
+                              /* blocks = ceil(cols / 32)                      */
+} sqn_quantised;
+
+/* x in 4-bit blocks: s - 127 = floor(log2 of the block's largest magnitude)
+ * - 2, at least -127; elements are x over the scale rounded to nearest, ties
+ * to the even code, magnitudes past 6 to 6.  A block that holds a NaN or an
+ * infinity gets s = 255 and stands for NaN throughout.
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
+sqn_status sqn_quantise(const sqn_matrix* x, const sqn_quantised* out, void* stream);
+
+/* The values that 4-bit blocks stand for, rounded once to out's dtype (exact
+ * in binary32 and bfloat16 down to their subnormals).
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
+sqn_status sqn_quantised_values(const sqn_quantised* x, const sqn_matrix* out, void* stream);
+
+/* A layer on 4-bit blocks: out = act(x w^T + bias), [points][units], with x
+ * [points][cols] and w [units][cols] in blocks, products and sums in
+ * binary32, rounded once to out's dtype; act is max(0, .) (a NaN stays) for
+ * relu = 1 and nothing for 0.
+ *   bias: device, binary32 [units], or NULL.
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_UNSUPPORTED (more than 2^23 tiles of
+ * 64 x 64 in out), SQN_ERR_DEVICE. */
+sqn_status sqn_quantised_product(const sqn_quantised* x, const sqn_quantised* w, const float* bias, int32_t relu,
+                                 const sqn_matrix* out, void* stream);
+
+/* sqn_quantise of x, then sqn_quantised_product of it: the same values.
+ *   workspace: sqn_quantised_layer_workspace(x->rows, x->cols) bytes.
+ * Errors: those of sqn_quantised_product. */
+sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, const float* bias, int32_t relu,
+                               const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t sqn_quantised_layer_workspace(int64_t rows, int64_t cols);
 
 /* Ray space of later renders with this handle.  ndc_near = 0 (the default):
  * world rays as above.  ndc_near > 0: forward-facing captures (the LLFF

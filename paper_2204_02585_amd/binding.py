@@ -16,13 +16,17 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libsqn.so")
 
 SQN_OK, SQN_ERR_INVALID_ARG, SQN_ERR_OUT_OF_MEMORY, SQN_ERR_DEVICE, SQN_ERR_UNSUPPORTED = range(5)
-SQN_F32, SQN_F16 = 0, 1
+SQN_F32, SQN_F16, SQN_BF16 = 0, 1, 2
+SQN_I32, SQN_I64 = 0, 1
 
 EXPORTS = ("sqn_create_caches", "sqn_create_linear_caches", "sqn_recreate_caches", "sqn_render", "sqn_render_stats",
            "sqn_set_lanes_per_ray", "sqn_tune_lanes_per_ray", "sqn_set_centre_block",
            "sqn_set_empty_space_skipping", "sqn_set_ndc", "sqn_cache_device_bytes",
            "sqn_destroy", "sqn_status_string", "sqn_last_error", "sqn_create_networks",
-           "sqn_generate_caches", "sqn_networks_device_bytes", "sqn_destroy_networks")
+           "sqn_generate_caches", "sqn_networks_device_bytes", "sqn_destroy_networks",
+           "sqn_lookup", "sqn_lookup_gradient", "sqn_lookup_gradient_workspace", "sqn_orthogonalise",
+           "sqn_orthogonalise_workspace", "sqn_quantise", "sqn_quantised_values", "sqn_quantised_product",
+           "sqn_quantised_layer", "sqn_quantised_layer_workspace")
 
 
 class CacheDesc(ctypes.Structure):
@@ -52,6 +56,22 @@ class Intrinsics(ctypes.Structure):
     _fields_ = [("fx", ctypes.c_float), ("fy", ctypes.c_float),
                 ("cx", ctypes.c_float), ("cy", ctypes.c_float),
                 ("width", ctypes.c_int32), ("height", ctypes.c_int32)]
+
+
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class Batch(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("batch_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("col_stride", ctypes.c_int64)]
+
+
+class QuantisedMatrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
 
 
 class SqnError(RuntimeError):
@@ -107,6 +127,21 @@ def _load() -> ctypes.CDLL:
     lib.sqn_cache_device_bytes.argtypes = [vp]
     lib.sqn_destroy.restype = None
     lib.sqn_destroy.argtypes = [vp]
+    i64, size = ctypes.c_int64, ctypes.c_size_t
+    mat, quant, batch = ctypes.POINTER(Matrix), ctypes.POINTER(QuantisedMatrix), ctypes.POINTER(Batch)
+    for name, result, args in (
+            ("sqn_lookup", ctypes.c_int, [mat, vp, i32, f32, mat, vp]),
+            ("sqn_lookup_gradient", ctypes.c_int, [mat, vp, i32, f32, i32, mat, vp, size, vp]),
+            ("sqn_lookup_gradient_workspace", size, [i64, i64, i64]),
+            ("sqn_orthogonalise", ctypes.c_int, [batch, i32, ctypes.POINTER(f32), f32, batch, vp, size, vp]),
+            ("sqn_orthogonalise_workspace", size, [i32, i32, i32, i32]),
+            ("sqn_quantise", ctypes.c_int, [mat, quant, vp]),
+            ("sqn_quantised_values", ctypes.c_int, [quant, mat, vp]),
+            ("sqn_quantised_product", ctypes.c_int, [quant, quant, vp, i32, mat, vp]),
+            ("sqn_quantised_layer", ctypes.c_int, [mat, quant, vp, i32, mat, vp, size, vp]),
+            ("sqn_quantised_layer_workspace", size, [i64, i64])):
+        call = getattr(lib, name)
+        call.restype, call.argtypes = result, args
     lib.sqn_status_string.restype = ctypes.c_char_p
     lib.sqn_status_string.argtypes = [ctypes.c_int]
     lib.sqn_last_error.restype = ctypes.c_char_p

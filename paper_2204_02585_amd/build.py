@@ -10,7 +10,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB_PATH = os.path.join(PKG, "libsqn.so")
 SOURCES = [os.path.join(CSRC, "api.hip"), os.path.join(CSRC, "render.hip"),
-           os.path.join(CSRC, "prepare.hip"), os.path.join(CSRC, "generate.hip")]
+           os.path.join(CSRC, "prepare.hip"), os.path.join(CSRC, "generate.hip"),
+           os.path.join(CSRC, "learn_api.hip"), os.path.join(CSRC, "rows.hip"),
+           os.path.join(CSRC, "orthogonal.hip"), os.path.join(CSRC, "quantise.hip")]
 # memory-level ceilings for the benchmark's roofline (not part of the render ABI)
 PROBE_PATH = os.path.join(PKG, "libsqn_probe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "probe.hip")]

@@ -48,13 +48,11 @@ struct sqn_networks {
     _Float16* enc_table;     // 3 x 8192 x (1 + 2 pos_freq) binary16
 };
 
-namespace {
+namespace sqn {
 
 // detail of the last failure on this thread; a fixed buffer, so that no
 // error path allocates
-thread_local char g_last_error[512];
-
-sqn_status fail(sqn_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+static thread_local char g_last_error[512];
 
 sqn_status fail(sqn_status s, const char* fmt, ...)
 {
@@ -66,10 +64,6 @@ sqn_status fail(sqn_status s, const char* fmt, ...)
 }
 
 void clear_error() { g_last_error[0] = '\0'; }
-
-size_t dtype_size(int32_t dt) { return dt == SQN_F16 ? 2 : 4; }
-
-bool valid_dtype(int32_t dt) { return dt == SQN_F32 || dt == SQN_F16; }
 
 // The pointer must lie in a HIP device allocation with at least `bytes`
 // bytes from it to the end of the allocation.
@@ -92,6 +86,18 @@ sqn_status check_device_range(const void* p, size_t bytes, const char* what)
                     p, bytes, size - (q - lo));
     return SQN_OK;
 }
+
+}  // namespace sqn
+
+namespace {
+
+using sqn::check_device_range;
+using sqn::clear_error;
+using sqn::fail;
+
+size_t dtype_size(int32_t dt) { return dt == SQN_F16 ? 2 : 4; }
+
+bool valid_dtype(int32_t dt) { return dt == SQN_F32 || dt == SQN_F16; }
 
 int64_t tau_threshold(float eps)
 {
@@ -1345,6 +1351,6 @@ const char* sqn_status_string(sqn_status status)
     return "unknown status";
 }
 
-const char* sqn_last_error(void) { return g_last_error; }
+const char* sqn_last_error(void) { return sqn::g_last_error; }
 
 }  // extern "C"

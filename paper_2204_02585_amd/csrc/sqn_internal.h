@@ -9,6 +9,18 @@
 
 namespace sqn {
 
+// ---- errors and checks of the C ABI (api.hip)
+
+// Notes the detail of a failure on this thread (sqn_last_error) and returns
+// its status.
+sqn_status fail(sqn_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+void clear_error();
+// SQN_OK if `p` lies in a HIP device allocation with at least `bytes` bytes
+// from it to the allocation's end.
+sqn_status check_device_range(const void* p, size_t bytes, const char* what);
+
+// ---- rendering (render.hip, prepare.hip)
+
 // Everything one render launch reads, passed by value as the kernel argument.
 struct RenderParams {
     // caches (library-owned device memory)
