@@ -11,8 +11,9 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_PATH = os.path.join(PKG, "libsqn.so")
 SOURCES = [os.path.join(CSRC, "api.hip"), os.path.join(CSRC, "render.hip"),
            os.path.join(CSRC, "prepare.hip"), os.path.join(CSRC, "generate.hip"),
-           os.path.join(CSRC, "learn_api.hip"), os.path.join(CSRC, "rows.hip"),
-           os.path.join(CSRC, "orthogonal.hip"), os.path.join(CSRC, "quantise.hip")]
+           os.path.join(CSRC, "rows.hip"), os.path.join(CSRC, "orthogonal.hip"), os.path.join(CSRC, "quantise.hip")]
+# parts of libsqn.so without device code
+HOST_SOURCES = [os.path.join(CSRC, "learn_api.hip")]
 # memory-level ceilings for the benchmark's roofline (not part of the render ABI)
 PROBE_PATH = os.path.join(PKG, "libsqn_probe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "probe.hip")]
@@ -72,7 +73,7 @@ def _compile(sources, path, verbose):
 
 def build(verbose: bool = False) -> str:
     """Compile libsqn.so and libsqn_probe.so (always recompiles)."""
-    _compile(SOURCES, LIB_PATH, verbose)
+    _compile(SOURCES + HOST_SOURCES, LIB_PATH, verbose)
     _compile(PROBE_SOURCES, PROBE_PATH, verbose)
     return LIB_PATH
 
