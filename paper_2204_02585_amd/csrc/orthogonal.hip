@@ -5,7 +5,7 @@
 //
 // X is held with its shorter side as rows (m <= n), so the square products
 // are m x m.  All products are of the form C = P Q^T with rows of P and Q
-// contiguous along the sum, on v_mfma_f32_16x16x32_f16:
+// contiguous along the sum, on v_mfma_f32_32x32x16_f16:
 //
 //   A   = X X^T      P = Q = X            only the tiles on and below the
 //   A A = A A^T      P = Q = A            diagonal, mirrored when written
@@ -30,16 +30,15 @@
 #include "learn.h"
 #include "numeric.h"
 #include "sqn_internal.h"
+#include "tile.h"
 
 namespace sqn {
 namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kPad = 64;                 // rows, columns and sums are padded to this
-constexpr int kNormBlocks = 64;          // workgroups per matrix that sum squares
+constexpr int kNormBlocks = 256;         // workgroups per matrix that sum squares
 
 constexpr float kScaleX = 4096.0f;       // hi + lo = 2^12 X
 constexpr float kScaleA = 4096.0f;       // 2^12 O
@@ -66,7 +65,6 @@ struct OrthParams {
     int32_t m, n, mp, np;
     int32_t in_dtype, out_dtype;
     float a, b, c, eps;
-    int32_t last;                        // the step writes `out`
 };
 
 __device__ __forceinline__ float load_any(const void* p, int64_t i, int32_t dtype)
@@ -88,21 +86,33 @@ __device__ __forceinline__ void store_any(void* p, int64_t i, float v, int32_t d
         static_cast<__bf16*>(p)[i] = static_cast<__bf16>(v);
 }
 
-// Sums of squares of a matrix, kNormBlocks of them, in binary64: gradients may
-// be small enough for their squares to vanish in binary32.
+// A matrix's sum of squares in kNormBlocks parts, in binary64: gradients may be
+// so small that their squares vanish in binary32.  Its lines along the smaller
+// stride go to the workgroups in turn, one line or, of short lines, several
+// to a workgroup at a time.
 __global__ __launch_bounds__(kThreads) void norm_kernel(OrthParams p)
 {
     const int64_t base = blockIdx.y * p.in_batch;
-    // along the contiguous side
     const bool rows_inner = p.in_row < p.in_col;
     const uint32_t inner = rows_inner ? p.m : p.n, outer = rows_inner ? p.n : p.m;
     const int64_t si = rows_inner ? p.in_row : p.in_col, so = rows_inner ? p.in_col : p.in_row;
+    // threads along a line: a power of two
+    uint32_t along = 32;
+    while (along < kThreads && along < inner)
+        along *= 2;
+    const uint32_t lines = kThreads / along, first = threadIdx.x % along;
     double sum = 0.0;
-    const uint64_t total = static_cast<uint64_t>(inner) * outer;
-    for (uint64_t k = blockIdx.x * kThreads + threadIdx.x; k < total; k += kNormBlocks * kThreads) {
-        const uint32_t j = static_cast<uint32_t>(k / inner), i = static_cast<uint32_t>(k - static_cast<uint64_t>(j) * inner);
-        const double v = load_any(p.in, base + i * si + j * so, p.in_dtype);
-        sum = __builtin_fma(v, v, sum);
+    for (uint32_t j = blockIdx.x * lines + threadIdx.x / along; j < outer; j += kNormBlocks * lines) {
+        const int64_t line = base + j * so;
+        for (uint32_t i = first; i < inner; i += 4 * along) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = i + k * along < inner ? load_any(p.in, line + (i + k * along) * si, p.in_dtype) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                sum = __builtin_fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sum);
+        }
     }
     for (int d = 32; d; d /= 2)
         sum += __shfl_xor(sum, d);
@@ -126,8 +136,10 @@ __global__ __launch_bounds__(kThreads) void start_kernel(OrthParams p)
     __shared__ float tile[64][65];
     const uint32_t b = blockIdx.z;
     double sum = 0.0;
-    for (int k = 0; k < kNormBlocks; ++k)
+    for (int k = threadIdx.x & 63; k < kNormBlocks; k += 64)
         sum += p.s.norms[b * kNormBlocks + k];
+    for (int d = 32; d; d /= 2)
+        sum += __shfl_xor(sum, d);
     const double norm = sqrt(sum) + static_cast<double>(p.eps);
     // a NaN or an infinity anywhere gives NaN everywhere
     const double scale = norm > 0.0 ? kScaleX / norm : 0.0;
@@ -174,85 +186,167 @@ __global__ __launch_bounds__(kThreads) void emit_kernel(OrthParams p)
     }
 }
 
-// ---- products: 64 x 64 of C a workgroup, 32 x 32 a wave
+// ---- products
 
-// acc[s][t]: rows 16 s + 4 (lane / 16) + q, column 16 t + lane % 16 of the wave's part.
-struct Part {
-    float4v acc[2][2];
-    uint32_t row, col;      // of acc[0][0][0]
+// A workgroup's tile: SIDE x SIDE of C by 2 x WN waves; padded sizes are
+// multiples of it.  Larger tiles read less of their factors per product
+// (from LDS above all); smaller ones give small matrices more workgroups.
+template <int SIDE_, bool SPLIT_>
+struct Shape {
+    static constexpr int SIDE = SIDE_;
+    static constexpr bool SPLIT = SPLIT_;
+    static constexpr int WN = SIDE == 256 ? 4 : 2;
+    static constexpr int WAVES = 2 * WN, THREADS = 64 * WAVES;
+    static constexpr int FM = SIDE / 64, FN = SIDE / (32 * WN);   // accumulators of a wave
+    static constexpr int FACTORS = SPLIT ? 4 : 2;             // P, Q, and their low parts
+    static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
+    static constexpr int BUFFER = FACTORS * ROWS;
+    static constexpr int PER_SIMD = SIDE == 256 || 4 * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
 };
 
-__device__ __forceinline__ half8 fragment(const _Float16* p) { return *reinterpret_cast<const half8*>(p); }
+struct Factor {
+    const char *hi, *lo;     // the tile's first row
+    uint32_t row_bytes;
+};
 
-__device__ __forceinline__ float4v multiply(half8 a, half8 b, float4v acc)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, acc, 0, 0, 0);
-}
-
-// The sums over all of `sum`.  With SPLIT the products of the high parts are
-// formed over stretches of 128 and added up outside the matrix cores, and the
-// small ones apart from them: in one running sum the error of an update of
-// low rank is 3.3e-5 of the result, a plain binary32 product's own is 1.2e-5.
-template <bool SPLIT>
-__device__ __forceinline__ void products(Part& c, const _Float16* p, const _Float16* p_lo, const _Float16* q,
-                                         const _Float16* q_lo, uint32_t ld_p, uint32_t ld_q, uint32_t sum,
-                                         uint32_t tile_row, uint32_t tile_col)
+template <typename S>
+__device__ __forceinline__ void bring_rows(const char* p, uint32_t row_bytes, uint32_t step, char* to)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t row = tile_row + (wave & 1) * 32, col = tile_col + (wave >> 1) * 32;
-    const uint64_t pf = static_cast<uint64_t>(row + (lane & 15)) * ld_p + 8 * (lane >> 4);
-    const uint64_t qf = static_cast<uint64_t>(col + (lane & 15)) * ld_q + 8 * (lane >> 4);
-    c.row = row + 4 * (lane >> 4);
-    c.col = col + (lane & 15);
+    const uint32_t mine = (8 * wave + (lane >> 3)) * row_bytes + brought_piece(lane) * kSlot;
+    p += static_cast<uint64_t>(step) * kStepBytes;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int i = 0; i < S::SIDE / (8 * S::WAVES); ++i)
+        bring(p + static_cast<uint64_t>(8 * S::WAVES * i) * row_bytes + mine, to + (S::WAVES * i + wave) * 1024);
+}
+
+template <typename S>
+__device__ __forceinline__ void bring_step(const Factor& p, const Factor& q, uint32_t step, char* buffer)
+{
+    bring_rows<S>(p.hi, p.row_bytes, step, buffer);
+    bring_rows<S>(q.hi, q.row_bytes, step, buffer + S::ROWS);
+    if constexpr (S::SPLIT) {
+        bring_rows<S>(p.lo, p.row_bytes, step, buffer + 2 * S::ROWS);
+        bring_rows<S>(q.lo, q.row_bytes, step, buffer + 3 * S::ROWS);
+    }
+    // the loads stay ahead of the products that hide them
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ float16v multiply(half8 a, half8 b, float16v acc)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, acc, 0, 0, 0);
+}
+
+template <typename S>
+using Acc = float16v[S::FM][S::FN];
+
+template <typename S>
+__device__ __forceinline__ void clear(Acc<S>& acc)
+{
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-            c.acc[s][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    float4v small[2][2] = {};
-    for (uint32_t k0 = 0; k0 < sum; k0 += 128) {
-        float4v part[2][2];
+    for (int s = 0; s < S::FM; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int t = 0; t < S::FN; ++t)
+            acc[s][t] = float16v{};
+}
+
+template <typename S>
+__device__ __forceinline__ void add(Acc<S>& acc, const Acc<S>& more)
+{
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                part[s][t] = SPLIT ? float4v{0.0f, 0.0f, 0.0f, 0.0f} : c.acc[s][t];
-        const uint32_t end = min(sum, k0 + 128);
-        for (uint32_t k = k0; k < end; k += 32) {
-            half8 a[2], b[2], a_lo[2], b_lo[2];
+    for (int s = 0; s < S::FM; ++s)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                a[s] = fragment(p + pf + static_cast<uint64_t>(16 * s) * ld_p + k);
-                b[s] = fragment(q + qf + static_cast<uint64_t>(16 * s) * ld_q + k);
-                if constexpr (SPLIT) {
-                    a_lo[s] = fragment(p_lo + pf + static_cast<uint64_t>(16 * s) * ld_p + k);
-                    b_lo[s] = fragment(q_lo + qf + static_cast<uint64_t>(16 * s) * ld_q + k);
-                }
-            }
+        for (int t = 0; t < S::FN; ++t)
+            acc[s][t] += more[s][t];
+}
+
+// With SPLIT, `acc` takes the products of the high parts of this step only and
+// `small` those of a high and a low part.
+template <typename S>
+__device__ __forceinline__ void multiply_step(const char* buffer, Acc<S>& acc, Acc<S>& small)
+{
+    constexpr uint32_t BLOCK = 32 * kStepBytes;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const char* p = buffer + (wave & 1) * (S::FM * BLOCK);
+    const char* q = buffer + S::ROWS + (wave >> 1) * (S::FN * BLOCK);
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+    for (int o = 0; o < 4; ++o) {
+        const uint32_t at = piece_at(lane, o);
+        half8 a[S::FM], b[S::FN], a_lo[S::FM], b_lo[S::FN];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if constexpr (SPLIT) {
-                        small[s][t] = multiply(a[s], b_lo[t], small[s][t]);
-                        small[s][t] = multiply(a_lo[s], b[t], small[s][t]);
-                    }
-                    part[s][t] = multiply(a[s], b[t], part[s][t]);
-                }
+        for (int s = 0; s < S::FM; ++s) {
+            a[s] = *reinterpret_cast<const half8*>(p + s * BLOCK + at);
+            if constexpr (S::SPLIT)
+                a_lo[s] = *reinterpret_cast<const half8*>(p + 2 * S::ROWS + s * BLOCK + at);
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int t = 0; t < S::FN; ++t) {
+            b[t] = *reinterpret_cast<const half8*>(q + t * BLOCK + at);
+            if constexpr (S::SPLIT)
+                b_lo[t] = *reinterpret_cast<const half8*>(q + 2 * S::ROWS + t * BLOCK + at);
+        }
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                c.acc[s][t] = SPLIT ? c.acc[s][t] + part[s][t] : part[s][t];
+        for (int s = 0; s < S::FM; ++s)
+#pragma unroll
+            for (int t = 0; t < S::FN; ++t) {
+                acc[s][t] = multiply(a[s], b[t], acc[s][t]);
+                if constexpr (S::SPLIT) {
+                    small[s][t] = multiply(a[s], b_lo[t], small[s][t]);
+                    small[s][t] = multiply(a_lo[s], b[t], small[s][t]);
+                }
+            }
     }
-    if constexpr (SPLIT) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-                c.acc[s][t] += small[s][t];
+}
+
+// The tile's sums over `steps` steps.  With SPLIT the products of the high
+// parts are summed a step at a time and added up outside the matrix cores, and
+// the small ones apart from them: in one running sum the error of an update of
+// low rank is 3.3e-5 of the result, a plain binary32 product's own is 1.2e-5.
+template <typename S>
+__device__ __forceinline__ void products(const Factor& p, const Factor& q, uint32_t steps, Acc<S>& acc)
+{
+    // two arrays, so that reads of one do not wait for loads into the other
+    __shared__ __align__(16) char buffer0[S::BUFFER];
+    __shared__ __align__(16) char buffer1[S::BUFFER];
+    Acc<S> part, small;
+    clear<S>(acc);
+    clear<S>(small);
+    auto work = [&](const char* buffer) {
+        if constexpr (S::SPLIT) {
+            clear<S>(part);
+            multiply_step<S>(buffer, part, small);
+            add<S>(acc, part);
+        } else {
+            multiply_step<S>(buffer, acc, small);
+        }
+    };
+    bring_step<S>(p, q, 0, buffer0);
+    uint32_t k = 0;
+    for (; k + 1 < steps; k += 2) {
+        __syncthreads();
+        bring_step<S>(p, q, k + 1, buffer1);
+        work(buffer0);
+        __syncthreads();
+        // past the end the last step once more, not read
+        bring_step<S>(p, q, min(k + 2, steps - 1), buffer0);
+        work(buffer1);
     }
+    if (k < steps) {
+        __syncthreads();
+        work(buffer0);
+    }
+    if constexpr (S::SPLIT)
+        add<S>(acc, small);
+}
+
+__device__ __forceinline__ Factor factor(const _Float16* hi, const _Float16* lo, uint64_t row, uint32_t cols)
+{
+    Factor f;
+    f.hi = reinterpret_cast<const char*>(hi + row * cols);
+    f.lo = reinterpret_cast<const char*>(lo + row * cols);
+    f.row_bytes = 2 * cols;
+    return f;
 }
 
 // The k-th tile on or below the diagonal, row by row.
@@ -267,108 +361,158 @@ __device__ __forceinline__ void lower_tile(uint32_t k, uint32_t& ti, uint32_t& t
     tj = k - i * (i + 1) / 2;
 }
 
-// f(i, j, value, mirror) over the workgroup's elements
-template <typename F>
-__device__ __forceinline__ void each(const Part& c, F f)
+// f(i, j, elements) over the blocks of the wave's part of tile (ti, tj):
+// element q is (i + row_of(q), j)
+template <typename S, typename F>
+__device__ __forceinline__ void each(const Acc<S>& acc, uint32_t ti, uint32_t tj, F f)
 {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                f(c.row + 16 * s + q, c.col + 16 * t, c.acc[s][t][q]);
+    const uint32_t wave = threadIdx.x >> 6;
+    const uint32_t row = ti * S::SIDE + (wave & 1) * (32 * S::FM), col = tj * S::SIDE + (wave >> 1) * (32 * S::FN);
+    each_block<S::FM, S::FN>(acc, [&](uint32_t i, uint32_t j, const float16v& v) { f(row + i, col + j, v); });
 }
 
-template <bool SPLIT>
-__global__ __launch_bounds__(kThreads) void gram_kernel(OrthParams p)
+// A block's elements as binary16 (`lo` what that leaves, where wanted), to
+// rows of `cols` at (i, j).
+__device__ __forceinline__ void store_block(_Float16* hi, _Float16* lo, uint32_t cols, uint32_t i, uint32_t j,
+                                            const float16v& v)
+{
+    const uint64_t at = static_cast<uint64_t>(i) * cols + j;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        _Float16 h, l;
+        split(v[q], h, l);
+        hi[at + row_of(q) * cols] = h;
+        if (lo)
+            lo[at + row_of(q) * cols] = l;
+    }
+}
+
+// ... and to the mirrored place: element q at (j, i + row_of(q)), four a store.
+__device__ __forceinline__ void store_mirrored(_Float16* hi, _Float16* lo, uint32_t cols, uint32_t i, uint32_t j,
+                                               const float16v& v)
+{
+    typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+    const uint64_t at = static_cast<uint64_t>(j) * cols + i;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        half4 h, l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            _Float16 a, b;
+            split(v[4 * g + r], a, b);
+            h[r] = a;
+            l[r] = b;
+        }
+        *reinterpret_cast<half4*>(hi + at + 8 * g) = h;
+        if (lo)
+            *reinterpret_cast<half4*>(lo + at + 8 * g) = l;
+    }
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void gram_kernel(OrthParams p)
 {
     uint32_t ti, tj;
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t x = static_cast<uint64_t>(blockIdx.y) * p.mp * p.np, o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
-    Part c;
-    products<SPLIT>(c, p.s.x + x, p.s.x_lo + x, p.s.x + x, p.s.x_lo + x, p.np, p.np, p.np, ti * 64, tj * 64);
-    each(c, [&](uint32_t i, uint32_t j, float v) {
-        if (i == j) {
-            p.s.d[blockIdx.y * p.mp + i] = v * (1.0f / (kScaleX * kScaleX));
-            v = 0.0f;
+    Acc<S> acc;
+    products<S>(factor(p.s.x + x, p.s.x_lo + x, ti * S::SIDE, p.np), factor(p.s.x + x, p.s.x_lo + x, tj * S::SIDE, p.np),
+                2 * p.np / kStepBytes, acc);
+    _Float16* hi = p.s.o + o;
+    _Float16* lo = S::SPLIT ? p.s.o_lo + o : nullptr;
+    float* d = p.s.d + blockIdx.y * p.mp;
+    each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, float16v v) {
+        v *= kScaleA / (kScaleX * kScaleX);
+        if (ti == tj) {
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (i + row_of(q) == j) {
+                    d[j] = v[q] * (1.0f / kScaleA);
+                    v[q] = 0.0f;
+                }
+        } else {
+            store_mirrored(hi, lo, p.mp, i, j, v);
         }
-        _Float16 hi, lo;
-        split(v * (kScaleA / (kScaleX * kScaleX)), hi, lo);
-        const uint64_t at = o + static_cast<uint64_t>(i) * p.mp + j, mirror = o + static_cast<uint64_t>(j) * p.mp + i;
-        p.s.o[at] = hi;
-        if (ti != tj)
-            p.s.o[mirror] = hi;
-        if constexpr (SPLIT) {
-            p.s.o_lo[at] = lo;
-            if (ti != tj)
-                p.s.o_lo[mirror] = lo;
-        }
+        store_block(hi, lo, p.mp, i, j, v);
     });
 }
 
-template <bool SPLIT>
-__global__ __launch_bounds__(kThreads) void square_kernel(OrthParams p)
+template <typename S>
+__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void square_kernel(OrthParams p)
 {
     uint32_t ti, tj;
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
+    const _Float16* o_hi = p.s.o + o;
+    const _Float16* o_lo = S::SPLIT ? p.s.o_lo + o : nullptr;
+    Acc<S> acc;
+    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), 2 * p.mp / kStepBytes, acc);
+    _Float16* hi = p.s.b + o;
+    _Float16* lo = S::SPLIT ? p.s.b_lo + o : nullptr;
     const float* d = p.s.d + blockIdx.y * p.mp;
-    Part c;
-    products<SPLIT>(c, p.s.o + o, p.s.o_lo + o, p.s.o + o, p.s.o_lo + o, p.mp, p.mp, p.mp, ti * 64, tj * 64);
-    each(c, [&](uint32_t i, uint32_t j, float v) {
-        const uint64_t at = o + static_cast<uint64_t>(i) * p.mp + j, mirror = o + static_cast<uint64_t>(j) * p.mp + i;
-        v *= 1.0f / (kScaleA * kScaleA);
-        if (i == j) {
-            p.s.d_b[blockIdx.y * p.mp + i] = p.a + p.b * d[i] + p.c * (d[i] * d[i] + v);
-            v = 0.0f;
-        } else {
-            float e = static_cast<float>(p.s.o[at]);
-            if constexpr (SPLIT)
-                e += static_cast<float>(p.s.o_lo[at]);
-            e *= 1.0f / kScaleA;
-            v = p.b * e + p.c * (v + (d[i] + d[j]) * e);
+    float* d_b = p.s.d_b + blockIdx.y * p.mp;
+    each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, const float16v& sum) {
+        float16v v;
+        float e[16], di[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const uint64_t at = static_cast<uint64_t>(i + row_of(q)) * p.mp + j;
+            e[q] = static_cast<float>(o_hi[at]);
+            if constexpr (S::SPLIT)
+                e[q] += static_cast<float>(o_lo[at]);
+            di[q] = d[i + row_of(q)];
         }
-        _Float16 hi, lo;
-        split(v * kScaleB, hi, lo);
-        p.s.b[at] = hi;
+        const float dj = d[j];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const float square = sum[q] * (1.0f / (kScaleA * kScaleA)), a = e[q] * (1.0f / kScaleA);
+            v[q] = kScaleB * (p.b * a + p.c * (square + (di[q] + dj) * a));
+            if (ti == tj && i + row_of(q) == j) {
+                d_b[j] = p.a + p.b * dj + p.c * (dj * dj + square);
+                v[q] = 0.0f;
+            }
+        }
         if (ti != tj)
-            p.s.b[mirror] = hi;
-        if constexpr (SPLIT) {
-            p.s.b_lo[at] = lo;
-            if (ti != tj)
-                p.s.b_lo[mirror] = lo;
-        }
+            store_mirrored(hi, lo, p.mp, i, j, v);
+        store_block(hi, lo, p.mp, i, j, v);
     });
 }
 
-template <bool SPLIT>
-__global__ __launch_bounds__(kThreads) void step_kernel(OrthParams p)
+template <typename S, bool LAST>
+__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void step_kernel(OrthParams p)
 {
-    const uint32_t b = blockIdx.z;
+    const uint32_t b = blockIdx.z, ti = blockIdx.y, tj = blockIdx.x;
     const uint64_t x = static_cast<uint64_t>(b) * p.mp * p.np, o = static_cast<uint64_t>(b) * p.mp * p.mp;
-    Part c;
-    products<SPLIT>(c, p.s.b + o, p.s.b_lo + o, p.s.xt + x, p.s.xt_lo + x, p.mp, p.mp, p.mp, blockIdx.y * 64,
-                    blockIdx.x * 64);
-    each(c, [&](uint32_t i, uint32_t j, float v) {
+    Acc<S> acc;
+    products<S>(factor(p.s.b + o, p.s.b_lo + o, ti * S::SIDE, p.mp),
+                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), 2 * p.mp / kStepBytes, acc);
+    const float* d_b = p.s.d_b + b * p.mp;
+    each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, const float16v& sum) {
         const uint64_t at = x + static_cast<uint64_t>(i) * p.np + j;
-        const float old = SPLIT ? p.s.x_full[at] : static_cast<float>(p.s.x[at]) + static_cast<float>(p.s.x_lo[at]);
-        v = __builtin_fmaf(p.s.d_b[b * p.mp + i], old, v * (1.0f / kScaleB));
-        if (p.last) {
-            if (i < static_cast<uint32_t>(p.m) && j < static_cast<uint32_t>(p.n))
-                store_any(p.out, b * p.out_batch + i * p.out_row + j * p.out_col, v * (1.0f / kScaleX), p.out_dtype);
-            return;
+        float16v v;
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            v[q] = S::SPLIT ? p.s.x_full[at + row_of(q) * p.np]
+                            : static_cast<float>(p.s.x[at + row_of(q) * p.np])
+                                  + static_cast<float>(p.s.x_lo[at + row_of(q) * p.np]);
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            v[q] = __builtin_fmaf(d_b[i + row_of(q)], v[q], sum[q] * (1.0f / kScaleB));
+        if constexpr (LAST) {
+            const int64_t to = b * p.out_batch + i * p.out_row + j * p.out_col;
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (i + row_of(q) < static_cast<uint32_t>(p.m) && j < static_cast<uint32_t>(p.n))
+                    store_any(p.out, to + row_of(q) * p.out_row, v[q] * (1.0f / kScaleX), p.out_dtype);
+        } else {
+            if constexpr (S::SPLIT) {
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    p.s.x_full[at + row_of(q) * p.np] = v[q];
+            }
+            store_block(p.s.x + x, p.s.x_lo + x, p.np, i, j, v);
+            store_mirrored(p.s.xt_to + x, S::SPLIT ? p.s.xt_to_lo + x : nullptr, p.mp, i, j, v);
         }
-        _Float16 hi, lo;
-        split(v, hi, lo);
-        p.s.x[at] = hi;
-        p.s.x_lo[at] = lo;
-        if constexpr (SPLIT)
-            p.s.x_full[at] = v;
-        const uint64_t to = x + static_cast<uint64_t>(j) * p.mp + i;
-        p.s.xt_to[to] = hi;
-        if constexpr (SPLIT)
-            p.s.xt_to_lo[to] = lo;
     });
 }
 
@@ -376,10 +520,22 @@ __global__ __launch_bounds__(kThreads) void step_kernel(OrthParams p)
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
+// Side of the tiles of a batch of matrices.
+int32_t tile_side(int32_t batch, int32_t m, int32_t n, bool split_all)
+{
+    auto tiles = [&](int64_t side) { return batch * ((m + side - 1) / side) * ((n + side - 1) / side); };
+    if (!split_all && tiles(256) >= 200)
+        return 256;
+    return tiles(128) >= 200 ? 128 : 64;
+}
+
+int32_t up_to(int32_t v, int32_t side) { return (v + side - 1) / side * side; }
+
 size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* base, Scratch* s)
 {
-    const size_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    const size_t mp = (m + kPad - 1) / kPad * kPad, np = (n + kPad - 1) / kPad * kPad;
+    const int32_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    const int32_t side = tile_side(batch, m, n, split_all);
+    const size_t mp = up_to(m, side), np = up_to(n, side);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         char* here = base + at;
@@ -409,16 +565,19 @@ size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* b
     return at;
 }
 
-template <bool SPLIT>
+template <typename S>
 hipError_t run_steps(OrthParams p, int32_t batch, int32_t steps, hipStream_t stream)
 {
-    const uint32_t tm = p.mp / 64, tn = p.np / 64;
-    const uint32_t lower = tm * (tm + 1) / 2;
+    const uint32_t tm = p.mp / S::SIDE, tn = p.np / S::SIDE;
+    const dim3 lower(tm * (tm + 1) / 2, batch), all(tn, tm, batch);
     for (int32_t k = 0; k < steps; ++k) {
-        p.last = k + 1 == steps;
-        gram_kernel<SPLIT><<<dim3(lower, batch), kThreads, 0, stream>>>(p);
-        square_kernel<SPLIT><<<dim3(lower, batch), kThreads, 0, stream>>>(p);
-        step_kernel<SPLIT><<<dim3(tn, tm, batch), kThreads, 0, stream>>>(p);
+        gram_kernel<S><<<lower, S::THREADS, 0, stream>>>(p);
+        square_kernel<S><<<lower, S::THREADS, 0, stream>>>(p);
+        if (k + 1 == steps) {
+            step_kernel<S, true><<<all, S::THREADS, 0, stream>>>(p);
+            break;
+        }
+        step_kernel<S, false><<<all, S::THREADS, 0, stream>>>(p);
         _Float16* t = p.s.xt;
         p.s.xt = p.s.xt_to;
         p.s.xt_to = t;
@@ -453,23 +612,28 @@ hipError_t launch_orthogonalise(const sqn_batch& updates, int32_t steps, const f
     p.out_col = tall ? out.row_stride : out.col_stride;
     p.m = tall ? updates.cols : updates.rows;
     p.n = tall ? updates.rows : updates.cols;
-    p.mp = (p.m + kPad - 1) / kPad * kPad;
-    p.np = (p.n + kPad - 1) / kPad * kPad;
+    const int32_t side = tile_side(updates.batch, p.m, p.n, split_all);
+    p.mp = up_to(p.m, side);
+    p.np = up_to(p.n, side);
     p.in_dtype = updates.dtype;
     p.out_dtype = out.dtype;
     p.a = coefficients[0];
     p.b = coefficients[1];
     p.c = coefficients[2];
     p.eps = eps;
-    p.last = 0;
     norm_kernel<<<dim3(kNormBlocks, updates.batch), kThreads, 0, stream>>>(p);
     start_kernel<<<dim3(p.np / 64, p.mp / 64, updates.batch), kThreads, 0, stream>>>(p);
     if (steps == 0) {
         emit_kernel<<<dim3(1, p.m, updates.batch), kThreads, 0, stream>>>(p);
         return hipGetLastError();
     }
-    return split_all ? run_steps<true>(p, updates.batch, steps, stream)
-                     : run_steps<false>(p, updates.batch, steps, stream);
+    if (split_all)
+        return side == 128 ? run_steps<Shape<128, true>>(p, updates.batch, steps, stream)
+                           : run_steps<Shape<64, true>>(p, updates.batch, steps, stream);
+    if (side == 256)
+        return run_steps<Shape<256, false>>(p, updates.batch, steps, stream);
+    return side == 128 ? run_steps<Shape<128, false>>(p, updates.batch, steps, stream)
+                       : run_steps<Shape<64, false>>(p, updates.batch, steps, stream);
 }
 
 }  // namespace sqn
