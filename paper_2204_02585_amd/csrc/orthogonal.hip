@@ -213,7 +213,8 @@ template <typename S>
 __device__ __forceinline__ void bring_rows(const char* p, uint32_t row_bytes, uint32_t step, char* to)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t mine = (8 * wave + (lane >> 3)) * row_bytes + brought_piece(lane) * kSlot;
+    // a wave's groups of 8 rows have its own parity
+    const uint32_t mine = (8 * wave + (lane >> 3)) * row_bytes + brought_piece(lane, wave) * kSlot;
     p += static_cast<uint64_t>(step) * kStepBytes;
 #pragma unroll
     for (int i = 0; i < S::SIDE / (8 * S::WAVES); ++i)
@@ -261,41 +262,64 @@ __device__ __forceinline__ void add(Acc<S>& acc, const Acc<S>& more)
             acc[s][t] += more[s][t];
 }
 
-// With SPLIT, `acc` takes the products of the high parts of this step only and
-// `small` those of a high and a low part.
+// One instruction depth's share of the factors.
 template <typename S>
-__device__ __forceinline__ void multiply_step(const char* buffer, Acc<S>& acc, Acc<S>& small)
+struct Fragments {
+    half8 a[S::FM], b[S::FN], a_lo[S::SPLIT ? S::FM : 1], b_lo[S::SPLIT ? S::FN : 1];
+};
+
+template <typename S>
+__device__ __forceinline__ void read_fragments(Fragments<S>& f, const char* buffer, uint32_t o)
 {
     constexpr uint32_t BLOCK = 32 * kStepBytes;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const char* p = buffer + (wave & 1) * (S::FM * BLOCK);
-    const char* q = buffer + S::ROWS + (wave >> 1) * (S::FN * BLOCK);
+    const char* p = buffer + (wave & 1) * (S::FM * BLOCK) + piece_at(lane, o);
+    const char* q = buffer + S::ROWS + (wave >> 1) * (S::FN * BLOCK) + piece_at(lane, o);
+#pragma unroll
+    for (int s = 0; s < S::FM; ++s) {
+        f.a[s] = *reinterpret_cast<const half8*>(p + s * BLOCK);
+        if constexpr (S::SPLIT)
+            f.a_lo[s] = *reinterpret_cast<const half8*>(p + 2 * S::ROWS + s * BLOCK);
+    }
+#pragma unroll
+    for (int t = 0; t < S::FN; ++t) {
+        f.b[t] = *reinterpret_cast<const half8*>(q + t * BLOCK);
+        if constexpr (S::SPLIT)
+            f.b_lo[t] = *reinterpret_cast<const half8*>(q + 2 * S::ROWS + t * BLOCK);
+    }
+}
+
+// With SPLIT, `acc` takes the products of the high parts of this step only and
+// `small` those of a high and a low part.  The next depth's fragments are read
+// between the products of this one.
+template <typename S>
+__device__ __forceinline__ void multiply_step(const char* buffer, Acc<S>& acc, Acc<S>& small)
+{
+    constexpr int READS = (S::FM + S::FN) * (S::SPLIT ? 2 : 1), PRODUCTS = S::FM * S::FN * (S::SPLIT ? 3 : 1);
+    Fragments<S> f[2];
+    read_fragments<S>(f[0], buffer, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
 #pragma unroll
     for (int o = 0; o < 4; ++o) {
-        const uint32_t at = piece_at(lane, o);
-        half8 a[S::FM], b[S::FN], a_lo[S::FM], b_lo[S::FN];
-#pragma unroll
-        for (int s = 0; s < S::FM; ++s) {
-            a[s] = *reinterpret_cast<const half8*>(p + s * BLOCK + at);
-            if constexpr (S::SPLIT)
-                a_lo[s] = *reinterpret_cast<const half8*>(p + 2 * S::ROWS + s * BLOCK + at);
-        }
-#pragma unroll
-        for (int t = 0; t < S::FN; ++t) {
-            b[t] = *reinterpret_cast<const half8*>(q + t * BLOCK + at);
-            if constexpr (S::SPLIT)
-                b_lo[t] = *reinterpret_cast<const half8*>(q + 2 * S::ROWS + t * BLOCK + at);
-        }
+        if (o < 3)
+            read_fragments<S>(f[(o + 1) & 1], buffer, o + 1);
+        const Fragments<S>& g = f[o & 1];
 #pragma unroll
         for (int s = 0; s < S::FM; ++s)
 #pragma unroll
             for (int t = 0; t < S::FN; ++t) {
-                acc[s][t] = multiply(a[s], b[t], acc[s][t]);
+                acc[s][t] = multiply(g.a[s], g.b[t], acc[s][t]);
                 if constexpr (S::SPLIT) {
-                    small[s][t] = multiply(a[s], b_lo[t], small[s][t]);
-                    small[s][t] = multiply(a_lo[s], b[t], small[s][t]);
+                    small[s][t] = multiply(g.a[s], g.b_lo[t], small[s][t]);
+                    small[s][t] = multiply(g.a_lo[s], g.b[t], small[s][t]);
                 }
             }
+        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+        for (int k = 0; k < PRODUCTS; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+        }
     }
 }
 
@@ -565,14 +589,15 @@ size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* b
     return at;
 }
 
-template <typename S>
+// The symmetric products in tiles of G, B X in tiles of S.
+template <typename S, typename G = S>
 hipError_t run_steps(OrthParams p, int32_t batch, int32_t steps, hipStream_t stream)
 {
-    const uint32_t tm = p.mp / S::SIDE, tn = p.np / S::SIDE;
-    const dim3 lower(tm * (tm + 1) / 2, batch), all(tn, tm, batch);
+    const uint32_t tg = p.mp / G::SIDE;
+    const dim3 lower(tg * (tg + 1) / 2, batch), all(p.np / S::SIDE, p.mp / S::SIDE, batch);
     for (int32_t k = 0; k < steps; ++k) {
-        gram_kernel<S><<<lower, S::THREADS, 0, stream>>>(p);
-        square_kernel<S><<<lower, S::THREADS, 0, stream>>>(p);
+        gram_kernel<G><<<lower, G::THREADS, 0, stream>>>(p);
+        square_kernel<G><<<lower, G::THREADS, 0, stream>>>(p);
         if (k + 1 == steps) {
             step_kernel<S, true><<<all, S::THREADS, 0, stream>>>(p);
             break;

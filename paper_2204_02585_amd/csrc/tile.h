@@ -8,8 +8,10 @@
 // instructions deep: instruction o takes from row r, in lane r % 32 + 32 g, the
 // row's 16-byte piece 4 g + o.  (Any assignment of pieces to lanes gives the
 // same sum; this one lets a lane's four scales of a 4-bit step lie side by
-// side.)  Piece c of row r lies in slot c ^ (r % 8) of its row, so the eight
-// lanes that LDS serves together read eight different groups of banks.
+// side.)  Piece c of row r lies in slot c ^ (r / 2 % 8) of its row: two rows
+// take the 64 banks once, so of the lanes that LDS serves together those in rows
+// of one parity must differ in their slot (with r % 8 instead a third of the
+// LDS cycles were conflicts).
 //
 // A wave's part of C is FM x FN accumulators of 32 x 32: element q of a lane is
 // row 8 (q / 4) + 4 (lane / 32) + q % 4, column lane % 32.
@@ -36,14 +38,17 @@ __device__ __forceinline__ void bring(const char* from, char* to)
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(from), reinterpret_cast<uint32_t*>(to), kSlot, 0, 0);
 }
 
-// The piece that lane `lane` brings (of 8 in a row).
-__device__ __forceinline__ uint32_t brought_piece(uint32_t lane) { return (lane & 7) ^ (lane >> 3); }
+// The piece that a lane brings into the group of 8 rows `group`.
+__device__ __forceinline__ uint32_t brought_piece(uint32_t lane, uint32_t group)
+{
+    return (lane & 7) ^ (4 * (group & 1) + (lane >> 4));
+}
 
 // Byte of piece 4 (lane / 32) + o of row lane % 32 in a step's buffer, from the
 // wave's first row.
 __device__ __forceinline__ uint32_t piece_at(uint32_t lane, uint32_t o)
 {
-    return (lane & 31) * kStepBytes + ((4 * (lane >> 5) + o) ^ (lane & 7)) * kSlot;
+    return (lane & 31) * kStepBytes + ((4 * (lane >> 5) + o) ^ (lane >> 1 & 7)) * kSlot;
 }
 
 // f(row, column, elements) over a wave's accumulators, from its first row and
