@@ -201,7 +201,8 @@ struct Shape {
     static constexpr int FACTORS = SPLIT ? 4 : 2;             // P, Q, and their low parts
     static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
     static constexpr int BUFFER = FACTORS * ROWS;
-    static constexpr int PER_SIMD = SIDE == 256 || 4 * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
+    static constexpr int LOADS = BUFFER / (1024 * WAVES);     // of a wave, a step
+    static constexpr int PER_SIMD = SIDE == 256 || 8 * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
 };
 
 struct Factor {
@@ -213,12 +214,11 @@ template <typename S>
 __device__ __forceinline__ void bring_rows(const char* p, uint32_t row_bytes, uint32_t step, char* to)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // a wave's groups of 8 rows have its own parity
-    const uint32_t mine = (8 * wave + (lane >> 3)) * row_bytes + brought_piece(lane, wave) * kSlot;
+    const uint32_t mine = (16 * wave + (lane >> 2)) * row_bytes + brought_piece(lane) * kSlot;
     p += static_cast<uint64_t>(step) * kStepBytes;
 #pragma unroll
-    for (int i = 0; i < S::SIDE / (8 * S::WAVES); ++i)
-        bring(p + static_cast<uint64_t>(8 * S::WAVES * i) * row_bytes + mine, to + (S::WAVES * i + wave) * 1024);
+    for (int i = 0; i < S::SIDE / (16 * S::WAVES); ++i)
+        bring(p + static_cast<uint64_t>(16 * S::WAVES * i) * row_bytes + mine, to + (S::WAVES * i + wave) * 1024);
 }
 
 template <typename S>
@@ -271,97 +271,81 @@ struct Fragments {
 template <typename S>
 __device__ __forceinline__ void read_fragments(Fragments<S>& f, const char* buffer, uint32_t o)
 {
-    constexpr uint32_t BLOCK = 32 * kStepBytes;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const char* p = buffer + (wave & 1) * (S::FM * BLOCK) + piece_at(lane, o);
-    const char* q = buffer + S::ROWS + (wave >> 1) * (S::FN * BLOCK) + piece_at(lane, o);
+    const char* p = buffer + (wave & 1) * (S::FM * kBlockBytes) + piece_at(lane, o);
+    const char* q = buffer + S::ROWS + (wave >> 1) * (S::FN * kBlockBytes) + piece_at(lane, o);
 #pragma unroll
     for (int s = 0; s < S::FM; ++s) {
-        f.a[s] = *reinterpret_cast<const half8*>(p + s * BLOCK);
+        f.a[s] = *reinterpret_cast<const half8*>(p + s * kBlockBytes);
         if constexpr (S::SPLIT)
-            f.a_lo[s] = *reinterpret_cast<const half8*>(p + 2 * S::ROWS + s * BLOCK);
+            f.a_lo[s] = *reinterpret_cast<const half8*>(p + 2 * S::ROWS + s * kBlockBytes);
     }
 #pragma unroll
     for (int t = 0; t < S::FN; ++t) {
-        f.b[t] = *reinterpret_cast<const half8*>(q + t * BLOCK);
+        f.b[t] = *reinterpret_cast<const half8*>(q + t * kBlockBytes);
         if constexpr (S::SPLIT)
-            f.b_lo[t] = *reinterpret_cast<const half8*>(q + 2 * S::ROWS + t * BLOCK);
+            f.b_lo[t] = *reinterpret_cast<const half8*>(q + 2 * S::ROWS + t * kBlockBytes);
     }
 }
 
-// With SPLIT, `acc` takes the products of the high parts of this step only and
-// `small` those of a high and a low part.  The next depth's fragments are read
-// between the products of this one.
+// With SPLIT, `acc` takes the products of the high parts and `small` those of a
+// high and a low part.  The reads issued before go between the products.
 template <typename S>
-__device__ __forceinline__ void multiply_step(const char* buffer, Acc<S>& acc, Acc<S>& small)
+__device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, Acc<S>& acc, Acc<S>& small)
 {
     constexpr int READS = (S::FM + S::FN) * (S::SPLIT ? 2 : 1), PRODUCTS = S::FM * S::FN * (S::SPLIT ? 3 : 1);
-    Fragments<S> f[2];
-    read_fragments<S>(f[0], buffer, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
 #pragma unroll
-    for (int o = 0; o < 4; ++o) {
-        if (o < 3)
-            read_fragments<S>(f[(o + 1) & 1], buffer, o + 1);
-        const Fragments<S>& g = f[o & 1];
+    for (int s = 0; s < S::FM; ++s)
 #pragma unroll
-        for (int s = 0; s < S::FM; ++s)
-#pragma unroll
-            for (int t = 0; t < S::FN; ++t) {
-                acc[s][t] = multiply(g.a[s], g.b[t], acc[s][t]);
-                if constexpr (S::SPLIT) {
-                    small[s][t] = multiply(g.a[s], g.b_lo[t], small[s][t]);
-                    small[s][t] = multiply(g.a_lo[s], g.b[t], small[s][t]);
-                }
+        for (int t = 0; t < S::FN; ++t) {
+            acc[s][t] = multiply(f.a[s], f.b[t], acc[s][t]);
+            if constexpr (S::SPLIT) {
+                small[s][t] = multiply(f.a[s], f.b_lo[t], small[s][t]);
+                small[s][t] = multiply(f.a_lo[s], f.b[t], small[s][t]);
             }
-        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
-#pragma unroll
-        for (int k = 0; k < PRODUCTS; ++k) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
         }
+    constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+    for (int k = 0; k < PRODUCTS; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
     }
 }
 
 // The tile's sums over `steps` steps.  With SPLIT the products of the high
-// parts are summed a step at a time and added up outside the matrix cores, and
+// parts are summed over 128 elements and added up outside the matrix cores, and
 // the small ones apart from them: in one running sum the error of an update of
 // low rank is 3.3e-5 of the result, a plain binary32 product's own is 1.2e-5.
 template <typename S>
 __device__ __forceinline__ void products(const Factor& p, const Factor& q, uint32_t steps, Acc<S>& acc)
 {
-    // two arrays, so that reads of one do not wait for loads into the other
+    // arrays of their own, so that reads of one do not wait for loads into another
     __shared__ __align__(16) char buffer0[S::BUFFER];
     __shared__ __align__(16) char buffer1[S::BUFFER];
+    __shared__ __align__(16) char buffer2[S::BUFFER];
+    __shared__ __align__(16) char buffer3[S::BUFFER];
     Acc<S> part, small;
     clear<S>(acc);
     clear<S>(small);
-    auto work = [&](const char* buffer) {
-        if constexpr (S::SPLIT) {
-            clear<S>(part);
-            multiply_step<S>(buffer, part, small);
+    pipeline<S::LOADS, Fragments<S>>(
+        steps, buffer0, buffer1, buffer2, buffer3, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
+        [&](Fragments<S>& f, const char* buffer, uint32_t o) { read_fragments<S>(f, buffer, o); },
+        [&](const Fragments<S>& f, int depth) {
+            if constexpr (S::SPLIT) {
+                if (depth == 0)
+                    clear<S>(part);
+                multiply_fragments<S>(f, part, small);
+                if (depth == 7)
+                    add<S>(acc, part);
+            } else {
+                multiply_fragments<S>(f, acc, small);
+            }
+        });
+    if constexpr (S::SPLIT) {
+        if (steps % 4)
             add<S>(acc, part);
-        } else {
-            multiply_step<S>(buffer, acc, small);
-        }
-    };
-    bring_step<S>(p, q, 0, buffer0);
-    uint32_t k = 0;
-    for (; k + 1 < steps; k += 2) {
-        __syncthreads();
-        bring_step<S>(p, q, k + 1, buffer1);
-        work(buffer0);
-        __syncthreads();
-        // past the end the last step once more, not read
-        bring_step<S>(p, q, min(k + 2, steps - 1), buffer0);
-        work(buffer1);
-    }
-    if (k < steps) {
-        __syncthreads();
-        work(buffer0);
-    }
-    if constexpr (S::SPLIT)
         add<S>(acc, small);
+    }
 }
 
 __device__ __forceinline__ Factor factor(const _Float16* hi, const _Float16* lo, uint64_t row, uint32_t cols)
