@@ -62,19 +62,11 @@ struct OrthParams {
     void* out;
     int64_t in_batch, in_row, in_col;    // elements, of X (rows <= cols)
     int64_t out_batch, out_row, out_col;
-    int32_t m, n, mp, np;
-    int32_t in_dtype, out_dtype;
+    int32_t m, n, mp, np;                // mp, np: rows and columns of the scratch
+    uint32_t steps_m, steps_n;           // of sums over m and n
+    int32_t out_dtype;
     float a, b, c, eps;
 };
-
-__device__ __forceinline__ float load_any(const void* p, int64_t i, int32_t dtype)
-{
-    if (dtype == SQN_F32)
-        return static_cast<const float*>(p)[i];
-    if (dtype == SQN_F16)
-        return static_cast<float>(static_cast<const _Float16*>(p)[i]);
-    return static_cast<float>(static_cast<const __bf16*>(p)[i]);
-}
 
 __device__ __forceinline__ void store_any(void* p, int64_t i, float v, int32_t dtype)
 {
@@ -86,36 +78,58 @@ __device__ __forceinline__ void store_any(void* p, int64_t i, float v, int32_t d
         static_cast<__bf16*>(p)[i] = static_cast<__bf16>(v);
 }
 
+// Whether X's rows run along the larger stride of the matrix, so that loads go
+// down a column.
+__device__ __forceinline__ bool down(const OrthParams& p) { return p.in_row < p.in_col; }
+
+// V elements from (i, j) on along the smaller stride, zeros past the matrix.
+template <typename T, int V>
+__device__ __forceinline__ void load_line(const OrthParams& p, int64_t base, uint32_t i, uint32_t j, float v[V])
+{
+    const bool d = down(p);
+    const uint32_t at = d ? i : j, end = d ? p.m : p.n, across = d ? j : i, lines = d ? p.n : p.m;
+    const int64_t step = d ? p.in_row : p.in_col;
+    const T* from = static_cast<const T*>(p.in) + base + i * p.in_row + j * p.in_col;
+    if (across < lines && at + V <= end && step == 1) {
+        load_run<T, V>(from, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] = across < lines && at + k < end ? to_f32(from[k * step]) : 0.0f;
+    }
+}
+
 // A matrix's sum of squares in kNormBlocks parts, in binary64: gradients may be
 // so small that their squares vanish in binary32.  Its lines along the smaller
 // stride go to the workgroups in turn, one line or, of short lines, several
 // to a workgroup at a time.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_kernel(OrthParams p)
 {
+    constexpr int V = 16 / sizeof(T);
     const int64_t base = blockIdx.y * p.in_batch;
-    const bool rows_inner = p.in_row < p.in_col;
-    const uint32_t inner = rows_inner ? p.m : p.n, outer = rows_inner ? p.n : p.m;
-    const int64_t si = rows_inner ? p.in_row : p.in_col, so = rows_inner ? p.in_col : p.in_row;
+    const bool d = down(p);
+    const uint32_t inner = d ? p.m : p.n, outer = d ? p.n : p.m;
     // threads along a line: a power of two
-    uint32_t along = 32;
-    while (along < kThreads && along < inner)
+    uint32_t along = 8;
+    while (along < kThreads && along * V < inner)
         along *= 2;
-    const uint32_t lines = kThreads / along, first = threadIdx.x % along;
+    const uint32_t lines = kThreads / along;
     double sum = 0.0;
-    for (uint32_t j = blockIdx.x * lines + threadIdx.x / along; j < outer; j += kNormBlocks * lines) {
-        const int64_t line = base + j * so;
-        for (uint32_t i = first; i < inner; i += 4 * along) {
-            float v[4];
+    for (uint32_t line = blockIdx.x * lines + threadIdx.x / along; line < outer; line += kNormBlocks * lines)
+        for (uint32_t at = threadIdx.x % along * V; at < inner; at += 2 * along * V) {
+            float v[2][V];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                v[k] = i + k * along < inner ? load_any(p.in, line + (i + k * along) * si, p.in_dtype) : 0.0f;
+            for (int k = 0; k < 2; ++k)
+                load_line<T, V>(p, base, d ? at + k * along * V : line, d ? line : at + k * along * V, v[k]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                sum = __builtin_fma(static_cast<double>(v[k]), static_cast<double>(v[k]), sum);
+            for (int k = 0; k < 2 * V; ++k) {
+                const double x = v[k / V][k % V];
+                sum = __builtin_fma(x, x, sum);
+            }
         }
-    }
-    for (int d = 32; d; d /= 2)
-        sum += __shfl_xor(sum, d);
+    for (int s = 32; s; s /= 2)
+        sum += __shfl_xor(sum, s);
     __shared__ double part[kThreads / 64];
     if ((threadIdx.x & 63) == 0)
         part[threadIdx.x / 64] = sum;
@@ -130,7 +144,9 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo)
     lo = static_cast<_Float16>(v - static_cast<float>(hi));
 }
 
-// X and X^T of 64 x 64 elements a workgroup, zeros past m and n.
+// X and X^T of 64 x 64 elements a workgroup, zeros past m and n; moved in runs
+// of eight elements, turned in LDS.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void start_kernel(OrthParams p)
 {
     __shared__ float tile[64][65];
@@ -138,40 +154,55 @@ __global__ __launch_bounds__(kThreads) void start_kernel(OrthParams p)
     double sum = 0.0;
     for (int k = threadIdx.x & 63; k < kNormBlocks; k += 64)
         sum += p.s.norms[b * kNormBlocks + k];
-    for (int d = 32; d; d /= 2)
-        sum += __shfl_xor(sum, d);
+    for (int s = 32; s; s /= 2)
+        sum += __shfl_xor(sum, s);
     const double norm = sqrt(sum) + static_cast<double>(p.eps);
-    // a NaN or an infinity anywhere gives NaN everywhere
     const double scale = norm > 0.0 ? kScaleX / norm : 0.0;
-    const float inv_nan = isfinite(norm) ? 0.0f : __builtin_nanf("");
+    // a NaN or an infinity anywhere gives NaN everywhere
+    const float nan = isfinite(norm) ? 0.0f : __builtin_nanf("");
     const uint32_t i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-    const bool rows_inner = p.in_row < p.in_col;
-    for (uint32_t k = threadIdx.x; k < 64 * 64; k += kThreads) {
-        const uint32_t fast = k & 63, slow = k >> 6;
-        const uint32_t i = rows_inner ? fast : slow, j = rows_inner ? slow : fast;
-        float v = 0.0f;
-        if (i0 + i < static_cast<uint32_t>(p.m) && j0 + j < static_cast<uint32_t>(p.n))
-            v = static_cast<float>(load_any(p.in, b * p.in_batch + (i0 + i) * p.in_row + (j0 + j) * p.in_col, p.in_dtype)
-                                   * scale)
-                + inv_nan;
-        tile[i][j] = v;
+    const bool d = down(p);
+#pragma unroll
+    for (uint32_t k = threadIdx.x; k < 512; k += kThreads) {
+        const uint32_t line = k >> 3, at = 8 * (k & 7);
+        float v[8];
+        load_line<T, 8>(p, b * p.in_batch, i0 + (d ? at : line), j0 + (d ? line : at), v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            tile[d ? at + e : line][d ? line : at + e] = static_cast<float>(v[e] * scale) + nan;
     }
     __syncthreads();
-    const uint64_t at = static_cast<uint64_t>(b) * p.mp * p.np;
-    for (uint32_t k = threadIdx.x; k < 64 * 64; k += kThreads) {
-        const uint32_t fast = k & 63, slow = k >> 6;
-        _Float16 hi, lo;
-        split(tile[slow][fast], hi, lo);
-        const uint64_t x = at + static_cast<uint64_t>(i0 + slow) * p.np + j0 + fast;
-        p.s.x[x] = hi;
-        p.s.x_lo[x] = lo;
-        if (p.s.x_full)
-            p.s.x_full[x] = tile[slow][fast];
-        split(tile[fast][slow], hi, lo);
-        const uint64_t xt = at + static_cast<uint64_t>(j0 + slow) * p.mp + i0 + fast;
-        p.s.xt[xt] = hi;
+    const uint64_t base = static_cast<uint64_t>(b) * p.mp * p.np;
+#pragma unroll
+    for (uint32_t k = threadIdx.x; k < 512; k += kThreads) {
+        const uint32_t line = k >> 3, at = 8 * (k & 7);
+        half8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            split(tile[line][at + e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        const uint64_t x = base + static_cast<uint64_t>(i0 + line) * p.np + j0 + at;
+        *reinterpret_cast<half8*>(p.s.x + x) = hi;
+        *reinterpret_cast<half8*>(p.s.x_lo + x) = lo;
+        if (p.s.x_full) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                p.s.x_full[x + e] = tile[line][at + e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            split(tile[at + e][line], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        const uint64_t xt = base + static_cast<uint64_t>(j0 + line) * p.mp + i0 + at;
+        *reinterpret_cast<half8*>(p.s.xt + xt) = hi;
         if (p.s.xt_lo)
-            p.s.xt_lo[xt] = lo;
+            *reinterpret_cast<half8*>(p.s.xt_lo + xt) = lo;
     }
 }
 
@@ -425,7 +456,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void gram_kernel(OrthParam
     const uint64_t x = static_cast<uint64_t>(blockIdx.y) * p.mp * p.np, o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
     Acc<S> acc;
     products<S>(factor(p.s.x + x, p.s.x_lo + x, ti * S::SIDE, p.np), factor(p.s.x + x, p.s.x_lo + x, tj * S::SIDE, p.np),
-                2 * p.np / kStepBytes, acc);
+                p.steps_n, acc);
     _Float16* hi = p.s.o + o;
     _Float16* lo = S::SPLIT ? p.s.o_lo + o : nullptr;
     float* d = p.s.d + blockIdx.y * p.mp;
@@ -454,7 +485,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void square_kernel(OrthPar
     const _Float16* o_hi = p.s.o + o;
     const _Float16* o_lo = S::SPLIT ? p.s.o_lo + o : nullptr;
     Acc<S> acc;
-    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), 2 * p.mp / kStepBytes, acc);
+    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, acc);
     _Float16* hi = p.s.b + o;
     _Float16* lo = S::SPLIT ? p.s.b_lo + o : nullptr;
     const float* d = p.s.d + blockIdx.y * p.mp;
@@ -493,7 +524,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void step_kernel(OrthParam
     const uint64_t x = static_cast<uint64_t>(b) * p.mp * p.np, o = static_cast<uint64_t>(b) * p.mp * p.mp;
     Acc<S> acc;
     products<S>(factor(p.s.b + o, p.s.b_lo + o, ti * S::SIDE, p.mp),
-                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), 2 * p.mp / kStepBytes, acc);
+                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), p.steps_m, acc);
     const float* d_b = p.s.d_b + b * p.mp;
     each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, const float16v& sum) {
         const uint64_t at = x + static_cast<uint64_t>(i) * p.np + j;
@@ -573,6 +604,13 @@ size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* b
     return at;
 }
 
+template <typename T>
+void launch_start(const OrthParams& p, int32_t batch, hipStream_t stream)
+{
+    norm_kernel<T><<<dim3(kNormBlocks, batch), kThreads, 0, stream>>>(p);
+    start_kernel<T><<<dim3(p.np / 64, p.mp / 64, batch), kThreads, 0, stream>>>(p);
+}
+
 // The symmetric products in tiles of G, B X in tiles of S.
 template <typename S, typename G = S>
 hipError_t run_steps(OrthParams p, int32_t batch, int32_t steps, hipStream_t stream)
@@ -624,14 +662,19 @@ hipError_t launch_orthogonalise(const sqn_batch& updates, int32_t steps, const f
     const int32_t side = tile_side(updates.batch, p.m, p.n, split_all);
     p.mp = up_to(p.m, side);
     p.np = up_to(p.n, side);
-    p.in_dtype = updates.dtype;
+    p.steps_m = (2 * p.m + kStepBytes - 1) / kStepBytes;
+    p.steps_n = (2 * p.n + kStepBytes - 1) / kStepBytes;
     p.out_dtype = out.dtype;
     p.a = coefficients[0];
     p.b = coefficients[1];
     p.c = coefficients[2];
     p.eps = eps;
-    norm_kernel<<<dim3(kNormBlocks, updates.batch), kThreads, 0, stream>>>(p);
-    start_kernel<<<dim3(p.np / 64, p.mp / 64, updates.batch), kThreads, 0, stream>>>(p);
+    if (updates.dtype == SQN_F32)
+        launch_start<float>(p, updates.batch, stream);
+    else if (updates.dtype == SQN_F16)
+        launch_start<_Float16>(p, updates.batch, stream);
+    else
+        launch_start<__bf16>(p, updates.batch, stream);
     if (steps == 0) {
         emit_kernel<<<dim3(1, p.m, updates.batch), kThreads, 0, stream>>>(p);
         return hipGetLastError();
