@@ -233,7 +233,7 @@ struct Shape {
     static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
     static constexpr int BUFFER = FACTORS * ROWS;
     static constexpr int LOADS = BUFFER / (1024 * WAVES);     // of a wave, a step
-    static constexpr int PER_SIMD = SIDE == 256 || 8 * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
+    static constexpr int PER_SIMD = SIDE == 256 || 4 * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
 };
 
 struct Factor {
@@ -245,11 +245,12 @@ template <typename S>
 __device__ __forceinline__ void bring_rows(const char* p, uint32_t row_bytes, uint32_t step, char* to)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t mine = (16 * wave + (lane >> 2)) * row_bytes + brought_piece(lane) * kSlot;
+    // a wave's groups of 8 rows have its own parity
+    const uint32_t mine = (8 * wave + (lane >> 3)) * row_bytes + brought_piece(lane, wave) * kSlot;
     p += static_cast<uint64_t>(step) * kStepBytes;
 #pragma unroll
-    for (int i = 0; i < S::SIDE / (16 * S::WAVES); ++i)
-        bring(p + static_cast<uint64_t>(16 * S::WAVES * i) * row_bytes + mine, to + (S::WAVES * i + wave) * 1024);
+    for (int i = 0; i < S::SIDE / (8 * S::WAVES); ++i)
+        bring(p + static_cast<uint64_t>(8 * S::WAVES * i) * row_bytes + mine, to + (S::WAVES * i + wave) * 1024);
 }
 
 template <typename S>
@@ -353,13 +354,11 @@ __device__ __forceinline__ void products(const Factor& p, const Factor& q, uint3
     // arrays of their own, so that reads of one do not wait for loads into another
     __shared__ __align__(16) char buffer0[S::BUFFER];
     __shared__ __align__(16) char buffer1[S::BUFFER];
-    __shared__ __align__(16) char buffer2[S::BUFFER];
-    __shared__ __align__(16) char buffer3[S::BUFFER];
     Acc<S> part, small;
     clear<S>(acc);
     clear<S>(small);
     pipeline<S::LOADS, Fragments<S>>(
-        steps, buffer0, buffer1, buffer2, buffer3, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
+        steps, buffer0, buffer1, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
         [&](Fragments<S>& f, const char* buffer, uint32_t o) { read_fragments<S>(f, buffer, o); },
         [&](const Fragments<S>& f, int depth) {
             if constexpr (S::SPLIT) {
@@ -373,7 +372,7 @@ __device__ __forceinline__ void products(const Factor& p, const Factor& q, uint3
             }
         });
     if constexpr (S::SPLIT) {
-        if (steps % 4)
+        if (steps % 2)
             add<S>(acc, part);
         add<S>(acc, small);
     }

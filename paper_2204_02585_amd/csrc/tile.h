@@ -1,20 +1,22 @@
 // Tiles of products C = P Q^T whose factors have their rows contiguous along
 // the sum, on the 32 x 32 matrix instructions.
 //
-// A workgroup computes a tile of C.  The sum goes in steps of 64 bytes of every
-// row (32 binary16 or 128 4-bit elements), whose rows stream from global memory
-// straight into one of four LDS buffers, three steps ahead.  A step is two
-// instructions deep: instruction o takes from row r, in lane r % 32 + 32 g, the
-// row's 16-byte piece 2 g + o.  (Any assignment of pieces to lanes gives the
-// same sum; with this one a lane's scales of 4-bit elements lie side by side.)
-// Piece c of row r lies in slot c ^ (r / 4 % 4) of its row: four rows take the
-// 64 banks once, so of the lanes that LDS serves together those whose rows are
-// the same modulo 4 must differ in their slot.
+// A workgroup computes a tile of C.  The sum goes in steps of 128 bytes (a
+// line of the caches) of every row, 64 binary16 or 256 4-bit elements, whose
+// rows stream from global memory straight into one of two LDS buffers.  A step
+// is four instructions deep: instruction o takes from row r, in lane r % 32 +
+// 32 g, the row's 16-byte piece 4 g + o.  (Any assignment of pieces to lanes
+// gives the same sum; with this one a lane's scales of 4-bit elements lie side
+// by side.)  Piece c of row r lies in slot c ^ (r / 2 % 8) of its row: two rows
+// take the 64 banks once, so of the lanes that LDS serves together those in rows
+// of one parity must differ in their slot (with r % 8 a third of the LDS
+// cycles were conflicts).
 //
-// The first fragments of a step are read before its barrier, between the
-// products of the step before: its rows have been there since the last one.
-// (Steps of 128 bytes in two buffers, whose first reads follow the barrier,
-// leave the matrix cores idle for a third of the time.)
+// A depth's fragments are read between the products of the one before.  The
+// barrier of a step stands before its last depth, whose fragments are then in
+// registers: behind it the buffer takes the step after the next, and the next
+// step's first fragments can be read at once.  So a step's loads have a
+// whole step to land, and no reads wait behind a barrier.
 //
 // A wave's part of C is FM x FN accumulators of 32 x 32: element q of a lane is
 // row 8 (q / 4) + 4 (lane / 32) + q % 4, column lane % 32.  Two waves share a
@@ -29,28 +31,32 @@ namespace sqn {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-constexpr uint32_t kStepBytes = 64;          // of a row, a step
+constexpr uint32_t kStepBytes = 128;         // of a row, a step
 constexpr uint32_t kSlot = 16;
 constexpr uint32_t kBlockBytes = 32 * kStepBytes;    // of the rows of an instruction
+constexpr int kDepths = 4;
 
-// 16 rows of a step, 64 pieces, by one wave: lane l brings slot l % 4 of row l / 4.
+// 8 rows of a step, 64 pieces, by one wave: lane l brings slot l % 8 of row l / 8.
 // `from` is the lane's own piece, `to` the wave's 1024 bytes.
 __device__ __forceinline__ void bring(const char* from, char* to)
 {
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(from), reinterpret_cast<uint32_t*>(to), kSlot, 0, 0);
 }
 
-// The piece that a lane brings.
-__device__ __forceinline__ uint32_t brought_piece(uint32_t lane) { return (lane & 3) ^ (lane >> 4); }
-
-// Byte of piece 2 (lane / 32) + o of row lane % 32, from the wave's first row.
-__device__ __forceinline__ uint32_t piece_at(uint32_t lane, uint32_t o)
+// The piece that a lane brings into the group of 8 rows `group`.
+__device__ __forceinline__ uint32_t brought_piece(uint32_t lane, uint32_t group)
 {
-    return (lane & 31) * kStepBytes + ((2 * (lane >> 5) + o) ^ (lane >> 2 & 3)) * kSlot;
+    return (lane & 7) ^ (4 * (group & 1) + (lane >> 4));
 }
 
-// All but the LATER newest of this wave's loads into LDS have landed, its reads
-// are done, and so for every wave of the workgroup.
+// Byte of piece 4 (lane / 32) + o of row lane % 32, from the wave's first row.
+__device__ __forceinline__ uint32_t piece_at(uint32_t lane, uint32_t o)
+{
+    return (lane & 31) * kStepBytes + ((4 * (lane >> 5) + o) ^ (lane >> 1 & 7)) * kSlot;
+}
+
+// This wave's loads into LDS but the LATER newest have landed, its reads are
+// done, and so for every wave of the workgroup.
 template <int LATER>
 __device__ __forceinline__ void landed()
 {
@@ -65,42 +71,38 @@ __device__ __forceinline__ void landed()
 
 // The steps of a tile's sum.  bring(step, buffer) issues LOADS loads a wave,
 // read(fragments, buffer, o) reads a depth's fragments and multiply(fragments,
-// depth) multiplies them: the steps go in rounds of four, of eight depths; the
-// last round may end early.
+// depth) multiplies them: the steps go in pairs, of eight depths; the last
+// step may be alone.
 template <int LOADS, typename Fragments, typename B, typename R, typename M>
-__device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, char* b2, char* b3, B bring_step, R read,
-                                         M multiply)
+__device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, B bring_step, R read, M multiply)
 {
     const uint32_t end = steps - 1;
     Fragments f0, f1;
     bring_step(0, b0);
     bring_step(min(1u, end), b1);
-    bring_step(min(2u, end), b2);
-    landed<2 * LOADS>();
+    landed<LOADS>();
     read(f0, b0, 0);
-    // `buffer` holds step k, `next` k + 1, `free` will hold k + 3; past the end
-    // the last step comes once more and is not used
-    auto work = [&](uint32_t k, int in_round, char* buffer, char* next, char* free) {
-        landed<LOADS>();
-        bring_step(min(k + in_round + 3, end), free);
+    // `buffer` holds step k and will hold k + 2; past the end the last step
+    // comes once more and is not used
+    auto work = [&](uint32_t k, int depth, char* buffer, char* next) {
         read(f1, buffer, 1);
-        multiply(f0, 2 * in_round);
+        multiply(f0, depth);
+        read(f0, buffer, 2);
+        multiply(f1, depth + 1);
+        read(f1, buffer, 3);
+        multiply(f0, depth + 2);
+        landed<0>();
+        bring_step(min(k + 2, end), buffer);
         read(f0, next, 0);
-        multiply(f1, 2 * in_round + 1);
+        multiply(f1, depth + 3);
     };
     uint32_t k = 0;
-    for (; k + 4 <= steps; k += 4) {
-        work(k, 0, b0, b1, b3);
-        work(k, 1, b1, b2, b0);
-        work(k, 2, b2, b3, b1);
-        work(k, 3, b3, b0, b2);
+    for (; k + 2 <= steps; k += 2) {
+        work(k, 0, b0, b1);
+        work(k + 1, 4, b1, b0);
     }
     if (k < steps)
-        work(k, 0, b0, b1, b3);
-    if (k + 1 < steps)
-        work(k, 1, b1, b2, b0);
-    if (k + 2 < steps)
-        work(k, 2, b2, b3, b1);
+        work(k, 0, b0, b1);
     // the loads still under way end before their buffers do
     landed<0>();
 }
