@@ -478,19 +478,22 @@ sqn_status sqn_quantised_values(const sqn_quantised* x, const sqn_matrix* out, v
 /* A layer on 4-bit blocks: out = act(x w^T + bias), [points][units], with x
  * [points][cols] and w [units][cols] in blocks, products and sums in
  * binary32, rounded once to out's dtype; act is max(0, .) (a NaN stays) for
- * relu = 1 and nothing for 0.
- *   bias: device, binary32 [units], or NULL.
+ * relu = 1 and nothing for 0.  units >= 1.
+ *   bias:      device, binary32 [units], or NULL;
+ *   workspace: sqn_quantised_product_workspace(points, units, cols) bytes.
  * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_UNSUPPORTED (more than 2^23 tiles of
  * 64 x 64 in out), SQN_ERR_DEVICE. */
 sqn_status sqn_quantised_product(const sqn_quantised* x, const sqn_quantised* w, const float* bias, int32_t relu,
-                                 const sqn_matrix* out, void* stream);
+                                 const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t sqn_quantised_product_workspace(int64_t points, int64_t units, int64_t cols);
 
-/* sqn_quantise of x, then sqn_quantised_product of it: the same values.
- *   workspace: sqn_quantised_layer_workspace(x->rows, x->cols) bytes.
+/* The same with x [points][cols] quantised in the call, as sqn_quantise does
+ * it; the sums may be taken in another order.
+ *   workspace: sqn_quantised_layer_workspace(points, units, cols) bytes.
  * Errors: those of sqn_quantised_product. */
 sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, const float* bias, int32_t relu,
                                const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream);
-size_t sqn_quantised_layer_workspace(int64_t rows, int64_t cols);
+size_t sqn_quantised_layer_workspace(int64_t points, int64_t units, int64_t cols);
 
 /* Ray space of later renders with this handle.  ndc_near = 0 (the default):
  * world rays as above.  ndc_near > 0: forward-facing captures (the LLFF

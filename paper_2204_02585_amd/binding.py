@@ -25,7 +25,7 @@ EXPORTS = ("sqn_create_caches", "sqn_create_linear_caches", "sqn_recreate_caches
            "sqn_destroy", "sqn_status_string", "sqn_last_error", "sqn_create_networks",
            "sqn_generate_caches", "sqn_networks_device_bytes", "sqn_destroy_networks",
            "sqn_lookup", "sqn_lookup_gradient", "sqn_lookup_gradient_workspace", "sqn_orthogonalise",
-           "sqn_orthogonalise_workspace", "sqn_quantise", "sqn_quantised_values", "sqn_quantised_product",
+           "sqn_orthogonalise_workspace", "sqn_quantise", "sqn_quantised_values", "sqn_quantised_product", "sqn_quantised_product_workspace",
            "sqn_quantised_layer", "sqn_quantised_layer_workspace")
 
 
@@ -137,9 +137,10 @@ def _load() -> ctypes.CDLL:
             ("sqn_orthogonalise_workspace", size, [i32, i32, i32, i32]),
             ("sqn_quantise", ctypes.c_int, [mat, quant, vp]),
             ("sqn_quantised_values", ctypes.c_int, [quant, mat, vp]),
-            ("sqn_quantised_product", ctypes.c_int, [quant, quant, vp, i32, mat, vp]),
+            ("sqn_quantised_product", ctypes.c_int, [quant, quant, vp, i32, mat, vp, size, vp]),
+            ("sqn_quantised_product_workspace", size, [i64, i64, i64]),
             ("sqn_quantised_layer", ctypes.c_int, [mat, quant, vp, i32, mat, vp, size, vp]),
-            ("sqn_quantised_layer_workspace", size, [i64, i64])):
+            ("sqn_quantised_layer_workspace", size, [i64, i64, i64])):
         call = getattr(lib, name)
         call.restype, call.argtypes = result, args
     lib.sqn_status_string.restype = ctypes.c_char_p

@@ -31,9 +31,10 @@ constexpr int64_t quant_blocks(int64_t cols) { return (cols + kQuantBlock - 1) /
 
 hipError_t launch_quantise(const sqn_matrix& x, const sqn_quantised& out, hipStream_t stream);
 hipError_t launch_quantised_values(const sqn_quantised& x, const sqn_matrix& out, hipStream_t stream);
+size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols);
 hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised& w, const float* bias, bool relu,
-                                    const sqn_matrix& out, hipStream_t stream);
-size_t quantised_layer_bytes(int64_t rows, int64_t cols);
+                                    const sqn_matrix& out, void* workspace, hipStream_t stream);
+size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols);
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
                                   const sqn_matrix& out, void* workspace, hipStream_t stream);
 

@@ -202,6 +202,8 @@ sqn_status check_layer(int64_t points, int64_t cols, const sqn_quantised* w, con
     if (cols != w->cols)
         return fail(SQN_ERR_INVALID_ARG, "x has %lld columns, w %lld", static_cast<long long>(cols),
                     static_cast<long long>(w->cols));
+    if (w->rows < 1)
+        return fail(SQN_ERR_INVALID_ARG, "w has no rows");
     if (out->rows != points || out->cols != w->rows)
         return fail(SQN_ERR_INVALID_ARG, "out is %lld x %lld, the product %lld x %lld", static_cast<long long>(out->rows),
                     static_cast<long long>(out->cols), static_cast<long long>(points), static_cast<long long>(w->rows));
@@ -216,6 +218,11 @@ sqn_status check_layer(int64_t points, int64_t cols, const sqn_quantised* w, con
         return check_device_range(bias, static_cast<size_t>(w->rows) * 4, "bias");
     }
     return SQN_OK;
+}
+
+bool valid_layer(int64_t points, int64_t units, int64_t cols)
+{
+    return points >= 0 && points <= kMaxRows && units >= 1 && units <= kMaxRows && cols >= 1 && cols <= kMaxCols;
 }
 
 sqn_status launched(hipError_t e, const char* what)
@@ -343,8 +350,15 @@ sqn_status sqn_quantised_values(const sqn_quantised* x, const sqn_matrix* out, v
     return launched(sqn::launch_quantised_values(*x, *out, static_cast<hipStream_t>(stream)), "values");
 }
 
+size_t sqn_quantised_product_workspace(int64_t points, int64_t units, int64_t cols)
+{
+    if (!valid_layer(points, units, cols))
+        return 0;
+    return sqn::quantised_product_bytes(points, units, cols);
+}
+
 sqn_status sqn_quantised_product(const sqn_quantised* x, const sqn_quantised* w, const float* bias, int32_t relu,
-                                 const sqn_matrix* out, void* stream)
+                                 const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream)
 {
     sqn_status s = check_quantised(x, "x");
     if (s != SQN_OK)
@@ -353,15 +367,19 @@ sqn_status sqn_quantised_product(const sqn_quantised* x, const sqn_quantised* w,
         return s;
     if (x->rows == 0)
         return SQN_OK;
-    return launched(sqn::launch_quantised_product(*x, *w, bias, relu != 0, *out, static_cast<hipStream_t>(stream)),
+    if ((s = check_workspace(workspace, workspace_bytes, sqn::quantised_product_bytes(x->rows, w->rows, x->cols)))
+        != SQN_OK)
+        return s;
+    return launched(sqn::launch_quantised_product(*x, *w, bias, relu != 0, *out, workspace,
+                                                  static_cast<hipStream_t>(stream)),
                     "product");
 }
 
-size_t sqn_quantised_layer_workspace(int64_t rows, int64_t cols)
+size_t sqn_quantised_layer_workspace(int64_t points, int64_t units, int64_t cols)
 {
-    if (rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols)
+    if (!valid_layer(points, units, cols))
         return 0;
-    return sqn::quantised_layer_bytes(rows, cols);
+    return sqn::quantised_layer_bytes(points, units, cols);
 }
 
 sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, const float* bias, int32_t relu,
@@ -374,7 +392,8 @@ sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, cons
         return s;
     if (x->rows == 0)
         return SQN_OK;
-    if ((s = check_workspace(workspace, workspace_bytes, sqn::quantised_layer_bytes(x->rows, x->cols))) != SQN_OK)
+    if ((s = check_workspace(workspace, workspace_bytes, sqn::quantised_layer_bytes(x->rows, w->rows, x->cols)))
+        != SQN_OK)
         return s;
     return launched(sqn::launch_quantised_layer(*x, *w, bias, relu != 0, *out, workspace,
                                                 static_cast<hipStream_t>(stream)),

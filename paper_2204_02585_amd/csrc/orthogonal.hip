@@ -358,7 +358,7 @@ __device__ __forceinline__ void products(const Factor& p, const Factor& q, uint3
     clear<S>(acc);
     clear<S>(small);
     pipeline<S::LOADS, Fragments<S>>(
-        steps, buffer0, buffer1, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
+        steps, buffer0, buffer1, [](uint32_t, int) {}, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
         [&](Fragments<S>& f, const char* buffer, uint32_t o) { read_fragments<S>(f, buffer, o); },
         [&](const Fragments<S>& f, int depth) {
             if constexpr (S::SPLIT) {

@@ -3,13 +3,13 @@
 #include "learn.h"
 #include "numeric.h"
 #include "sqn_internal.h"
+#include "tile.h"
 
 namespace sqn {
 namespace {
 
 typedef int int8v __attribute__((ext_vector_type(8)));
 typedef int int4v __attribute__((ext_vector_type(4)));
-typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr uint32_t kOne = 127;           // E8M0 of 1
@@ -25,6 +25,60 @@ struct QuantParams {
     int64_t stride;          // elements
     uint32_t cols, blocks;
 };
+
+// ---- scales beside the tiles' products
+//
+// An instruction of a tile takes 32 rows, and a lane of it a scale byte, that
+// of block 8 k + 4 g + o of row lane % 32 for instruction o of step k, with g =
+// lane / 32.  The packed scales of a matrix hold these bytes as the lanes take
+// them: a word for each of 64 lanes (o its byte) for each step of each 32 rows.
+// Blocks past the matrix's have the scale of 1, so that the zeros there stay
+// zeros.
+
+struct PackedScales {
+    uint8_t* to;             // [rows / 32, rounded up to a tile][steps][64] words
+    uint32_t steps;
+};
+
+__host__ __device__ constexpr uint32_t steps_of(uint32_t blocks) { return (blocks + 7) / 8; }
+
+// Where the byte of a row's block lies.
+__device__ __forceinline__ uint64_t packed_at(uint32_t row, uint32_t block, uint32_t steps)
+{
+    const uint32_t lane = (row & 31) + 32 * (block >> 2 & 1);
+    return (static_cast<uint64_t>(row >> 5) * steps + (block >> 3)) * 256 + 4 * lane + (block & 3);
+}
+
+struct PackParams {
+    const uint8_t* from;     // [rows][blocks]
+    PackedScales packed;
+    uint64_t words;          // rows * steps * 2
+    uint32_t blocks;
+};
+
+// A workgroup's share of the words: row by row, a word of four blocks a thread.
+__device__ __forceinline__ void pack_share(const PackParams& p, uint32_t group, uint32_t groups)
+{
+    const uint32_t per_row = 2 * p.packed.steps;
+    for (uint64_t i = static_cast<uint64_t>(group) * kThreads + threadIdx.x; i < p.words;
+         i += static_cast<uint64_t>(groups) * kThreads) {
+        const uint32_t row = static_cast<uint32_t>(i / per_row), block = 4 * static_cast<uint32_t>(i - row * static_cast<uint64_t>(per_row));
+        uint32_t word = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+            word |= (block + k < p.blocks ? p.from[static_cast<uint64_t>(row) * p.blocks + block + k] : kOne) << (8 * k);
+        *reinterpret_cast<uint32_t*>(p.packed.to + packed_at(row, block, p.packed.steps)) = word;
+    }
+}
+
+// Two matrices' scales (of Quantised factors).
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackParams a, PackParams b, uint32_t groups_a)
+{
+    if (blockIdx.x < groups_a)
+        pack_share(a, blockIdx.x, groups_a);
+    else
+        pack_share(b, blockIdx.x - groups_a, gridDim.x - groups_a);
+}
 
 // The largest magnitude's exponent field (0 for subnormals and zero) to the
 // block's scale byte; 255 marks a NaN or an infinity.
@@ -94,6 +148,34 @@ __global__ __launch_bounds__(kThreads) void quantise_kernel(QuantParams p)
     }
 }
 
+// x to blocks with their scales packed, and by further workgroups the scales
+// of w.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void quantise_packed_kernel(QuantParams p, PackedScales packed, PackParams w,
+                                                                   uint32_t groups)
+{
+    if (blockIdx.x >= groups) {
+        pack_share(w, blockIdx.x - groups, gridDim.x - groups);
+        return;
+    }
+    // all blocks of the steps, the scales of those past the matrix too
+    const uint32_t per_row = 32 * packed.steps;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.items;
+         i += static_cast<uint64_t>(groups) * kThreads) {
+        const uint32_t r = static_cast<uint32_t>(i / per_row);
+        const uint32_t q = static_cast<uint32_t>(i - r * static_cast<uint64_t>(per_row)), block = q >> 2;
+        uint32_t byte = kOne;
+        if (block < p.blocks) {
+            float v[8];
+            load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols, v);
+            byte = shared_scale(v);
+            reinterpret_cast<uint32_t*>(p.codes)[static_cast<uint64_t>(r) * 4 * p.blocks + q] = encode8(v, byte);
+        }
+        if ((q & 3) == 0)
+            packed.to[packed_at(r, block, packed.steps)] = static_cast<uint8_t>(byte);
+    }
+}
+
 // the magnitude of a 3-bit code, from the bits of binary32: subnormal 0.5, then 1 + m / 2
 __device__ __forceinline__ float decode1(uint32_t code)
 {
@@ -140,120 +222,283 @@ uint32_t stream_blocks(uint64_t items)
 
 // ---- products
 //
-// out^T = W x^T on v_mfma_scale_f32_16x16x128_f8f6f4: W is the first factor,
-// so a lane ends with four consecutive units of one point.  A lane's share of
-// a factor is one block of one row, 16 bytes, with its scale.
+// out^T = W x^T on v_mfma_scale_f32_32x32x64_f8f6f4, in the tiles of tile.h:
+// W is the first factor, so a lane holds units of one point, of which a swap
+// between the halves of a wave makes sixteen in a row.
 
 struct ProductParams {
-    const uint8_t *x, *x_scales, *w, *w_scales;
+    const uint8_t *x, *x_packed, *w, *w_packed;
     const float* bias;
     void* out;
     int64_t out_stride;
-    uint32_t points, units, blocks;
-    int32_t relu, dtype;
+    uint32_t points, units, blocks, steps;
+    int32_t relu;
 };
 
-struct Fragment {
-    int8v codes;
-    int scale;
+template <int SIDE_>
+struct Shape {
+    static constexpr int SIDE = SIDE_;
+    static constexpr int WN = SIDE == 256 ? 4 : 2;
+    static constexpr int WAVES = 2 * WN, THREADS = 64 * WAVES;
+    static constexpr int FM = SIDE / 64, FN = SIDE / (32 * WN);    // blocks of units and points of a wave
+    static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
+    static constexpr int BUFFER = 2 * ROWS;
+    static constexpr int LOADS = BUFFER / (1024 * WAVES);
+    static constexpr int BRINGS = LOADS / 2;                       // of either factor
 };
 
-__device__ __forceinline__ Fragment load_fragment(const uint8_t* codes, const uint8_t* scales, uint32_t row,
-                                                  uint32_t block, uint32_t blocks)
+template <typename S>
+struct Fragments {
+    int4v w[S::FM], x[S::FN];
+};
+
+// what lanes bring whose piece lies past the row
+__device__ const int4v kZeros = {0, 0, 0, 0};
+
+template <typename S>
+__device__ __forceinline__ void bring_rows(const uint8_t* rows, const uint32_t (&at)[S::BRINGS], bool inside, uint32_t k,
+                                           char* to)
 {
-    Fragment f;
-    int4v c = {0, 0, 0, 0};
-    f.scale = kOne;
-    if (block < blocks) {
-        const uint64_t at = static_cast<uint64_t>(row) * blocks + block;
-        c = *reinterpret_cast<const int4v*>(codes + 16 * at);
-        f.scale = scales[at];
+    const uint32_t wave = threadIdx.x >> 6;
+    const char* from = reinterpret_cast<const char*>(rows) + static_cast<uint64_t>(k) * kStepBytes;
+#pragma unroll
+    for (int i = 0; i < S::BRINGS; ++i)
+        bring(inside ? from + at[i] : reinterpret_cast<const char*>(&kZeros), to + (S::WAVES * i + wave) * 1024);
+}
+
+template <int O>
+__device__ __forceinline__ float16v multiply(int4v a, int4v b, int scale_a, int scale_b, float16v acc)
+{
+    const int8v a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+    const int8v b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, acc, 4, 4, O, scale_a, O, scale_b);
+}
+
+template <typename S, int O>
+__device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, const int (&scale_w)[S::FM],
+                                                   const int (&scale_x)[S::FN], float16v (&acc)[S::FM][S::FN])
+{
+    constexpr int READS = S::FM + S::FN, PRODUCTS = S::FM * S::FN;
+#pragma unroll
+    for (int s = 0; s < S::FM; ++s)
+#pragma unroll
+        for (int t = 0; t < S::FN; ++t)
+            acc[s][t] = multiply<O>(f.w[s], f.x[t], scale_w[s], scale_x[t], acc[s][t]);
+    constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+    for (int k = 0; k < PRODUCTS; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
     }
-    f.codes = int8v{c[0], c[1], c[2], c[3], 0, 0, 0, 0};
-    return f;
 }
 
-__device__ __forceinline__ float4v multiply(const Fragment& a, const Fragment& b, float4v acc)
+// Bias, activation and rounding of a block, and its store: element q of the
+// lane is unit + row_of(q), of `point`; `unit` and `point` of element 0.
+template <typename T>
+__device__ __forceinline__ void store_units(const ProductParams& p, uint32_t unit, uint32_t point, const float16v& acc)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.codes, b.codes, acc, 4, 4, 0, a.scale, 0, b.scale);
-}
-
-// Bias and activation; the store is of the units inside the matrix.
-__device__ __forceinline__ void finish4(const ProductParams& p, uint32_t unit, uint32_t point, float4v acc)
-{
+    constexpr int WORDS = sizeof(T);         // of four units
+    const uint32_t half = (threadIdx.x >> 5) & 1;
+    uint32_t word[4][WORDS];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        T e[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float v = acc[4 * g + r];
+            const uint32_t u = unit + 8 * g + r;
+            if (p.bias)
+                v += p.bias[min(u, p.units - 1)];
+            if (p.relu)
+                v = v < 0.0f ? 0.0f : v;
+            e[r] = from_f32<T>(v);
+        }
+        __builtin_memcpy(word[g], e, sizeof(e));
+    }
+    // the lower half of the wave gives its groups 2 and 3 for the upper half's 0 and 1
+    Run<T, 16> row;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            const auto swapped = __builtin_amdgcn_permlane32_swap(word[g][w], word[g + 2][w], false, false);
+            row.word[2 * g * WORDS + w] = swapped[0];
+            row.word[(2 * g + 1) * WORDS + w] = swapped[1];
+        }
     if (point >= p.points)
         return;
+    const uint32_t first = unit - 4 * half + 16 * half;
+    T* to = static_cast<T*>(p.out) + point * p.out_stride + first;
+    if (first + 16 <= p.units) {
+        *reinterpret_cast<Run<T, 16>*>(to) = row;
+    } else {
+        T e[16];
+        __builtin_memcpy(e, &row, sizeof(e));
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (unit + q >= p.units)
-            return;
-        float v = acc[q];
-        if (p.bias)
-            v += p.bias[unit + q];
-        if (p.relu)
-            v = v < 0.0f ? 0.0f : v;
-        const int64_t at = point * p.out_stride + unit + q;
-        if (p.dtype == SQN_F32)
-            static_cast<float*>(p.out)[at] = v;
-        else if (p.dtype == SQN_F16)
-            static_cast<_Float16*>(p.out)[at] = static_cast<_Float16>(v);
-        else
-            static_cast<__bf16*>(p.out)[at] = static_cast<__bf16>(v);
+        for (int k = 0; k < 16; ++k)
+            if (first + k < p.units)
+                to[k] = e[k];
     }
 }
 
-__global__ __launch_bounds__(kThreads) void product_kernel(ProductParams p)
+template <typename S, typename T>
+__global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
 {
+    // arrays of their own, so that reads of one do not wait for loads into another
+    __shared__ __align__(16) char buffer0[S::BUFFER];
+    __shared__ __align__(16) char buffer1[S::BUFFER];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t point_tiles = (p.points + 63) / 64;
-    const uint32_t ti = blockIdx.x / point_tiles, tj = blockIdx.x - ti * point_tiles;
-    const uint32_t unit0 = ti * 64 + (wave & 1) * 32, point0 = tj * 64 + (wave >> 1) * 32;
-    uint32_t unit[2], point[2];
-    float4v acc[2][2];
+    const uint32_t unit_tiles = (p.units + S::SIDE - 1) / S::SIDE;
+    const uint32_t tj = blockIdx.x / unit_tiles, ti = blockIdx.x - tj * unit_tiles;
+    const uint32_t unit0 = ti * S::SIDE, point0 = tj * S::SIDE;
+    const uint32_t row_bytes = 16 * p.blocks;
+    const uint8_t* w = p.w + static_cast<uint64_t>(unit0) * row_bytes;
+    const uint8_t* x = p.x + static_cast<uint64_t>(point0) * row_bytes;
+    // this lane's pieces; rows past the end read the last one, and are not stored
+    const uint32_t piece = brought_piece(lane, wave);
+    uint32_t w_at[S::BRINGS], x_at[S::BRINGS];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        // rows past the end read the last one, and are not stored
-        unit[s] = min(unit0 + 16 * s + (lane & 15), p.units - 1);
-        point[s] = min(point0 + 16 * s + (lane & 15), p.points - 1);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            acc[s][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < S::BRINGS; ++i) {
+        const uint32_t row = 8 * (S::WAVES * i + wave) + (lane >> 3);
+        w_at[i] = min(row, p.units - 1 - unit0) * row_bytes + piece * kSlot;
+        x_at[i] = min(row, p.points - 1 - point0) * row_bytes + piece * kSlot;
     }
-    for (uint32_t k = lane >> 4; k < (p.blocks + 3) / 4 * 4; k += 4) {
-        Fragment a[2], b[2];
+    const uint32_t wave_u = (wave & 1) * S::FM, wave_p = (wave >> 1) * S::FN;      // blocks of 32
+    const int* w_packed = reinterpret_cast<const int*>(p.w_packed) + static_cast<uint64_t>(unit0 / 32 + wave_u) * p.steps * 64 + lane;
+    const int* x_packed = reinterpret_cast<const int*>(p.x_packed) + static_cast<uint64_t>(point0 / 32 + wave_p) * p.steps * 64 + lane;
+    int scale_w[2][S::FM], scale_x[2][S::FN];
+    float16v acc[S::FM][S::FN];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            a[s] = load_fragment(p.w, p.w_scales, unit[s], k, p.blocks);
-            b[s] = load_fragment(p.x, p.x_scales, point[s], k, p.blocks);
-        }
+    for (int s = 0; s < S::FM; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int t = 0; t < S::FN; ++t)
+            acc[s][t] = float16v{};
+    pipeline<S::LOADS, Fragments<S>>(
+        p.steps, buffer0, buffer1,
+        [&](uint32_t k, int in_pair) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                acc[s][t] = multiply(a[s], b[t], acc[s][t]);
-    }
+            for (int s = 0; s < S::FM; ++s)
+                scale_w[in_pair][s] = w_packed[(s * p.steps + k) * 64];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+            for (int t = 0; t < S::FN; ++t)
+                scale_x[in_pair][t] = x_packed[(t * p.steps + k) * 64];
+        },
+        [&](uint32_t k, char* buffer) {
+            const bool inside = 8 * k + piece < p.blocks;
+            bring_rows<S>(w, w_at, inside, k, buffer);
+            bring_rows<S>(x, x_at, inside, k, buffer + S::ROWS);
+            // the loads stay ahead of the products that hide them
+            __builtin_amdgcn_sched_barrier(0);
+        },
+        [&](Fragments<S>& f, const char* buffer, uint32_t o) {
+            const char* from_w = buffer + wave_u * kBlockBytes + piece_at(lane, o);
+            const char* from_x = buffer + S::ROWS + wave_p * kBlockBytes + piece_at(lane, o);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-            finish4(p, unit0 + 16 * s + 4 * (lane >> 4), point0 + 16 * t + (lane & 15), acc[s][t]);
+            for (int s = 0; s < S::FM; ++s)
+                f.w[s] = *reinterpret_cast<const int4v*>(from_w + s * kBlockBytes);
+#pragma unroll
+            for (int t = 0; t < S::FN; ++t)
+                f.x[t] = *reinterpret_cast<const int4v*>(from_x + t * kBlockBytes);
+        },
+        [&](const Fragments<S>& f, int depth) {
+            const int k = depth >> 2;
+            switch (depth & 3) {
+            case 0: multiply_fragments<S, 0>(f, scale_w[k], scale_x[k], acc); break;
+            case 1: multiply_fragments<S, 1>(f, scale_w[k], scale_x[k], acc); break;
+            case 2: multiply_fragments<S, 2>(f, scale_w[k], scale_x[k], acc); break;
+            default: multiply_fragments<S, 3>(f, scale_w[k], scale_x[k], acc); break;
+            }
+        });
+    each_block<S::FM, S::FN>(acc, [&](uint32_t i, uint32_t j, const float16v& v) {
+        store_units<T>(p, unit0 + 32 * wave_u + i, point0 + 32 * wave_p + j, v);
+    });
 }
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// The packed scales of a product's factors, rows up to whole tiles.
+struct ProductScratch {
+    PackedScales x_packed, w_packed;
+    size_t bytes;
+
+    ProductScratch(int64_t points, int64_t units, int64_t cols, void* base)
+    {
+        const uint32_t steps = steps_of(static_cast<uint32_t>(quant_blocks(cols)));
+        auto size = [&](int64_t rows) { return static_cast<size_t>((rows + 255) / 256) * 8 * steps * 256; };
+        x_packed.to = static_cast<uint8_t*>(base);
+        w_packed.to = x_packed.to + size(points);
+        x_packed.steps = w_packed.steps = steps;
+        bytes = size(points) + size(units);
+    }
+};
+
+PackParams pack_of(const sqn_quantised& x, const PackedScales& packed)
+{
+    PackParams p;
+    p.from = static_cast<const uint8_t*>(x.scales);
+    p.packed = packed;
+    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
+    p.words = static_cast<uint64_t>(x.rows) * packed.steps * 2;
+    return p;
+}
+
+QuantParams quant_of(const sqn_matrix& x, const sqn_quantised& q)
+{
+    QuantParams p;
+    p.x = x.data;
+    p.values = nullptr;
+    p.codes = static_cast<uint8_t*>(q.codes);
+    p.scales = static_cast<uint8_t*>(q.scales);
+    p.stride = x.row_stride;
+    p.cols = static_cast<uint32_t>(x.cols);
+    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
+    p.items = static_cast<uint64_t>(x.rows) * p.blocks * 4;
+    return p;
+}
+
+template <typename S>
+void launch_shape(const ProductParams& p, int32_t dtype, hipStream_t stream)
+{
+    const uint32_t grid = (p.points + S::SIDE - 1) / S::SIDE * ((p.units + S::SIDE - 1) / S::SIDE);
+    if (dtype == SQN_F32)
+        product_kernel<S, float><<<grid, S::THREADS, 0, stream>>>(p);
+    else if (dtype == SQN_F16)
+        product_kernel<S, _Float16><<<grid, S::THREADS, 0, stream>>>(p);
+    else
+        product_kernel<S, __bf16><<<grid, S::THREADS, 0, stream>>>(p);
+}
+
+hipError_t launch_tiles(const sqn_quantised& x, const ProductScratch& t, const sqn_quantised& w, const float* bias,
+                        bool relu, const sqn_matrix& out, hipStream_t stream)
+{
+    ProductParams p;
+    p.x = static_cast<const uint8_t*>(x.codes);
+    p.x_packed = t.x_packed.to;
+    p.w = static_cast<const uint8_t*>(w.codes);
+    p.w_packed = t.w_packed.to;
+    p.bias = bias;
+    p.out = out.data;
+    p.out_stride = out.row_stride;
+    p.points = static_cast<uint32_t>(x.rows);
+    p.units = static_cast<uint32_t>(w.rows);
+    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
+    p.steps = t.x_packed.steps;
+    p.relu = relu ? 1 : 0;
+    auto tiles = [&](int64_t side) { return ((p.points + side - 1) / side) * ((p.units + side - 1) / side); };
+    if (tiles(256) >= 200)
+        launch_shape<Shape<256>>(p, out.dtype, stream);
+    else if (tiles(128) >= 200)
+        launch_shape<Shape<128>>(p, out.dtype, stream);
+    else
+        launch_shape<Shape<64>>(p, out.dtype, stream);
+    return hipGetLastError();
+}
 
 }  // namespace
 
 hipError_t launch_quantise(const sqn_matrix& x, const sqn_quantised& out, hipStream_t stream)
 {
-    QuantParams p;
-    p.x = x.data;
-    p.values = nullptr;
-    p.codes = static_cast<uint8_t*>(out.codes);
-    p.scales = static_cast<uint8_t*>(out.scales);
-    p.stride = x.row_stride;
-    p.cols = static_cast<uint32_t>(x.cols);
-    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
-    p.items = static_cast<uint64_t>(x.rows) * p.blocks * 4;
+    const QuantParams p = quant_of(x, out);
     const uint32_t grid = stream_blocks(p.items);
     if (x.dtype == SQN_F32)
         quantise_kernel<float><<<grid, kThreads, 0, stream>>>(p);
@@ -286,29 +531,23 @@ hipError_t launch_quantised_values(const sqn_quantised& x, const sqn_matrix& out
 }
 
 hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised& w, const float* bias, bool relu,
-                                    const sqn_matrix& out, hipStream_t stream)
+                                    const sqn_matrix& out, void* workspace, hipStream_t stream)
 {
-    ProductParams p;
-    p.x = static_cast<const uint8_t*>(x.codes);
-    p.x_scales = static_cast<const uint8_t*>(x.scales);
-    p.w = static_cast<const uint8_t*>(w.codes);
-    p.w_scales = static_cast<const uint8_t*>(w.scales);
-    p.bias = bias;
-    p.out = out.data;
-    p.out_stride = out.row_stride;
-    p.points = static_cast<uint32_t>(x.rows);
-    p.units = static_cast<uint32_t>(w.rows);
-    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
-    p.relu = relu ? 1 : 0;
-    p.dtype = out.dtype;
-    product_kernel<<<(p.points + 63) / 64 * ((p.units + 63) / 64), kThreads, 0, stream>>>(p);
-    return hipGetLastError();
+    const ProductScratch t(x.rows, w.rows, x.cols, workspace);
+    const PackParams pw = pack_of(w, t.w_packed), px = pack_of(x, t.x_packed);
+    const uint32_t groups_w = stream_blocks(pw.words), groups_x = stream_blocks(px.words);
+    pack_kernel<<<groups_w + groups_x, kThreads, 0, stream>>>(pw, px, groups_w);
+    return launch_tiles(x, t, w, bias, relu, out, stream);
 }
 
-size_t quantised_layer_bytes(int64_t rows, int64_t cols)
+size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols)
 {
-    const size_t blocks = static_cast<size_t>(rows) * quant_blocks(cols);
-    return padded(16 * blocks) + padded(blocks);
+    return ProductScratch(points, units, cols, nullptr).bytes;
+}
+
+size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols)
+{
+    return padded(16 * static_cast<size_t>(points) * quant_blocks(cols)) + quantised_product_bytes(points, units, cols);
 }
 
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
@@ -318,11 +557,20 @@ hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, c
     q.rows = x.rows;
     q.cols = x.cols;
     q.codes = workspace;
-    q.scales = static_cast<char*>(workspace) + padded(16 * static_cast<size_t>(x.rows) * quant_blocks(x.cols));
-    const hipError_t e = launch_quantise(x, q, stream);
-    if (e != hipSuccess)
-        return e;
-    return launch_quantised_product(q, w, bias, relu, out, stream);
+    q.scales = nullptr;
+    const ProductScratch t(x.rows, w.rows, x.cols,
+                           static_cast<char*>(workspace) + padded(16 * static_cast<size_t>(x.rows) * quant_blocks(x.cols)));
+    QuantParams p = quant_of(x, q);
+    p.items = static_cast<uint64_t>(x.rows) * t.x_packed.steps * 32;
+    const PackParams pw = pack_of(w, t.w_packed);
+    const uint32_t groups = stream_blocks(p.items), grid = groups + stream_blocks(pw.words);
+    if (x.dtype == SQN_F32)
+        quantise_packed_kernel<float><<<grid, kThreads, 0, stream>>>(p, t.x_packed, pw, groups);
+    else if (x.dtype == SQN_F16)
+        quantise_packed_kernel<_Float16><<<grid, kThreads, 0, stream>>>(p, t.x_packed, pw, groups);
+    else
+        quantise_packed_kernel<__bf16><<<grid, kThreads, 0, stream>>>(p, t.x_packed, pw, groups);
+    return launch_tiles(q, t, w, bias, relu, out, stream);
 }
 
 }  // namespace sqn

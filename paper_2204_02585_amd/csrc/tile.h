@@ -72,12 +72,14 @@ __device__ __forceinline__ void landed()
 // The steps of a tile's sum.  bring(step, buffer) issues LOADS loads a wave,
 // read(fragments, buffer, o) reads a depth's fragments and multiply(fragments,
 // depth) multiplies them: the steps go in pairs, of eight depths; the last
-// step may be alone.
-template <int LOADS, typename Fragments, typename B, typename R, typename M>
-__device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, B bring_step, R read, M multiply)
+// step may be alone.  ahead(step, in_pair) starts what a step takes from
+// elsewhere, a step before it.
+template <int LOADS, typename Fragments, typename A, typename B, typename R, typename M>
+__device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, A ahead, B bring_step, R read, M multiply)
 {
     const uint32_t end = steps - 1;
     Fragments f0, f1;
+    ahead(0u, 0);
     bring_step(0, b0);
     bring_step(min(1u, end), b1);
     landed<LOADS>();
@@ -85,6 +87,7 @@ __device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, B b
     // `buffer` holds step k and will hold k + 2; past the end the last step
     // comes once more and is not used
     auto work = [&](uint32_t k, int depth, char* buffer, char* next) {
+        ahead(min(k + 1, end), depth ? 0 : 1);
         read(f1, buffer, 1);
         multiply(f0, depth);
         read(f0, buffer, 2);

@@ -265,11 +265,13 @@ def product(x, w: Quantised, bias: Optional[torch.Tensor] = None, relu: bool = F
     into = _matrix(_rows(out), "out")
     at = None if bias is None else bias.data_ptr()
     if blocks:
-        _check(lib.sqn_quantised_product(x._arg(), w._arg(), at, 1 if relu else 0, into,
-                                         _on(stream, x.codes, x.scales, w.codes, w.scales, bias, out)))
+        size = lib.sqn_quantised_product_workspace(x.shape[0], w.shape[0], w.cols)
+        work = _workspace(size, device)
+        _check(lib.sqn_quantised_product(x._arg(), w._arg(), at, 1 if relu else 0, into, work.data_ptr(), size,
+                                         _on(stream, x.codes, x.scales, w.codes, w.scales, bias, out, work)))
         return out
     source = _rows(x)
-    size = lib.sqn_quantised_layer_workspace(source.shape[0], source.shape[1])
+    size = lib.sqn_quantised_layer_workspace(source.shape[0], w.shape[0], w.cols)
     work = _workspace(size, device)
     _check(lib.sqn_quantised_layer(_matrix(source, "x"), w._arg(), at, 1 if relu else 0, into, work.data_ptr(), size,
                                    _on(stream, source, w.codes, w.scales, bias, out, work)))
