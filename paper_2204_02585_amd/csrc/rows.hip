@@ -8,6 +8,8 @@
 // sorted by index (a stable radix sort), cut into tiles of the sorted order,
 // and each tile sums its runs of equal indices; runs that cross tiles leave
 // partial sums that a second kernel joins in tile order.
+#include <type_traits>
+
 #include "learn.h"
 #include "numeric.h"
 #include "sqn_internal.h"
@@ -94,21 +96,27 @@ hipError_t lookup(const LookupParams& base, bool ids64, hipStream_t stream)
 
 // ---- gradient: sorting
 //
-// Least significant digit first, kDigitBits a pass; each pass counts the
-// digits of every workgroup's stretch of keys, then places them.  Within a
-// stretch a wave takes consecutive keys, 64 at a time; equal digits among the
-// 64 find their order with one ballot per bit.  Indices outside the table
-// sort as the key `rows`, behind all others.
+// Least significant digit first, as few digits as ten bits each allow.  A pass
+// counts the digits of every workgroup's stretch of keys, then places them.
+// Within a stretch a wave takes consecutive keys, 64 at a time; equal digits
+// among the 64 find their order with one ballot per bit.  Up to kStep keys one
+// workgroup goes through all passes in LDS, in one launch.  Indices outside
+// the table sort as the key `rows`, behind all others.
 //
 // While it sorts the chip is nearly idle, so the rows of the gradient are
 // cleared by further workgroups of the same launches.
 
-constexpr int kDigitBits = 8;
-constexpr int kBins = 1 << kDigitBits;
-constexpr int kWaves = kThreads / 64;
+constexpr int kMaxDigitBits = 10;
+constexpr int kMaxBins = 1 << kMaxDigitBits;
+constexpr int kSortThreads = 1024;
+constexpr int kWaves = kSortThreads / 64;
 constexpr int kKeysPerThread = 16;
-constexpr int kStep = kThreads * kKeysPerThread;    // keys a workgroup places at a time
-constexpr int kMaxStretches = 256;
+constexpr int kStep = kSortThreads * kKeysPerThread;    // keys a workgroup places at a time
+constexpr int kMaxStretches = 64;
+
+struct __attribute__((aligned(8))) Pair {
+    uint32_t key, at;
+};
 
 struct Clear {
     char* data;
@@ -119,15 +127,14 @@ struct Clear {
 
 struct SortParams {
     const void* ids;                    // first pass: the indices
-    const uint32_t* keys_in;            // later passes
-    const uint32_t* at_in;
-    uint32_t* keys_out;
-    uint32_t* at_out;
-    uint32_t* counts;                   // [kBins][stretches]
+    const Pair* in;                     // later passes
+    Pair* out;
+    uint32_t* counts;                   // [stretches][bins]
     uint32_t n, rows;
     uint32_t stretch;                   // keys per workgroup, a multiple of kStep
     uint32_t stretches;
-    int shift;
+    int shift, bits;                    // of the digit
+    int passes;
     Clear clear;
 };
 
@@ -137,8 +144,8 @@ __device__ void clear_share(const Clear& c, uint32_t block)
 {
     struct __attribute__((packed, aligned(2))) Piece { uint32_t w[4]; };
     const uint64_t per_row = (c.row_bytes + 15) / 16;
-    for (uint64_t i = c.first + static_cast<uint64_t>(block) * kThreads + threadIdx.x; i < c.last;
-         i += static_cast<uint64_t>(c.blocks) * kThreads) {
+    for (uint64_t i = c.first + static_cast<uint64_t>(block) * kSortThreads + threadIdx.x; i < c.last;
+         i += static_cast<uint64_t>(c.blocks) * kSortThreads) {
         const uint64_t r = c.rows == 1 ? 0 : i / per_row;
         const uint64_t at = (i - r * per_row) * 16;
         char* row = c.data + r * c.stride_bytes;
@@ -151,124 +158,211 @@ __device__ void clear_share(const Clear& c, uint32_t block)
     }
 }
 
+// the type of `ids` in the passes after the first
+struct Sorted {};
+
 template <typename I>
-__device__ __forceinline__ uint32_t key_of(const SortParams& p, uint32_t i)
+__device__ __forceinline__ Pair pair_at(const SortParams& p, uint32_t i)
 {
-    if constexpr (sizeof(I) == 1) {      // later passes
-        return p.keys_in[i];
+    if constexpr (std::is_same<I, Sorted>::value) {
+        return p.in[i];
     } else {
         const int64_t id = static_cast<const I*>(p.ids)[i];
-        return static_cast<uint64_t>(id) < p.rows ? static_cast<uint32_t>(id) : p.rows;
+        return Pair{static_cast<uint64_t>(id) < p.rows ? static_cast<uint32_t>(id) : p.rows, i};
     }
 }
 
+// Thread t's key k of a step is number 1024 (t / 64) + 64 k + t % 64.
+__device__ __forceinline__ uint32_t number_of(int k)
+{
+    return (threadIdx.x >> 6) * (64 * kKeysPerThread) + 64 * k + (threadIdx.x & 63);
+}
+
+// A step's keys ranked among those of their digit in their wave, which counts
+// them in seen[digit]; keys from `n` on are not there.
+__device__ __forceinline__ void rank_keys(const Pair (&pair)[kKeysPerThread], uint32_t n, int shift, int bits, uint32_t* seen,
+                                          uint32_t (&rank)[kKeysPerThread])
+{
+    const uint32_t mask = (1u << bits) - 1;
+    const uint64_t below = (uint64_t{1} << (threadIdx.x & 63)) - 1;
+#pragma unroll
+    for (int k = 0; k < kKeysPerThread; ++k) {
+        const bool there = number_of(k) < n;
+        const uint32_t digit = pair[k].key >> shift & mask;
+        uint64_t same = __ballot(there);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+        // the wave's LDS accesses stay in program order
+        const uint32_t had = seen[digit];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        rank[k] = had + __popcll(same & below);
+        if (there && (same & below) == 0)
+            seen[digit] = had + __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Exclusive sums over `bins` values, one a thread (0 from `bins` on).
+__device__ __forceinline__ uint32_t exclusive_sum(uint32_t v, uint32_t* wave_sums)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t t = __shfl_up(s, d);
+        s += lane >= d ? t : 0;
+    }
+    __syncthreads();
+    if (lane == 63)
+        wave_sums[wave] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < wave; ++w)
+        before += wave_sums[w];
+    return before + s - v;
+}
+
+// seen[wave][bin] from counts to where the wave's first key of the bin goes,
+// given where the step's first goes; returns where the next step's does.
+__device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[kMaxBins], uint32_t bin, uint32_t at)
+{
+    for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = seen[w][bin];
+        seen[w][bin] = at;
+        at += c;
+    }
+    return at;
+}
+
 template <typename I>
-__global__ __launch_bounds__(kThreads) void count_kernel(SortParams p)
+__global__ __launch_bounds__(kSortThreads) void count_kernel(SortParams p)
 {
     if (blockIdx.x >= p.stretches) {
         clear_share(p.clear, blockIdx.x - p.stretches);
         return;
     }
-    __shared__ uint32_t bins[kBins];
+    __shared__ uint32_t bins[kMaxBins];
     bins[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * p.stretch;
     const uint32_t last = min(p.n, first + p.stretch);
-    for (uint32_t i = first + threadIdx.x; i < last; i += kThreads)
-        atomicAdd(&bins[(key_of<I>(p, i) >> p.shift) & (kBins - 1)], 1u);
+    const uint32_t mask = (1u << p.bits) - 1;
+#pragma unroll 4
+    for (uint32_t i = first + threadIdx.x; i < last; i += kSortThreads)
+        atomicAdd(&bins[pair_at<I>(p, i).key >> p.shift & mask], 1u);
     __syncthreads();
-    p.counts[threadIdx.x * p.stretches + blockIdx.x] = bins[threadIdx.x];
+    if (threadIdx.x <= mask)
+        p.counts[blockIdx.x * (mask + 1) + threadIdx.x] = bins[threadIdx.x];
 }
 
 template <typename I>
-__global__ __launch_bounds__(kThreads) void place_kernel(SortParams p)
+__global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
 {
     if (blockIdx.x >= p.stretches) {
         clear_share(p.clear, blockIdx.x - p.stretches);
         return;
     }
-    __shared__ uint32_t base[kBins];             // where the stretch's next key of a digit goes
-    __shared__ uint32_t seen[kWaves][kBins];     // of a step, per wave
-    __shared__ uint32_t sums[kBins];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ uint32_t seen[kWaves][kMaxBins];    // of a step, per wave
+    __shared__ uint32_t wave_sums[kWaves];
+    const uint32_t bins = 1u << p.bits, tid = threadIdx.x, wave = tid >> 6;
 
     // this digit's keys in all stretches, and in those before this one
     uint32_t total = 0, before = 0;
-    for (uint32_t s = 0; s < p.stretches; ++s) {
-        const uint32_t c = p.counts[tid * p.stretches + s];
-        before += s < blockIdx.x ? c : 0;
-        total += c;
+    if (tid < bins) {
+#pragma unroll 8
+        for (uint32_t s = 0; s < p.stretches; ++s) {
+            const uint32_t c = p.counts[s * bins + tid];
+            before += s < blockIdx.x ? c : 0;
+            total += c;
+        }
     }
-    sums[tid] = total;
-    __syncthreads();
-    for (int d = 1; d < kBins; d *= 2) {
-        const uint32_t add = tid >= d ? sums[tid - d] : 0;
-        __syncthreads();
-        sums[tid] += add;
-        __syncthreads();
-    }
-    base[tid] = sums[tid] - total + before;
+    uint32_t base = exclusive_sum(total, wave_sums) + before;
 
     const uint32_t first = blockIdx.x * p.stretch;
     const uint32_t last = min(p.n, first + p.stretch);
     for (uint32_t step = first; step < last; step += kStep) {
+        Pair pair[kKeysPerThread];
+        uint32_t rank[kKeysPerThread];
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k)
+            pair[k] = number_of(k) < last - step ? pair_at<I>(p, step + number_of(k)) : Pair{0, 0};
         for (int w = 0; w < kWaves; ++w)
             seen[w][tid] = 0;
         __syncthreads();
-        uint32_t key[kKeysPerThread], rank[kKeysPerThread];
-        const uint32_t mine = step + wave * (64 * kKeysPerThread) + lane;
+        rank_keys(pair, last - step, p.shift, p.bits, seen[wave], rank);
+        __syncthreads();
+        base = counts_to_starts(seen, tid, base);
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < kKeysPerThread; ++k)
-            key[k] = mine + 64 * k < last ? key_of<I>(p, mine + 64 * k) : 0;
-#pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k) {
-            const bool there = mine + 64 * k < last;
-            const uint32_t digit = (key[k] >> p.shift) & (kBins - 1);
-            uint64_t same = __ballot(there);
-#pragma unroll
-            for (int b = 0; b < kDigitBits; ++b) {
-                const uint64_t set = __ballot((digit >> b) & 1);
-                same &= (digit >> b) & 1 ? set : ~set;
-            }
-            // the wave's LDS accesses stay in program order
-            const uint32_t had = seen[wave][digit];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            const uint64_t lower = same & ((uint64_t{1} << lane) - 1);
-            rank[k] = had + __popcll(lower);
-            if (there && lower == 0)
-                seen[wave][digit] = had + __popcll(same);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
-        __syncthreads();
-        // counts of the step to starts, wave after wave
-        uint32_t at = base[tid];
-        for (int w = 0; w < kWaves; ++w) {
-            const uint32_t c = seen[w][tid];
-            seen[w][tid] = at;
-            at += c;
-        }
-        base[tid] = at;
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k) {
-            const uint32_t i = mine + 64 * k;
-            if (i < last) {
-                const uint32_t to = seen[wave][(key[k] >> p.shift) & (kBins - 1)] + rank[k];
-                p.keys_out[to] = key[k];
-                p.at_out[to] = sizeof(I) == 1 ? p.at_in[i] : i;
-            }
-        }
+            if (number_of(k) < last - step)
+                p.out[seen[wave][pair[k].key >> p.shift & (bins - 1)] + rank[k]] = pair[k];
         __syncthreads();
     }
+}
+
+// All passes over at most kStep keys.
+template <typename I>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
+{
+    if (blockIdx.x >= 1) {
+        clear_share(p.clear, blockIdx.x - 1);
+        return;
+    }
+    // the counts' place first, then the pairs'
+    __shared__ __align__(16) char shared[kStep * sizeof(Pair)];
+    __shared__ uint32_t wave_sums[kWaves];
+    uint32_t (*seen)[kMaxBins] = reinterpret_cast<uint32_t (*)[kMaxBins]>(shared);
+    Pair* pairs = reinterpret_cast<Pair*>(shared);
+    static_assert(sizeof(uint32_t) * kWaves * kMaxBins <= sizeof(shared), "the counts fit");
+    const uint32_t tid = threadIdx.x, wave = tid >> 6;
+    Pair pair[kKeysPerThread];
+    uint32_t to[kKeysPerThread];
+#pragma unroll
+    for (int k = 0; k < kKeysPerThread; ++k)
+        pair[k] = number_of(k) < p.n ? pair_at<I>(p, number_of(k)) : Pair{0, 0};
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * p.bits;
+        const uint32_t mask = (1u << p.bits) - 1;
+        for (int w = 0; w < kWaves; ++w)
+            seen[w][tid] = 0;
+        __syncthreads();
+        rank_keys(pair, p.n, shift, p.bits, seen[wave], to);
+        __syncthreads();
+        uint32_t total = 0;
+        for (int w = 0; w < kWaves; ++w)
+            total += seen[w][tid];
+        counts_to_starts(seen, tid, exclusive_sum(total, wave_sums));
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k)
+            to[k] += seen[wave][pair[k].key >> shift & mask];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k)
+            if (number_of(k) < p.n)
+                pairs[to[k]] = pair[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kKeysPerThread; ++k)
+            if (number_of(k) < p.n)
+                pair[k] = pairs[number_of(k)];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kKeysPerThread; ++k)
+        if (number_of(k) < p.n)
+            p.out[number_of(k)] = pair[k];
 }
 
 // ---- gradient: sums
 
 struct SumParams {
-    const uint32_t* keys;      // sorted
-    const uint32_t* at;
+    const Pair* pairs;         // sorted
     const void* grad;
     void* out;
     float* head;               // [tiles][width]: a tile's part of a run begun before it
@@ -309,6 +403,9 @@ __device__ __forceinline__ void finish(const SumParams& p, uint32_t key, uint32_
     }
 }
 
+// Entries whose rows are under way together.
+constexpr int kAhead = 8;
+
 template <typename T, typename O, int V>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumParams p)
 {
@@ -319,8 +416,8 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumParams p)
     const uint32_t e = min(c * V, p.cols - V), skip = c * V - e;
     const uint32_t first = group * p.tile, last = min(p.n, first + p.tile);
     const T* grad = static_cast<const T*>(p.grad) + e;
-    uint32_t key = p.keys[first];
-    bool before = first > 0 && p.keys[first - 1] == key;
+    uint32_t key = p.pairs[first].key;
+    bool before = first > 0 && p.pairs[first - 1].key == key;
     float acc[V];
 #pragma unroll
     for (int k = 0; k < V; ++k)
@@ -330,60 +427,143 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumParams p)
         for (int k = 0; k < V; ++k)
             to[static_cast<uint64_t>(group) * p.width + c * V + k] = acc[k];
     };
-    for (uint32_t i = first; i < last; ++i) {
-        const uint32_t next = p.keys[i];
-        if (next != key) {
-            if (before)
-                part(p.head);
-            else
-                finish<O, V>(p, key, e, skip, acc);
-            before = false;
-            key = next;
+    for (uint32_t i = first; i < last; i += kAhead) {
+        Pair pair[kAhead];
+        float v[kAhead][V];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            pair[a] = p.pairs[min(i + a, last - 1)];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            if (i + a < last && pair[a].key < p.rows)
+                load_run<T, V>(grad + pair[a].at * p.grad_stride, v[a]);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            if (i + a >= last)
+                break;
+            if (pair[a].key != key) {
+                if (before)
+                    part(p.head);
+                else
+                    finish<O, V>(p, key, e, skip, acc);
+                before = false;
+                key = pair[a].key;
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    acc[k] = 0.0f;
+            }
+            if (key >= p.rows)
+                return;                     // indices outside the table come last
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                acc[k] = 0.0f;
+                acc[k] += v[a][k];
         }
-        if (key >= p.rows)
-            return;                     // indices outside the table come last
-        float v[V];
-        load_run<T, V>(grad + p.at[i] * p.grad_stride, v);
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-            acc[k] += v[k];
     }
     if (before)
         part(p.head);
-    else if (last < p.n && p.keys[last] == key)
+    else if (last < p.n && p.pairs[last].key == key)
         part(p.tail);
     else
         finish<O, V>(p, key, e, skip, acc);
 }
 
-// A tile whose last run began in it and goes on: that run's parts in order.
-template <typename O, int V>
-__global__ __launch_bounds__(kThreads) void join_kernel(SumParams p)
+// Runs over more than kLong tiles are joined by a workgroup each.
+constexpr uint32_t kLong = 16;
+
+// Whether tile t's last run begins in it and goes on into the next.
+__device__ __forceinline__ bool opens(const SumParams& p, uint32_t t, uint32_t& key)
 {
-    const uint32_t group = (blockIdx.x * kThreads + threadIdx.x) / p.lanes;
+    if (t + 1 >= p.tiles)
+        return false;
+    const uint32_t first = t * p.tile, last = first + p.tile;
+    key = p.pairs[last - 1].key;
+    return p.pairs[last].key == key && key < p.rows && !(first > 0 && p.pairs[first - 1].key == key);
+}
+
+// Whether a run of `key` that reaches tile t - 1 reaches tile t.
+__device__ __forceinline__ bool reaches(const SumParams& p, uint32_t t, uint32_t key)
+{
+    return t < p.tiles && p.pairs[static_cast<uint64_t>(t) * p.tile].key == key;
+}
+
+// The parts of the runs that cross tiles, in order: short ones by the lanes
+// of a tile, in the first workgroups; long ones by the others, each looking
+// after kLong tiles, in which at most one long run can begin.
+template <typename O, int V>
+__global__ __launch_bounds__(kThreads) void join_kernel(SumParams p, uint32_t short_blocks)
+{
     const uint32_t c = blockIdx.y * p.lanes + threadIdx.x % p.lanes;
-    if (group + 1 >= p.tiles || c >= p.runs)
-        return;
-    const uint32_t first = group * p.tile, last = first + p.tile;
-    const uint32_t key = p.keys[last - 1];
-    if (p.keys[last] != key || key >= p.rows)
-        return;
-    if (first > 0 && p.keys[first - 1] == key)
-        return;                         // begun in a tile before
+    const uint64_t at = c * V;
+    const uint32_t e = min(c * V, p.cols - V), skip = c * V - e;
     float acc[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k)
-        acc[k] = p.tail[static_cast<uint64_t>(group) * p.width + c * V + k];
-    for (uint32_t t = group + 1; t < p.tiles && p.keys[t * p.tile] == key; ++t) {
+    uint32_t key;
+    if (blockIdx.x < short_blocks) {
+        const uint32_t t = (blockIdx.x * kThreads + threadIdx.x) / p.lanes;
+        if (c >= p.runs || !opens(p, t, key) || reaches(p, t + kLong + 1, key))
+            return;
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            acc[k] += p.head[static_cast<uint64_t>(t) * p.width + c * V + k];
+            acc[k] = p.tail[t * static_cast<uint64_t>(p.width) + at + k];
+        for (uint32_t u = t + 1; reaches(p, u, key); ++u) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                acc[k] += p.head[u * static_cast<uint64_t>(p.width) + at + k];
+        }
+        finish<O, V>(p, key, e, skip, acc);
+        return;
     }
-    const uint32_t e = min(c * V, p.cols - V);
-    finish<O, V>(p, key, e, c * V - e, acc);
+    __shared__ uint32_t begin, end;
+    __shared__ float parts[kThreads][V];
+    const uint32_t t0 = (blockIdx.x - short_blocks) * kLong;
+    if (threadIdx.x == 0)
+        begin = p.tiles;
+    __syncthreads();
+    if (threadIdx.x < kLong && opens(p, t0 + threadIdx.x, key) && reaches(p, t0 + threadIdx.x + kLong + 1, key))
+        begin = t0 + threadIdx.x;
+    __syncthreads();
+    const uint32_t t = begin;
+    if (t >= p.tiles)
+        return;
+    key = p.pairs[(t + 1) * static_cast<uint64_t>(p.tile) - 1].key;
+    // the first tile that the run does not reach: 64 probes a round
+    if (threadIdx.x < 64) {
+        uint32_t low = t + kLong + 1, high = p.tiles;      // it reaches low, and not high
+        while (high - low > 1) {
+            const uint32_t stride = (high - low + 63) / 64;
+            const uint32_t probe = low + (threadIdx.x + 1) * stride;
+            const uint64_t yes = __ballot(probe < high && reaches(p, probe, key));
+            const uint32_t more = static_cast<uint32_t>(__popcll(yes));
+            high = min(high, low + (more + 1) * stride);
+            low += more * stride;
+        }
+        if (threadIdx.x == 0)
+            end = low + 1;
+    }
+    __syncthreads();
+    // groups of lanes take the run's tiles in turn, then add up
+    const uint32_t groups = kThreads / p.lanes, group = threadIdx.x / p.lanes;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        acc[k] = group == 0 && c < p.runs ? p.tail[t * static_cast<uint64_t>(p.width) + at + k] : 0.0f;
+    if (c < p.runs) {
+#pragma unroll 4
+        for (uint32_t u = t + 1 + group; u < end; u += groups) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                acc[k] += p.head[u * static_cast<uint64_t>(p.width) + at + k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        parts[threadIdx.x][k] = acc[k];
+    __syncthreads();
+    if (group > 0 || c >= p.runs)
+        return;
+    for (uint32_t g = 1; g < groups; ++g)
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            acc[k] += parts[g * p.lanes + threadIdx.x][k];
+    finish<O, V>(p, key, e, skip, acc);
 }
 
 // ---- gradient: layout and launches
@@ -391,8 +571,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(SumParams p)
 constexpr uint32_t kTile = 32;
 
 struct Plan {
-    uint32_t passes, stretch, stretches, tiles, width;
-    size_t keys[2], at[2], counts, head, tail, bytes;
+    uint32_t passes, bits, stretch, stretches, tiles;
+    size_t pairs[2], counts, head, tail, bytes;
 };
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -400,28 +580,27 @@ size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 Plan plan_of(int64_t n, int64_t rows, int64_t cols)
 {
     Plan q;
-    int bits = 1;
+    uint32_t bits = 1;
     while ((rows >> bits) != 0)
         ++bits;                          // the largest key is `rows`
-    q.passes = (bits + kDigitBits - 1) / kDigitBits;
+    q.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
+    q.bits = (bits + q.passes - 1) / q.passes;
     const int64_t steps = (n + kStep - 1) / kStep;
     q.stretch = static_cast<uint32_t>((steps + kMaxStretches - 1) / kMaxStretches * kStep);
     q.stretches = q.stretch ? static_cast<uint32_t>((n + q.stretch - 1) / q.stretch) : 0;
     q.tiles = static_cast<uint32_t>((n + kTile - 1) / kTile);
-    q.width = static_cast<uint32_t>((cols + 7) / 8 * 8);
+    const size_t width = static_cast<size_t>(cols + 7) / 8 * 8;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at += padded(bytes);
         return here;
     };
-    for (int k = 0; k < 2; ++k) {
-        q.keys[k] = take(4 * static_cast<size_t>(n));
-        q.at[k] = take(4 * static_cast<size_t>(n));
-    }
-    q.counts = take(4 * static_cast<size_t>(kBins) * q.stretches);
-    q.head = take(4 * static_cast<size_t>(q.tiles) * q.width);
-    q.tail = take(4 * static_cast<size_t>(q.tiles) * q.width);
+    for (int k = 0; k < 2; ++k)
+        q.pairs[k] = take(sizeof(Pair) * static_cast<size_t>(n));
+    q.counts = take(4 * static_cast<size_t>(kMaxBins) * q.stretches);
+    q.head = take(4 * q.tiles * width);
+    q.tail = take(4 * q.tiles * width);
     q.bytes = at;
     return q;
 }
@@ -438,7 +617,7 @@ void launch_sums(SumParams p, hipStream_t stream)
     const dim3 grid((p.tiles + per_block - 1) / per_block, (p.runs + p.lanes - 1) / p.lanes);
     sum_kernel<T, O, V><<<grid, kThreads, 0, stream>>>(p);
     if (p.tiles > 1)
-        join_kernel<O, V><<<grid, kThreads, 0, stream>>>(p);
+        join_kernel<O, V><<<dim3(grid.x + (p.tiles + kLong - 1) / kLong, grid.y), kThreads, 0, stream>>>(p, grid.x);
 }
 
 template <typename T, typename O>
@@ -491,8 +670,7 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
 {
     const Plan q = plan_of(grad.rows, table_grad.rows, table_grad.cols);
     char* ws = static_cast<char*>(workspace);
-    uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + q.keys[0]), reinterpret_cast<uint32_t*>(ws + q.keys[1])};
-    uint32_t* at[2] = {reinterpret_cast<uint32_t*>(ws + q.at[0]), reinterpret_cast<uint32_t*>(ws + q.at[1])};
+    Pair* pairs[2] = {reinterpret_cast<Pair*>(ws + q.pairs[0]), reinterpret_cast<Pair*>(ws + q.pairs[1])};
 
     SortParams s;
     s.ids = ids;
@@ -512,46 +690,56 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
         c.rows = 1;
     }
     const uint64_t pieces = accumulate ? 0 : c.rows * ((c.row_bytes + 15) / 16);
-    const uint32_t launches = s.n ? 2 * q.passes : 1;
+    s.bits = static_cast<int>(q.bits);
+    s.passes = static_cast<int>(q.passes);
+    s.shift = 0;
+    s.in = nullptr;
+    s.out = pairs[0];
+    const bool small = s.n <= kStep;
+    const uint32_t launches = small ? 1 : 2 * q.passes;
     uint32_t launch = 0;
-    auto share = [&]() {
+    // the next launch's grid, with its share of the clearing
+    auto grid = [&]() {
         c.first = pieces / launches * launch;
         c.last = ++launch == launches ? pieces : pieces / launches * launch;
-        const uint64_t want = (c.last - c.first + kThreads - 1) / kThreads;
-        c.blocks = static_cast<uint32_t>(want < 2048 ? want : 2048);
+        const uint64_t want = (c.last - c.first + 4 * kSortThreads - 1) / (4 * kSortThreads);
+        c.blocks = static_cast<uint32_t>(want < 512 ? want : 512);
         s.clear = c;
-        return dim3(q.stretches + c.blocks);
+        return dim3((small ? 1 : q.stretches) + c.blocks);
     };
-    if (s.n == 0) {
-        const dim3 grid = share();
-        if (grid.x)
-            count_kernel<uint8_t><<<grid, kThreads, 0, stream>>>(s);
-        return hipGetLastError();
-    }
-    for (uint32_t pass = 0; pass < q.passes; ++pass) {
-        s.shift = static_cast<int>(pass) * kDigitBits;
-        s.keys_in = keys[(pass + 1) & 1];
-        s.at_in = at[(pass + 1) & 1];
-        s.keys_out = keys[pass & 1];
-        s.at_out = at[pass & 1];
-        const dim3 count_grid = share();
-        if (pass > 0)
-            count_kernel<uint8_t><<<count_grid, kThreads, 0, stream>>>(s);
-        else if (ids64)
-            count_kernel<int64_t><<<count_grid, kThreads, 0, stream>>>(s);
+    if (small) {
+        if (s.n == 0 && pieces == 0)
+            return hipSuccess;
+        const dim3 sort_grid = grid();
+        if (ids64)
+            sort_kernel<int64_t><<<sort_grid, kSortThreads, 0, stream>>>(s);
         else
-            count_kernel<int32_t><<<count_grid, kThreads, 0, stream>>>(s);
-        const dim3 place_grid = share();
-        if (pass > 0)
-            place_kernel<uint8_t><<<place_grid, kThreads, 0, stream>>>(s);
-        else if (ids64)
-            place_kernel<int64_t><<<place_grid, kThreads, 0, stream>>>(s);
-        else
-            place_kernel<int32_t><<<place_grid, kThreads, 0, stream>>>(s);
+            sort_kernel<int32_t><<<sort_grid, kSortThreads, 0, stream>>>(s);
+        if (s.n == 0)
+            return hipGetLastError();
+    } else {
+        for (uint32_t pass = 0; pass < q.passes; ++pass) {
+            s.shift = static_cast<int>(pass * q.bits);
+            s.in = pairs[(pass + 1) & 1];
+            s.out = pairs[pass & 1];
+            const dim3 count_grid = grid();
+            if (pass > 0)
+                count_kernel<Sorted><<<count_grid, kSortThreads, 0, stream>>>(s);
+            else if (ids64)
+                count_kernel<int64_t><<<count_grid, kSortThreads, 0, stream>>>(s);
+            else
+                count_kernel<int32_t><<<count_grid, kSortThreads, 0, stream>>>(s);
+            const dim3 place_grid = grid();
+            if (pass > 0)
+                place_kernel<Sorted><<<place_grid, kSortThreads, 0, stream>>>(s);
+            else if (ids64)
+                place_kernel<int64_t><<<place_grid, kSortThreads, 0, stream>>>(s);
+            else
+                place_kernel<int32_t><<<place_grid, kSortThreads, 0, stream>>>(s);
+        }
     }
     SumParams p;
-    p.keys = s.keys_out;
-    p.at = s.at_out;
+    p.pairs = s.out;
     p.grad = grad.data;
     p.out = table_grad.data;
     p.head = reinterpret_cast<float*>(ws + q.head);
