@@ -33,6 +33,8 @@ struct LookupParams {
     float scale;
 };
 
+constexpr int kAhead = 4;        // runs of a thread under way together
+
 // A thread copies runs of V elements (16 bytes); the last run of a row ends
 // with it and may overlap the one before, whose elements it writes again with
 // the same values.
@@ -47,22 +49,30 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupParams p)
     const I* ids = static_cast<const I*>(p.ids) + t0;
     const T* table = static_cast<const T*>(p.table);
     T* out = static_cast<T*>(p.out) + t0 * p.out_stride;
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-        const uint32_t r = (c0 + i) / p.runs;
-        const uint32_t e = min((c0 + i - r * p.runs) * V, p.cols - V);
-        const int64_t id = ids[r];
-        float v[V];
-        if (static_cast<uint64_t>(id) < p.rows) {
-            load_run<T, V>(table + id * p.table_stride + e, v);
+    for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kAhead * kThreads) {
+        // the loads of all runs first
+        float v[kAhead][V];
+        int64_t id[kAhead];
+        uint32_t r[kAhead], e[kAhead];
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                v[k] *= p.scale;
-        } else {
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                v[k] = 0.0f;
+        for (int a = 0; a < kAhead; ++a) {
+            const uint32_t i = min(i0 + a * kThreads, n - 1);
+            r[a] = (c0 + i) / p.runs;
+            e[a] = min((c0 + i - r[a] * p.runs) * V, p.cols - V);
+            id[a] = ids[r[a]];
         }
-        store_run<T, V>(out + r * p.out_stride + e, v);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            load_run<T, V>(table + (static_cast<uint64_t>(id[a]) < p.rows ? id[a] : 0) * p.table_stride + e[a], v[a]);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const bool inside = static_cast<uint64_t>(id[a]) < p.rows;
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                v[a][k] = inside ? v[a][k] * p.scale : 0.0f;
+            if (i0 + a * kThreads < n)
+                store_run<T, V>(out + r[a] * p.out_stride + e[a], v[a]);
+        }
     }
 }
 
@@ -99,7 +109,7 @@ hipError_t lookup(const LookupParams& base, bool ids64, hipStream_t stream)
 // Least significant digit first, as few digits as ten bits each allow.  A pass
 // counts the digits of every workgroup's stretch of keys, then places them.
 // Within a stretch a wave takes consecutive keys, 64 at a time; equal digits
-// among the 64 find their order with one ballot per bit.  Up to kStep keys one
+// among the 64 find their order with one ballot per bit.  Up to kSortStep keys one
 // workgroup goes through all passes in LDS, in one launch.  Indices outside
 // the table sort as the key `rows`, behind all others.
 //
@@ -108,11 +118,13 @@ hipError_t lookup(const LookupParams& base, bool ids64, hipStream_t stream)
 
 constexpr int kMaxDigitBits = 10;
 constexpr int kMaxBins = 1 << kMaxDigitBits;
-constexpr int kSortThreads = 1024;
-constexpr int kWaves = kSortThreads / 64;
 constexpr int kKeysPerThread = 16;
-constexpr int kStep = kSortThreads * kKeysPerThread;    // keys a workgroup places at a time
-constexpr int kMaxStretches = 64;
+// Threads that place a stretch's keys, and that sort all of few.  Twice as many
+// for a stretch leave half of the CUs idle (640,000 keys: 28 us a pass for
+// 16), half as many spend it on the counts of the stretches before.
+constexpr int kPlaceThreads = 512, kSortThreads = 1024;
+constexpr int kPlaceStep = kPlaceThreads * kKeysPerThread, kSortStep = kSortThreads * kKeysPerThread;   // keys at a time
+constexpr int kMaxStretches = 128;
 
 struct __attribute__((aligned(8))) Pair {
     uint32_t key, at;
@@ -131,7 +143,7 @@ struct SortParams {
     Pair* out;
     uint32_t* counts;                   // [stretches][bins]
     uint32_t n, rows;
-    uint32_t stretch;                   // keys per workgroup, a multiple of kStep
+    uint32_t stretch;                   // keys per workgroup, a multiple of kPlaceStep
     uint32_t stretches;
     int shift, bits;                    // of the digit
     int passes;
@@ -144,8 +156,8 @@ __device__ void clear_share(const Clear& c, uint32_t block)
 {
     struct __attribute__((packed, aligned(2))) Piece { uint32_t w[4]; };
     const uint64_t per_row = (c.row_bytes + 15) / 16;
-    for (uint64_t i = c.first + static_cast<uint64_t>(block) * kSortThreads + threadIdx.x; i < c.last;
-         i += static_cast<uint64_t>(c.blocks) * kSortThreads) {
+    for (uint64_t i = c.first + static_cast<uint64_t>(block) * blockDim.x + threadIdx.x; i < c.last;
+         i += static_cast<uint64_t>(c.blocks) * blockDim.x) {
         const uint64_t r = c.rows == 1 ? 0 : i / per_row;
         const uint64_t at = (i - r * per_row) * 16;
         char* row = c.data + r * c.stride_bytes;
@@ -228,9 +240,11 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t v, uint32_t* wave_sum
 
 // seen[wave][bin] from counts to where the wave's first key of the bin goes,
 // given where the step's first goes; returns where the next step's does.
+template <int WAVES>
 __device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[kMaxBins], uint32_t bin, uint32_t at)
 {
-    for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
         const uint32_t c = seen[w][bin];
         seen[w][bin] = at;
         at += c;
@@ -239,63 +253,72 @@ __device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[kMaxBins],
 }
 
 template <typename I>
-__global__ __launch_bounds__(kSortThreads) void count_kernel(SortParams p)
+__global__ __launch_bounds__(kPlaceThreads) void count_kernel(SortParams p)
 {
     if (blockIdx.x >= p.stretches) {
         clear_share(p.clear, blockIdx.x - p.stretches);
         return;
     }
     __shared__ uint32_t bins[kMaxBins];
-    bins[threadIdx.x] = 0;
+    for (uint32_t b = threadIdx.x; b < kMaxBins; b += kPlaceThreads)
+        bins[b] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * p.stretch;
     const uint32_t last = min(p.n, first + p.stretch);
-    const uint32_t mask = (1u << p.bits) - 1;
-#pragma unroll 4
-    for (uint32_t i = first + threadIdx.x; i < last; i += kSortThreads)
-        atomicAdd(&bins[pair_at<I>(p, i).key >> p.shift & mask], 1u);
+    const uint32_t count = 1u << p.bits;
+#pragma unroll 8
+    for (uint32_t i = first + threadIdx.x; i < last; i += kPlaceThreads)
+        atomicAdd(&bins[pair_at<I>(p, i).key >> p.shift & (count - 1)], 1u);
     __syncthreads();
-    if (threadIdx.x <= mask)
-        p.counts[blockIdx.x * (mask + 1) + threadIdx.x] = bins[threadIdx.x];
+    for (uint32_t b = threadIdx.x; b < count; b += kPlaceThreads)
+        p.counts[blockIdx.x * count + b] = bins[b];
 }
 
 template <typename I>
-__global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
+__global__ __launch_bounds__(kPlaceThreads) void place_kernel(SortParams p)
 {
     if (blockIdx.x >= p.stretches) {
         clear_share(p.clear, blockIdx.x - p.stretches);
         return;
     }
-    __shared__ uint32_t seen[kWaves][kMaxBins];    // of a step, per wave
-    __shared__ uint32_t wave_sums[kWaves];
+    constexpr int WAVES = kPlaceThreads / 64;
+    static_assert(kMaxBins == 2 * kPlaceThreads, "two bins a thread");
+    __shared__ uint32_t seen[WAVES][kMaxBins];    // of a step, per wave
+    __shared__ uint32_t wave_sums[WAVES];
     const uint32_t bins = 1u << p.bits, tid = threadIdx.x, wave = tid >> 6;
 
-    // this digit's keys in all stretches, and in those before this one
-    uint32_t total = 0, before = 0;
-    if (tid < bins) {
+    // bins 2 tid and 2 tid + 1: their keys in all stretches, and in those before this one
+    uint32_t total[2] = {0, 0}, base[2] = {0, 0};
+    if (2 * tid < bins) {
+        const uint32_t other = min(2 * tid + 1, bins - 1);
 #pragma unroll 8
         for (uint32_t s = 0; s < p.stretches; ++s) {
-            const uint32_t c = p.counts[s * bins + tid];
-            before += s < blockIdx.x ? c : 0;
-            total += c;
+            const uint32_t c0 = p.counts[s * bins + 2 * tid], c1 = p.counts[s * bins + other];
+            base[0] += s < blockIdx.x ? c0 : 0;
+            base[1] += s < blockIdx.x ? c1 : 0;
+            total[0] += c0;
+            total[1] += c1;
         }
     }
-    uint32_t base = exclusive_sum(total, wave_sums) + before;
+    const uint32_t start = exclusive_sum(total[0] + total[1], wave_sums);
+    base[0] += start;
+    base[1] += start + total[0];
 
     const uint32_t first = blockIdx.x * p.stretch;
     const uint32_t last = min(p.n, first + p.stretch);
-    for (uint32_t step = first; step < last; step += kStep) {
+    for (uint32_t step = first; step < last; step += kPlaceStep) {
         Pair pair[kKeysPerThread];
         uint32_t rank[kKeysPerThread];
 #pragma unroll
         for (int k = 0; k < kKeysPerThread; ++k)
             pair[k] = number_of(k) < last - step ? pair_at<I>(p, step + number_of(k)) : Pair{0, 0};
-        for (int w = 0; w < kWaves; ++w)
-            seen[w][tid] = 0;
+        for (uint32_t b = tid; b < WAVES * kMaxBins; b += kPlaceThreads)
+            seen[0][b] = 0;
         __syncthreads();
         rank_keys(pair, last - step, p.shift, p.bits, seen[wave], rank);
         __syncthreads();
-        base = counts_to_starts(seen, tid, base);
+        base[0] = counts_to_starts<WAVES>(seen, 2 * tid, base[0]);
+        base[1] = counts_to_starts<WAVES>(seen, 2 * tid + 1, base[1]);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kKeysPerThread; ++k)
@@ -305,7 +328,7 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
     }
 }
 
-// All passes over at most kStep keys.
+// All passes over at most kSortStep keys.
 template <typename I>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
 {
@@ -313,12 +336,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
         clear_share(p.clear, blockIdx.x - 1);
         return;
     }
+    constexpr int WAVES = kSortThreads / 64;
+    static_assert(kMaxBins == kSortThreads, "a bin a thread");
     // the counts' place first, then the pairs'
-    __shared__ __align__(16) char shared[kStep * sizeof(Pair)];
-    __shared__ uint32_t wave_sums[kWaves];
+    __shared__ __align__(16) char shared[kSortStep * sizeof(Pair)];
+    __shared__ uint32_t wave_sums[WAVES];
     uint32_t (*seen)[kMaxBins] = reinterpret_cast<uint32_t (*)[kMaxBins]>(shared);
     Pair* pairs = reinterpret_cast<Pair*>(shared);
-    static_assert(sizeof(uint32_t) * kWaves * kMaxBins <= sizeof(shared), "the counts fit");
+    static_assert(sizeof(uint32_t) * WAVES * kMaxBins <= sizeof(shared), "the counts fit");
     const uint32_t tid = threadIdx.x, wave = tid >> 6;
     Pair pair[kKeysPerThread];
     uint32_t to[kKeysPerThread];
@@ -328,15 +353,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.bits;
         const uint32_t mask = (1u << p.bits) - 1;
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < WAVES; ++w)
             seen[w][tid] = 0;
         __syncthreads();
         rank_keys(pair, p.n, shift, p.bits, seen[wave], to);
         __syncthreads();
         uint32_t total = 0;
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < WAVES; ++w)
             total += seen[w][tid];
-        counts_to_starts(seen, tid, exclusive_sum(total, wave_sums));
+        counts_to_starts<WAVES>(seen, tid, exclusive_sum(total, wave_sums));
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kKeysPerThread; ++k)
@@ -403,8 +428,9 @@ __device__ __forceinline__ void finish(const SumParams& p, uint32_t key, uint32_
     }
 }
 
-// Entries whose rows are under way together.
-constexpr int kAhead = 8;
+// Entries whose rows are under way together; also of those past the tile and
+// of indices outside the table, whose positions are rows of `grad` too.
+constexpr int kSumAhead = 8;
 
 template <typename T, typename O, int V>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumParams p)
@@ -427,18 +453,17 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumParams p)
         for (int k = 0; k < V; ++k)
             to[static_cast<uint64_t>(group) * p.width + c * V + k] = acc[k];
     };
-    for (uint32_t i = first; i < last; i += kAhead) {
-        Pair pair[kAhead];
-        float v[kAhead][V];
+    for (uint32_t i = first; i < last; i += kSumAhead) {
+        Pair pair[kSumAhead];
+        float v[kSumAhead][V];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
+        for (int a = 0; a < kSumAhead; ++a)
             pair[a] = p.pairs[min(i + a, last - 1)];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (i + a < last && pair[a].key < p.rows)
-                load_run<T, V>(grad + pair[a].at * p.grad_stride, v[a]);
+        for (int a = 0; a < kSumAhead; ++a)
+            load_run<T, V>(grad + pair[a].at * p.grad_stride, v[a]);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
+        for (int a = 0; a < kSumAhead; ++a) {
             if (i + a >= last)
                 break;
             if (pair[a].key != key) {
@@ -585,8 +610,8 @@ Plan plan_of(int64_t n, int64_t rows, int64_t cols)
         ++bits;                          // the largest key is `rows`
     q.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     q.bits = (bits + q.passes - 1) / q.passes;
-    const int64_t steps = (n + kStep - 1) / kStep;
-    q.stretch = static_cast<uint32_t>((steps + kMaxStretches - 1) / kMaxStretches * kStep);
+    const int64_t steps = (n + kPlaceStep - 1) / kPlaceStep;
+    q.stretch = static_cast<uint32_t>((steps + kMaxStretches - 1) / kMaxStretches * kPlaceStep);
     q.stretches = q.stretch ? static_cast<uint32_t>((n + q.stretch - 1) / q.stretch) : 0;
     q.tiles = static_cast<uint32_t>((n + kTile - 1) / kTile);
     const size_t width = static_cast<size_t>(cols + 7) / 8 * 8;
@@ -656,6 +681,12 @@ hipError_t launch_lookup(const sqn_matrix& table, const void* ids, bool ids64, f
     p.items = static_cast<uint64_t>(out.rows);
     p.cols = static_cast<uint32_t>(table.cols);
     p.scale = scale;
+    if (table.rows == 0) {
+        // every index is outside: a row of the output stands in for the one
+        // that is read and not used
+        p.table = out.data;
+        p.table_stride = 0;
+    }
     if (table.dtype == SQN_F32)
         return lookup<float>(p, ids64, stream);
     if (table.dtype == SQN_F16)
@@ -695,14 +726,14 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
     s.shift = 0;
     s.in = nullptr;
     s.out = pairs[0];
-    const bool small = s.n <= kStep;
+    const bool small = s.n <= kSortStep;
     const uint32_t launches = small ? 1 : 2 * q.passes;
     uint32_t launch = 0;
     // the next launch's grid, with its share of the clearing
     auto grid = [&]() {
         c.first = pieces / launches * launch;
         c.last = ++launch == launches ? pieces : pieces / launches * launch;
-        const uint64_t want = (c.last - c.first + 4 * kSortThreads - 1) / (4 * kSortThreads);
+        const uint64_t want = (c.last - c.first + 4096 - 1) / 4096;
         c.blocks = static_cast<uint32_t>(want < 512 ? want : 512);
         s.clear = c;
         return dim3((small ? 1 : q.stretches) + c.blocks);
@@ -724,18 +755,18 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
             s.out = pairs[pass & 1];
             const dim3 count_grid = grid();
             if (pass > 0)
-                count_kernel<Sorted><<<count_grid, kSortThreads, 0, stream>>>(s);
+                count_kernel<Sorted><<<count_grid, kPlaceThreads, 0, stream>>>(s);
             else if (ids64)
-                count_kernel<int64_t><<<count_grid, kSortThreads, 0, stream>>>(s);
+                count_kernel<int64_t><<<count_grid, kPlaceThreads, 0, stream>>>(s);
             else
-                count_kernel<int32_t><<<count_grid, kSortThreads, 0, stream>>>(s);
+                count_kernel<int32_t><<<count_grid, kPlaceThreads, 0, stream>>>(s);
             const dim3 place_grid = grid();
             if (pass > 0)
-                place_kernel<Sorted><<<place_grid, kSortThreads, 0, stream>>>(s);
+                place_kernel<Sorted><<<place_grid, kPlaceThreads, 0, stream>>>(s);
             else if (ids64)
-                place_kernel<int64_t><<<place_grid, kSortThreads, 0, stream>>>(s);
+                place_kernel<int64_t><<<place_grid, kPlaceThreads, 0, stream>>>(s);
             else
-                place_kernel<int32_t><<<place_grid, kSortThreads, 0, stream>>>(s);
+                place_kernel<int32_t><<<place_grid, kPlaceThreads, 0, stream>>>(s);
         }
     }
     SumParams p;
