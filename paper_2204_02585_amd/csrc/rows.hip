@@ -201,11 +201,16 @@ __device__ __forceinline__ void rank_keys(const Pair (&pair)[kKeysPerThread], ui
     for (int k = 0; k < kKeysPerThread; ++k) {
         const bool there = number_of(k) < n;
         const uint32_t digit = pair[k].key >> shift & mask;
-        uint64_t same = __ballot(there);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot(digit >> b & 1);
-            same &= digit >> b & 1 ? set : ~set;
+        // lanes whose digit differs from this one's in some bit
+        uint32_t other_low = 0, other_high = 0;
+#pragma unroll
+        for (int b = 0; b < kMaxDigitBits; ++b) {
+            const uint32_t bit = static_cast<uint32_t>(static_cast<int32_t>(digit << (31 - b)) >> 31);   // 0 or all ones
+            const uint64_t set = __ballot(bit != 0);
+            other_low |= static_cast<uint32_t>(set) ^ bit;
+            other_high |= static_cast<uint32_t>(set >> 32) ^ bit;
         }
+        const uint64_t same = __ballot(there) & ~(static_cast<uint64_t>(other_high) << 32 | other_low);
         // the wave's LDS accesses stay in program order
         const uint32_t had = seen[digit];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -290,14 +295,14 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(SortParams p)
     // bins 2 tid and 2 tid + 1: their keys in all stretches, and in those before this one
     uint32_t total[2] = {0, 0}, base[2] = {0, 0};
     if (2 * tid < bins) {
-        const uint32_t other = min(2 * tid + 1, bins - 1);
-#pragma unroll 8
+        const uint2* counts = reinterpret_cast<const uint2*>(p.counts) + tid;
+#pragma unroll 16
         for (uint32_t s = 0; s < p.stretches; ++s) {
-            const uint32_t c0 = p.counts[s * bins + 2 * tid], c1 = p.counts[s * bins + other];
-            base[0] += s < blockIdx.x ? c0 : 0;
-            base[1] += s < blockIdx.x ? c1 : 0;
-            total[0] += c0;
-            total[1] += c1;
+            const uint2 c = counts[s * (bins / 2)];
+            base[0] += s < blockIdx.x ? c.x : 0;
+            base[1] += s < blockIdx.x ? c.y : 0;
+            total[0] += c.x;
+            total[1] += c.y;
         }
     }
     const uint32_t start = exclusive_sum(total[0] + total[1], wave_sums);
