@@ -118,13 +118,14 @@ hipError_t lookup(const LookupParams& base, bool ids64, hipStream_t stream)
 
 constexpr int kMaxDigitBits = 10;
 constexpr int kMaxBins = 1 << kMaxDigitBits;
-constexpr int kKeysPerThread = 16;
-// Threads that place a stretch's keys, and that sort all of few.  Twice as many
-// for a stretch leave half of the CUs idle (640,000 keys: 28 us a pass for
-// 16), half as many spend it on the counts of the stretches before.
-constexpr int kPlaceThreads = 512, kSortThreads = 1024;
-constexpr int kPlaceStep = kPlaceThreads * kKeysPerThread, kSortStep = kSortThreads * kKeysPerThread;   // keys at a time
+constexpr int kSortThreads = 1024;
+// Keys that a thread places of a stretch, and sorts of few in all.  Longer
+// stretches leave CUs idle, shorter ones are spent on the counts of the
+// stretches before (640,000 keys, us a pass: 16 keys a thread 25, 8 keys 22).
+constexpr int kPlaceKeys = 8, kSortKeys = 16;
+constexpr int kPlaceStep = kSortThreads * kPlaceKeys, kSortStep = kSortThreads * kSortKeys;
 constexpr int kMaxStretches = 128;
+constexpr int kWaves = kSortThreads / 64;
 
 struct __attribute__((aligned(8))) Pair {
     uint32_t key, at;
@@ -184,22 +185,24 @@ __device__ __forceinline__ Pair pair_at(const SortParams& p, uint32_t i)
     }
 }
 
-// Thread t's key k of a step is number 1024 (t / 64) + 64 k + t % 64.
+// The number in its step of a thread's key k of KEYS: a wave's keys lie together.
+template <int KEYS>
 __device__ __forceinline__ uint32_t number_of(int k)
 {
-    return (threadIdx.x >> 6) * (64 * kKeysPerThread) + 64 * k + (threadIdx.x & 63);
+    return (threadIdx.x >> 6) * (64 * KEYS) + 64 * k + (threadIdx.x & 63);
 }
 
 // A step's keys ranked among those of their digit in their wave, which counts
 // them in seen[digit]; keys from `n` on are not there.
-__device__ __forceinline__ void rank_keys(const Pair (&pair)[kKeysPerThread], uint32_t n, int shift, int bits, uint32_t* seen,
-                                          uint32_t (&rank)[kKeysPerThread])
+template <int KEYS>
+__device__ __forceinline__ void rank_keys(const Pair (&pair)[KEYS], uint32_t n, int shift, int bits, uint32_t* seen,
+                                          uint32_t (&rank)[KEYS])
 {
     const uint32_t mask = (1u << bits) - 1;
     const uint64_t below = (uint64_t{1} << (threadIdx.x & 63)) - 1;
 #pragma unroll
-    for (int k = 0; k < kKeysPerThread; ++k) {
-        const bool there = number_of(k) < n;
+    for (int k = 0; k < KEYS; ++k) {
+        const bool there = number_of<KEYS>(k) < n;
         const uint32_t digit = pair[k].key >> shift & mask;
         // lanes whose digit differs from this one's in some bit
         uint32_t other_low = 0, other_high = 0;
@@ -245,11 +248,10 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t v, uint32_t* wave_sum
 
 // seen[wave][bin] from counts to where the wave's first key of the bin goes,
 // given where the step's first goes; returns where the next step's does.
-template <int WAVES>
 __device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[kMaxBins], uint32_t bin, uint32_t at)
 {
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
         const uint32_t c = seen[w][bin];
         seen[w][bin] = at;
         at += c;
@@ -258,76 +260,69 @@ __device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[kMaxBins],
 }
 
 template <typename I>
-__global__ __launch_bounds__(kPlaceThreads) void count_kernel(SortParams p)
+__global__ __launch_bounds__(kSortThreads) void count_kernel(SortParams p)
 {
     if (blockIdx.x >= p.stretches) {
         clear_share(p.clear, blockIdx.x - p.stretches);
         return;
     }
+    static_assert(kMaxBins == kSortThreads, "a bin a thread");
     __shared__ uint32_t bins[kMaxBins];
-    for (uint32_t b = threadIdx.x; b < kMaxBins; b += kPlaceThreads)
-        bins[b] = 0;
+    bins[threadIdx.x] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * p.stretch;
     const uint32_t last = min(p.n, first + p.stretch);
     const uint32_t count = 1u << p.bits;
 #pragma unroll 8
-    for (uint32_t i = first + threadIdx.x; i < last; i += kPlaceThreads)
+    for (uint32_t i = first + threadIdx.x; i < last; i += kSortThreads)
         atomicAdd(&bins[pair_at<I>(p, i).key >> p.shift & (count - 1)], 1u);
     __syncthreads();
-    for (uint32_t b = threadIdx.x; b < count; b += kPlaceThreads)
-        p.counts[blockIdx.x * count + b] = bins[b];
+    if (threadIdx.x < count)
+        p.counts[blockIdx.x * count + threadIdx.x] = bins[threadIdx.x];
 }
 
 template <typename I>
-__global__ __launch_bounds__(kPlaceThreads) void place_kernel(SortParams p)
+__global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
 {
     if (blockIdx.x >= p.stretches) {
         clear_share(p.clear, blockIdx.x - p.stretches);
         return;
     }
-    constexpr int WAVES = kPlaceThreads / 64;
-    static_assert(kMaxBins == 2 * kPlaceThreads, "two bins a thread");
-    __shared__ uint32_t seen[WAVES][kMaxBins];    // of a step, per wave
-    __shared__ uint32_t wave_sums[WAVES];
+    __shared__ uint32_t seen[kWaves][kMaxBins];    // of a step, per wave
+    __shared__ uint32_t wave_sums[kWaves];
     const uint32_t bins = 1u << p.bits, tid = threadIdx.x, wave = tid >> 6;
 
-    // bins 2 tid and 2 tid + 1: their keys in all stretches, and in those before this one
-    uint32_t total[2] = {0, 0}, base[2] = {0, 0};
-    if (2 * tid < bins) {
-        const uint2* counts = reinterpret_cast<const uint2*>(p.counts) + tid;
+    // this bin's keys in all stretches, and in those before this one
+    uint32_t total = 0, base = 0;
+    if (tid < bins) {
 #pragma unroll 16
         for (uint32_t s = 0; s < p.stretches; ++s) {
-            const uint2 c = counts[s * (bins / 2)];
-            base[0] += s < blockIdx.x ? c.x : 0;
-            base[1] += s < blockIdx.x ? c.y : 0;
-            total[0] += c.x;
-            total[1] += c.y;
+            const uint32_t c = p.counts[s * bins + tid];
+            base += s < blockIdx.x ? c : 0;
+            total += c;
         }
     }
-    const uint32_t start = exclusive_sum(total[0] + total[1], wave_sums);
-    base[0] += start;
-    base[1] += start + total[0];
+    base += exclusive_sum(total, wave_sums);
 
     const uint32_t first = blockIdx.x * p.stretch;
     const uint32_t last = min(p.n, first + p.stretch);
     for (uint32_t step = first; step < last; step += kPlaceStep) {
-        Pair pair[kKeysPerThread];
-        uint32_t rank[kKeysPerThread];
+        Pair pair[kPlaceKeys];
+        uint32_t rank[kPlaceKeys];
 #pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k)
-            pair[k] = number_of(k) < last - step ? pair_at<I>(p, step + number_of(k)) : Pair{0, 0};
-        for (uint32_t b = tid; b < WAVES * kMaxBins; b += kPlaceThreads)
-            seen[0][b] = 0;
+        for (int k = 0; k < kPlaceKeys; ++k)
+            pair[k] = number_of<kPlaceKeys>(k) < last - step ? pair_at<I>(p, step + number_of<kPlaceKeys>(k)) : Pair{0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            seen[w][tid] = 0;
         __syncthreads();
         rank_keys(pair, last - step, p.shift, p.bits, seen[wave], rank);
         __syncthreads();
-        base[0] = counts_to_starts<WAVES>(seen, 2 * tid, base[0]);
-        base[1] = counts_to_starts<WAVES>(seen, 2 * tid + 1, base[1]);
+        base = counts_to_starts(seen, tid, base);
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k)
-            if (number_of(k) < last - step)
+        for (int k = 0; k < kPlaceKeys; ++k)
+            if (number_of<kPlaceKeys>(k) < last - step)
                 p.out[seen[wave][pair[k].key >> p.shift & (bins - 1)] + rank[k]] = pair[k];
         __syncthreads();
     }
@@ -341,52 +336,50 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
         clear_share(p.clear, blockIdx.x - 1);
         return;
     }
-    constexpr int WAVES = kSortThreads / 64;
-    static_assert(kMaxBins == kSortThreads, "a bin a thread");
     // the counts' place first, then the pairs'
     __shared__ __align__(16) char shared[kSortStep * sizeof(Pair)];
-    __shared__ uint32_t wave_sums[WAVES];
+    __shared__ uint32_t wave_sums[kWaves];
     uint32_t (*seen)[kMaxBins] = reinterpret_cast<uint32_t (*)[kMaxBins]>(shared);
     Pair* pairs = reinterpret_cast<Pair*>(shared);
-    static_assert(sizeof(uint32_t) * WAVES * kMaxBins <= sizeof(shared), "the counts fit");
+    static_assert(sizeof(uint32_t) * kWaves * kMaxBins <= sizeof(shared), "the counts fit");
     const uint32_t tid = threadIdx.x, wave = tid >> 6;
-    Pair pair[kKeysPerThread];
-    uint32_t to[kKeysPerThread];
+    Pair pair[kSortKeys];
+    uint32_t to[kSortKeys];
 #pragma unroll
-    for (int k = 0; k < kKeysPerThread; ++k)
-        pair[k] = number_of(k) < p.n ? pair_at<I>(p, number_of(k)) : Pair{0, 0};
+    for (int k = 0; k < kSortKeys; ++k)
+        pair[k] = number_of<kSortKeys>(k) < p.n ? pair_at<I>(p, number_of<kSortKeys>(k)) : Pair{0, 0};
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.bits;
         const uint32_t mask = (1u << p.bits) - 1;
-        for (int w = 0; w < WAVES; ++w)
+        for (int w = 0; w < kWaves; ++w)
             seen[w][tid] = 0;
         __syncthreads();
         rank_keys(pair, p.n, shift, p.bits, seen[wave], to);
         __syncthreads();
         uint32_t total = 0;
-        for (int w = 0; w < WAVES; ++w)
+        for (int w = 0; w < kWaves; ++w)
             total += seen[w][tid];
-        counts_to_starts<WAVES>(seen, tid, exclusive_sum(total, wave_sums));
+        counts_to_starts(seen, tid, exclusive_sum(total, wave_sums));
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k)
+        for (int k = 0; k < kSortKeys; ++k)
             to[k] += seen[wave][pair[k].key >> shift & mask];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k)
-            if (number_of(k) < p.n)
+        for (int k = 0; k < kSortKeys; ++k)
+            if (number_of<kSortKeys>(k) < p.n)
                 pairs[to[k]] = pair[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kKeysPerThread; ++k)
-            if (number_of(k) < p.n)
-                pair[k] = pairs[number_of(k)];
+        for (int k = 0; k < kSortKeys; ++k)
+            if (number_of<kSortKeys>(k) < p.n)
+                pair[k] = pairs[number_of<kSortKeys>(k)];
         __syncthreads();
     }
 #pragma unroll
-    for (int k = 0; k < kKeysPerThread; ++k)
-        if (number_of(k) < p.n)
-            p.out[number_of(k)] = pair[k];
+    for (int k = 0; k < kSortKeys; ++k)
+        if (number_of<kSortKeys>(k) < p.n)
+            p.out[number_of<kSortKeys>(k)] = pair[k];
 }
 
 // ---- gradient: sums
@@ -760,18 +753,18 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
             s.out = pairs[pass & 1];
             const dim3 count_grid = grid();
             if (pass > 0)
-                count_kernel<Sorted><<<count_grid, kPlaceThreads, 0, stream>>>(s);
+                count_kernel<Sorted><<<count_grid, kSortThreads, 0, stream>>>(s);
             else if (ids64)
-                count_kernel<int64_t><<<count_grid, kPlaceThreads, 0, stream>>>(s);
+                count_kernel<int64_t><<<count_grid, kSortThreads, 0, stream>>>(s);
             else
-                count_kernel<int32_t><<<count_grid, kPlaceThreads, 0, stream>>>(s);
+                count_kernel<int32_t><<<count_grid, kSortThreads, 0, stream>>>(s);
             const dim3 place_grid = grid();
             if (pass > 0)
-                place_kernel<Sorted><<<place_grid, kPlaceThreads, 0, stream>>>(s);
+                place_kernel<Sorted><<<place_grid, kSortThreads, 0, stream>>>(s);
             else if (ids64)
-                place_kernel<int64_t><<<place_grid, kPlaceThreads, 0, stream>>>(s);
+                place_kernel<int64_t><<<place_grid, kSortThreads, 0, stream>>>(s);
             else
-                place_kernel<int32_t><<<place_grid, kPlaceThreads, 0, stream>>>(s);
+                place_kernel<int32_t><<<place_grid, kSortThreads, 0, stream>>>(s);
         }
     }
     SumParams p;
