@@ -1,5 +1,7 @@
 // Matrices in 4-bit blocks (MXFP4: 32 E2M1 elements and an E8M0 scale) and
 // the layers evaluated on them.
+#include <type_traits>
+
 #include "learn.h"
 #include "numeric.h"
 #include "sqn_internal.h"
@@ -10,6 +12,7 @@ namespace {
 
 typedef int int8v __attribute__((ext_vector_type(8)));
 typedef int int4v __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr uint32_t kOne = 127;           // E8M0 of 1
@@ -414,6 +417,167 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
     });
 }
 
+// ---- products of few points
+//
+// Up to kFew points (one token's activations among them) the weights' bytes are
+// all that takes time, and a launch of its own for the activations' blocks
+// would take longer than the product.  A workgroup computes 16 units of all
+// points on v_mfma_scale_f32_16x16x128_f8f6f4; its waves share the sum and add
+// up in LDS, in the order of the waves.  Every wave puts the points' elements
+// of its stretch into blocks by itself.  4096 x 4096 of one point: 8.9 MB of
+// weights from the caches.
+
+constexpr uint32_t kFew = 16;
+constexpr int kFewAhead = 4;         // steps whose weights are under way together
+constexpr int kFewMaxWaves = 16;
+
+struct FewParams {
+    const uint8_t *w, *w_scales;
+    const void* x;                   // rows of elements, or codes
+    const uint8_t* x_scales;         // of codes
+    const float* bias;
+    void* out;
+    int64_t x_stride, out_stride;    // elements
+    uint32_t points, units, cols, blocks;
+    uint32_t steps;                  // of four blocks, per wave
+    int32_t relu, dtype;
+};
+
+// the type of x where it is in blocks already
+struct Blocks {};
+
+struct Operand {
+    int4v codes;
+    int scale;
+};
+
+// A lane's block of a row in blocks; zeros past the row.
+__device__ __forceinline__ Operand load_block(const uint8_t* codes, const uint8_t* scales, uint32_t row, uint32_t block,
+                                              uint32_t blocks, bool there)
+{
+    Operand o = {int4v{0, 0, 0, 0}, static_cast<int>(kOne)};
+    if (there && block < blocks) {
+        const uint64_t at = static_cast<uint64_t>(row) * blocks + block;
+        o.codes = *reinterpret_cast<const int4v*>(codes + 16 * at);
+        o.scale = scales[at];
+    }
+    return o;
+}
+
+// ... of a row of elements.
+template <typename T>
+__device__ __forceinline__ Operand encode_block(const T* row, uint32_t block, uint32_t cols, bool there)
+{
+    float v[4][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (there) {
+            load_eight<T>(row, 32 * block + 8 * q, cols, v[q]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v[q][k] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            top = max(top, __float_as_uint(v[q][k]) & 0x7fffffffu);
+    }
+    Operand o;
+    o.scale = static_cast<int>(scale_byte(top));
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        o.codes[q] = static_cast<int>(encode8(v[q], o.scale));
+    return o;
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kFewMaxWaves) void few_kernel(FewParams p)
+{
+    __shared__ float4v sums[kFewMaxWaves][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t row = lane & 15, unit = min(blockIdx.x * 16 + row, p.units - 1);
+    const bool there = row < p.points;
+    const uint32_t first = wave * p.steps, last = min(first + p.steps, (p.blocks + 3) / 4);
+    float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t k = first; k < last; k += kFewAhead) {
+        Operand w[kFewAhead], x[kFewAhead];
+#pragma unroll
+        for (int a = 0; a < kFewAhead; ++a)
+            w[a] = load_block(p.w, p.w_scales, unit, 4 * (k + a) + (lane >> 4), p.blocks, k + a < last);
+#pragma unroll
+        for (int a = 0; a < kFewAhead; ++a) {
+            const uint32_t block = 4 * (k + a) + (lane >> 4);
+            if constexpr (std::is_same<T, Blocks>::value)
+                x[a] = load_block(static_cast<const uint8_t*>(p.x), p.x_scales, row, block, p.blocks, there && k + a < last);
+            else
+                x[a] = encode_block(static_cast<const T*>(p.x) + row * p.x_stride, block, p.cols, there && k + a < last);
+        }
+#pragma unroll
+        for (int a = 0; a < kFewAhead; ++a) {
+            const int8v w8 = __builtin_shufflevector(w[a].codes, w[a].codes, 0, 1, 2, 3, -1, -1, -1, -1);
+            const int8v x8 = __builtin_shufflevector(x[a].codes, x[a].codes, 0, 1, 2, 3, -1, -1, -1, -1);
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, acc, 4, 4, 0, w[a].scale, 0, x[a].scale);
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave > 0)
+        return;
+    for (uint32_t k = 1; k < waves; ++k)
+        acc += sums[k][lane];
+    // element q: unit 4 (lane / 16) + q of point lane % 16
+    if (!there)
+        return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t u = blockIdx.x * 16 + 4 * (lane >> 4) + q;
+        if (u >= p.units)
+            break;
+        float v = acc[q];
+        if (p.bias)
+            v += p.bias[u];
+        if (p.relu)
+            v = v < 0.0f ? 0.0f : v;
+        const int64_t at = row * p.out_stride + u;
+        if (p.dtype == SQN_F32)
+            static_cast<float*>(p.out)[at] = v;
+        else if (p.dtype == SQN_F16)
+            static_cast<_Float16*>(p.out)[at] = static_cast<_Float16>(v);
+        else
+            static_cast<__bf16*>(p.out)[at] = static_cast<__bf16>(v);
+    }
+}
+
+template <typename T>
+hipError_t launch_few(const void* x, const uint8_t* x_scales, int64_t x_stride, int64_t points, const sqn_quantised& w,
+                      const float* bias, bool relu, const sqn_matrix& out, hipStream_t stream)
+{
+    FewParams p;
+    p.w = static_cast<const uint8_t*>(w.codes);
+    p.w_scales = static_cast<const uint8_t*>(w.scales);
+    p.x = x;
+    p.x_scales = x_scales;
+    p.bias = bias;
+    p.out = out.data;
+    p.x_stride = x_stride;
+    p.out_stride = out.row_stride;
+    p.points = static_cast<uint32_t>(points);
+    p.units = static_cast<uint32_t>(w.rows);
+    p.cols = static_cast<uint32_t>(w.cols);
+    p.blocks = static_cast<uint32_t>(quant_blocks(w.cols));
+    p.relu = relu ? 1 : 0;
+    p.dtype = out.dtype;
+    // a wave takes a batch of steps or more, unless that leaves CUs with little
+    const uint32_t groups = (p.units + 15) / 16, steps = (p.blocks + 3) / 4;
+    uint32_t waves = 1;
+    while (waves < kFewMaxWaves && waves < steps && (groups * waves < 2048 || steps > waves * kFewAhead))
+        waves *= 2;
+    p.steps = (steps + waves - 1) / waves;
+    few_kernel<T><<<groups, 64 * waves, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // The packed scales of a product's factors, rows up to whole tiles.
@@ -533,6 +697,8 @@ hipError_t launch_quantised_values(const sqn_quantised& x, const sqn_matrix& out
 hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised& w, const float* bias, bool relu,
                                     const sqn_matrix& out, void* workspace, hipStream_t stream)
 {
+    if (x.rows <= kFew)
+        return launch_few<Blocks>(x.codes, static_cast<const uint8_t*>(x.scales), 0, x.rows, w, bias, relu, out, stream);
     const ProductScratch t(x.rows, w.rows, x.cols, workspace);
     const PackParams pw = pack_of(w, t.w_packed), px = pack_of(x, t.x_packed);
     const uint32_t groups_w = stream_blocks(pw.words), groups_x = stream_blocks(px.words);
@@ -542,17 +708,26 @@ hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised&
 
 size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols)
 {
-    return ProductScratch(points, units, cols, nullptr).bytes;
+    return points <= kFew ? 0 : ProductScratch(points, units, cols, nullptr).bytes;
 }
 
 size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols)
 {
+    if (points <= kFew)
+        return 0;
     return padded(16 * static_cast<size_t>(points) * quant_blocks(cols)) + quantised_product_bytes(points, units, cols);
 }
 
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
                                   const sqn_matrix& out, void* workspace, hipStream_t stream)
 {
+    if (x.rows <= kFew) {
+        if (x.dtype == SQN_F32)
+            return launch_few<float>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
+        if (x.dtype == SQN_F16)
+            return launch_few<_Float16>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
+        return launch_few<__bf16>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
+    }
     sqn_quantised q;
     q.rows = x.rows;
     q.cols = x.cols;

@@ -32,11 +32,11 @@ def _code(dtype: torch.dtype, name: str) -> int:
     return code
 
 
-def _on_gpu(t: torch.Tensor, name: str, device=None) -> None:
-    if t.device.type != "cuda":
+def _on_gpu(t: torch.Tensor, name: str, beside: Optional[torch.Tensor] = None) -> None:
+    if not t.is_cuda:
         raise ValueError(f"{name} must live on a CUDA device")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} must live on {device}, not {t.device}")
+    if beside is not None and t.get_device() != beside.get_device():
+        raise ValueError(f"{name} must live on {beside.device}, not {t.device}")
 
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
@@ -55,19 +55,23 @@ def _matrix(t: torch.Tensor, name: str) -> binding.Matrix:
     return binding.Matrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, _code(t.dtype, name), 0)
 
 
-def _out(out: Optional[torch.Tensor], shape, dtype, device, name: str = "out") -> torch.Tensor:
-    """A new tensor, or the caller's, whose rows must lie apart."""
+def _out(out: Optional[torch.Tensor], shape, dtype, beside: torch.Tensor, name: str = "out") -> torch.Tensor:
+    """A new tensor beside another, or the caller's, whose rows must lie apart."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}")
+        return torch.empty(shape, dtype=dtype, device=beside.device)
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.device != beside.device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {beside.device}")
     if not out.is_contiguous() and not (out.dim() == 2 and out.stride(1) == 1 and out.stride(0) >= out.shape[1]):
         raise ValueError(f"{name} must be contiguous, or a matrix of contiguous rows")
     return out
 
 
-def _workspace(size: int, device) -> torch.Tensor:
-    return torch.empty(size, dtype=torch.uint8, device=device)
+def _workspace(size: int, beside: torch.Tensor) -> Optional[torch.Tensor]:
+    return torch.empty(size, dtype=torch.uint8, device=beside.device) if size else None
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def _on(stream, *tensors) -> int:
@@ -80,10 +84,10 @@ def _on(stream, *tensors) -> int:
 
 # ---------------------------------------------------------------- rows of a table
 
-def _ids(ids: torch.Tensor, device) -> torch.Tensor:
+def _ids(ids: torch.Tensor, beside: torch.Tensor) -> torch.Tensor:
     if ids.dtype not in _IDS:
         raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
-    _on_gpu(ids, "ids", device)
+    _on_gpu(ids, "ids", beside)
     return ids if ids.is_contiguous() else ids.contiguous()
 
 
@@ -91,8 +95,8 @@ def _lookup(table, ids, scale, out, stream):
     _on_gpu(table, "table")
     if table.dim() != 2:
         raise ValueError(f"table must be a matrix, got shape {tuple(table.shape)}")
-    source, ids = _rows(table), _ids(ids, table.device)
-    out = _out(out, (*ids.shape, table.shape[1]), table.dtype, table.device)
+    source, ids = _rows(table), _ids(ids, table)
+    out = _out(out, (*ids.shape, table.shape[1]), table.dtype, table)
     _check(lib.sqn_lookup(_matrix(source, "table"), ids.data_ptr(), _IDS[ids.dtype], float(scale),
                           _matrix(_rows(out), "out"), _on(stream, source, ids, out)))
     return out
@@ -118,7 +122,7 @@ def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Opti
     requires a gradient (without `out` and `stream`), by lookup_gradient."""
     if out is None and stream is None and table.requires_grad and torch.is_grad_enabled():
         return _Lookup.apply(table, ids, float(scale))
-    return _lookup(table.detach(), ids, scale, out, stream)
+    return _lookup(table, ids, scale, out, stream)
 
 
 def lookup_gradient(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 1.0,
@@ -132,15 +136,15 @@ def lookup_gradient(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: flo
         raise ValueError(f"grad of shape {tuple(grad.shape)} does not go with ids of shape {tuple(ids.shape)}")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    ids, device = _ids(ids, grad.device), grad.device
+    ids = _ids(ids, grad)
     if out is not None and dtype is None:
         dtype = out.dtype
-    out = _out(out, (int(rows), grad.shape[-1]), dtype or grad.dtype, device)
+    out = _out(out, (int(rows), grad.shape[-1]), dtype or grad.dtype, grad)
     source = _rows(grad)
     size = lib.sqn_lookup_gradient_workspace(ids.numel(), out.shape[0], out.shape[1])
-    work = _workspace(size, device)
+    work = _workspace(size, grad)
     _check(lib.sqn_lookup_gradient(_matrix(source, "grad"), ids.data_ptr(), _IDS[ids.dtype], float(scale),
-                                   1 if accumulate else 0, _matrix(out, "out"), work.data_ptr(), size,
+                                   1 if accumulate else 0, _matrix(out, "out"), _ptr(work), size,
                                    _on(stream, source, ids, out, work)))
     return out
 
@@ -172,9 +176,9 @@ def orthogonalise(updates: torch.Tensor, steps: int = 5, coefficients=MUON, eps:
         return out
     into = _batch(target, "out")
     size = lib.sqn_orthogonalise_workspace(into.batch, into.rows, into.cols, into.dtype)
-    work = _workspace(size, updates.device)
+    work = _workspace(size, updates)
     k = (ctypes.c_float * 3)(*coefficients)
-    _check(lib.sqn_orthogonalise(_batch(source, "updates"), int(steps), k, float(eps), into, work.data_ptr(), size,
+    _check(lib.sqn_orthogonalise(_batch(source, "updates"), int(steps), k, float(eps), into, _ptr(work), size,
                                  _on(stream, updates, out, work)))
     return out
 
@@ -195,7 +199,7 @@ class Quantised:
             raise ValueError(f"codes uint8 [rows, {16 * blocks}] and scales uint8 [rows, {blocks}] hold {cols} columns, "
                              f"got {codes.dtype} {tuple(codes.shape)} and {scales.dtype} {tuple(scales.shape)}")
         _on_gpu(codes, "codes")
-        _on_gpu(scales, "scales", codes.device)
+        _on_gpu(scales, "scales", codes)
         if not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales must be contiguous")
         self.codes, self.scales, self.cols = codes, scales, int(cols)
@@ -214,7 +218,7 @@ class Quantised:
     def values(self, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """sqn_quantised_values: what the blocks stand for, [rows, cols]."""
         _code(dtype, "dtype")
-        out = _out(out, self.shape, dtype, self.device)
+        out = _out(out, self.shape, dtype, self.codes)
         _check(lib.sqn_quantised_values(self._arg(), _matrix(out, "out"), _on(stream, self.codes, self.scales, out)))
         return out
 
@@ -243,36 +247,31 @@ def product(x, w: Quantised, bias: Optional[torch.Tensor] = None, relu: bool = F
     blocks = isinstance(x, Quantised)
     if not isinstance(w, Quantised):
         raise TypeError("w must be Quantised")
-    device = w.device
-    if not blocks:
-        _on_gpu(x, "x", device)
-        if x.dim() < 1:
-            raise ValueError("x must have a last axis of columns")
-    elif x.device != device:
-        raise ValueError(f"x must live on {device}, not {x.device}")
-    if x.shape[-1] != w.cols:
-        raise ValueError(f"x has {x.shape[-1]} columns, w {w.cols}")
+    _on_gpu(x.codes if blocks else x, "x", w.codes)
+    shape = x.shape
+    if len(shape) < 1 or shape[-1] != w.cols:
+        raise ValueError(f"x must have w's {w.cols} columns, got shape {tuple(shape)}")
+    units = w.codes.shape[0]
     if bias is not None:
-        _on_gpu(bias, "bias", device)
-        if bias.dtype != torch.float32 or tuple(bias.shape) != (w.shape[0],) or not bias.is_contiguous():
-            raise ValueError(f"bias must be a contiguous float32 tensor of shape {(w.shape[0],)}")
+        _on_gpu(bias, "bias", w.codes)
+        if bias.dtype != torch.float32 or bias.shape != (units,) or not bias.is_contiguous():
+            raise ValueError(f"bias must be a contiguous float32 tensor of shape {(units,)}")
     if dtype is None:
         dtype = out.dtype if out is not None else torch.float32 if blocks else x.dtype
     _code(dtype, "dtype")
-    out = _out(out, (*x.shape[:-1], w.shape[0]), dtype, device)
+    out = _out(out, (*shape[:-1], units), dtype, w.codes)
     if out.numel() == 0:
         return out
     into = _matrix(_rows(out), "out")
-    at = None if bias is None else bias.data_ptr()
     if blocks:
-        size = lib.sqn_quantised_product_workspace(x.shape[0], w.shape[0], w.cols)
-        work = _workspace(size, device)
-        _check(lib.sqn_quantised_product(x._arg(), w._arg(), at, 1 if relu else 0, into, work.data_ptr(), size,
+        size = lib.sqn_quantised_product_workspace(shape[0], units, w.cols)
+        work = _workspace(size, out)
+        _check(lib.sqn_quantised_product(x._arg(), w._arg(), _ptr(bias), 1 if relu else 0, into, _ptr(work), size,
                                          _on(stream, x.codes, x.scales, w.codes, w.scales, bias, out, work)))
         return out
     source = _rows(x)
-    size = lib.sqn_quantised_layer_workspace(source.shape[0], w.shape[0], w.cols)
-    work = _workspace(size, device)
-    _check(lib.sqn_quantised_layer(_matrix(source, "x"), w._arg(), at, 1 if relu else 0, into, work.data_ptr(), size,
+    size = lib.sqn_quantised_layer_workspace(source.shape[0], units, w.cols)
+    work = _workspace(size, out)
+    _check(lib.sqn_quantised_layer(_matrix(source, "x"), w._arg(), _ptr(bias), 1 if relu else 0, into, _ptr(work), size,
                                    _on(stream, source, w.codes, w.scales, bias, out, work)))
     return out
