@@ -428,7 +428,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
 // weights from the caches.
 
 constexpr uint32_t kFew = 16;
-constexpr int kFewAhead = 4;         // steps whose weights are under way together
+constexpr int kFewAhead = 2;         // steps whose weights are under way together
 constexpr int kFewMaxWaves = 16;
 
 struct FewParams {
@@ -451,43 +451,64 @@ struct Operand {
     int scale;
 };
 
-// A lane's block of a row in blocks; zeros past the row.
+// The loads of a block are the same for every lane, from a place inside the
+// row where it has none, so that all of a wave's are under way together; zeros
+// of scale 1 take the place of what is not there.
+
 __device__ __forceinline__ Operand load_block(const uint8_t* codes, const uint8_t* scales, uint32_t row, uint32_t block,
                                               uint32_t blocks, bool there)
 {
-    Operand o = {int4v{0, 0, 0, 0}, static_cast<int>(kOne)};
-    if (there && block < blocks) {
-        const uint64_t at = static_cast<uint64_t>(row) * blocks + block;
-        o.codes = *reinterpret_cast<const int4v*>(codes + 16 * at);
-        o.scale = scales[at];
-    }
+    const uint64_t at = static_cast<uint64_t>(row) * blocks + min(block, blocks - 1);
+    Operand o;
+    o.codes = *reinterpret_cast<const int4v*>(codes + 16 * at);
+    o.scale = scales[at];
+    if (!there || block >= blocks)
+        o = Operand{int4v{0, 0, 0, 0}, static_cast<int>(kOne)};
     return o;
 }
 
-// ... of a row of elements.
+// A block of a row of elements as it lies in memory.
 template <typename T>
-__device__ __forceinline__ Operand encode_block(const T* row, uint32_t block, uint32_t cols, bool there)
+struct Elements {
+    Run<T, 8> part[4];
+};
+
+template <typename T>
+__device__ __forceinline__ Elements<T> load_elements(const T* row, uint32_t block, uint32_t cols)
 {
-    float v[4][8];
+    Elements<T> e;
+    if (cols >= 32) {
+        const T* from = row + min(32 * block, cols - 32);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            e.part[q] = *reinterpret_cast<const Run<T, 8>*>(from + 8 * q);
+    }
+    return e;
+}
+
+template <typename T>
+__device__ __forceinline__ Operand encode_block(const Elements<T>& e, const T* row, uint32_t block, uint32_t cols,
+                                                bool there)
+{
+    float v[32];
+    T raw[32];
+    __builtin_memcpy(raw, &e, sizeof(raw));
+    if (32 * block + 32 > cols) {        // a row's last block, or none
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            raw[k] = 32 * block + k < cols ? row[32 * block + k] : from_f32<T>(0.0f);
+    }
     uint32_t top = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (there) {
-            load_eight<T>(row, 32 * block + 8 * q, cols, v[q]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                v[q][k] = 0.0f;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            top = max(top, __float_as_uint(v[q][k]) & 0x7fffffffu);
+    for (int k = 0; k < 32; ++k) {
+        v[k] = there ? to_f32(raw[k]) : 0.0f;
+        top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
     }
     Operand o;
     o.scale = static_cast<int>(scale_byte(top));
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        o.codes[q] = static_cast<int>(encode8(v[q], o.scale));
+        o.codes[q] = static_cast<int>(encode8(v + 8 * q, o.scale));
     return o;
 }
 
@@ -502,19 +523,24 @@ __global__ __launch_bounds__(64 * kFewMaxWaves) void few_kernel(FewParams p)
     float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (uint32_t k = first; k < last; k += kFewAhead) {
         Operand w[kFewAhead], x[kFewAhead];
-#pragma unroll
-        for (int a = 0; a < kFewAhead; ++a)
-            w[a] = load_block(p.w, p.w_scales, unit, 4 * (k + a) + (lane >> 4), p.blocks, k + a < last);
+        Elements<std::conditional_t<std::is_same<T, Blocks>::value, float, T>> e[kFewAhead];
+        const T* row_x = nullptr;
+        if constexpr (!std::is_same<T, Blocks>::value)
+            row_x = static_cast<const T*>(p.x) + (there ? row : 0) * p.x_stride;
 #pragma unroll
         for (int a = 0; a < kFewAhead; ++a) {
             const uint32_t block = 4 * (k + a) + (lane >> 4);
+            w[a] = load_block(p.w, p.w_scales, unit, block, p.blocks, k + a < last);
             if constexpr (std::is_same<T, Blocks>::value)
-                x[a] = load_block(static_cast<const uint8_t*>(p.x), p.x_scales, row, block, p.blocks, there && k + a < last);
+                x[a] = load_block(static_cast<const uint8_t*>(p.x), p.x_scales, there ? row : 0, block, p.blocks,
+                                  there && k + a < last);
             else
-                x[a] = encode_block(static_cast<const T*>(p.x) + row * p.x_stride, block, p.cols, there && k + a < last);
+                e[a] = load_elements(row_x, block, p.cols);
         }
 #pragma unroll
         for (int a = 0; a < kFewAhead; ++a) {
+            if constexpr (!std::is_same<T, Blocks>::value)
+                x[a] = encode_block(e[a], row_x, 4 * (k + a) + (lane >> 4), p.cols, there && k + a < last);
             const int8v w8 = __builtin_shufflevector(w[a].codes, w[a].codes, 0, 1, 2, 3, -1, -1, -1, -1);
             const int8v x8 = __builtin_shufflevector(x[a].codes, x[a].codes, 0, 1, 2, 3, -1, -1, -1, -1);
             acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, acc, 4, 4, 0, w[a].scale, 0, x[a].scale);
