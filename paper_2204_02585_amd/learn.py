@@ -16,7 +16,7 @@ from typing import Optional
 import torch
 
 from . import binding
-from .binding import _check, _current_stream, _order_after_current, lib
+from .binding import Matrix, _check, _current_stream, _order_after_current, lib
 
 BLOCK = 32                                      # elements of a 4-bit block
 MUON = (3.4445, -4.7750, 2.0315)                # the Muon optimiser's coefficients
@@ -49,15 +49,20 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     return t
 
 
-def _matrix(t: torch.Tensor, name: str) -> binding.Matrix:
+def _matrix(t: torch.Tensor, name: str) -> Matrix:
     """`t` is of _rows()'s form."""
     rows, cols = t.shape
-    return binding.Matrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, _code(t.dtype, name), 0)
+    code = _CODES.get(t.dtype)
+    if code is None:
+        code = _code(t.dtype, name)
+    return Matrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, code, 0)
 
 
 def _out(out: Optional[torch.Tensor], shape, dtype, beside: torch.Tensor, name: str = "out") -> torch.Tensor:
     """A new tensor beside another, or the caller's, whose rows must lie apart."""
     if out is None:
+        if type(beside) is torch.Tensor:
+            return beside.new_empty(shape, dtype=dtype)
         return torch.empty(shape, dtype=dtype, device=beside.device)
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.device != beside.device:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {beside.device}")
@@ -92,13 +97,20 @@ def _ids(ids: torch.Tensor, beside: torch.Tensor) -> torch.Tensor:
 
 
 def _lookup(table, ids, scale, out, stream):
+    # a few rows take less time on the GPU (3 us for 32 of 2 KB) than this call
+    # takes to issue (8 us), so what is known here is not looked up again
     _on_gpu(table, "table")
     if table.dim() != 2:
         raise ValueError(f"table must be a matrix, got shape {tuple(table.shape)}")
     source, ids = _rows(table), _ids(ids, table)
-    out = _out(out, (*ids.shape, table.shape[1]), table.dtype, table)
-    _check(lib.sqn_lookup(_matrix(source, "table"), ids.data_ptr(), _IDS[ids.dtype], float(scale),
-                          _matrix(_rows(out), "out"), _on(stream, source, ids, out)))
+    of = _matrix(source, "table")
+    if out is None:
+        out = _out(None, (*ids.shape, of.cols), table.dtype, table)
+        into = Matrix(out.data_ptr(), ids.numel(), of.cols, of.cols, of.dtype, 0)
+    else:
+        out = _out(out, (*ids.shape, of.cols), table.dtype, table)
+        into = _matrix(_rows(out), "out")
+    _check(lib.sqn_lookup(of, ids.data_ptr(), _IDS[ids.dtype], scale, into, _on(stream, source, ids, out)))
     return out
 
 
@@ -107,7 +119,7 @@ class _Lookup(torch.autograd.Function):
     def forward(ctx, table, ids, scale):
         ctx.save_for_backward(ids)
         ctx.rows, ctx.scale, ctx.dtype = table.shape[0], scale, table.dtype
-        return _lookup(table, ids, scale, None, None)
+        return _lookup(table.detach(), ids, scale, None, None)
 
     @staticmethod
     def backward(ctx, grad):
@@ -122,7 +134,7 @@ def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Opti
     requires a gradient (without `out` and `stream`), by lookup_gradient."""
     if out is None and stream is None and table.requires_grad and torch.is_grad_enabled():
         return _Lookup.apply(table, ids, float(scale))
-    return _lookup(table, ids, scale, out, stream)
+    return _lookup(table, ids, float(scale), out, stream)
 
 
 def lookup_gradient(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 1.0,
@@ -193,9 +205,8 @@ class Quantised:
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int):
         blocks = (cols + BLOCK - 1) // BLOCK
-        rows = codes.shape[0]
-        if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (rows, 16 * blocks)
-                or tuple(scales.shape) != (rows, blocks) or cols < 1):
+        if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or cols < 1
+                or codes.shape[1] != 16 * blocks or scales.shape != (codes.shape[0], blocks)):
             raise ValueError(f"codes uint8 [rows, {16 * blocks}] and scales uint8 [rows, {blocks}] hold {cols} columns, "
                              f"got {codes.dtype} {tuple(codes.shape)} and {scales.dtype} {tuple(scales.shape)}")
         _on_gpu(codes, "codes")
