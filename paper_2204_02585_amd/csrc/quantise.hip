@@ -57,6 +57,9 @@ struct PackParams {
     PackedScales packed;
     uint64_t words;          // rows * steps * 2
     uint32_t blocks;
+    // codes to copy with rows filled up to whole steps by zeros, or null
+    const uint4* codes;
+    uint4* codes_to;
 };
 
 // A workgroup's share of the words: row by row, a word of four blocks a thread.
@@ -71,6 +74,12 @@ __device__ __forceinline__ void pack_share(const PackParams& p, uint32_t group, 
         for (uint32_t k = 0; k < 4; ++k)
             word |= (block + k < p.blocks ? p.from[static_cast<uint64_t>(row) * p.blocks + block + k] : kOne) << (8 * k);
         *reinterpret_cast<uint32_t*>(p.packed.to + packed_at(row, block, p.packed.steps)) = word;
+        if (p.codes) {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)
+                p.codes_to[row * static_cast<uint64_t>(4 * per_row) + block + k]
+                    = block + k < p.blocks ? p.codes[static_cast<uint64_t>(row) * p.blocks + block + k] : uint4{0, 0, 0, 0};
+        }
     }
 }
 
@@ -161,19 +170,20 @@ __global__ __launch_bounds__(kThreads) void quantise_packed_kernel(QuantParams p
         pack_share(w, blockIdx.x - groups, gridDim.x - groups);
         return;
     }
-    // all blocks of the steps, the scales of those past the matrix too
+    // all blocks of the steps, zeros in those past the matrix
     const uint32_t per_row = 32 * packed.steps;
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.items;
          i += static_cast<uint64_t>(groups) * kThreads) {
         const uint32_t r = static_cast<uint32_t>(i / per_row);
         const uint32_t q = static_cast<uint32_t>(i - r * static_cast<uint64_t>(per_row)), block = q >> 2;
-        uint32_t byte = kOne;
+        uint32_t byte = kOne, codes = 0;
         if (block < p.blocks) {
             float v[8];
             load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols, v);
             byte = shared_scale(v);
-            reinterpret_cast<uint32_t*>(p.codes)[static_cast<uint64_t>(r) * 4 * p.blocks + q] = encode8(v, byte);
+            codes = encode8(v, byte);
         }
+        reinterpret_cast<uint32_t*>(p.codes)[i] = codes;
         if ((q & 3) == 0)
             packed.to[packed_at(r, block, packed.steps)] = static_cast<uint8_t>(byte);
     }
@@ -234,7 +244,8 @@ struct ProductParams {
     const float* bias;
     void* out;
     int64_t out_stride;
-    uint32_t points, units, blocks, steps;
+    uint32_t points, units, steps;
+    uint32_t x_row, w_row;           // bytes from row to row of the codes
     int32_t relu;
 };
 
@@ -255,18 +266,15 @@ struct Fragments {
     int4v w[S::FM], x[S::FN];
 };
 
-// what lanes bring whose piece lies past the row
-__device__ const int4v kZeros = {0, 0, 0, 0};
-
+// A step's rows of one factor, each lane's pieces from `at` on; pieces past
+// `limit` are that one instead.
 template <typename S>
-__device__ __forceinline__ void bring_rows(const uint8_t* rows, const uint32_t (&at)[S::BRINGS], bool inside, uint32_t k,
-                                           char* to)
+__device__ __forceinline__ void bring_rows(const uint8_t* rows, const uint32_t (&at)[S::BRINGS], uint32_t limit,
+                                           uint32_t wave, char* to)
 {
-    const uint32_t wave = threadIdx.x >> 6;
-    const char* from = reinterpret_cast<const char*>(rows) + static_cast<uint64_t>(k) * kStepBytes;
 #pragma unroll
     for (int i = 0; i < S::BRINGS; ++i)
-        bring(inside ? from + at[i] : reinterpret_cast<const char*>(&kZeros), to + (S::WAVES * i + wave) * 1024);
+        bring(reinterpret_cast<const char*>(rows) + min(at[i], limit), to + (S::WAVES * i + wave) * 1024);
 }
 
 template <int O>
@@ -384,25 +392,27 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
     // arrays of their own, so that reads of one do not wait for loads into another
     __shared__ __align__(16) char buffer0[S::BUFFER];
     __shared__ __align__(16) char buffer1[S::BUFFER];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t unit_tiles = (p.units + S::SIDE - 1) / S::SIDE;
     const uint32_t tj = blockIdx.x / unit_tiles, ti = blockIdx.x - tj * unit_tiles;
     const uint32_t unit0 = ti * S::SIDE, point0 = tj * S::SIDE;
-    const uint32_t row_bytes = 16 * p.blocks;
-    const uint8_t* w = p.w + static_cast<uint64_t>(unit0) * row_bytes;
-    const uint8_t* x = p.x + static_cast<uint64_t>(point0) * row_bytes;
+    const uint8_t* w = p.w + static_cast<uint64_t>(unit0) * p.w_row;
+    const uint8_t* x = p.x + static_cast<uint64_t>(point0) * p.x_row;
     // this lane's pieces; rows past the end read the last one, and are not stored
-    const uint32_t piece = brought_piece(lane, wave);
     uint32_t w_at[S::BRINGS], x_at[S::BRINGS];
 #pragma unroll
     for (int i = 0; i < S::BRINGS; ++i) {
-        const uint32_t row = 8 * (S::WAVES * i + wave) + (lane >> 3);
-        w_at[i] = min(row, p.units - 1 - unit0) * row_bytes + piece * kSlot;
-        x_at[i] = min(row, p.points - 1 - point0) * row_bytes + piece * kSlot;
+        const uint32_t row = 8 * (S::WAVES * i + wave) + (lane >> 3), piece = brought_piece(lane, wave) * kSlot;
+        w_at[i] = min(row, p.units - 1 - unit0) * p.w_row + piece;
+        x_at[i] = min(row, p.points - 1 - point0) * p.x_row + piece;
     }
+    // past a row's end a step takes what lies there, the rows' last piece at most:
+    // x has zeros there
+    const uint64_t w_bytes = static_cast<uint64_t>(p.units - unit0) * p.w_row - kSlot;
+    const uint32_t w_limit = static_cast<uint32_t>(min(w_bytes, uint64_t{0xffffffffu}));
     const uint32_t wave_u = (wave & 1) * S::FM, wave_p = (wave >> 1) * S::FN;      // blocks of 32
-    const int* w_packed = reinterpret_cast<const int*>(p.w_packed) + static_cast<uint64_t>(unit0 / 32 + wave_u) * p.steps * 64 + lane;
-    const int* x_packed = reinterpret_cast<const int*>(p.x_packed) + static_cast<uint64_t>(point0 / 32 + wave_p) * p.steps * 64 + lane;
+    const int* w_packed = reinterpret_cast<const int*>(p.w_packed) + static_cast<uint64_t>(unit0 / 32 + wave_u) * p.steps * 64;
+    const int* x_packed = reinterpret_cast<const int*>(p.x_packed) + static_cast<uint64_t>(point0 / 32 + wave_p) * p.steps * 64;
     int scale_w[2][S::FM], scale_x[2][S::FN];
     float16v acc[S::FM][S::FN];
 #pragma unroll
@@ -415,15 +425,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
         [&](uint32_t k, int in_pair) {
 #pragma unroll
             for (int s = 0; s < S::FM; ++s)
-                scale_w[in_pair][s] = w_packed[(s * p.steps + k) * 64];
+                scale_w[in_pair][s] = (w_packed + (s * p.steps + k) * 64)[lane];
 #pragma unroll
             for (int t = 0; t < S::FN; ++t)
-                scale_x[in_pair][t] = x_packed[(t * p.steps + k) * 64];
+                scale_x[in_pair][t] = (x_packed + (t * p.steps + k) * 64)[lane];
         },
         [&](uint32_t k, char* buffer) {
-            const bool inside = 8 * k + piece < p.blocks;
-            bring_rows<S>(w, w_at, inside, k, buffer);
-            bring_rows<S>(x, x_at, inside, k, buffer + S::ROWS);
+            const uint32_t on = k * kStepBytes;
+            bring_rows<S>(w + on, w_at, w_limit - on, wave, buffer);
+            bring_rows<S>(x + on, x_at, 0xffffffffu, wave, buffer + S::ROWS);
             // the loads stay ahead of the products that hide them
             __builtin_amdgcn_sched_barrier(0);
         },
@@ -644,9 +654,11 @@ hipError_t launch_few(const void* x, const uint8_t* x_scales, int64_t x_stride, 
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The packed scales of a product's factors, rows up to whole tiles.
+// Scratch of a product in tiles: the packed scales of its factors, rows up to
+// whole tiles, and the codes of x with rows of whole steps.
 struct ProductScratch {
     PackedScales x_packed, w_packed;
+    uint8_t* x_codes;
     size_t bytes;
 
     ProductScratch(int64_t points, int64_t units, int64_t cols, void* base)
@@ -655,8 +667,9 @@ struct ProductScratch {
         auto size = [&](int64_t rows) { return static_cast<size_t>((rows + 255) / 256) * 8 * steps * 256; };
         x_packed.to = static_cast<uint8_t*>(base);
         w_packed.to = x_packed.to + size(points);
+        x_codes = w_packed.to + size(units);
         x_packed.steps = w_packed.steps = steps;
-        bytes = size(points) + size(units);
+        bytes = size(points) + size(units) + static_cast<size_t>(points) * steps * kStepBytes;
     }
 };
 
@@ -667,6 +680,8 @@ PackParams pack_of(const sqn_quantised& x, const PackedScales& packed)
     p.packed = packed;
     p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
     p.words = static_cast<uint64_t>(x.rows) * packed.steps * 2;
+    p.codes = nullptr;
+    p.codes_to = nullptr;
     return p;
 }
 
@@ -696,21 +711,23 @@ void launch_shape(const ProductParams& p, int32_t dtype, hipStream_t stream)
         product_kernel<S, __bf16><<<grid, S::THREADS, 0, stream>>>(p);
 }
 
-hipError_t launch_tiles(const sqn_quantised& x, const ProductScratch& t, const sqn_quantised& w, const float* bias,
-                        bool relu, const sqn_matrix& out, hipStream_t stream)
+// The codes of x in rows of whole steps.
+hipError_t launch_tiles(const void* x_codes, int64_t points, const ProductScratch& t, const sqn_quantised& w,
+                        const float* bias, bool relu, const sqn_matrix& out, hipStream_t stream)
 {
     ProductParams p;
-    p.x = static_cast<const uint8_t*>(x.codes);
+    p.x = static_cast<const uint8_t*>(x_codes);
     p.x_packed = t.x_packed.to;
     p.w = static_cast<const uint8_t*>(w.codes);
     p.w_packed = t.w_packed.to;
     p.bias = bias;
     p.out = out.data;
     p.out_stride = out.row_stride;
-    p.points = static_cast<uint32_t>(x.rows);
+    p.points = static_cast<uint32_t>(points);
     p.units = static_cast<uint32_t>(w.rows);
-    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
     p.steps = t.x_packed.steps;
+    p.x_row = p.steps * kStepBytes;
+    p.w_row = static_cast<uint32_t>(16 * quant_blocks(w.cols));
     p.relu = relu ? 1 : 0;
     auto tiles = [&](int64_t side) { return ((p.points + side - 1) / side) * ((p.units + side - 1) / side); };
     if (tiles(256) >= 200)
@@ -764,10 +781,17 @@ hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised&
     if (x.rows <= kFew)
         return launch_few<Blocks>(x.codes, static_cast<const uint8_t*>(x.scales), 0, x.rows, w, bias, relu, out, stream);
     const ProductScratch t(x.rows, w.rows, x.cols, workspace);
-    const PackParams pw = pack_of(w, t.w_packed), px = pack_of(x, t.x_packed);
+    const PackParams pw = pack_of(w, t.w_packed);
+    PackParams px = pack_of(x, t.x_packed);
+    const void* codes = x.codes;
+    if (px.blocks % 8 != 0) {
+        px.codes = static_cast<const uint4*>(x.codes);
+        px.codes_to = reinterpret_cast<uint4*>(t.x_codes);
+        codes = t.x_codes;
+    }
     const uint32_t groups_w = stream_blocks(pw.words), groups_x = stream_blocks(px.words);
     pack_kernel<<<groups_w + groups_x, kThreads, 0, stream>>>(pw, px, groups_w);
-    return launch_tiles(x, t, w, bias, relu, out, stream);
+    return launch_tiles(codes, x.rows, t, w, bias, relu, out, stream);
 }
 
 size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols)
@@ -777,9 +801,7 @@ size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols)
 
 size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols)
 {
-    if (points <= kFew)
-        return 0;
-    return padded(16 * static_cast<size_t>(points) * quant_blocks(cols)) + quantised_product_bytes(points, units, cols);
+    return quantised_product_bytes(points, units, cols);
 }
 
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
@@ -792,13 +814,12 @@ hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, c
             return launch_few<_Float16>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
         return launch_few<__bf16>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
     }
+    const ProductScratch t(x.rows, w.rows, x.cols, workspace);
     sqn_quantised q;
     q.rows = x.rows;
     q.cols = x.cols;
-    q.codes = workspace;
+    q.codes = t.x_codes;
     q.scales = nullptr;
-    const ProductScratch t(x.rows, w.rows, x.cols,
-                           static_cast<char*>(workspace) + padded(16 * static_cast<size_t>(x.rows) * quant_blocks(x.cols)));
     QuantParams p = quant_of(x, q);
     p.items = static_cast<uint64_t>(x.rows) * t.x_packed.steps * 32;
     const PackParams pw = pack_of(w, t.w_packed);
@@ -809,7 +830,7 @@ hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, c
         quantise_packed_kernel<_Float16><<<grid, kThreads, 0, stream>>>(p, t.x_packed, pw, groups);
     else
         quantise_packed_kernel<__bf16><<<grid, kThreads, 0, stream>>>(p, t.x_packed, pw, groups);
-    return launch_tiles(q, t, w, bias, relu, out, stream);
+    return launch_tiles(t.x_codes, x.rows, t, w, bias, relu, out, stream);
 }
 
 }  // namespace sqn
