@@ -46,10 +46,10 @@ constexpr float kScaleB = 2048.0f;       // 2^11 (b A + c A A) off the diagonal
 
 // One matrix's scratch; the matrices of a batch follow each other.
 struct Scratch {
-    _Float16 *x, *x_lo;                  // [mp][np]
-    float* x_full;                       // [mp][np], where factors are split
-    _Float16 *xt, *xt_lo;                // [np][mp], read by the step
-    _Float16 *xt_to, *xt_to_lo;          // [np][mp], written by it
+    _Float16 *x, *x_lo;                  // [mp][np]; x_lo where factors are split
+    _Float16 *xt, *xt_to;                // [np][mp], read and written by a step
+    _Float16 *xt_lo, *xt_to_lo;          // the same where factors are split, one and the same otherwise
+    float* xt_full;                      // [np][mp], where factors are split
     _Float16 *o, *o_lo;                  // [mp][mp]
     _Float16 *b, *b_lo;                  // [mp][mp]
     float *d, *d_b;                      // [mp] diagonals of A, and of a + b A + c A A
@@ -186,23 +186,20 @@ __global__ __launch_bounds__(kThreads) void start_kernel(OrthParams p)
         }
         const uint64_t x = base + static_cast<uint64_t>(i0 + line) * p.np + j0 + at;
         *reinterpret_cast<half8*>(p.s.x + x) = hi;
-        *reinterpret_cast<half8*>(p.s.x_lo + x) = lo;
-        if (p.s.x_full) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                p.s.x_full[x + e] = tile[line][at + e];
-        }
+        if (p.s.x_lo)
+            *reinterpret_cast<half8*>(p.s.x_lo + x) = lo;
+        const uint64_t xt = base + static_cast<uint64_t>(j0 + line) * p.mp + i0 + at;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             _Float16 h, l;
             split(tile[at + e][line], h, l);
             hi[e] = h;
             lo[e] = l;
+            if (p.s.xt_full)
+                p.s.xt_full[xt + e] = tile[at + e][line];
         }
-        const uint64_t xt = base + static_cast<uint64_t>(j0 + line) * p.mp + i0 + at;
         *reinterpret_cast<half8*>(p.s.xt + xt) = hi;
-        if (p.s.xt_lo)
-            *reinterpret_cast<half8*>(p.s.xt_lo + xt) = lo;
+        *reinterpret_cast<half8*>(p.s.xt_lo + xt) = lo;
     }
 }
 
@@ -211,8 +208,8 @@ __global__ __launch_bounds__(kThreads) void emit_kernel(OrthParams p)
 {
     const uint32_t b = blockIdx.z, i = blockIdx.y;
     for (uint32_t j = threadIdx.x; j < static_cast<uint32_t>(p.n); j += kThreads) {
-        const uint64_t x = (static_cast<uint64_t>(b) * p.mp + i) * p.np + j;
-        const float v = p.s.x_full ? p.s.x_full[x] : static_cast<float>(p.s.x[x]) + static_cast<float>(p.s.x_lo[x]);
+        const uint64_t xt = (static_cast<uint64_t>(b) * p.np + j) * p.mp + i;
+        const float v = p.s.xt_full ? p.s.xt_full[xt] : static_cast<float>(p.s.xt[xt]) + static_cast<float>(p.s.xt_lo[xt]);
         store_any(p.out, b * p.out_batch + i * p.out_row + j * p.out_col, v * (1.0f / kScaleX), p.out_dtype);
     }
 }
@@ -349,11 +346,9 @@ __device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, Acc<S>
 // the small ones apart from them: in one running sum the error of an update of
 // low rank is 3.3e-5 of the result, a plain binary32 product's own is 1.2e-5.
 template <typename S>
-__device__ __forceinline__ void products(const Factor& p, const Factor& q, uint32_t steps, Acc<S>& acc)
+__device__ __forceinline__ void products(const Factor& p, const Factor& q, uint32_t steps, char* buffer0, char* buffer1,
+                                         Acc<S>& acc)
 {
-    // arrays of their own, so that reads of one do not wait for loads into another
-    __shared__ __align__(16) char buffer0[S::BUFFER];
-    __shared__ __align__(16) char buffer1[S::BUFFER];
     Acc<S> part, small;
     clear<S>(acc);
     clear<S>(small);
@@ -399,157 +394,435 @@ __device__ __forceinline__ void lower_tile(uint32_t k, uint32_t& ti, uint32_t& t
     tj = k - i * (i + 1) / 2;
 }
 
-// f(i, j, elements) over the blocks of the wave's part of tile (ti, tj):
-// element q is (i + row_of(q), j)
-template <typename S, typename F>
-__device__ __forceinline__ void each(const Acc<S>& acc, uint32_t ti, uint32_t tj, F f)
+// A wave's part of tile (ti, tj): its first row and column.
+template <typename S>
+struct Place {
+    uint32_t row, col;
+
+    __device__ __forceinline__ Place(uint32_t ti, uint32_t tj)
+    {
+        const uint32_t wave = threadIdx.x >> 6;
+        row = ti * S::SIDE + (wave & 1) * (32 * S::FM);
+        col = tj * S::SIDE + (wave >> 1) * (32 * S::FN);
+    }
+};
+
+// Between two ways out of C: no conversion of it is kept from the one to the
+// other, which would take as many registers again.
+template <typename S>
+__device__ __forceinline__ void forget(Acc<S>& acc)
 {
-    const uint32_t wave = threadIdx.x >> 6;
-    const uint32_t row = ti * S::SIDE + (wave & 1) * (32 * S::FM), col = tj * S::SIDE + (wave >> 1) * (32 * S::FN);
-    each_block<S::FM, S::FN>(acc, [&](uint32_t i, uint32_t j, const float16v& v) { f(row + i, col + j, v); });
+#pragma unroll
+    for (int s = 0; s < S::FM; ++s)
+#pragma unroll
+        for (int t = 0; t < S::FN; ++t)
+            asm volatile("" : "+v"(acc[s][t]));
 }
 
-// A block's elements as binary16 (`lo` what that leaves, where wanted), to
-// rows of `cols` at (i, j).
-__device__ __forceinline__ void store_block(_Float16* hi, _Float16* lo, uint32_t cols, uint32_t i, uint32_t j,
-                                            const float16v& v)
+__device__ __forceinline__ _Float16 high(float v) { return static_cast<_Float16>(v); }
+__device__ __forceinline__ _Float16 low(float v) { return static_cast<_Float16>(v - static_cast<float>(high(v))); }
+
+// The wave's part to rows of `ld` binary16, high parts and, where wanted, low ones.
+template <typename S>
+__device__ __forceinline__ void store_rows(_Float16* hi, _Float16* lo, uint32_t ld, const Place<S>& at, Acc<S>& acc,
+                                           char* own)
 {
-    const uint64_t at = static_cast<uint64_t>(i) * cols + j;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-        _Float16 h, l;
-        split(v[q], h, l);
-        hi[at + row_of(q) * cols] = h;
-        if (lo)
-            lo[at + row_of(q) * cols] = l;
+    auto to = [&](_Float16* x) {
+        return [=](uint32_t i, uint32_t j, const uint4& run) {
+            *reinterpret_cast<uint4*>(x + static_cast<uint64_t>(at.row + i) * ld + at.col + j) = run;
+        };
+    };
+    forget<S>(acc);
+    rows_out<_Float16>(acc, own, high, to(hi));
+    if constexpr (S::SPLIT) {
+        forget<S>(acc);
+        rows_out<_Float16>(acc, own, low, to(lo));
     }
 }
 
-// ... and to the mirrored place: element q at (j, i + row_of(q)), four a store.
-__device__ __forceinline__ void store_mirrored(_Float16* hi, _Float16* lo, uint32_t cols, uint32_t i, uint32_t j,
-                                               const float16v& v)
+// ... and turned, to columns as rows.
+template <typename T, typename S, typename C>
+__device__ __forceinline__ void store_turned(T* x, uint32_t ld, const Place<S>& at, Acc<S>& acc, char* own, C convert)
+{
+    forget<S>(acc);
+    columns_out<T>(acc, own, convert, [=](uint32_t j, uint32_t i, const uint4& run) {
+        *reinterpret_cast<uint4*>(x + static_cast<uint64_t>(at.col + j) * ld + at.row + i) = run;
+    });
+}
+
+// A block's elements of a turned matrix, four a load.
+__device__ __forceinline__ void load_turned(const _Float16* x, uint64_t at, float v[16])
 {
     typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-    const uint64_t at = static_cast<uint64_t>(j) * cols + i;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        half4 h, l;
+        const half4 h = *reinterpret_cast<const half4*>(x + at + 8 * g);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            _Float16 a, b;
-            split(v[4 * g + r], a, b);
-            h[r] = a;
-            l[r] = b;
-        }
-        *reinterpret_cast<half4*>(hi + at + 8 * g) = h;
-        if (lo)
-            *reinterpret_cast<half4*>(lo + at + 8 * g) = l;
+        for (int r = 0; r < 4; ++r)
+            v[4 * g + r] = static_cast<float>(h[r]);
+    }
+}
+
+__device__ __forceinline__ void load_turned(const float* x, uint64_t at, float v[16])
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const float4 f = *reinterpret_cast<const float4*>(x + at + 8 * g);
+        v[4 * g] = f.x;
+        v[4 * g + 1] = f.y;
+        v[4 * g + 2] = f.z;
+        v[4 * g + 3] = f.w;
     }
 }
 
 template <typename S>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void gram_kernel(OrthParams p)
 {
+    // arrays of their own, so that reads of one do not wait for loads into another
+    __shared__ __align__(16) char buffer0[S::BUFFER];
+    __shared__ __align__(16) char buffer1[S::BUFFER];
     uint32_t ti, tj;
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t x = static_cast<uint64_t>(blockIdx.y) * p.mp * p.np, o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
     Acc<S> acc;
     products<S>(factor(p.s.x + x, p.s.x_lo + x, ti * S::SIDE, p.np), factor(p.s.x + x, p.s.x_lo + x, tj * S::SIDE, p.np),
-                p.steps_n, acc);
+                p.steps_n, buffer0, buffer1, acc);
     _Float16* hi = p.s.o + o;
-    _Float16* lo = S::SPLIT ? p.s.o_lo + o : nullptr;
+    _Float16* lo = p.s.o_lo + o;
     float* d = p.s.d + blockIdx.y * p.mp;
-    each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, float16v v) {
+    const Place<S> at(ti, tj);
+    char* own = own_part<S::FM, S::BUFFER>(buffer0, buffer1, threadIdx.x >> 6);
+    each_block(acc, [&](uint32_t i, uint32_t j, float16v& v) {
         v *= kScaleA / (kScaleX * kScaleX);
         if (ti == tj) {
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                if (i + row_of(q) == j) {
-                    d[j] = v[q] * (1.0f / kScaleA);
+                if (at.row + i + row_of(q) == at.col + j) {
+                    d[at.col + j] = v[q] * (1.0f / kScaleA);
                     v[q] = 0.0f;
                 }
-        } else {
-            store_mirrored(hi, lo, p.mp, i, j, v);
         }
-        store_block(hi, lo, p.mp, i, j, v);
     });
+    store_rows<S>(hi, lo, p.mp, at, acc, own);
+    if (ti != tj) {
+        store_turned(hi, p.mp, at, acc, own, high);
+        if constexpr (S::SPLIT)
+            store_turned(lo, p.mp, at, acc, own, low);
+    }
 }
 
 template <typename S>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void square_kernel(OrthParams p)
 {
+    __shared__ __align__(16) char buffer0[S::BUFFER];
+    __shared__ __align__(16) char buffer1[S::BUFFER];
     uint32_t ti, tj;
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
     const _Float16* o_hi = p.s.o + o;
-    const _Float16* o_lo = S::SPLIT ? p.s.o_lo + o : nullptr;
+    const _Float16* o_lo = p.s.o_lo + o;
     Acc<S> acc;
-    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, acc);
+    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, buffer0, buffer1,
+                acc);
     _Float16* hi = p.s.b + o;
-    _Float16* lo = S::SPLIT ? p.s.b_lo + o : nullptr;
+    _Float16* lo = p.s.b_lo + o;
     const float* d = p.s.d + blockIdx.y * p.mp;
     float* d_b = p.s.d_b + blockIdx.y * p.mp;
-    each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, const float16v& sum) {
-        float16v v;
-        float e[16], di[16];
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const uint64_t at = static_cast<uint64_t>(i + row_of(q)) * p.mp + j;
-            e[q] = static_cast<float>(o_hi[at]);
-            if constexpr (S::SPLIT)
-                e[q] += static_cast<float>(o_lo[at]);
-            di[q] = d[i + row_of(q)];
-        }
+    const Place<S> at(ti, tj);
+    char* own = own_part<S::FM, S::BUFFER>(buffer0, buffer1, threadIdx.x >> 6);
+    each_block(acc, [&](uint32_t bi, uint32_t bj, float16v& v) {
+        const uint32_t i = at.row + bi, j = at.col + bj;
+        // O is symmetric: its row j has the block's column
+        float e[16], more[16], di[16];
+        const uint64_t turned = static_cast<uint64_t>(j) * p.mp + i;
+        load_turned(o_hi, turned, e);
+        if constexpr (S::SPLIT)
+            load_turned(o_lo, turned, more);
+        load_turned(d, i, di);
         const float dj = d[j];
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
-            const float square = sum[q] * (1.0f / (kScaleA * kScaleA)), a = e[q] * (1.0f / kScaleA);
+            const float square = v[q] * (1.0f / (kScaleA * kScaleA));
+            const float a = (S::SPLIT ? e[q] + more[q] : e[q]) * (1.0f / kScaleA);
             v[q] = kScaleB * (p.b * a + p.c * (square + (di[q] + dj) * a));
             if (ti == tj && i + row_of(q) == j) {
                 d_b[j] = p.a + p.b * dj + p.c * (dj * dj + square);
                 v[q] = 0.0f;
             }
         }
-        if (ti != tj)
-            store_mirrored(hi, lo, p.mp, i, j, v);
-        store_block(hi, lo, p.mp, i, j, v);
     });
+    store_rows<S>(hi, lo, p.mp, at, acc, own);
+    if (ti != tj) {
+        store_turned(hi, p.mp, at, acc, own, high);
+        if constexpr (S::SPLIT)
+            store_turned(lo, p.mp, at, acc, own, low);
+    }
+}
+
+// The result of a wave's part in the layout of `out`: along or down it where
+// either side is contiguous.
+template <typename T, typename S>
+__device__ __forceinline__ void store_result(const OrthParams& p, uint32_t b, const Place<S>& at, Acc<S>& acc, char* own)
+{
+    forget<S>(acc);
+    T* out = static_cast<T*>(p.out) + b * p.out_batch;
+    if (p.out_col == 1) {
+        rows_out<T>(acc, own, from_f32<T>, [&](uint32_t i, uint32_t j, const uint4& run) {
+            if (at.row + i < static_cast<uint32_t>(p.m))
+                store_inside(out + (at.row + i) * p.out_row + at.col + j, static_cast<int64_t>(p.n) - at.col - j, run);
+        });
+    } else {
+        columns_out<T>(acc, own, from_f32<T>, [&](uint32_t j, uint32_t i, const uint4& run) {
+            if (at.col + j >= static_cast<uint32_t>(p.n))
+                return;
+            T* to = out + (at.col + j) * p.out_col + (at.row + i) * p.out_row;
+            const int64_t left = static_cast<int64_t>(p.m) - at.row - i;
+            if (p.out_row == 1) {
+                store_inside(to, left, run);
+            } else {
+                T e[16 / sizeof(T)];
+                __builtin_memcpy(e, &run, 16);
+#pragma unroll
+                for (uint32_t k = 0; k < 16 / sizeof(T); ++k)
+                    if (k < left)
+                        to[k * p.out_row] = e[k];
+            }
+        });
+    }
 }
 
 template <typename S, bool LAST>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void step_kernel(OrthParams p)
 {
+    __shared__ __align__(16) char buffer0[S::BUFFER];
+    __shared__ __align__(16) char buffer1[S::BUFFER];
     const uint32_t b = blockIdx.z, ti = blockIdx.y, tj = blockIdx.x;
     const uint64_t x = static_cast<uint64_t>(b) * p.mp * p.np, o = static_cast<uint64_t>(b) * p.mp * p.mp;
     Acc<S> acc;
     products<S>(factor(p.s.b + o, p.s.b_lo + o, ti * S::SIDE, p.mp),
-                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), p.steps_m, acc);
+                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), p.steps_m, buffer0, buffer1, acc);
     const float* d_b = p.s.d_b + b * p.mp;
-    each<S>(acc, ti, tj, [&](uint32_t i, uint32_t j, const float16v& sum) {
-        const uint64_t at = x + static_cast<uint64_t>(i) * p.np + j;
-        float16v v;
+    const Place<S> at(ti, tj);
+    char* own = own_part<S::FM, S::BUFFER>(buffer0, buffer1, threadIdx.x >> 6);
+    each_block(acc, [&](uint32_t bi, uint32_t bj, float16v& v) {
+        const uint64_t turned = x + static_cast<uint64_t>(at.col + bj) * p.mp + at.row + bi;
+        float old[16], more[16], d[16];
+        if constexpr (S::SPLIT) {
+            load_turned(p.s.xt_full, turned, old);
+        } else {
+            load_turned(p.s.xt, turned, old);
+            load_turned(p.s.xt_lo, turned, more);
+        }
+        load_turned(d_b, at.row + bi, d);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            v[q] = __builtin_fmaf(d[q], S::SPLIT ? old[q] : old[q] + more[q], v[q] * (1.0f / kScaleB));
+            if constexpr (LAST)
+                v[q] *= 1.0f / kScaleX;
+        }
+    });
+    if constexpr (LAST && !S::SPLIT) {
+        store_result<__bf16>(p, b, at, acc, own);
+    } else if constexpr (LAST) {
+        if (p.out_dtype == SQN_F32)
+            store_result<float>(p, b, at, acc, own);
+        else
+            store_result<_Float16>(p, b, at, acc, own);
+    } else {
+        store_rows<S>(p.s.x + x, p.s.x_lo + x, p.np, at, acc, own);
+        store_turned(p.s.xt_to + x, p.mp, at, acc, own, high);
+        store_turned(p.s.xt_to_lo + x, p.mp, at, acc, own, low);
+        if constexpr (S::SPLIT)
+            store_turned(p.s.xt_full + x, p.mp, at, acc, own, [](float v) { return v; });
+    }
+}
+
+// ---- small matrices: one workgroup each, all steps in one launch
+//
+// X stays in registers, in binary32, as the accumulators of its blocks; LDS
+// holds the factor that a product reads: X, then O, then X^T in X's place and B
+// in O's.  The launches of the tiles take 17 times 4 us whatever the size.
+
+constexpr int kSmallThreads = 512;
+constexpr int kSmallWaves = kSmallThreads / 64;
+
+// M x N blocks of 32 x 32.
+template <int M_, int N_, bool SPLIT_>
+struct Small {
+    static constexpr int M = M_, N = N_;
+    static constexpr bool SPLIT = SPLIT_;
+    static constexpr int XB = (M * N + kSmallWaves - 1) / kSmallWaves;    // blocks of X a wave
+    static constexpr int OB = (M * M + kSmallWaves - 1) / kSmallWaves;    // of O and B
+    // bytes of a row of a factor: its elements, of at least 128, so that 16 rows differ in their slots
+    static constexpr uint32_t PITCH_N = (N > 4 ? N : 4) * 64, PITCH_M = 4 * 64;
+    static constexpr uint32_t X_BYTES = M * 32 * PITCH_N > N * 32 * PITCH_M ? M * 32 * PITCH_N : N * 32 * PITCH_M;
+    static constexpr uint32_t O_BYTES = M * 32 * PITCH_M;
+};
+
+// Byte of element k of a factor's row: pieces of 16 bytes in a slot of their own
+// for each of 16 rows.
+__device__ __forceinline__ uint32_t small_at(uint32_t row, uint32_t k, uint32_t pitch)
+{
+    return row * pitch + ((k >> 3) ^ (row & 15)) * 16 + (k & 7) * 2;
+}
+
+// A block's elements to rows of a factor: element q at (i + row_of(q), j).
+__device__ __forceinline__ void small_store(char* hi, char* lo, uint32_t pitch, uint32_t i, uint32_t j, const float16v& v)
+{
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        *reinterpret_cast<_Float16*>(hi + small_at(i + row_of(q), j, pitch)) = high(v[q]);
+        if (lo)
+            *reinterpret_cast<_Float16*>(lo + small_at(i + row_of(q), j, pitch)) = low(v[q]);
+    }
+}
+
+// ... turned, element q at (j, i + row_of(q)).
+__device__ __forceinline__ void small_store_turned(char* hi, char* lo, uint32_t pitch, uint32_t i, uint32_t j,
+                                                   const float16v& v)
+{
+    typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        half4 h, l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            h[r] = high(v[4 * g + r]);
+            l[r] = low(v[4 * g + r]);
+        }
+        *reinterpret_cast<half4*>(hi + small_at(j, i + 8 * g, pitch)) = h;
+        if (lo)
+            *reinterpret_cast<half4*>(lo + small_at(j, i + 8 * g, pitch)) = l;
+    }
+}
+
+// A block of P Q^T over `depth` elements, rows i of P and j of Q on.
+template <bool SPLIT>
+__device__ __forceinline__ float16v small_product(const char* p, const char* p_lo, uint32_t i, const char* q, const char* q_lo,
+                                                  uint32_t j, uint32_t pitch, uint32_t depth)
+{
+    const uint32_t lane = threadIdx.x & 63, row = lane & 31, k0 = 8 * (lane >> 5);
+    auto read = [&](const char* x, uint32_t r, uint32_t k) {
+        return *reinterpret_cast<const half8*>(x + small_at(r + row, k + k0, pitch));
+    };
+    float16v acc = {}, small = {};
+#pragma unroll 4
+    for (uint32_t k = 0; k < depth; k += 16) {
+        const half8 a = read(p, i, k), b = read(q, j, k);
+        if constexpr (SPLIT) {
+            small = multiply(a, read(q_lo, j, k), small);
+            small = multiply(read(p_lo, i, k), b, small);
+        }
+        acc = multiply(a, b, acc);
+    }
+    if constexpr (SPLIT)
+        acc += small;
+    return acc;
+}
+
+template <typename S, typename T, typename O>
+__global__ __launch_bounds__(kSmallThreads) void small_kernel(OrthParams p, int32_t steps)
+{
+    constexpr int M = S::M, N = S::N;
+    __shared__ __align__(16) char x[(S::SPLIT ? 2 : 1) * S::X_BYTES];
+    __shared__ __align__(16) char o[(S::SPLIT ? 2 : 1) * S::O_BYTES];
+    __shared__ float d[32 * M], d_b[32 * M];
+    __shared__ double sums[kSmallWaves];
+    char* const x_lo = S::SPLIT ? x + S::X_BYTES : nullptr;
+    char* const o_lo = S::SPLIT ? o + S::O_BYTES : nullptr;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t m = p.m, n = p.n, di = 4 * (lane >> 5), dj = lane & 31;
+    // f(c, i, j) over the wave's blocks of `rows` x `cols`: its c-th, whose element q
+    // of this lane is (i + row_of(q), j)
+    auto blocks = [&](int rows, int cols, auto f) {
+#pragma unroll
+        for (int c = 0; c < (rows * cols + kSmallWaves - 1) / kSmallWaves; ++c) {
+            const uint32_t b = wave + kSmallWaves * c;
+            if (b < static_cast<uint32_t>(rows * cols))
+                f(c, 32 * (b % rows) + di, 32 * (b / rows) + dj);
+        }
+    };
+
+    float16v v[S::XB];
+    double sum = 0.0;
+    const T* in = static_cast<const T*>(p.in) + blockIdx.x * p.in_batch;
+    blocks(M, N, [&](int c, uint32_t i, uint32_t j) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const uint32_t r = i + row_of(q);
+            v[c][q] = r < m && j < n ? to_f32(in[r * p.in_row + j * p.in_col]) : 0.0f;
+        }
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-            v[q] = S::SPLIT ? p.s.x_full[at + row_of(q) * p.np]
-                            : static_cast<float>(p.s.x[at + row_of(q) * p.np])
-                                  + static_cast<float>(p.s.x_lo[at + row_of(q) * p.np]);
+            sum = __builtin_fma(static_cast<double>(v[c][q]), static_cast<double>(v[c][q]), sum);
+    });
+    for (int s = 32; s; s /= 2)
+        sum += __shfl_xor(sum, s);
+    if (lane == 0)
+        sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < kSmallWaves; ++w)
+        sum += sums[w];
+    const double norm = sqrt(sum) + static_cast<double>(p.eps);
+    const double scale = norm > 0.0 ? kScaleX / norm : 0.0;
+    // a NaN or an infinity anywhere gives NaN everywhere
+    const float nan = isfinite(norm) ? 0.0f : __builtin_nanf("");
+    blocks(M, N, [&](int c, uint32_t, uint32_t) {
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-            v[q] = __builtin_fmaf(d_b[i + row_of(q)], v[q], sum[q] * (1.0f / kScaleB));
-        if constexpr (LAST) {
-            const int64_t to = b * p.out_batch + i * p.out_row + j * p.out_col;
+            v[c][q] = static_cast<float>(v[c][q] * scale) + nan;
+    });
+
+    for (int32_t step = 0; step < steps; ++step) {
+        blocks(M, N, [&](int c, uint32_t i, uint32_t j) { small_store(x, x_lo, S::PITCH_N, i, j, v[c]); });
+        __syncthreads();
+        float16v a[S::OB];
+        blocks(M, M, [&](int c, uint32_t i, uint32_t j) {
+            a[c] = small_product<S::SPLIT>(x, x_lo, i - di, x, x_lo, j - dj, S::PITCH_N, 32 * N);
+            a[c] *= kScaleA / (kScaleX * kScaleX);
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                if (i + row_of(q) < static_cast<uint32_t>(p.m) && j < static_cast<uint32_t>(p.n))
-                    store_any(p.out, to + row_of(q) * p.out_row, v[q] * (1.0f / kScaleX), p.out_dtype);
-        } else {
-            if constexpr (S::SPLIT) {
+                if (i + row_of(q) == j) {
+                    d[j] = a[c][q] * (1.0f / kScaleA);
+                    a[c][q] = 0.0f;
+                }
+            small_store_turned(o, o_lo, S::PITCH_M, i, j, a[c]);
+        });
+        __syncthreads();
+        blocks(M, N, [&](int c, uint32_t i, uint32_t j) { small_store_turned(x, x_lo, S::PITCH_M, i, j, v[c]); });
+        blocks(M, M, [&](int c, uint32_t i, uint32_t j) {
+            const float16v square = small_product<S::SPLIT>(o, o_lo, i - di, o, o_lo, j - dj, S::PITCH_M, 32 * M);
+            const float dcol = d[j];
 #pragma unroll
-                for (int q = 0; q < 16; ++q)
-                    p.s.x_full[at + row_of(q) * p.np] = v[q];
+            for (int q = 0; q < 16; ++q) {
+                const float s = square[q] * (1.0f / (kScaleA * kScaleA)), e = a[c][q] * (1.0f / kScaleA);
+                a[c][q] = kScaleB * (p.b * e + p.c * (s + (d[i + row_of(q)] + dcol) * e));
+                if (i + row_of(q) == j) {
+                    d_b[j] = p.a + p.b * dcol + p.c * (dcol * dcol + s);
+                    a[c][q] = 0.0f;
+                }
             }
-            store_block(p.s.x + x, p.s.x_lo + x, p.np, i, j, v);
-            store_mirrored(p.s.xt_to + x, S::SPLIT ? p.s.xt_to_lo + x : nullptr, p.mp, i, j, v);
+        });
+        __syncthreads();
+        blocks(M, M, [&](int c, uint32_t i, uint32_t j) { small_store_turned(o, o_lo, S::PITCH_M, i, j, a[c]); });
+        __syncthreads();
+        blocks(M, N, [&](int c, uint32_t i, uint32_t j) {
+            const float16v more = small_product<S::SPLIT>(o, o_lo, i - di, x, x_lo, j - dj, S::PITCH_M, 32 * M);
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                v[c][q] = __builtin_fmaf(d_b[i + row_of(q)], v[c][q], more[q] * (1.0f / kScaleB));
+        });
+        __syncthreads();
+    }
+
+    O* out = static_cast<O*>(p.out) + blockIdx.x * p.out_batch;
+    blocks(M, N, [&](int c, uint32_t i, uint32_t j) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const uint32_t r = i + row_of(q);
+            if (r < m && j < n)
+                out[r * p.out_row + j * p.out_col] = from_f32<O>(v[c][q] * (1.0f / kScaleX));
         }
     });
 }
@@ -557,6 +830,44 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void step_kernel(OrthParam
 // ---- layout and launches
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Whether one workgroup does a matrix of m <= n: its factors, and their low
+// parts where they are split, lie in the 160 KB of a CU.
+bool is_small(int32_t m, int32_t n, bool split_all) { return m <= 128 && n <= (split_all ? 128 : 256); }
+
+template <typename S, typename T>
+void launch_small_to(const OrthParams& p, int32_t batch, int32_t steps, hipStream_t stream)
+{
+    if constexpr (!S::SPLIT)
+        small_kernel<S, T, __bf16><<<batch, kSmallThreads, 0, stream>>>(p, steps);
+    else if (p.out_dtype == SQN_F32)
+        small_kernel<S, T, float><<<batch, kSmallThreads, 0, stream>>>(p, steps);
+    else
+        small_kernel<S, T, _Float16><<<batch, kSmallThreads, 0, stream>>>(p, steps);
+}
+
+template <typename T>
+hipError_t launch_small(const OrthParams& p, int32_t batch, int32_t steps, bool split_all, hipStream_t stream)
+{
+    const bool low = p.m <= 64;
+    if (split_all) {
+        if (low)
+            launch_small_to<Small<2, 4, true>, T>(p, batch, steps, stream);
+        else
+            launch_small_to<Small<4, 4, true>, T>(p, batch, steps, stream);
+    } else if (p.n <= 128) {
+        if (low)
+            launch_small_to<Small<2, 4, false>, T>(p, batch, steps, stream);
+        else
+            launch_small_to<Small<4, 4, false>, T>(p, batch, steps, stream);
+    } else {
+        if (low)
+            launch_small_to<Small<2, 8, false>, T>(p, batch, steps, stream);
+        else
+            launch_small_to<Small<4, 8, false>, T>(p, batch, steps, stream);
+    }
+    return hipGetLastError();
+}
 
 // Side of the tiles of a batch of matrices.
 int32_t tile_side(int32_t batch, int32_t m, int32_t n, bool split_all)
@@ -572,6 +883,8 @@ int32_t up_to(int32_t v, int32_t side) { return (v + side - 1) / side * side; }
 size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* base, Scratch* s)
 {
     const int32_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (is_small(m, n, split_all))
+        return 0;
     const int32_t side = tile_side(batch, m, n, split_all);
     const size_t mp = up_to(m, side), np = up_to(n, side);
     size_t at = 0;
@@ -585,12 +898,12 @@ size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* b
     };
     Scratch t;
     t.x = halves(mp * np, true);
-    t.x_lo = halves(mp * np, true);
-    t.x_full = split_all ? reinterpret_cast<float*>(take(4 * mp * np)) : nullptr;
+    t.x_lo = halves(mp * np, split_all);
     t.xt = halves(mp * np, true);
     t.xt_to = halves(mp * np, true);
-    t.xt_lo = halves(mp * np, split_all);
-    t.xt_to_lo = halves(mp * np, split_all);
+    t.xt_lo = halves(mp * np, true);
+    t.xt_to_lo = split_all ? halves(mp * np, true) : t.xt_lo;
+    t.xt_full = split_all ? reinterpret_cast<float*>(take(4 * mp * np)) : nullptr;
     t.o = halves(mp * mp, true);
     t.b = halves(mp * mp, true);
     t.o_lo = halves(mp * mp, split_all);
@@ -668,6 +981,13 @@ hipError_t launch_orthogonalise(const sqn_batch& updates, int32_t steps, const f
     p.b = coefficients[1];
     p.c = coefficients[2];
     p.eps = eps;
+    if (is_small(p.m, p.n, split_all)) {
+        if (updates.dtype == SQN_F32)
+            return launch_small<float>(p, updates.batch, steps, split_all, stream);
+        if (updates.dtype == SQN_F16)
+            return launch_small<_Float16>(p, updates.batch, steps, split_all, stream);
+        return launch_small<__bf16>(p, updates.batch, steps, split_all, stream);
+    }
     if (updates.dtype == SQN_F32)
         launch_start<float>(p, updates.batch, stream);
     else if (updates.dtype == SQN_F16)

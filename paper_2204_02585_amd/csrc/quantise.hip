@@ -303,89 +303,6 @@ __device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, const 
     }
 }
 
-// A wave's outputs of 32 points: bias, activation, rounding, then through its
-// own LDS, so that a point's units leave in whole cache lines (stored as the
-// lanes hold them, 32 bytes each, lines went to memory twice).  `unit` and
-// `point` are the wave's first.
-template <typename S, typename T>
-__device__ __forceinline__ void store_points(const ProductParams& p, uint32_t unit, uint32_t point,
-                                             const float16v (&acc)[S::FM][S::FN], int t, char* own)
-{
-    constexpr int WORDS = sizeof(T);                              // of four units
-    constexpr uint32_t PITCH = S::FM * 32 * sizeof(T), PIECES = PITCH / 16;    // of a point
-    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, mine = lane & 31;
-#pragma unroll
-    for (int s = 0; s < S::FM; ++s) {
-        uint32_t word[4][WORDS];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const uint32_t u = unit + 32 * s + 8 * g + 4 * half;
-            float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (p.bias) {
-                if (u + 4 <= p.units) {
-                    load_run<float, 4>(p.bias + u, bias);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        bias[r] = p.bias[min(u + r, p.units - 1)];
-                }
-            }
-            T e[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float v = acc[s][t][4 * g + r] + bias[r];
-                if (p.relu)
-                    v = v < 0.0f ? 0.0f : v;
-                e[r] = from_f32<T>(v);
-            }
-            __builtin_memcpy(word[g], e, sizeof(e));
-        }
-        // the lower half of the wave gives its groups 2 and 3 for the upper
-        // half's 0 and 1: a lane then has 16 units in a row
-        uint4 piece[WORDS];
-        uint32_t* w16 = reinterpret_cast<uint32_t*>(piece);
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-            for (int w = 0; w < WORDS; ++w) {
-                const auto swapped = __builtin_amdgcn_permlane32_swap(word[g][w], word[g + 2][w], false, false);
-                w16[2 * g * WORDS + w] = swapped[0];
-                w16[(2 * g + 1) * WORDS + w] = swapped[1];
-            }
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) {
-            const uint32_t at = (2 * s + half) * WORDS + k;       // piece of the point
-            *reinterpret_cast<uint4*>(own + mine * PITCH + (at ^ (mine & (PIECES - 1))) * 16) = piece[k];
-        }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (uint32_t i = 0; i < 32 * PIECES / 64; ++i) {
-        const uint32_t row = (64 * i + lane) / PIECES, at = lane & (PIECES - 1);
-        const uint4 piece = *reinterpret_cast<const uint4*>(own + row * PITCH + (at ^ (row & (PIECES - 1))) * 16);
-        constexpr uint32_t N = 16 / sizeof(T);
-        const uint32_t u = unit + at * N, q = point + 32 * t + row;
-        if (q < p.points) {
-            T* to = static_cast<T*>(p.out) + q * p.out_stride + u;
-            Run<T, N> run;
-            __builtin_memcpy(&run, &piece, 16);
-            if (u + N <= p.units) {
-                *reinterpret_cast<Run<T, N>*>(to) = run;
-            } else {
-                T e[N];
-                __builtin_memcpy(e, &piece, 16);
-#pragma unroll
-                for (uint32_t k = 0; k < N; ++k)
-                    if (u + k < p.units)
-                        to[k] = e[k];
-            }
-        }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 template <typename S, typename T>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
 {
@@ -456,13 +373,36 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
             default: multiply_fragments<S, 3>(f, scale_w[k], scale_x[k], acc); break;
             }
         });
-    // the buffers are free: 32 points of a wave's units, at most four bytes each
-    constexpr int OWN = S::FM * 32 * 32 * 4;
-    static_assert(OWN * S::WAVES <= 2 * S::BUFFER && S::BUFFER % OWN == 0, "the outputs fit");
-    char* own = static_cast<int>(wave) * OWN < S::BUFFER ? buffer0 + wave * OWN : buffer1 + wave * OWN - S::BUFFER;
+    const uint32_t unit = unit0 + 32 * wave_u, point = point0 + 32 * wave_p;
 #pragma unroll
-    for (int t = 0; t < S::FN; ++t)
-        store_points<S, T>(p, unit0 + 32 * wave_u, point0 + 32 * wave_p, acc, t, own);
+    for (int s = 0; s < S::FM; ++s) {
+        // the lane's units of the block
+        float bias[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t u = unit + 32 * s + 8 * g + 4 * (lane >> 5);
+            if (p.bias && u + 4 <= p.units) {
+                load_run<float, 4>(p.bias + u, bias + 4 * g);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    bias[4 * g + r] = p.bias ? p.bias[min(u + r, p.units - 1)] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < S::FN; ++t)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const float v = acc[s][t][q] + bias[q];
+                acc[s][t][q] = p.relu && v < 0.0f ? 0.0f : v;
+            }
+    }
+    columns_out<T>(acc, own_part<S::FM, S::BUFFER>(buffer0, buffer1, wave), from_f32<T>,
+                   [&](uint32_t q, uint32_t u, const uint4& run) {
+                       if (point + q < p.points)
+                           store_inside(static_cast<T*>(p.out) + (point + q) * p.out_stride + unit + u,
+                                        static_cast<int64_t>(p.units) - unit - u, run);
+                   });
 }
 
 // ---- products of few points
@@ -651,8 +591,6 @@ hipError_t launch_few(const void* x, const uint8_t* x_scales, int64_t x_stride, 
     few_kernel<T><<<groups, 64 * waves, 0, stream>>>(p);
     return hipGetLastError();
 }
-
-size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Scratch of a product in tiles: the packed scales of its factors, rows up to
 // whole tiles, and the codes of x with rows of whole steps.

@@ -27,6 +27,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "numeric.h"
+
 namespace sqn {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
@@ -111,18 +113,143 @@ __device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, A a
 }
 
 // f(row, column, elements) over a wave's accumulators, from its first row and
-// column: element q is at row + row_of(q).
+// column: element q is at row + row_of(q).  The loads of one row of blocks are
+// under way together; those of more would not fit the registers.
 template <int FM, int FN, typename F>
-__device__ __forceinline__ void each_block(const float16v (&acc)[FM][FN], F f)
+__device__ __forceinline__ void each_block(float16v (&acc)[FM][FN], F f)
 {
     const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-    for (int s = 0; s < FM; ++s)
+    for (int s = 0; s < FM; ++s) {
 #pragma unroll
         for (int t = 0; t < FN; ++t)
             f(32 * s + 4 * (lane >> 5), 32 * t + (lane & 31), acc[s][t]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 constexpr uint32_t row_of(int q) { return 8 * (q >> 2) + (q & 3); }
+
+// ---- a wave's part of C on its way out
+//
+// As the lanes hold it, C would leave in pieces of 8 to 32 bytes, and cache
+// lines go to memory more than once (of a product's outputs 1.9 times).  It
+// goes through LDS instead, kOwn bytes of it a wave, and leaves in runs of 16
+// bytes that fill lines: emit(column, row, run) for runs down the columns,
+// emit(row, column, run) for runs along the rows, from the wave's first row
+// and column.  convert(value) is an element as it is stored.
+
+template <int FM>
+constexpr int kOwn = FM * 32 * 32 * 4;
+
+// The wave's own bytes of the buffers.
+template <int FM, int BUFFER>
+__device__ __forceinline__ char* own_part(char* b0, char* b1, uint32_t wave)
+{
+    static_assert(BUFFER % kOwn<FM> == 0, "no part lies in both buffers");
+    const int at = static_cast<int>(wave) * kOwn<FM>;
+    return at < BUFFER ? b0 + at : b1 + at - BUFFER;
+}
+
+// LDS accesses of a wave stay on their side.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <typename T, int FM, int FN, typename C, typename E>
+__device__ __forceinline__ void columns_out(const float16v (&acc)[FM][FN], char* own, C convert, E emit)
+{
+    constexpr int WORDS = sizeof(T);                              // of four elements
+    constexpr uint32_t PITCH = FM * 32 * sizeof(T), PIECES = PITCH / 16;
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5, mine = lane & 31;
+#pragma unroll
+    for (int t = 0; t < FN; ++t) {
+#pragma unroll
+        for (int s = 0; s < FM; ++s) {
+            uint32_t word[4][WORDS];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                T e[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    e[r] = convert(acc[s][t][4 * g + r]);
+                __builtin_memcpy(word[g], e, sizeof(e));
+            }
+            // the lower half of the wave gives its groups 2 and 3 for the upper
+            // half's 0 and 1: a lane then has 16 rows running
+            uint32_t run[WORDS][4];
+            uint32_t* flat = &run[0][0];
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int w = 0; w < WORDS; ++w) {
+                    const auto swapped = __builtin_amdgcn_permlane32_swap(word[g][w], word[g + 2][w], false, false);
+                    flat[2 * g * WORDS + w] = swapped[0];
+                    flat[(2 * g + 1) * WORDS + w] = swapped[1];
+                }
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) {
+                const uint32_t at = (2 * s + half) * WORDS + k;       // piece of the column
+                *reinterpret_cast<uint4*>(own + mine * PITCH + (at ^ (mine & (PIECES - 1))) * 16)
+                    = uint4{run[k][0], run[k][1], run[k][2], run[k][3]};
+            }
+        }
+        wave_fence();
+#pragma unroll
+        for (uint32_t i = 0; i < 32 * PIECES / 64; ++i) {
+            const uint32_t column = (64 * i + lane) / PIECES, at = lane & (PIECES - 1);
+            emit(32 * t + column, at * (16 / sizeof(T)),
+                 *reinterpret_cast<const uint4*>(own + column * PITCH + (at ^ (column & (PIECES - 1))) * 16));
+        }
+        wave_fence();
+    }
+}
+
+template <typename T, int FM, int FN, typename C, typename E>
+__device__ __forceinline__ void rows_out(const float16v (&acc)[FM][FN], char* own, C convert, E emit)
+{
+    constexpr uint32_t PITCH = FN * 32 * sizeof(T), PIECES = PITCH / 16;
+    const uint32_t lane = threadIdx.x & 63, mine = lane & 31;
+    // rows r and r + 4 are written together: apart by half a row
+    auto slot = [](uint32_t row, uint32_t piece) { return row * PITCH + (piece ^ (row >> 2 & 1) * (PIECES / 2)) * 16; };
+#pragma unroll
+    for (int s = 0; s < FM; ++s) {
+#pragma unroll
+        for (int t = 0; t < FN; ++t)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const uint32_t byte = (32 * t + mine) * sizeof(T);
+                *reinterpret_cast<T*>(own + slot(row_of(q) + 4 * (lane >> 5), byte >> 4) + (byte & 15)) = convert(acc[s][t][q]);
+            }
+        wave_fence();
+#pragma unroll
+        for (uint32_t i = 0; i < 32 * PIECES / 64; ++i) {
+            const uint32_t row = (64 * i + lane) / PIECES, at = lane & (PIECES - 1);
+            emit(32 * s + row, at * (16 / sizeof(T)), *reinterpret_cast<const uint4*>(own + slot(row, at)));
+        }
+        wave_fence();
+    }
+}
+
+// A run of 16 bytes to `to`, of whose places `left` are inside the matrix.
+template <typename T>
+__device__ __forceinline__ void store_inside(T* to, int64_t left, const uint4& run)
+{
+    constexpr int N = 16 / sizeof(T);
+    if (left >= N) {
+        Run<T, N> r;
+        __builtin_memcpy(&r, &run, 16);
+        *reinterpret_cast<Run<T, N>*>(to) = r;
+    } else {
+        T e[N];
+        __builtin_memcpy(e, &run, 16);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (k < left)
+                to[k] = e[k];
+    }
+}
 
 }  // namespace sqn
