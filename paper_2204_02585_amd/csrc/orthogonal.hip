@@ -696,28 +696,45 @@ __device__ __forceinline__ void small_store_turned(char* hi, char* lo, uint32_t 
     }
 }
 
-// A block of P Q^T over `depth` elements, rows i of P and j of Q on.
-template <bool SPLIT>
-__device__ __forceinline__ float16v small_product(const char* p, const char* p_lo, uint32_t i, const char* q, const char* q_lo,
-                                                  uint32_t j, uint32_t pitch, uint32_t depth)
+// Blocks of P Q^T over `depth` elements: rows i of P on, and j, j + apart, ...
+// of Q.  P's fragment serves all of them.
+template <bool SPLIT, int B>
+__device__ __forceinline__ void small_products(const char* p, const char* p_lo, uint32_t i, const char* q, const char* q_lo,
+                                               uint32_t j, uint32_t apart, uint32_t pitch, uint32_t depth,
+                                               float16v (&acc)[B])
 {
     const uint32_t lane = threadIdx.x & 63, row = lane & 31, k0 = 8 * (lane >> 5);
     auto read = [&](const char* x, uint32_t r, uint32_t k) {
         return *reinterpret_cast<const half8*>(x + small_at(r + row, k + k0, pitch));
     };
-    float16v acc = {}, small = {};
+    float16v small[B];
+#pragma unroll
+    for (int c = 0; c < B; ++c)
+        acc[c] = small[c] = float16v{};
 #pragma unroll 4
     for (uint32_t k = 0; k < depth; k += 16) {
-        const half8 a = read(p, i, k), b = read(q, j, k);
+        const half8 a = read(p, i, k);
+        half8 b[B];
+#pragma unroll
+        for (int c = 0; c < B; ++c)
+            b[c] = read(q, j + c * apart, k);
         if constexpr (SPLIT) {
-            small = multiply(a, read(q_lo, j, k), small);
-            small = multiply(read(p_lo, i, k), b, small);
+            const half8 a_lo = read(p_lo, i, k);
+#pragma unroll
+            for (int c = 0; c < B; ++c) {
+                small[c] = multiply(a, read(q_lo, j + c * apart, k), small[c]);
+                small[c] = multiply(a_lo, b[c], small[c]);
+            }
         }
-        acc = multiply(a, b, acc);
+#pragma unroll
+        for (int c = 0; c < B; ++c)
+            acc[c] = multiply(a, b[c], acc[c]);
     }
-    if constexpr (SPLIT)
-        acc += small;
-    return acc;
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int c = 0; c < B; ++c)
+            acc[c] += small[c];
+    }
 }
 
 template <typename S, typename T, typename O>
@@ -732,21 +749,24 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(OrthParams p, int3
     char* const o_lo = S::SPLIT ? o + S::O_BYTES : nullptr;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t m = p.m, n = p.n, di = 4 * (lane >> 5), dj = lane & 31;
-    // f(c, i, j) over the wave's blocks of `rows` x `cols`: its c-th, whose element q
-    // of this lane is (i + row_of(q), j)
-    auto blocks = [&](int rows, int cols, auto f) {
+    // The wave's blocks are in one row of blocks, their columns `apart`; of O's
+    // and B's a wave has OB or none.
+    static_assert(kSmallWaves % M == 0 && (M * N) % kSmallWaves == 0, "whole rounds of waves");
+    constexpr uint32_t apart = 32 * kSmallWaves / M;
+    const uint32_t bi = 32 * (wave % M), bj = 32 * (wave / M);
+    const bool has_o = wave < M * M;
+    // f(c, i, j) over the wave's first `count` blocks: the c-th, whose element q of
+    // this lane is (i + row_of(q), j)
+    auto blocks = [&](int count, auto f) {
 #pragma unroll
-        for (int c = 0; c < (rows * cols + kSmallWaves - 1) / kSmallWaves; ++c) {
-            const uint32_t b = wave + kSmallWaves * c;
-            if (b < static_cast<uint32_t>(rows * cols))
-                f(c, 32 * (b % rows) + di, 32 * (b / rows) + dj);
-        }
+        for (int c = 0; c < count; ++c)
+            f(c, bi + di, bj + c * apart + dj);
     };
 
     float16v v[S::XB];
     double sum = 0.0;
     const T* in = static_cast<const T*>(p.in) + blockIdx.x * p.in_batch;
-    blocks(M, N, [&](int c, uint32_t i, uint32_t j) {
+    blocks(S::XB, [&](int c, uint32_t i, uint32_t j) {
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
             const uint32_t r = i + row_of(q);
@@ -768,56 +788,63 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(OrthParams p, int3
     const double scale = norm > 0.0 ? kScaleX / norm : 0.0;
     // a NaN or an infinity anywhere gives NaN everywhere
     const float nan = isfinite(norm) ? 0.0f : __builtin_nanf("");
-    blocks(M, N, [&](int c, uint32_t, uint32_t) {
+    blocks(S::XB, [&](int c, uint32_t, uint32_t) {
 #pragma unroll
         for (int q = 0; q < 16; ++q)
             v[c][q] = static_cast<float>(v[c][q] * scale) + nan;
     });
 
     for (int32_t step = 0; step < steps; ++step) {
-        blocks(M, N, [&](int c, uint32_t i, uint32_t j) { small_store(x, x_lo, S::PITCH_N, i, j, v[c]); });
+        blocks(S::XB, [&](int c, uint32_t i, uint32_t j) { small_store(x, x_lo, S::PITCH_N, i, j, v[c]); });
         __syncthreads();
         float16v a[S::OB];
-        blocks(M, M, [&](int c, uint32_t i, uint32_t j) {
-            a[c] = small_product<S::SPLIT>(x, x_lo, i - di, x, x_lo, j - dj, S::PITCH_N, 32 * N);
-            a[c] *= kScaleA / (kScaleX * kScaleX);
+        if (has_o) {
+            small_products<S::SPLIT, S::OB>(x, x_lo, bi, x, x_lo, bj, apart, S::PITCH_N, 32 * N, a);
+            blocks(S::OB, [&](int c, uint32_t i, uint32_t j) {
+                a[c] *= kScaleA / (kScaleX * kScaleX);
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                    if (i + row_of(q) == j) {
+                        d[j] = a[c][q] * (1.0f / kScaleA);
+                        a[c][q] = 0.0f;
+                    }
+                small_store_turned(o, o_lo, S::PITCH_M, i, j, a[c]);
+            });
+        }
+        __syncthreads();
+        blocks(S::XB, [&](int c, uint32_t i, uint32_t j) { small_store_turned(x, x_lo, S::PITCH_M, i, j, v[c]); });
+        if (has_o) {
+            float16v square[S::OB];
+            small_products<S::SPLIT, S::OB>(o, o_lo, bi, o, o_lo, bj, apart, S::PITCH_M, 32 * M, square);
+            blocks(S::OB, [&](int c, uint32_t i, uint32_t j) {
+                const float dcol = d[j];
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const float s = square[c][q] * (1.0f / (kScaleA * kScaleA)), e = a[c][q] * (1.0f / kScaleA);
+                    a[c][q] = kScaleB * (p.b * e + p.c * (s + (d[i + row_of(q)] + dcol) * e));
+                    if (i + row_of(q) == j) {
+                        d_b[j] = p.a + p.b * dcol + p.c * (dcol * dcol + s);
+                        a[c][q] = 0.0f;
+                    }
+                }
+            });
+        }
+        __syncthreads();
+        if (has_o)
+            blocks(S::OB, [&](int c, uint32_t i, uint32_t j) { small_store_turned(o, o_lo, S::PITCH_M, i, j, a[c]); });
+        __syncthreads();
+        float16v more[S::XB];
+        small_products<S::SPLIT, S::XB>(o, o_lo, bi, x, x_lo, bj, apart, S::PITCH_M, 32 * M, more);
+        blocks(S::XB, [&](int c, uint32_t i, uint32_t) {
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-                if (i + row_of(q) == j) {
-                    d[j] = a[c][q] * (1.0f / kScaleA);
-                    a[c][q] = 0.0f;
-                }
-            small_store_turned(o, o_lo, S::PITCH_M, i, j, a[c]);
-        });
-        __syncthreads();
-        blocks(M, N, [&](int c, uint32_t i, uint32_t j) { small_store_turned(x, x_lo, S::PITCH_M, i, j, v[c]); });
-        blocks(M, M, [&](int c, uint32_t i, uint32_t j) {
-            const float16v square = small_product<S::SPLIT>(o, o_lo, i - di, o, o_lo, j - dj, S::PITCH_M, 32 * M);
-            const float dcol = d[j];
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const float s = square[q] * (1.0f / (kScaleA * kScaleA)), e = a[c][q] * (1.0f / kScaleA);
-                a[c][q] = kScaleB * (p.b * e + p.c * (s + (d[i + row_of(q)] + dcol) * e));
-                if (i + row_of(q) == j) {
-                    d_b[j] = p.a + p.b * dcol + p.c * (dcol * dcol + s);
-                    a[c][q] = 0.0f;
-                }
-            }
-        });
-        __syncthreads();
-        blocks(M, M, [&](int c, uint32_t i, uint32_t j) { small_store_turned(o, o_lo, S::PITCH_M, i, j, a[c]); });
-        __syncthreads();
-        blocks(M, N, [&](int c, uint32_t i, uint32_t j) {
-            const float16v more = small_product<S::SPLIT>(o, o_lo, i - di, x, x_lo, j - dj, S::PITCH_M, 32 * M);
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-                v[c][q] = __builtin_fmaf(d_b[i + row_of(q)], v[c][q], more[q] * (1.0f / kScaleB));
+                v[c][q] = __builtin_fmaf(d_b[i + row_of(q)], v[c][q], more[c][q] * (1.0f / kScaleB));
         });
         __syncthreads();
     }
 
     O* out = static_cast<O*>(p.out) + blockIdx.x * p.out_batch;
-    blocks(M, N, [&](int c, uint32_t i, uint32_t j) {
+    blocks(S::XB, [&](int c, uint32_t i, uint32_t j) {
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
             const uint32_t r = i + row_of(q);
