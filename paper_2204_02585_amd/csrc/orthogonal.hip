@@ -230,7 +230,8 @@ struct Shape {
     static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
     static constexpr int BUFFER = FACTORS * ROWS;
     static constexpr int LOADS = BUFFER / (1024 * WAVES);     // of a wave, a step
-    static constexpr int PER_SIMD = SIDE == 256 || 4 * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
+    static constexpr int BUFFERS = SIDE == 64 ? 4 : 2;
+    static constexpr int PER_SIMD = SIDE == 256 || 2 * BUFFERS * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
 };
 
 struct Factor {
@@ -346,21 +347,21 @@ __device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, Acc<S>
 // the small ones apart from them: in one running sum the error of an update of
 // low rank is 3.3e-5 of the result, a plain binary32 product's own is 1.2e-5.
 template <typename S>
-__device__ __forceinline__ void products(const Factor& p, const Factor& q, uint32_t steps, char* buffer0, char* buffer1,
-                                         Acc<S>& acc)
+__device__ __forceinline__ void products(const Factor& p, const Factor& q, uint32_t steps,
+                                         char* (&buffers)[S::BUFFERS], Acc<S>& acc)
 {
     Acc<S> part, small;
     clear<S>(acc);
     clear<S>(small);
     pipeline<S::LOADS, Fragments<S>>(
-        steps, buffer0, buffer1, [](uint32_t, int) {}, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
+        steps, buffers, [](uint32_t, int) {}, [&](uint32_t k, char* buffer) { bring_step<S>(p, q, k, buffer); },
         [&](Fragments<S>& f, const char* buffer, uint32_t o) { read_fragments<S>(f, buffer, o); },
         [&](const Fragments<S>& f, int depth) {
             if constexpr (S::SPLIT) {
-                if (depth == 0)
+                if (depth % 8 == 0)
                     clear<S>(part);
                 multiply_fragments<S>(f, part, small);
-                if (depth == 7)
+                if (depth % 8 == 7)
                     add<S>(acc, part);
             } else {
                 multiply_fragments<S>(f, acc, small);
@@ -478,20 +479,18 @@ __device__ __forceinline__ void load_turned(const float* x, uint64_t at, float v
 template <typename S>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void gram_kernel(OrthParams p)
 {
-    // arrays of their own, so that reads of one do not wait for loads into another
-    __shared__ __align__(16) char buffer0[S::BUFFER];
-    __shared__ __align__(16) char buffer1[S::BUFFER];
+    BUFFERS_IN_LDS(S)
     uint32_t ti, tj;
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t x = static_cast<uint64_t>(blockIdx.y) * p.mp * p.np, o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
     Acc<S> acc;
     products<S>(factor(p.s.x + x, p.s.x_lo + x, ti * S::SIDE, p.np), factor(p.s.x + x, p.s.x_lo + x, tj * S::SIDE, p.np),
-                p.steps_n, buffer0, buffer1, acc);
+                p.steps_n, buffers, acc);
     _Float16* hi = p.s.o + o;
     _Float16* lo = p.s.o_lo + o;
     float* d = p.s.d + blockIdx.y * p.mp;
     const Place<S> at(ti, tj);
-    char* own = own_part<S::FM, S::BUFFER>(buffer0, buffer1, threadIdx.x >> 6);
+    char* own = own_part<S::FM, S::BUFFER>(buffers[0], buffers[1], threadIdx.x >> 6);
     each_block(acc, [&](uint32_t i, uint32_t j, float16v& v) {
         v *= kScaleA / (kScaleX * kScaleX);
         if (ti == tj) {
@@ -514,22 +513,20 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void gram_kernel(OrthParam
 template <typename S>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void square_kernel(OrthParams p)
 {
-    __shared__ __align__(16) char buffer0[S::BUFFER];
-    __shared__ __align__(16) char buffer1[S::BUFFER];
+    BUFFERS_IN_LDS(S)
     uint32_t ti, tj;
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
     const _Float16* o_hi = p.s.o + o;
     const _Float16* o_lo = p.s.o_lo + o;
     Acc<S> acc;
-    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, buffer0, buffer1,
-                acc);
+    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, buffers, acc);
     _Float16* hi = p.s.b + o;
     _Float16* lo = p.s.b_lo + o;
     const float* d = p.s.d + blockIdx.y * p.mp;
     float* d_b = p.s.d_b + blockIdx.y * p.mp;
     const Place<S> at(ti, tj);
-    char* own = own_part<S::FM, S::BUFFER>(buffer0, buffer1, threadIdx.x >> 6);
+    char* own = own_part<S::FM, S::BUFFER>(buffers[0], buffers[1], threadIdx.x >> 6);
     each_block(acc, [&](uint32_t bi, uint32_t bj, float16v& v) {
         const uint32_t i = at.row + bi, j = at.col + bj;
         // O is symmetric: its row j has the block's column
@@ -594,16 +591,15 @@ __device__ __forceinline__ void store_result(const OrthParams& p, uint32_t b, co
 template <typename S, bool LAST>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void step_kernel(OrthParams p)
 {
-    __shared__ __align__(16) char buffer0[S::BUFFER];
-    __shared__ __align__(16) char buffer1[S::BUFFER];
+    BUFFERS_IN_LDS(S)
     const uint32_t b = blockIdx.z, ti = blockIdx.y, tj = blockIdx.x;
     const uint64_t x = static_cast<uint64_t>(b) * p.mp * p.np, o = static_cast<uint64_t>(b) * p.mp * p.mp;
     Acc<S> acc;
     products<S>(factor(p.s.b + o, p.s.b_lo + o, ti * S::SIDE, p.mp),
-                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), p.steps_m, buffer0, buffer1, acc);
+                factor(p.s.xt + x, p.s.xt_lo + x, tj * S::SIDE, p.mp), p.steps_m, buffers, acc);
     const float* d_b = p.s.d_b + b * p.mp;
     const Place<S> at(ti, tj);
-    char* own = own_part<S::FM, S::BUFFER>(buffer0, buffer1, threadIdx.x >> 6);
+    char* own = own_part<S::FM, S::BUFFER>(buffers[0], buffers[1], threadIdx.x >> 6);
     each_block(acc, [&](uint32_t bi, uint32_t bj, float16v& v) {
         const uint64_t turned = x + static_cast<uint64_t>(at.col + bj) * p.mp + at.row + bi;
         float old[16], more[16], d[16];
@@ -659,21 +655,22 @@ struct Small {
     static constexpr uint32_t O_BYTES = M * 32 * PITCH_M;
 };
 
-// Byte of element k of a factor's row: pieces of 16 bytes in a slot of their own
-// for each of 16 rows.
-__device__ __forceinline__ uint32_t small_at(uint32_t row, uint32_t k, uint32_t pitch)
-{
-    return row * pitch + ((k >> 3) ^ (row & 15)) * 16 + (k & 7) * 2;
-}
+// Element k of row r of a factor lies in the piece of 16 bytes (k / 8) ^ (r % 16)
+// of the row, so 16 rows' pieces are in slots of their own.  Rows and elements
+// of a lane are a part that the lane fixes and one that the code does, in
+// different bits: the slots are one exclusive or of both.
 
-// A block's elements to rows of a factor: element q at (i + row_of(q), j).
+// A block's elements to rows of a factor: element q at (i + row_of(q), j), i a
+// multiple of 32 plus 0 or 4.
 __device__ __forceinline__ void small_store(char* hi, char* lo, uint32_t pitch, uint32_t i, uint32_t j, const float16v& v)
 {
+    const uint32_t slot = ((j >> 3) ^ (i & 4)) * 16 + (j & 7) * 2;
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-        *reinterpret_cast<_Float16*>(hi + small_at(i + row_of(q), j, pitch)) = high(v[q]);
+        const uint32_t at = i * pitch + (slot ^ (row_of(q) & 15) * 16) + row_of(q) * pitch;
+        *reinterpret_cast<_Float16*>(hi + at) = high(v[q]);
         if (lo)
-            *reinterpret_cast<_Float16*>(lo + small_at(i + row_of(q), j, pitch)) = low(v[q]);
+            *reinterpret_cast<_Float16*>(lo + at) = low(v[q]);
     }
 }
 
@@ -682,6 +679,7 @@ __device__ __forceinline__ void small_store_turned(char* hi, char* lo, uint32_t 
                                                    const float16v& v)
 {
     typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+    const uint32_t slot = ((i >> 3) ^ (j & 15)) * 16 + (i & 4) * 2;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         half4 h, l;
@@ -690,9 +688,10 @@ __device__ __forceinline__ void small_store_turned(char* hi, char* lo, uint32_t 
             h[r] = high(v[4 * g + r]);
             l[r] = low(v[4 * g + r]);
         }
-        *reinterpret_cast<half4*>(hi + small_at(j, i + 8 * g, pitch)) = h;
+        const uint32_t at = j * pitch + (slot ^ g * 16);
+        *reinterpret_cast<half4*>(hi + at) = h;
         if (lo)
-            *reinterpret_cast<half4*>(lo + small_at(j, i + 8 * g, pitch)) = l;
+            *reinterpret_cast<half4*>(lo + at) = l;
     }
 }
 
@@ -703,9 +702,9 @@ __device__ __forceinline__ void small_products(const char* p, const char* p_lo, 
                                                uint32_t j, uint32_t apart, uint32_t pitch, uint32_t depth,
                                                float16v (&acc)[B])
 {
-    const uint32_t lane = threadIdx.x & 63, row = lane & 31, k0 = 8 * (lane >> 5);
+    const uint32_t lane = threadIdx.x & 63, row = lane & 31, slot = ((lane >> 5) ^ (row & 15)) * 16;
     auto read = [&](const char* x, uint32_t r, uint32_t k) {
-        return *reinterpret_cast<const half8*>(x + small_at(r + row, k + k0, pitch));
+        return *reinterpret_cast<const half8*>(x + r * pitch + (row * pitch + (slot ^ 2 * k)));
     };
     float16v small[B];
 #pragma unroll

@@ -259,6 +259,7 @@ struct Shape {
     static constexpr int BUFFER = 2 * ROWS;
     static constexpr int LOADS = BUFFER / (1024 * WAVES);
     static constexpr int BRINGS = LOADS / 2;                       // of either factor
+    static constexpr int BUFFERS = SIDE == 64 ? 4 : 2;
 };
 
 template <typename S>
@@ -306,9 +307,7 @@ __device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, const 
 template <typename S, typename T>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
 {
-    // arrays of their own, so that reads of one do not wait for loads into another
-    __shared__ __align__(16) char buffer0[S::BUFFER];
-    __shared__ __align__(16) char buffer1[S::BUFFER];
+    BUFFERS_IN_LDS(S)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t unit_tiles = (p.units + S::SIDE - 1) / S::SIDE;
     const uint32_t tj = blockIdx.x / unit_tiles, ti = blockIdx.x - tj * unit_tiles;
@@ -330,7 +329,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
     const uint32_t wave_u = (wave & 1) * S::FM, wave_p = (wave >> 1) * S::FN;      // blocks of 32
     const int* w_packed = reinterpret_cast<const int*>(p.w_packed) + static_cast<uint64_t>(unit0 / 32 + wave_u) * p.steps * 64;
     const int* x_packed = reinterpret_cast<const int*>(p.x_packed) + static_cast<uint64_t>(point0 / 32 + wave_p) * p.steps * 64;
-    int scale_w[2][S::FM], scale_x[2][S::FN];
+    int scale_w[S::BUFFERS][S::FM], scale_x[S::BUFFERS][S::FN];
     float16v acc[S::FM][S::FN];
 #pragma unroll
     for (int s = 0; s < S::FM; ++s)
@@ -338,14 +337,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
         for (int t = 0; t < S::FN; ++t)
             acc[s][t] = float16v{};
     pipeline<S::LOADS, Fragments<S>>(
-        p.steps, buffer0, buffer1,
-        [&](uint32_t k, int in_pair) {
+        p.steps, buffers,
+        [&](uint32_t k, int in_round) {
 #pragma unroll
             for (int s = 0; s < S::FM; ++s)
-                scale_w[in_pair][s] = (w_packed + (s * p.steps + k) * 64)[lane];
+                scale_w[in_round][s] = (w_packed + (s * p.steps + k) * 64)[lane];
 #pragma unroll
             for (int t = 0; t < S::FN; ++t)
-                scale_x[in_pair][t] = (x_packed + (t * p.steps + k) * 64)[lane];
+                scale_x[in_round][t] = (x_packed + (t * p.steps + k) * 64)[lane];
         },
         [&](uint32_t k, char* buffer) {
             const uint32_t on = k * kStepBytes;
@@ -397,7 +396,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
                 acc[s][t][q] = p.relu && v < 0.0f ? 0.0f : v;
             }
     }
-    columns_out<T>(acc, own_part<S::FM, S::BUFFER>(buffer0, buffer1, wave), from_f32<T>,
+    columns_out<T>(acc, own_part<S::FM, S::BUFFER>(buffers[0], buffers[1], wave), from_f32<T>,
                    [&](uint32_t q, uint32_t u, const uint4& run) {
                        if (point + q < p.points)
                            store_inside(static_cast<T*>(p.out) + (point + q) * p.out_stride + unit + u,

@@ -71,43 +71,66 @@ __device__ __forceinline__ void landed()
     asm volatile("" ::: "memory");
 }
 
+// A kernel's LDS for the steps of shape S: arrays of their own, so that reads of
+// one do not wait for loads into another.
+#define BUFFERS_IN_LDS(S)                                                            \
+    __shared__ __align__(16) char buffer0[S::BUFFER];                                \
+    __shared__ __align__(16) char buffer1[S::BUFFER];                                \
+    __shared__ __align__(16) char buffer2[S::BUFFERS == 4 ? S::BUFFER : 16];         \
+    __shared__ __align__(16) char buffer3[S::BUFFERS == 4 ? S::BUFFER : 16];         \
+    char* buffers[S::BUFFERS];                                                       \
+    buffers[0] = buffer0;                                                            \
+    buffers[1] = buffer1;                                                            \
+    if constexpr (S::BUFFERS == 4) {                                                 \
+        buffers[2] = buffer2;                                                        \
+        buffers[3] = buffer3;                                                        \
+    }
+
 // The steps of a tile's sum.  bring(step, buffer) issues LOADS loads a wave,
 // read(fragments, buffer, o) reads a depth's fragments and multiply(fragments,
-// depth) multiplies them: the steps go in pairs, of eight depths; the last
-// step may be alone.  ahead(step, in_pair) starts what a step takes from
-// elsewhere, a step before it.
-template <int LOADS, typename Fragments, typename A, typename B, typename R, typename M>
-__device__ __forceinline__ void pipeline(uint32_t steps, char* b0, char* b1, A ahead, B bring_step, R read, M multiply)
+// depth) multiplies them: the steps go in rounds of as many as there are
+// buffers, the last round may end early.  ahead(step, in_round) starts what a
+// step takes from elsewhere.
+template <int LOADS, typename Fragments, int BUFFERS, typename A, typename B, typename R, typename M>
+__device__ __forceinline__ void pipeline(uint32_t steps, char* (&buffers)[BUFFERS], A ahead, B bring_step, R read,
+                                         M multiply)
 {
     const uint32_t end = steps - 1;
     Fragments f0, f1;
-    ahead(0u, 0);
-    bring_step(0, b0);
-    bring_step(min(1u, end), b1);
-    landed<LOADS>();
-    read(f0, b0, 0);
-    // `buffer` holds step k and will hold k + 2; past the end the last step
+#pragma unroll
+    for (int b = 0; b < BUFFERS - 1; ++b)
+        ahead(min(static_cast<uint32_t>(b), end), b);
+#pragma unroll
+    for (int b = 0; b < BUFFERS; ++b)
+        bring_step(min(static_cast<uint32_t>(b), end), buffers[b]);
+    landed<(BUFFERS - 1) * LOADS>();
+    read(f0, buffers[0], 0);
+    // buffer b holds step k and will hold k + BUFFERS; past the end the last step
     // comes once more and is not used
-    auto work = [&](uint32_t k, int depth, char* buffer, char* next) {
-        ahead(min(k + 1, end), depth ? 0 : 1);
-        read(f1, buffer, 1);
-        multiply(f0, depth);
-        read(f0, buffer, 2);
-        multiply(f1, depth + 1);
-        read(f1, buffer, 3);
-        multiply(f0, depth + 2);
-        landed<0>();
-        bring_step(min(k + 2, end), buffer);
-        read(f0, next, 0);
-        multiply(f1, depth + 3);
+    auto work = [&](uint32_t k, int b) {
+        ahead(min(k + BUFFERS - 1, end), (b + BUFFERS - 1) % BUFFERS);
+        read(f1, buffers[b], 1);
+        multiply(f0, kDepths * b);
+        read(f0, buffers[b], 2);
+        multiply(f1, kDepths * b + 1);
+        read(f1, buffers[b], 3);
+        multiply(f0, kDepths * b + 2);
+        // what `ahead` loads may be among the newest too: then more has landed
+        landed<(BUFFERS - 2) * LOADS>();
+        bring_step(min(k + BUFFERS, end), buffers[b]);
+        read(f0, buffers[(b + 1) % BUFFERS], 0);
+        multiply(f1, kDepths * b + 3);
     };
     uint32_t k = 0;
-    for (; k + 2 <= steps; k += 2) {
-        work(k, 0, b0, b1);
-        work(k + 1, 4, b1, b0);
+    for (; k + BUFFERS <= steps; k += BUFFERS) {
+#pragma unroll
+        for (int b = 0; b < BUFFERS; ++b)
+            work(k + b, b);
     }
-    if (k < steps)
-        work(k, 0, b0, b1);
+#pragma unroll
+    for (int b = 0; b < BUFFERS - 1; ++b)
+        if (k + b < steps)
+            work(k + b, b);
     // the loads still under way end before their buffers do
     landed<0>();
 }
