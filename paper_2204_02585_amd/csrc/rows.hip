@@ -328,8 +328,13 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
     }
 }
 
-// All passes over at most kSortStep keys.
-template <typename I>
+// All passes over at most 1024 KEYS keys.
+template <int KEYS>
+constexpr size_t kSortBytes = kSortThreads * KEYS * sizeof(Pair) > sizeof(uint32_t) * kWaves * kMaxBins
+                                 ? kSortThreads * KEYS * sizeof(Pair)
+                                 : sizeof(uint32_t) * kWaves * kMaxBins;
+
+template <typename I, int KEYS>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
 {
     if (blockIdx.x >= 1) {
@@ -337,17 +342,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
         return;
     }
     // the counts' place first, then the pairs'
-    __shared__ __align__(16) char shared[kSortStep * sizeof(Pair)];
+    __shared__ __align__(16) char shared[kSortBytes<KEYS>];
     __shared__ uint32_t wave_sums[kWaves];
     uint32_t (*seen)[kMaxBins] = reinterpret_cast<uint32_t (*)[kMaxBins]>(shared);
     Pair* pairs = reinterpret_cast<Pair*>(shared);
-    static_assert(sizeof(uint32_t) * kWaves * kMaxBins <= sizeof(shared), "the counts fit");
     const uint32_t tid = threadIdx.x, wave = tid >> 6;
-    Pair pair[kSortKeys];
-    uint32_t to[kSortKeys];
+    Pair pair[KEYS];
+    uint32_t to[KEYS];
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k)
-        pair[k] = number_of<kSortKeys>(k) < p.n ? pair_at<I>(p, number_of<kSortKeys>(k)) : Pair{0, 0};
+    for (int k = 0; k < KEYS; ++k)
+        pair[k] = number_of<KEYS>(k) < p.n ? pair_at<I>(p, number_of<KEYS>(k)) : Pair{0, 0};
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.bits;
         const uint32_t mask = (1u << p.bits) - 1;
@@ -362,24 +366,24 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
         counts_to_starts(seen, tid, exclusive_sum(total, wave_sums));
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kSortKeys; ++k)
+        for (int k = 0; k < KEYS; ++k)
             to[k] += seen[wave][pair[k].key >> shift & mask];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kSortKeys; ++k)
-            if (number_of<kSortKeys>(k) < p.n)
+        for (int k = 0; k < KEYS; ++k)
+            if (number_of<KEYS>(k) < p.n)
                 pairs[to[k]] = pair[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kSortKeys; ++k)
-            if (number_of<kSortKeys>(k) < p.n)
-                pair[k] = pairs[number_of<kSortKeys>(k)];
+        for (int k = 0; k < KEYS; ++k)
+            if (number_of<KEYS>(k) < p.n)
+                pair[k] = pairs[number_of<KEYS>(k)];
         __syncthreads();
     }
 #pragma unroll
-    for (int k = 0; k < kSortKeys; ++k)
-        if (number_of<kSortKeys>(k) < p.n)
-            p.out[number_of<kSortKeys>(k)] = pair[k];
+    for (int k = 0; k < KEYS; ++k)
+        if (number_of<KEYS>(k) < p.n)
+            p.out[number_of<KEYS>(k)] = pair[k];
 }
 
 // ---- gradient: sums
@@ -628,6 +632,18 @@ Plan plan_of(int64_t n, int64_t rows, int64_t cols)
     return q;
 }
 
+// One key a thread, or as many as there are for: a key's ballots take the time.
+template <typename I>
+void launch_sort(const SortParams& s, dim3 grid, hipStream_t stream)
+{
+    if (s.n <= kSortThreads)
+        sort_kernel<I, 1><<<grid, kSortThreads, 0, stream>>>(s);
+    else if (s.n <= 4 * kSortThreads)
+        sort_kernel<I, 4><<<grid, kSortThreads, 0, stream>>>(s);
+    else
+        sort_kernel<I, kSortKeys><<<grid, kSortThreads, 0, stream>>>(s);
+}
+
 template <typename T, typename O, int V>
 void launch_sums(SumParams p, hipStream_t stream)
 {
@@ -741,9 +757,9 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
             return hipSuccess;
         const dim3 sort_grid = grid();
         if (ids64)
-            sort_kernel<int64_t><<<sort_grid, kSortThreads, 0, stream>>>(s);
+            launch_sort<int64_t>(s, sort_grid, stream);
         else
-            sort_kernel<int32_t><<<sort_grid, kSortThreads, 0, stream>>>(s);
+            launch_sort<int32_t>(s, sort_grid, stream);
         if (s.n == 0)
             return hipGetLastError();
     } else {
