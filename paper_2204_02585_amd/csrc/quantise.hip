@@ -304,6 +304,37 @@ __device__ __forceinline__ void multiply_fragments(const Fragments<S>& f, const 
     }
 }
 
+// Bias and activation of a wave's part, units `unit` on.
+template <int FM, int FN>
+__device__ __forceinline__ void activate(const float* bias, int32_t relu, uint32_t units, uint32_t unit,
+                                         float16v (&acc)[FM][FN])
+{
+    const uint32_t half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < FM; ++s) {
+        // the lane's units of the block
+        float b[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t u = unit + 32 * s + 8 * g + 4 * half;
+            if (bias && u + 4 <= units) {
+                load_run<float, 4>(bias + u, b + 4 * g);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    b[4 * g + r] = bias ? bias[min(u + r, units - 1)] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < FN; ++t)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const float v = acc[s][t][q] + b[q];
+                acc[s][t][q] = relu && v < 0.0f ? 0.0f : v;
+            }
+    }
+}
+
 template <typename S, typename T>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
 {
@@ -373,29 +404,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
             }
         });
     const uint32_t unit = unit0 + 32 * wave_u, point = point0 + 32 * wave_p;
-#pragma unroll
-    for (int s = 0; s < S::FM; ++s) {
-        // the lane's units of the block
-        float bias[16];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const uint32_t u = unit + 32 * s + 8 * g + 4 * (lane >> 5);
-            if (p.bias && u + 4 <= p.units) {
-                load_run<float, 4>(p.bias + u, bias + 4 * g);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    bias[4 * g + r] = p.bias ? p.bias[min(u + r, p.units - 1)] : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < S::FN; ++t)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const float v = acc[s][t][q] + bias[q];
-                acc[s][t][q] = p.relu && v < 0.0f ? 0.0f : v;
-            }
-    }
+    activate(p.bias, p.relu, p.units, unit, acc);
     columns_out<T>(acc, own_part<S::FM, S::BUFFER>(buffers[0], buffers[1], wave), from_f32<T>,
                    [&](uint32_t q, uint32_t u, const uint4& run) {
                        if (point + q < p.points)
@@ -403,6 +412,180 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(ProductParams p)
                                         static_cast<int64_t>(p.units) - unit - u, run);
                    });
 }
+
+// ---- layers of up to 256 units and 8 to 512 inputs
+//
+// All weights fit LDS beside the blocks of 128 points, so the points' blocks
+// need not go through memory: a workgroup loads its points, puts them into
+// blocks in LDS, multiplies and stores; 8 waves, of 128 units and 32 points
+// each.  Workgroups on a CU fill each other's waits (one that went through
+// many tiles with its weights kept lost more to spilled addresses).
+
+constexpr uint32_t kLayerUnits = 256, kLayerPoints = 128;
+constexpr int kLayerThreads = 512;
+
+struct LayerParams {
+    const uint8_t *w, *w_scales;
+    const void* x;
+    const float* bias;
+    void* out;
+    int64_t x_stride, out_stride;
+    uint32_t points, units, cols, blocks;
+    int32_t relu;
+};
+
+template <typename X, typename T, int STEPS>
+__global__ __launch_bounds__(kLayerThreads) void layer_kernel(LayerParams p)
+{
+    constexpr uint32_t W_STEP = kLayerUnits * kStepBytes, X_STEP = kLayerPoints * kStepBytes;
+    constexpr int FM = 4, PARTS = sizeof(T) == 4 ? 4 : 2;         // blocks of units; parts of them that leave together
+    constexpr uint32_t OWN = 32 * 128;                            // a wave's bytes on the way out: a line of 32 points
+    constexpr int EIGHTHS = 8 * STEPS;                            // of blocks, a thread
+    __shared__ __align__(16) char w[STEPS * W_STEP];
+    __shared__ __align__(16) char x[STEPS * X_STEP > 8 * OWN ? STEPS * X_STEP : 8 * OWN];
+    __shared__ __align__(4) uint8_t w_packed[STEPS * kLayerUnits * 8];
+    __shared__ __align__(4) uint8_t x_packed[STEPS * kLayerPoints * 8];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // the weights, as the tiles bring them
+    const uint32_t row_bytes = 16 * p.blocks, limit = p.units * row_bytes - kSlot;
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k)
+#pragma unroll
+        for (uint32_t i = 0; i < kLayerUnits / 64; ++i) {
+            const uint32_t row = 8 * (8 * i + wave) + (lane >> 3);
+            const uint32_t at = min(row, p.units - 1) * row_bytes + brought_piece(lane, wave) * kSlot + k * kStepBytes;
+            bring(reinterpret_cast<const char*>(p.w) + min(at, limit), w + k * W_STEP + (8 * i + wave) * 1024);
+        }
+    for (uint32_t i = tid; i < kLayerUnits * 8 * STEPS; i += kLayerThreads) {
+        const uint32_t row = i / (8 * STEPS), block = i % (8 * STEPS);
+        w_packed[packed_at(row, block, STEPS)]
+            = row < p.units && block < p.blocks ? p.w_scales[row * p.blocks + block] : static_cast<uint8_t>(kOne);
+    }
+
+    // eighth e of the blocks: eight elements of point e / (32 STEPS)
+    const uint32_t first = blockIdx.x * kLayerPoints;
+    Run<X, 8> raw[EIGHTHS];
+#pragma unroll
+    for (int i = 0; i < EIGHTHS; ++i) {
+        const uint32_t e = tid + kLayerThreads * i, q = e % (32 * STEPS);
+        const uint32_t point = min(first + e / (32 * STEPS), p.points - 1);
+        // past the row's last eight elements, those
+        raw[i] = *reinterpret_cast<const Run<X, 8>*>(static_cast<const X*>(p.x) + point * p.x_stride
+                                                     + min(8 * q, p.cols - 8));
+    }
+#pragma unroll
+    for (int i = 0; i < EIGHTHS; ++i) {
+        const uint32_t e = tid + kLayerThreads * i, q = e % (32 * STEPS), row = e / (32 * STEPS), block = q >> 2;
+        float v[8];
+        X elements[8];
+        __builtin_memcpy(elements, &raw[i], sizeof(elements));
+        // what was read lies `early` before the eighth
+        const uint32_t early = 8 * q - min(8 * q, p.cols - 8);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = to_f32(elements[k]);
+        if (p.cols & 7) {
+#pragma unroll
+            for (uint32_t b = 4; b; b /= 2)
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k)
+                    v[k] = early & b ? (k + b < 8 ? v[k + b] : 0.0f) : v[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = early < 8 ? v[k] : 0.0f;
+        const uint32_t byte = block < p.blocks ? shared_scale(v) : kOne;
+        *reinterpret_cast<uint32_t*>(x + (block >> 3) * X_STEP + row * kStepBytes
+                                     + ((block & 7) ^ (row >> 1 & 7)) * kSlot + (q & 3) * 4) = encode8(v, byte);
+        if ((q & 3) == 0)
+            x_packed[packed_at(row, block, STEPS)] = static_cast<uint8_t>(byte);
+    }
+    landed<0>();
+    const uint32_t wave_u = (wave & 1) * FM, wave_p = wave >> 1;          // blocks of 32
+    float16v acc[FM][1];
+#pragma unroll
+    for (int s = 0; s < FM; ++s)
+        acc[s][0] = float16v{};
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+        int scale_w[FM];
+#pragma unroll
+        for (int s = 0; s < FM; ++s)
+            scale_w[s] = reinterpret_cast<const int*>(w_packed)[((wave_u + s) * STEPS + k) * 64 + lane];
+        const int scale_x = reinterpret_cast<const int*>(x_packed)[(wave_p * STEPS + k) * 64 + lane];
+        const char* from_w = w + k * W_STEP + wave_u * kBlockBytes;
+        const char* from_x = x + k * X_STEP + wave_p * kBlockBytes;
+        auto depth = [&](auto o) {
+            constexpr int O = decltype(o)::value;
+            const int4v b = *reinterpret_cast<const int4v*>(from_x + piece_at(lane, O));
+#pragma unroll
+            for (int s = 0; s < FM; ++s)
+                acc[s][0] = multiply<O>(*reinterpret_cast<const int4v*>(from_w + s * kBlockBytes + piece_at(lane, O)), b,
+                                        scale_w[s], scale_x, acc[s][0]);
+        };
+        depth(std::integral_constant<int, 0>());
+        depth(std::integral_constant<int, 1>());
+        depth(std::integral_constant<int, 2>());
+        depth(std::integral_constant<int, 3>());
+    }
+    __syncthreads();          // the blocks of the points make room for what leaves
+    const uint32_t unit = 32 * wave_u, point = first + 32 * wave_p;
+    activate(p.bias, p.relu, p.units, unit, acc);
+    auto emit = [&](uint32_t q, uint32_t u, const uint4& run) {
+        if (point + q < p.points)
+            store_inside(static_cast<T*>(p.out) + (point + q) * p.out_stride + unit + u,
+                         static_cast<int64_t>(p.units) - unit - u, run);
+    };
+    char* own = x + wave * OWN;
+    if constexpr (PARTS == 2) {
+        columns_out_of<T, 0, 2>(acc, own, from_f32<T>, emit);
+        columns_out_of<T, 2, 2>(acc, own, from_f32<T>, emit);
+    } else {
+        columns_out_of<T, 0, 1>(acc, own, from_f32<T>, emit);
+        columns_out_of<T, 1, 1>(acc, own, from_f32<T>, emit);
+        columns_out_of<T, 2, 1>(acc, own, from_f32<T>, emit);
+        columns_out_of<T, 3, 1>(acc, own, from_f32<T>, emit);
+    }
+}
+
+template <typename X, typename T>
+void launch_layer_steps(const LayerParams& p, hipStream_t stream)
+{
+    const uint32_t grid = (p.points + kLayerPoints - 1) / kLayerPoints;
+    if (p.blocks <= 8)
+        layer_kernel<X, T, 1><<<grid, kLayerThreads, 0, stream>>>(p);
+    else
+        layer_kernel<X, T, 2><<<grid, kLayerThreads, 0, stream>>>(p);
+}
+
+template <typename X>
+hipError_t launch_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu, const sqn_matrix& out,
+                        hipStream_t stream)
+{
+    LayerParams p;
+    p.w = static_cast<const uint8_t*>(w.codes);
+    p.w_scales = static_cast<const uint8_t*>(w.scales);
+    p.x = x.data;
+    p.bias = bias;
+    p.out = out.data;
+    p.x_stride = x.row_stride;
+    p.out_stride = out.row_stride;
+    p.points = static_cast<uint32_t>(x.rows);
+    p.units = static_cast<uint32_t>(w.rows);
+    p.cols = static_cast<uint32_t>(x.cols);
+    p.blocks = static_cast<uint32_t>(quant_blocks(x.cols));
+    p.relu = relu ? 1 : 0;
+    if (out.dtype == SQN_F32)
+        launch_layer_steps<X, float>(p, stream);
+    else if (out.dtype == SQN_F16)
+        launch_layer_steps<X, _Float16>(p, stream);
+    else
+        launch_layer_steps<X, __bf16>(p, stream);
+    return hipGetLastError();
+}
+
+bool is_layer(int64_t units, int64_t cols) { return units <= kLayerUnits && cols >= 8 && quant_blocks(cols) <= 16; }
 
 // ---- products of few points
 //
@@ -738,7 +921,7 @@ size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols)
 
 size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols)
 {
-    return quantised_product_bytes(points, units, cols);
+    return is_layer(units, cols) ? 0 : quantised_product_bytes(points, units, cols);
 }
 
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
@@ -750,6 +933,13 @@ hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, c
         if (x.dtype == SQN_F16)
             return launch_few<_Float16>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
         return launch_few<__bf16>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
+    }
+    if (is_layer(w.rows, w.cols)) {
+        if (x.dtype == SQN_F32)
+            return launch_layer<float>(x, w, bias, relu, out, stream);
+        if (x.dtype == SQN_F16)
+            return launch_layer<_Float16>(x, w, bias, relu, out, stream);
+        return launch_layer<__bf16>(x, w, bias, relu, out, stream);
     }
     const ProductScratch t(x.rows, w.rows, x.cols, workspace);
     sqn_quantised q;

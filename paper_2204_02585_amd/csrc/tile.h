@@ -181,23 +181,24 @@ __device__ __forceinline__ void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
-template <typename T, int FM, int FN, typename C, typename E>
-__device__ __forceinline__ void columns_out(const float16v (&acc)[FM][FN], char* own, C convert, E emit)
+// COUNT rows of blocks from S0 on; kOwn<COUNT> bytes.
+template <typename T, int S0, int COUNT, int FM, int FN, typename C, typename E>
+__device__ __forceinline__ void columns_out_of(const float16v (&acc)[FM][FN], char* own, C convert, E emit)
 {
     constexpr int WORDS = sizeof(T);                              // of four elements
-    constexpr uint32_t PITCH = FM * 32 * sizeof(T), PIECES = PITCH / 16;
+    constexpr uint32_t PITCH = COUNT * 32 * sizeof(T), PIECES = PITCH / 16;
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5, mine = lane & 31;
 #pragma unroll
     for (int t = 0; t < FN; ++t) {
 #pragma unroll
-        for (int s = 0; s < FM; ++s) {
+        for (int s = 0; s < COUNT; ++s) {
             uint32_t word[4][WORDS];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 T e[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    e[r] = convert(acc[s][t][4 * g + r]);
+                    e[r] = convert(acc[S0 + s][t][4 * g + r]);
                 __builtin_memcpy(word[g], e, sizeof(e));
             }
             // the lower half of the wave gives its groups 2 and 3 for the upper
@@ -223,11 +224,17 @@ __device__ __forceinline__ void columns_out(const float16v (&acc)[FM][FN], char*
 #pragma unroll
         for (uint32_t i = 0; i < 32 * PIECES / 64; ++i) {
             const uint32_t column = (64 * i + lane) / PIECES, at = lane & (PIECES - 1);
-            emit(32 * t + column, at * (16 / sizeof(T)),
+            emit(32 * t + column, 32 * S0 + at * (16 / sizeof(T)),
                  *reinterpret_cast<const uint4*>(own + column * PITCH + (at ^ (column & (PIECES - 1))) * 16));
         }
         wave_fence();
     }
+}
+
+template <typename T, int FM, int FN, typename C, typename E>
+__device__ __forceinline__ void columns_out(const float16v (&acc)[FM][FN], char* own, C convert, E emit)
+{
+    columns_out_of<T, 0, FM>(acc, own, convert, emit);
 }
 
 template <typename T, int FM, int FN, typename C, typename E>
