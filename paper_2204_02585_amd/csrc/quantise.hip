@@ -100,47 +100,99 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top_bits)
     return e == 255 ? 255u : e > 2 ? e - 2 : 0u;
 }
 
-// Eight elements over 2^(byte - 127), as codes.  The product is exact up to
-// elements too small to matter; the conversion rounds to nearest even and
-// stops at 6.
-__device__ __forceinline__ uint32_t encode8(const float v[8], uint32_t byte)
+// Eight elements of a row as they lie in memory.
+template <typename T>
+using Eight = Run<T, 8>;
+
+// The largest magnitude's bits, of T.
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const Eight<T>& e)
 {
-    const float inv = byte == 255 ? 0.0f : __uint_as_float((254 - byte) << 23);
-    uint32_t c = 0;
-    float s[8];
+    uint32_t top = 0;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        s[k] = byte == 255 ? 0.0f : v[k] * inv;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, s[0], s[1], 1.0f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, s[2], s[3], 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, s[4], s[5], 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, s[6], s[7], 1.0f, 3);
+        for (int k = 0; k < 8; ++k)
+            top = max(top, e.word[k] & 0x7fffffffu);
+    } else {
+        typedef uint16_t ushort2v __attribute__((ext_vector_type(2)));
+        ushort2v most = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2v, e.word[k] & 0x7fff7fffu));
+        top = max(most[0], most[1]);
+    }
+    return top;
+}
+
+// ... to the block's scale byte.
+template <typename T>
+__device__ __forceinline__ uint32_t byte_of(uint32_t top)
+{
+    if constexpr (sizeof(T) == 4)
+        return scale_byte(top);
+    else
+        return scale_byte(__float_as_uint(to_f32(__builtin_bit_cast(T, static_cast<uint16_t>(top)))));
+}
+
+// Eight elements over 2^(byte - 127), as codes: rounded to nearest even, at
+// most 6.
+template <typename T>
+__device__ __forceinline__ uint32_t encode(const Eight<T>& e, uint32_t byte)
+{
+    // a marked block's codes are those of scale 1
+    const float scale = byte == 255 ? 1.0f : byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
+    uint32_t c = 0;
+    if constexpr (sizeof(T) == 4) {
+        float v[8];
+        __builtin_memcpy(v, &e, sizeof(v));
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+    } else {
+        typedef T pair __attribute__((ext_vector_type(2)));
+        pair v[4];
+        __builtin_memcpy(v, &e, sizeof(v));
+        if constexpr (std::is_same<T, _Float16>::value) {
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, v[0], scale, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, v[1], scale, 1);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, v[2], scale, 2);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, v[3], scale, 3);
+        } else {
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[0], scale, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[1], scale, 1);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[2], scale, 2);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, v[3], scale, 3);
+        }
+    }
     return c;
 }
 
 // Elements at..at+8 of a row, zeros past its end.
 template <typename T>
-__device__ __forceinline__ void load_eight(const T* row, uint32_t at, uint32_t cols, float v[8])
+__device__ __forceinline__ Eight<T> load_eight(const T* row, uint32_t at, uint32_t cols)
 {
+    Eight<T> e;
     if (at + 8 <= cols) {
-        load_run<T, 8>(row + at, v);
+        e = *reinterpret_cast<const Eight<T>*>(row + at);
     } else {
+        T v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            v[k] = at + k < cols ? to_f32(row[at + k]) : 0.0f;
+            v[k] = at + k < cols ? row[at + k] : from_f32<T>(0.0f);
+        __builtin_memcpy(&e, v, sizeof(e));
     }
+    return e;
 }
 
-// The scale byte of the four lanes' elements.
-__device__ __forceinline__ uint32_t shared_scale(const float v[8])
+// The scale byte of four lanes' elements.
+template <typename T>
+__device__ __forceinline__ uint32_t shared_scale(const Eight<T>& e)
 {
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+    uint32_t top = top_of<T>(e);
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
-    return scale_byte(top);
+    return byte_of<T>(top);
 }
 
 template <typename T>
@@ -151,10 +203,9 @@ __global__ __launch_bounds__(kThreads) void quantise_kernel(QuantParams p)
          i += static_cast<uint64_t>(gridDim.x) * kThreads) {
         const uint64_t r = i / per_row;
         const uint32_t q = static_cast<uint32_t>(i - r * per_row);
-        float v[8];
-        load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols, v);
-        const uint32_t byte = shared_scale(v);
-        reinterpret_cast<uint32_t*>(p.codes)[i] = encode8(v, byte);
+        const Eight<T> e = load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols);
+        const uint32_t byte = shared_scale<T>(e);
+        reinterpret_cast<uint32_t*>(p.codes)[i] = encode<T>(e, byte);
         if ((i & 3) == 0)
             p.scales[i >> 2] = static_cast<uint8_t>(byte);
     }
@@ -178,10 +229,9 @@ __global__ __launch_bounds__(kThreads) void quantise_packed_kernel(QuantParams p
         const uint32_t q = static_cast<uint32_t>(i - r * static_cast<uint64_t>(per_row)), block = q >> 2;
         uint32_t byte = kOne, codes = 0;
         if (block < p.blocks) {
-            float v[8];
-            load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols, v);
-            byte = shared_scale(v);
-            codes = encode8(v, byte);
+            const Eight<T> e = load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols);
+            byte = shared_scale<T>(e);
+            codes = encode<T>(e, byte);
         }
         reinterpret_cast<uint32_t*>(p.codes)[i] = codes;
         if ((q & 3) == 0)
@@ -465,39 +515,38 @@ __global__ __launch_bounds__(kLayerThreads) void layer_kernel(LayerParams p)
 
     // eighth e of the blocks: eight elements of point e / (32 STEPS)
     const uint32_t first = blockIdx.x * kLayerPoints;
-    Run<X, 8> raw[EIGHTHS];
+    Eight<X> raw[EIGHTHS];
 #pragma unroll
     for (int i = 0; i < EIGHTHS; ++i) {
         const uint32_t e = tid + kLayerThreads * i, q = e % (32 * STEPS);
         const uint32_t point = min(first + e / (32 * STEPS), p.points - 1);
         // past the row's last eight elements, those
-        raw[i] = *reinterpret_cast<const Run<X, 8>*>(static_cast<const X*>(p.x) + point * p.x_stride
+        raw[i] = *reinterpret_cast<const Eight<X>*>(static_cast<const X*>(p.x) + point * p.x_stride
                                                      + min(8 * q, p.cols - 8));
     }
 #pragma unroll
     for (int i = 0; i < EIGHTHS; ++i) {
         const uint32_t e = tid + kLayerThreads * i, q = e % (32 * STEPS), row = e / (32 * STEPS), block = q >> 2;
-        float v[8];
-        X elements[8];
-        __builtin_memcpy(elements, &raw[i], sizeof(elements));
-        // what was read lies `early` before the eighth
-        const uint32_t early = 8 * q - min(8 * q, p.cols - 8);
+        if (p.cols < 256 * STEPS) {
+            // what was read lies `early` before the eighth
+            const uint32_t early = 8 * q - min(8 * q, p.cols - 8);
+            X v[8];
+            __builtin_memcpy(v, &raw[i], sizeof(v));
+            if (p.cols & 7) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = to_f32(elements[k]);
-        if (p.cols & 7) {
+                for (uint32_t b = 4; b; b /= 2)
 #pragma unroll
-            for (uint32_t b = 4; b; b /= 2)
+                    for (uint32_t k = 0; k < 8; ++k)
+                        v[k] = early & b ? (k + b < 8 ? v[k + b] : from_f32<X>(0.0f)) : v[k];
+            }
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k)
-                    v[k] = early & b ? (k + b < 8 ? v[k + b] : 0.0f) : v[k];
+            for (int k = 0; k < 8; ++k)
+                v[k] = early < 8 ? v[k] : from_f32<X>(0.0f);
+            __builtin_memcpy(&raw[i], v, sizeof(v));
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = early < 8 ? v[k] : 0.0f;
-        const uint32_t byte = block < p.blocks ? shared_scale(v) : kOne;
+        const uint32_t byte = block < p.blocks ? shared_scale<X>(raw[i]) : kOne;
         *reinterpret_cast<uint32_t*>(x + (block >> 3) * X_STEP + row * kStepBytes
-                                     + ((block & 7) ^ (row >> 1 & 7)) * kSlot + (q & 3) * 4) = encode8(v, byte);
+                                     + ((block & 7) ^ (row >> 1 & 7)) * kSlot + (q & 3) * 4) = encode<X>(raw[i], byte);
         if ((q & 3) == 0)
             x_packed[packed_at(row, block, STEPS)] = static_cast<uint8_t>(byte);
     }
@@ -640,7 +689,7 @@ __device__ __forceinline__ Operand load_block(const uint8_t* codes, const uint8_
 // A block of a row of elements as it lies in memory.
 template <typename T>
 struct Elements {
-    Run<T, 8> part[4];
+    Eight<T> part[4];
 };
 
 template <typename T>
@@ -651,34 +700,30 @@ __device__ __forceinline__ Elements<T> load_elements(const T* row, uint32_t bloc
         const T* from = row + min(32 * block, cols - 32);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            e.part[q] = *reinterpret_cast<const Run<T, 8>*>(from + 8 * q);
+            e.part[q] = *reinterpret_cast<const Eight<T>*>(from + 8 * q);
     }
     return e;
 }
 
 template <typename T>
-__device__ __forceinline__ Operand encode_block(const Elements<T>& e, const T* row, uint32_t block, uint32_t cols,
-                                                bool there)
+__device__ __forceinline__ Operand encode_block(Elements<T> e, const T* row, uint32_t block, uint32_t cols, bool there)
 {
-    float v[32];
-    T raw[32];
-    __builtin_memcpy(raw, &e, sizeof(raw));
-    if (32 * block + 32 > cols) {        // a row's last block, or none
+    if (!there) {
+        e = Elements<T>{};
+    } else if (32 * block + 32 > cols) {        // a row's last block, or none
 #pragma unroll
-        for (int k = 0; k < 32; ++k)
-            raw[k] = 32 * block + k < cols ? row[32 * block + k] : from_f32<T>(0.0f);
+        for (int q = 0; q < 4; ++q)
+            e.part[q] = load_eight<T>(row, 32 * block + 8 * q, cols);
     }
     uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        v[k] = there ? to_f32(raw[k]) : 0.0f;
-        top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-    }
+    for (int q = 0; q < 4; ++q)
+        top = max(top, top_of<T>(e.part[q]));
     Operand o;
-    o.scale = static_cast<int>(scale_byte(top));
+    o.scale = static_cast<int>(byte_of<T>(top));
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        o.codes[q] = static_cast<int>(encode8(v + 8 * q, o.scale));
+        o.codes[q] = static_cast<int>(encode<T>(e.part[q], o.scale));
     return o;
 }
 
