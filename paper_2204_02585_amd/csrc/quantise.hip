@@ -29,6 +29,15 @@ struct QuantParams {
     uint32_t cols, blocks;
 };
 
+// Row and place in it of item i of a matrix with `per_row` in a row.  The 64-bit
+// division is most of a kernel's instructions, so it is left to matrices of
+// 2^32 items or more.
+__device__ __forceinline__ void split_item(uint64_t i, uint32_t per_row, uint64_t items, uint32_t& row, uint32_t& at)
+{
+    row = items >> 32 ? static_cast<uint32_t>(i / per_row) : static_cast<uint32_t>(i) / per_row;
+    at = static_cast<uint32_t>(i) - row * per_row;
+}
+
 // ---- scales beside the tiles' products
 //
 // An instruction of a tile takes 32 rows, and a lane of it a scale byte, that
@@ -68,7 +77,9 @@ __device__ __forceinline__ void pack_share(const PackParams& p, uint32_t group, 
     const uint32_t per_row = 2 * p.packed.steps;
     for (uint64_t i = static_cast<uint64_t>(group) * kThreads + threadIdx.x; i < p.words;
          i += static_cast<uint64_t>(groups) * kThreads) {
-        const uint32_t row = static_cast<uint32_t>(i / per_row), block = 4 * static_cast<uint32_t>(i - row * static_cast<uint64_t>(per_row));
+        uint32_t row, block;
+        split_item(i, per_row, p.words, row, block);
+        block *= 4;
         uint32_t word = 0;
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k)
@@ -201,8 +212,8 @@ __global__ __launch_bounds__(kThreads) void quantise_kernel(QuantParams p)
     const uint32_t per_row = 4 * p.blocks;
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.items;
          i += static_cast<uint64_t>(gridDim.x) * kThreads) {
-        const uint64_t r = i / per_row;
-        const uint32_t q = static_cast<uint32_t>(i - r * per_row);
+        uint32_t r, q;
+        split_item(i, per_row, p.items, r, q);
         const Eight<T> e = load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols);
         const uint32_t byte = shared_scale<T>(e);
         reinterpret_cast<uint32_t*>(p.codes)[i] = encode<T>(e, byte);
@@ -225,8 +236,9 @@ __global__ __launch_bounds__(kThreads) void quantise_packed_kernel(QuantParams p
     const uint32_t per_row = 32 * packed.steps;
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.items;
          i += static_cast<uint64_t>(groups) * kThreads) {
-        const uint32_t r = static_cast<uint32_t>(i / per_row);
-        const uint32_t q = static_cast<uint32_t>(i - r * static_cast<uint64_t>(per_row)), block = q >> 2;
+        uint32_t r, q;
+        split_item(i, per_row, p.items, r, q);
+        const uint32_t block = q >> 2;
         uint32_t byte = kOne, codes = 0;
         if (block < p.blocks) {
             const Eight<T> e = load_eight<T>(static_cast<const T*>(p.x) + r * p.stride, 8 * q, p.cols);
@@ -239,18 +251,37 @@ __global__ __launch_bounds__(kThreads) void quantise_packed_kernel(QuantParams p
     }
 }
 
-// the magnitude of a 3-bit code, from the bits of binary32: subnormal 0.5, then 1 + m / 2
-__device__ __forceinline__ float decode1(uint32_t code)
+// The values of eight codes, rounded once to T: NaN for a marked block.
+template <typename T>
+__device__ __forceinline__ Eight<T> decode(uint32_t codes, uint32_t byte)
 {
-    const uint32_t m = code & 7;
-    const float mag = m < 2 ? 0.5f * m : __uint_as_float(((m >> 1) + 126) << 23 | (m & 1) << 22);
-    return __uint_as_float(__float_as_uint(mag) | (code & 8) << 28);
-}
-
-// 2^(byte - 127); NaN for 255
-__device__ __forceinline__ float decode_scale(uint32_t byte)
-{
-    return byte == 255 ? __builtin_nanf("") : byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
+    const float scale = byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
+    Eight<T> e;
+    typedef T pair __attribute__((ext_vector_type(2)));
+    pair v[4];
+    if constexpr (sizeof(T) == 4) {
+        v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
+        v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+        v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2);
+        v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+    } else if constexpr (std::is_same<T, _Float16>::value) {
+        v[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0);
+        v[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1);
+        v[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2);
+        v[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3);
+    } else {
+        v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+        v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+        v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+        v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    }
+    if (byte == 255) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = pair{from_f32<T>(__builtin_nanf("")), from_f32<T>(__builtin_nanf(""))};
+    }
+    __builtin_memcpy(&e, v, sizeof(e));
+    return e;
 }
 
 template <typename T>
@@ -259,20 +290,19 @@ __global__ __launch_bounds__(kThreads) void values_kernel(QuantParams p)
     const uint32_t per_row = 4 * p.blocks;
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.items;
          i += static_cast<uint64_t>(gridDim.x) * kThreads) {
-        const uint64_t r = i / per_row;
-        const uint32_t at = 8 * static_cast<uint32_t>(i - r * per_row);
-        const uint32_t c = reinterpret_cast<const uint32_t*>(p.codes)[i];
-        const float scale = decode_scale(p.scales[i >> 2]);
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = decode1(c >> (4 * k)) * scale;
+        uint32_t r, q;
+        split_item(i, per_row, p.items, r, q);
+        const Eight<T> e = decode<T>(reinterpret_cast<const uint32_t*>(p.codes)[i], p.scales[i >> 2]);
         T* row = static_cast<T*>(p.values) + r * p.stride;
-        if (at + 8 <= p.cols) {
-            store_run<T, 8>(row + at, v);
+        if (8 * q + 8 <= p.cols) {
+            *reinterpret_cast<Eight<T>*>(row + 8 * q) = e;
         } else {
-            for (uint32_t k = 0; at + k < p.cols; ++k)
-                row[at + k] = from_f32<T>(v[k]);
+            T v[8];
+            __builtin_memcpy(v, &e, sizeof(v));
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+                if (8 * q + k < p.cols)
+                    row[8 * q + k] = v[k];
         }
     }
 }
