@@ -3,7 +3,7 @@
 //
 // A workgroup computes a tile of C.  The sum goes in steps of 128 bytes (a
 // line of the caches) of every row, 64 binary16 or 256 4-bit elements, whose
-// rows stream from global memory straight into one of two LDS buffers.  A step
+// rows stream from global memory straight into one of the LDS buffers.  A step
 // is four instructions deep: instruction o takes from row r, in lane r % 32 +
 // 32 g, the row's 16-byte piece 4 g + o.  (Any assignment of pieces to lanes
 // gives the same sum; with this one a lane's scales of 4-bit elements lie side
@@ -14,14 +14,15 @@
 //
 // A depth's fragments are read between the products of the one before.  The
 // barrier of a step stands before its last depth, whose fragments are then in
-// registers: behind it the buffer takes the step after the next, and the next
-// step's first fragments can be read at once.  So a step's loads have a
-// whole step to land, and no reads wait behind a barrier.
+// registers: behind it the buffer takes the step that comes when all others are
+// through, and the next step's first fragments can be read at once.  So with
+// two buffers a step's loads have a whole step to land, with four (the tiles
+// of 64, whose steps are short) three, and no reads wait behind a barrier.
 //
 // A wave's part of C is FM x FN accumulators of 32 x 32: element q of a lane is
 // row 8 (q / 4) + 4 (lane / 32) + q % 4, column lane % 32.  Two waves share a
-// SIMD in every shape (eight waves in the largest tile, two workgroups of four
-// otherwise).
+// SIMD (eight waves in the largest tile, two workgroups of four otherwise),
+// one where high and low parts of the factors fill a CU's LDS.
 #pragma once
 
 #include <hip/hip_runtime.h>

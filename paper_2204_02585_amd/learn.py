@@ -122,6 +122,7 @@ class _Lookup(torch.autograd.Function):
         return _lookup(table.detach(), ids, scale, None, None)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         (ids,) = ctx.saved_tensors
         return lookup_gradient(grad, ids, ctx.rows, scale=ctx.scale, dtype=ctx.dtype), None, None
@@ -254,7 +255,8 @@ def product(x, w: Quantised, bias: Optional[torch.Tensor] = None, relu: bool = F
     """A layer on 4-bit blocks, act(x w^T + bias): x is Quantised [points, cols]
     (sqn_quantised_product) or a tensor [..., cols] that is quantised in the
     call (sqn_quantised_layer); w Quantised [units, cols]; bias float32
-    [units].  `dtype` is the result's: x's own, float32 for a Quantised x."""
+    [units].  `dtype` is the result's: x's own, float32 for a Quantised x.
+    No gradient passes through it: it is the form for evaluation."""
     blocks = isinstance(x, Quantised)
     if not isinstance(w, Quantised):
         raise TypeError("w must be Quantised")
