@@ -130,6 +130,15 @@ def test_gradient_of_many_indices(learn):
     _check_gradient(learn, _randn(9, 1_300_003, 4, dtype=torch.float16), ids, 50021)
 
 
+def test_gradient_of_long_stretches(learn):
+    """Stretches of 2^16 keys, all of one digit in the first ones: a count that
+    16 bits do not hold."""
+    count = 7 * 128 * 8192 + 5
+    ids = _ids(4, 1500, (count,), torch.int32)
+    ids[:200_000] = 3
+    _check_gradient(learn, _randn(9, count, 2, dtype=torch.float16), ids, 1500)
+
+
 def test_gradient_empty_and_outside(learn):
     """No indices, or none inside: zeros, or what was there."""
     for ids in (torch.zeros((0,), dtype=torch.int64), torch.full((100,), -1), torch.full((33,), 50)):
