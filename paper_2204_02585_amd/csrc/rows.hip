@@ -109,9 +109,9 @@ hipError_t lookup(const LookupParams& base, bool ids64, hipStream_t stream)
 // Least significant digit first, as few digits as ten bits each allow.  A pass
 // counts the digits of every workgroup's stretch of keys, then places them.
 // Within a stretch a wave takes consecutive keys, 64 at a time; equal digits
-// among the 64 find their order with one ballot per bit.  Up to kSortStep keys one
-// workgroup goes through all passes in LDS, in one launch.  Indices outside
-// the table sort as the key `rows`, behind all others.
+// among the 64 find their order with one ballot per bit.  Indices outside the
+// table sort as the key `rows`, behind all others.  Fewer keys are
+// sorted in one launch instead, by buckets of rows.
 //
 // While it sorts the chip is nearly idle, so the rows of the gradient are
 // cleared by further workgroups of the same launches.
@@ -119,11 +119,11 @@ hipError_t lookup(const LookupParams& base, bool ids64, hipStream_t stream)
 constexpr int kMaxDigitBits = 10;
 constexpr int kMaxBins = 1 << kMaxDigitBits;
 constexpr int kSortThreads = 1024;
-// Keys that a thread places of a stretch, and sorts of few in all.  Longer
-// stretches leave CUs idle, shorter ones are spent on the counts of the
-// stretches before (640,000 keys, us a pass: 16 keys a thread 25, 8 keys 22).
-constexpr int kPlaceKeys = 8, kSortKeys = 16;
-constexpr int kPlaceStep = kSortThreads * kPlaceKeys, kSortStep = kSortThreads * kSortKeys;
+// Keys that a thread places of a stretch.  Longer stretches leave CUs idle,
+// shorter ones are spent on the counts of the stretches before (640,000 keys, us
+// a pass: 16 keys a thread 25, 8 keys 22).
+constexpr int kPlaceKeys = 8;
+constexpr int kPlaceStep = kSortThreads * kPlaceKeys;
 constexpr int kMaxStretches = 128;
 constexpr int kWaves = kSortThreads / 64;
 
@@ -153,7 +153,6 @@ struct SortParams {
     uint32_t stretch;                   // keys per workgroup, a multiple of kPlaceStep
     uint32_t stretches;
     int shift, bits;                    // of the digit
-    int passes;
     Clear clear;
 };
 
@@ -181,14 +180,19 @@ __device__ void clear_share(const Clear& c, uint32_t block)
 struct Sorted {};
 
 template <typename I>
+__device__ __forceinline__ uint32_t key_at(const void* ids, uint32_t i, uint32_t rows)
+{
+    const int64_t id = static_cast<const I*>(ids)[i];
+    return static_cast<uint64_t>(id) < rows ? static_cast<uint32_t>(id) : rows;
+}
+
+template <typename I>
 __device__ __forceinline__ Pair pair_at(const SortParams& p, uint32_t i)
 {
-    if constexpr (std::is_same<I, Sorted>::value) {
+    if constexpr (std::is_same<I, Sorted>::value)
         return p.in[i];
-    } else {
-        const int64_t id = static_cast<const I*>(p.ids)[i];
-        return Pair{static_cast<uint64_t>(id) < p.rows ? static_cast<uint32_t>(id) : p.rows, i};
-    }
+    else
+        return Pair{key_at<I>(p.ids, i, p.rows), i};
 }
 
 // The number in its step of a thread's key k of KEYS: a wave's keys lie together.
@@ -198,20 +202,19 @@ __device__ __forceinline__ uint32_t number_of(int k)
     return (threadIdx.x >> 6) * (64 * KEYS) + 64 * k + (threadIdx.x & 63);
 }
 
-// A step's keys ranked among those of their digit in their wave, which counts
-// them in seen[digit]; keys from `n` on are not there.  begin(k) and end(k) stand
-// around the k-th key's ballots.
-template <int KEYS, typename B, typename E>
-__device__ __forceinline__ void rank_keys(const Pair (&pair)[KEYS], uint32_t n, int shift, int bits, uint32_t* seen,
-                                          uint32_t (&rank)[KEYS], B begin, E end)
+// A step's digits, digit(k) a thread's k-th, ranked among the equal ones of their
+// wave, which counts them in seen[digit]; keys from `n` on are not there.
+// begin(k) and end(k) stand around the k-th key's ballots.
+template <int KEYS, typename D, typename B, typename E>
+__device__ __forceinline__ void rank_keys(D digit_of, uint32_t n, uint32_t* seen, uint32_t (&rank)[KEYS],
+                                          B begin, E end)
 {
-    const uint32_t mask = (1u << bits) - 1;
     const uint64_t below = (uint64_t{1} << (threadIdx.x & 63)) - 1;
 #pragma unroll
     for (int k = 0; k < KEYS; ++k) {
         begin(k);
         const bool there = number_of<KEYS>(k) < n;
-        const uint32_t digit = pair[k].key >> shift & mask;
+        const uint32_t digit = digit_of(k);
         // lanes whose digit differs from this one's in some bit
         uint32_t other_low = 0, other_high = 0;
 #pragma unroll
@@ -257,7 +260,8 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t v, uint32_t* wave_sum
 
 // seen[wave][bin] from counts to where the wave's first key of the bin goes,
 // given where the step's first goes; returns where the next step's does.
-__device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[kMaxBins], uint32_t bin, uint32_t at)
+template <int BINS>
+__device__ __forceinline__ uint32_t counts_to_starts(uint32_t (*seen)[BINS], uint32_t bin, uint32_t at)
 {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
@@ -327,8 +331,8 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
         for (int w = 0; w < kWaves; ++w)
             seen[w][tid] = 0;
         __syncthreads();
-        rank_keys(
-            pair, last - step, p.shift, p.bits, seen[wave], rank,
+        rank_keys<kPlaceKeys>(
+            [&](int k) { return pair[k].key >> p.shift & (bins - 1); }, last - step, seen[wave], rank,
             [&](int k) {
                 if (sum && k * kCountsAhead * turns < p.stretches) {
 #pragma unroll
@@ -377,62 +381,222 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
         place(step, std::false_type());
 }
 
-// All passes over at most 1024 KEYS keys.
-template <int KEYS>
-constexpr size_t kSortBytes = kSortThreads * KEYS * sizeof(Pair) > sizeof(uint32_t) * kWaves * kMaxBins
-                                 ? kSortThreads * KEYS * sizeof(Pair)
-                                 : sizeof(uint32_t) * kWaves * kMaxBins;
+// ---- gradient: sorting in one launch
+//
+// A workgroup a bucket of 2^low rows: it reads all indices, keeps those of its
+// bucket in their order and counts those of the buckets before, which is where
+// its own go.  Those that it keeps fit LDS, as the row in the bucket and the
+// position in one word, and are sorted there by the row's bits; more than that
+// (many indices on few rows) go through global memory in steps.  A further
+// workgroup writes the marks of indices outside the table.  (Of 16,000 indices
+// into 30,000 rows the sort alone took 39 us in one workgroup.)
 
-template <typename I, int KEYS>
-__global__ __launch_bounds__(kSortThreads) void sort_kernel(SortParams p)
+constexpr uint32_t kPositionBits = 17;
+constexpr uint32_t kMaxLow = 32 - kPositionBits, kMaxBuckets = 1024;
+// Indices for each pass that the other sort takes.  (The call with one against
+// the other, us: 33,000 into 700 rows 29 and 31, 66,000 40 and 31; 66,000 into
+// 30,000 rows 38 and 51, 131,000 56 and 54; 66,000 into 2^20 47 and 71.)
+constexpr uint32_t kBucketPass = 40960;
+static_assert(3 * kBucketPass <= 1u << kPositionBits, "up to 2^25 rows take three passes");
+// Half of a CU's LDS, for a second workgroup that clears: indices that a wave can
+// keep, and bits of a pass.
+constexpr uint32_t kSegment = 512;
+constexpr int kBucketBits = 9, kBucketBins = 1 << kBucketBits;
+static_assert(2 * kBucketBits >= kMaxLow, "two passes");
+constexpr int kScanAhead = 8;
+
+struct BucketParams {
+    const void* ids;
+    Pair *out, *spare;
+    uint32_t n, rows;
+    uint32_t low, buckets;
+    int passes;                        // over the bits of the row in the bucket
+    Clear clear;
+};
+
+// emit(key, i) for the wave's indices in their order, by all lanes; the key
+// ~0 is none.
+template <typename I, typename E>
+__device__ __forceinline__ void scan_ids(const BucketParams& p, E emit)
 {
-    if (blockIdx.x >= 1) {
-        clear_share(p.clear, blockIdx.x - 1);
-        return;
+    const uint32_t span = (p.n + 64 * kWaves - 1) / (64 * kWaves) * 64;
+    const uint32_t lane = threadIdx.x & 63, first = (threadIdx.x >> 6) * span, last = min(p.n, first + span);
+    for (uint32_t i = first; i < last; i += 64 * kScanAhead) {
+        uint32_t key[kScanAhead];
+#pragma unroll
+        for (int a = 0; a < kScanAhead; ++a)
+            key[a] = key_at<I>(p.ids, min(i + 64 * a + lane, p.n - 1), p.rows);
+#pragma unroll
+        for (int a = 0; a < kScanAhead; ++a)
+            emit(i + 64 * a + lane < last ? key[a] : ~0u, i + 64 * a + lane);
     }
-    // the counts' place first, then the pairs'
-    __shared__ __align__(16) char shared[kSortBytes<KEYS>];
-    __shared__ uint32_t wave_sums[kWaves];
-    uint32_t (*seen)[kMaxBins] = reinterpret_cast<uint32_t (*)[kMaxBins]>(shared);
-    Pair* pairs = reinterpret_cast<Pair*>(shared);
+}
+
+__device__ __forceinline__ int shift_of(const BucketParams& p, int pass) { return p.low * pass / p.passes; }
+
+// The m kept words of `list`, in order, to out[start..].
+template <int KEYS>
+__device__ __forceinline__ void sort_list(const BucketParams& p, uint32_t first, uint32_t m, uint32_t start,
+                                          uint32_t (*seen)[kBucketBins], uint32_t* list, uint32_t* wave_sums)
+{
     const uint32_t tid = threadIdx.x, wave = tid >> 6;
-    Pair pair[KEYS];
-    uint32_t to[KEYS];
+    uint32_t v[KEYS], to[KEYS];
 #pragma unroll
     for (int k = 0; k < KEYS; ++k)
-        pair[k] = number_of<KEYS>(k) < p.n ? pair_at<I>(p, number_of<KEYS>(k)) : Pair{0, 0};
+        v[k] = number_of<KEYS>(k) < m ? list[number_of<KEYS>(k)] : 0;
     for (int pass = 0; pass < p.passes; ++pass) {
-        const int shift = pass * p.bits;
-        const uint32_t mask = (1u << p.bits) - 1;
-        for (int w = 0; w < kWaves; ++w)
-            seen[w][tid] = 0;
+        const int shift = shift_of(p, pass), bits = shift_of(p, pass + 1) - shift;
+        const uint32_t bins = 1u << bits;
+        auto digit = [&](int k) { return v[k] >> (kPositionBits + shift) & (bins - 1); };
+        if (tid < bins) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+                seen[w][tid] = 0;
+        }
         __syncthreads();
-        rank_keys(pair, p.n, shift, p.bits, seen[wave], to, [](int) {}, [](int) {});
+        rank_keys<KEYS>(digit, m, seen[wave], to, [](int) {}, [](int) {});
         __syncthreads();
         uint32_t total = 0;
-        for (int w = 0; w < kWaves; ++w)
-            total += seen[w][tid];
-        counts_to_starts(seen, tid, exclusive_sum(total, wave_sums));
+        if (tid < bins) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+                total += seen[w][tid];
+        }
+        const uint32_t base = exclusive_sum(total, wave_sums);
+        if (tid < bins)
+            counts_to_starts(seen, tid, base);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < KEYS; ++k)
-            to[k] += seen[wave][pair[k].key >> shift & mask];
-        __syncthreads();
+            to[k] += seen[wave][digit(k)];
+        if (pass + 1 < p.passes) {
 #pragma unroll
-        for (int k = 0; k < KEYS; ++k)
-            if (number_of<KEYS>(k) < p.n)
-                pairs[to[k]] = pair[k];
-        __syncthreads();
+            for (int k = 0; k < KEYS; ++k)
+                if (number_of<KEYS>(k) < m)
+                    list[to[k]] = v[k];
+            __syncthreads();
 #pragma unroll
-        for (int k = 0; k < KEYS; ++k)
-            if (number_of<KEYS>(k) < p.n)
-                pair[k] = pairs[number_of<KEYS>(k)];
-        __syncthreads();
+            for (int k = 0; k < KEYS; ++k)
+                v[k] = number_of<KEYS>(k) < m ? list[number_of<KEYS>(k)] : 0;
+        }
     }
 #pragma unroll
     for (int k = 0; k < KEYS; ++k)
-        if (number_of<KEYS>(k) < p.n)
-            p.out[number_of<KEYS>(k)] = pair[k];
+        if (number_of<KEYS>(k) < m)
+            p.out[start + to[k]] = Pair{first + (v[k] >> kPositionBits), v[k] & ((1u << kPositionBits) - 1)};
+}
+
+template <typename I>
+__global__ __launch_bounds__(kSortThreads) void bucket_kernel(BucketParams p)
+{
+    if (blockIdx.x > p.buckets) {
+        clear_share(p.clear, blockIdx.x - p.buckets - 1);
+        return;
+    }
+    __shared__ uint32_t list[kWaves * kSegment];
+    __shared__ uint32_t seen[kWaves][kBucketBins];
+    __shared__ uint32_t wave_sums[kWaves], kept_by[kWaves], before_by[kWaves];
+    static_assert(sizeof(list) <= sizeof(seen), "the list moves there and back");
+    const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const uint64_t below = (uint64_t{1} << lane) - 1;
+    const bool marks = blockIdx.x == p.buckets;
+    const uint32_t first = marks ? p.rows : blockIdx.x << p.low, count = marks ? 0 : min(1u << p.low, p.rows - first);
+
+    uint32_t kept = 0, before = 0;
+    scan_ids<I>(p, [&](uint32_t key, uint32_t i) {
+        const bool mine = key - first < count;
+        const uint64_t all = __ballot(mine);
+        before += __popcll(__ballot(key < first));
+        const uint32_t at = kept + __popcll(all & below);
+        if (mine && at < kSegment)
+            list[wave * kSegment + at] = (key - first) << kPositionBits | i;
+        kept += __popcll(all);
+    });
+    if (lane == 0) {
+        kept_by[wave] = kept;
+        before_by[wave] = before;
+    }
+    __syncthreads();
+    uint32_t m = 0, start = 0, offset = 0;
+    bool fits = true;
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) {
+        offset += w < wave ? kept_by[w] : 0;
+        m += kept_by[w];
+        start += before_by[w];
+        fits = fits && kept_by[w] <= kSegment;
+    }
+    if (marks) {
+        for (uint32_t i = start + tid; i < p.n; i += kSortThreads)
+            p.out[i] = Pair{p.rows, 0};
+        return;
+    }
+    if (m == 0)
+        return;
+    if (fits) {
+        uint32_t* whole = &seen[0][0];
+        for (uint32_t i = lane; i < kept; i += 64)
+            whole[offset + i] = list[wave * kSegment + i];
+        __syncthreads();
+        for (uint32_t i = tid; i < m; i += kSortThreads)
+            list[i] = whole[i];
+        __syncthreads();
+        if (m <= kSortThreads)
+            sort_list<1>(p, first, m, start, seen, list, wave_sums);
+        else if (m <= 4 * kSortThreads)
+            sort_list<4>(p, first, m, start, seen, list, wave_sums);
+        else
+            sort_list<8>(p, first, m, start, seen, list, wave_sums);
+        return;
+    }
+
+    // more than LDS holds: to global memory in order, then pass by pass
+    Pair *from = (p.passes & 1 ? p.spare : p.out) + start, *to = (p.passes & 1 ? p.out : p.spare) + start;
+    scan_ids<I>(p, [&](uint32_t key, uint32_t i) {
+        const bool mine = key - first < count;
+        const uint64_t all = __ballot(mine);
+        if (mine)
+            from[offset + __popcll(all & below)] = Pair{key, i};
+        offset += __popcll(all);
+    });
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = shift_of(p, pass), bits = shift_of(p, pass + 1) - shift;
+        const uint32_t bins = 1u << bits;
+        if (tid < bins)
+            list[tid] = 0;
+        __syncthreads();
+        for (uint32_t i = tid; i < m; i += kSortThreads)
+            atomicAdd(&list[(from[i].key - first) >> shift & (bins - 1)], 1u);
+        __syncthreads();
+        uint32_t base = exclusive_sum(tid < bins ? list[tid] : 0, wave_sums);
+        for (uint32_t step = 0; step < m; step += kPlaceStep) {
+            Pair pair[kPlaceKeys];
+            uint32_t rank[kPlaceKeys];
+            auto digit = [&](int k) { return (pair[k].key - first) >> shift & (bins - 1); };
+#pragma unroll
+            for (int k = 0; k < kPlaceKeys; ++k)
+                pair[k] = number_of<kPlaceKeys>(k) < m - step ? from[step + number_of<kPlaceKeys>(k)] : Pair{first, 0};
+            if (tid < bins) {
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    seen[w][tid] = 0;
+            }
+            __syncthreads();
+            rank_keys<kPlaceKeys>(digit, m - step, seen[wave], rank, [](int) {}, [](int) {});
+            __syncthreads();
+            if (tid < bins)
+                base = counts_to_starts(seen, tid, base);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kPlaceKeys; ++k)
+                if (number_of<kPlaceKeys>(k) < m - step)
+                    to[seen[wave][digit(k)] + rank[k]] = pair[k];
+            __syncthreads();
+        }
+        Pair* t = from;
+        from = to;
+        to = t;
+    }
 }
 
 // ---- gradient: sums
@@ -746,10 +910,16 @@ __global__ __launch_bounds__(kThreads) void direct_kernel(DirectParams p)
 
 // ---- gradient: layout and launches
 
-constexpr uint32_t kTile = 32;
+// Sorted entries that a group of lanes sums: where there are few lanes one
+// round of loads, else more, with fewer sums to join.  (The call in tiles of 8
+// and of 32, us: 4,000 indices of 64 columns 17.4 and 21.2, 33,000 27 and 33,
+// 131,000 61 and 57; 640,000 of 24 105 and 85.)
+constexpr uint32_t kTile = 32, kShortTile = kSumAhead;
+constexpr int64_t kShortLanes = 1 << 17;
 
 struct Plan {
-    uint32_t passes, bits, stretch, stretches, tiles;
+    uint32_t passes, bits, stretch, stretches, tile, tiles;
+    uint32_t low, buckets;              // 0 where the sort goes by digits
     size_t pairs[2], counts, head, tail, bytes;
 };
 
@@ -763,10 +933,16 @@ Plan plan_of(int64_t n, int64_t rows, int64_t cols)
         ++bits;                          // the largest key is `rows`
     q.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     q.bits = bits < 2 ? 2 : bits;        // counts are read by fours
+    // 64 to 128 buckets, so that a CU has one, and others clear
+    q.low = bits <= 10 ? 3 : bits - 7 < kMaxLow ? bits - 7 : kMaxLow;
+    q.buckets = static_cast<uint32_t>((rows + (int64_t{1} << q.low) - 1) >> q.low);
+    if (n > int64_t{kBucketPass} * q.passes || q.buckets > kMaxBuckets)
+        q.buckets = 0;
     const int64_t steps = (n + kPlaceStep - 1) / kPlaceStep;
     q.stretch = static_cast<uint32_t>((steps + kMaxStretches - 1) / kMaxStretches * kPlaceStep);
     q.stretches = q.stretch ? static_cast<uint32_t>((n + q.stretch - 1) / q.stretch) : 0;
-    q.tiles = static_cast<uint32_t>((n + kTile - 1) / kTile);
+    q.tile = n / kShortTile * ((cols + 3) / 4) <= kShortLanes ? kShortTile : kTile;
+    q.tiles = static_cast<uint32_t>((n + q.tile - 1) / q.tile);
     const size_t width = static_cast<size_t>(cols + 7) / 8 * 8;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -781,18 +957,6 @@ Plan plan_of(int64_t n, int64_t rows, int64_t cols)
     q.tail = take(4 * q.tiles * width);
     q.bytes = at;
     return q;
-}
-
-// One key a thread, or as many as there are for: a key's ballots take the time.
-template <typename I>
-void launch_sort(const SortParams& s, dim3 grid, hipStream_t stream)
-{
-    if (s.n <= kSortThreads)
-        sort_kernel<I, 1><<<grid, kSortThreads, 0, stream>>>(s);
-    else if (s.n <= 4 * kSortThreads)
-        sort_kernel<I, 4><<<grid, kSortThreads, 0, stream>>>(s);
-    else
-        sort_kernel<I, kSortKeys><<<grid, kSortThreads, 0, stream>>>(s);
 }
 
 // A pass; grid() sets s.clear to a launch's share and is its grid.
@@ -922,8 +1086,7 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
     p.n = static_cast<uint32_t>(grad.rows);
     p.rows = static_cast<uint32_t>(table_grad.rows);
     p.cols = static_cast<uint32_t>(grad.cols);
-    p.tile = kTile;
-    p.tiles = 0;
+    p.tile = p.tiles = 0;
     p.scale = scale;
     p.accumulate = accumulate ? 1 : 0;
     if (p.n <= kDirect) {
@@ -953,29 +1116,28 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
         c.rows = 1;
     }
     const uint64_t pieces = accumulate ? 0 : c.rows * ((c.row_bytes + 15) / 16);
-    s.bits = static_cast<int>((q.bits + q.passes - 1) / q.passes);
-    s.passes = static_cast<int>(q.passes);
-    s.shift = 0;
+    s.bits = s.shift = 0;
     s.in = nullptr;
     s.out = pairs[0];
-    const bool small = p.n <= kSortStep;
-    const uint32_t launches = small ? 1 : 2 * q.passes;
+    const uint32_t launches = q.buckets ? 1 : 2 * q.passes;
     uint32_t launch = 0;
     // the next launch's grid, with its share of the clearing
     auto grid = [&]() {
         c.first = pieces / launches * launch;
         c.last = ++launch == launches ? pieces : pieces / launches * launch;
         const uint64_t want = (c.last - c.first + 4096 - 1) / 4096;
-        c.blocks = static_cast<uint32_t>(want < 512 ? want : 512);
+        // many more than there are CUs: they do not begin together
+        c.blocks = static_cast<uint32_t>(want < 2048 ? want : 2048);
         s.clear = c;
-        return dim3((small ? 1 : q.stretches) + c.blocks);
+        return dim3((q.buckets ? q.buckets + 1 : q.stretches) + c.blocks);
     };
-    if (small) {
-        const dim3 sort_grid = grid();
+    if (q.buckets) {
+        const dim3 all = grid();
+        const BucketParams b{ids, pairs[0], pairs[1], s.n, s.rows, q.low, q.buckets, (static_cast<int>(q.low) + kBucketBits - 1) / kBucketBits, c};
         if (ids64)
-            launch_sort<int64_t>(s, sort_grid, stream);
+            bucket_kernel<int64_t><<<all, kSortThreads, 0, stream>>>(b);
         else
-            launch_sort<int32_t>(s, sort_grid, stream);
+            bucket_kernel<int32_t><<<all, kSortThreads, 0, stream>>>(b);
     } else {
         for (uint32_t pass = 0; pass < q.passes; ++pass) {
             s.shift = static_cast<int>(q.bits * pass / q.passes);
@@ -993,6 +1155,7 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
     p.pairs = s.out;
     p.head = reinterpret_cast<float*>(ws + q.head);
     p.tail = reinterpret_cast<float*>(ws + q.tail);
+    p.tile = q.tile;
     p.tiles = q.tiles;
     launch_sums_from(p, grad.dtype, table_grad.dtype, Indices{ids, ids64, false}, stream);
     return hipGetLastError();
