@@ -375,8 +375,9 @@ void sqn_destroy_networks(sqn_networks* nets);
  * Every call is asynchronous on `stream`, allocates nothing, keeps nothing
  * between calls and gives the same bits for the same arguments every time.
  * Scratch is the caller's: the *_workspace functions say how many bytes
- * (any alignment to 256 bytes; its contents need not be set and are left
- * unspecified); it must stay valid until the stream has finished the call.
+ * (aligned to 256 bytes, NULL where it is none; its contents need not be set
+ * and are left unspecified); it must stay valid until the stream has finished
+ * the call.
  * Outputs must not overlap inputs except where stated. */
 
 /* A matrix in device memory: element (i, j) of `dtype` at data +
@@ -434,8 +435,8 @@ typedef struct {
  * map), with (a, b, c) = coefficients: X's singular values go through
  * s -> a s + b s^3 + c s^5 each step, near 1 in the end.  Sums are binary32.
  * For a bfloat16 output the products take binary16 factors, the diagonals
- * of A and b A + c A A kept apart in binary32 and X in 22 bits; for
- * binary16 and binary32 outputs every factor has 22 bits.
+ * of A and b A + c A A kept apart in binary32 and X in 22 bits or more; for
+ * binary16 and binary32 outputs every factor has 22 bits and X 24.
  *   coefficients: host, finite; refused where the steps could take a singular
  *                 value past 2 or b s^2 + c s^4 past 16 in magnitude, the
  *                 range the binary16 factors are scaled for;
