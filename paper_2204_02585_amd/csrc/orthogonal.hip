@@ -234,6 +234,22 @@ struct Shape {
     static constexpr int PER_SIMD = SIDE == 256 || 2 * BUFFERS * BUFFER <= 160 * 1024 ? 2 : 1;    // waves
 };
 
+// A tile of 32 x 32 of a symmetric product by four waves, which take its steps in
+// turn, each in LDS of its own, and add up: for matrices whose larger tiles
+// would leave CUs idle.
+template <bool SPLIT_>
+struct Narrow {
+    static constexpr int SIDE = 32;
+    static constexpr bool SPLIT = SPLIT_;
+    static constexpr int WAVES = 4, THREADS = 64 * WAVES, FM = 1, FN = 1;
+    static constexpr int FACTORS = SPLIT ? 4 : 2;
+    static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
+    static constexpr int STEP = FACTORS * ROWS;               // bytes of a wave's step
+    static constexpr int BUFFER = WAVES * STEP, BUFFERS = 2;
+    static constexpr int LOADS = STEP / 1024;
+    static constexpr int PER_SIMD = 2 * BUFFERS * BUFFER <= 160 * 1024 ? 2 : 1;
+};
+
 struct Factor {
     const char *hi, *lo;     // the tile's first row
     uint32_t row_bytes;
@@ -374,6 +390,103 @@ __device__ __forceinline__ void products(const Factor& p, const Factor& q, uint3
     }
 }
 
+// The same of a narrow tile, in the first wave.
+template <typename S>
+__device__ __forceinline__ void products_in_turn(const Factor& p, const Factor& q, uint32_t steps, char* (&buffers)[2],
+                                                 Acc<S>& acc)
+{
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Acc<S> part, small;
+    clear<S>(acc);
+    clear<S>(small);
+    auto rows = [&](const char* from, uint32_t row_bytes, uint32_t step, char* to) {
+        from += static_cast<uint64_t>(step) * kStepBytes;
+#pragma unroll
+        for (uint32_t i = 0; i < S::SIDE / 8; ++i)
+            bring(from + (8 * i + (lane >> 3)) * row_bytes + brought_piece(lane, i) * kSlot, to + i * 1024);
+    };
+    auto bring_own = [&](uint32_t step, char* to) {
+        rows(p.hi, p.row_bytes, step, to);
+        rows(q.hi, q.row_bytes, step, to + S::ROWS);
+        if constexpr (S::SPLIT) {
+            rows(p.lo, p.row_bytes, step, to + 2 * S::ROWS);
+            rows(q.lo, q.row_bytes, step, to + 3 * S::ROWS);
+        }
+    };
+    auto work = [&](uint32_t step, char* own) {
+        // its loads have landed but those of the wave's next step
+        if (step + S::WAVES < steps)
+            landed_own<S::LOADS>();
+        else
+            landed_own<0>();
+        Fragments<S> f[kDepths];
+#pragma unroll
+        for (int o = 0; o < kDepths; ++o) {
+            const char* at = own + piece_at(lane, o);
+            f[o].a[0] = *reinterpret_cast<const half8*>(at);
+            f[o].b[0] = *reinterpret_cast<const half8*>(at + S::ROWS);
+            if constexpr (S::SPLIT) {
+                f[o].a_lo[0] = *reinterpret_cast<const half8*>(at + 2 * S::ROWS);
+                f[o].b_lo[0] = *reinterpret_cast<const half8*>(at + 3 * S::ROWS);
+            }
+        }
+        reads_done();
+        if (step + 2 * S::WAVES < steps)
+            bring_own(step + 2 * S::WAVES, own);
+        if constexpr (S::SPLIT)
+            clear<S>(part);
+#pragma unroll
+        for (int o = 0; o < kDepths; ++o) {
+            if constexpr (S::SPLIT) {
+                part[0][0] = multiply(f[o].a[0], f[o].b[0], part[0][0]);
+                small[0][0] = multiply(f[o].a[0], f[o].b_lo[0], small[0][0]);
+                small[0][0] = multiply(f[o].a_lo[0], f[o].b[0], small[0][0]);
+            } else {
+                acc[0][0] = multiply(f[o].a[0], f[o].b[0], acc[0][0]);
+            }
+        }
+        if constexpr (S::SPLIT)
+            add<S>(acc, part);
+    };
+    char* own0 = buffers[0] + wave * S::STEP;
+    char* own1 = buffers[1] + wave * S::STEP;
+    if (wave < steps)
+        bring_own(wave, own0);
+    if (wave + S::WAVES < steps)
+        bring_own(wave + S::WAVES, own1);
+    for (uint32_t k = wave; k < steps; k += 2 * S::WAVES) {
+        work(k, own0);
+        if (k + S::WAVES < steps)
+            work(k + S::WAVES, own1);
+    }
+    if constexpr (S::SPLIT)
+        add<S>(acc, small);
+    __syncthreads();
+    float16v* sums = reinterpret_cast<float16v*>(buffers[1]);
+    if (wave > 0)
+        sums[(wave - 1) * 64 + lane] = acc[0][0];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (int w = 0; w < S::WAVES - 1; ++w)
+            acc[0][0] += sums[w * 64 + lane];
+    }
+}
+
+// A symmetric product's tile (ti, tj); false for the waves that have no part of it.
+template <typename S>
+__device__ __forceinline__ bool symmetric(const Factor& p, const Factor& q, uint32_t steps, char* (&buffers)[S::BUFFERS],
+                                          Acc<S>& acc)
+{
+    if constexpr (S::SIDE == 32) {
+        products_in_turn<S>(p, q, steps, buffers, acc);
+        return threadIdx.x < 64;
+    } else {
+        products<S>(p, q, steps, buffers, acc);
+        return true;
+    }
+}
+
 __device__ __forceinline__ Factor factor(const _Float16* hi, const _Float16* lo, uint64_t row, uint32_t cols)
 {
     Factor f;
@@ -484,8 +597,9 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void gram_kernel(OrthParam
     lower_tile(blockIdx.x, ti, tj);
     const uint64_t x = static_cast<uint64_t>(blockIdx.y) * p.mp * p.np, o = static_cast<uint64_t>(blockIdx.y) * p.mp * p.mp;
     Acc<S> acc;
-    products<S>(factor(p.s.x + x, p.s.x_lo + x, ti * S::SIDE, p.np), factor(p.s.x + x, p.s.x_lo + x, tj * S::SIDE, p.np),
-                p.steps_n, buffers, acc);
+    if (!symmetric<S>(factor(p.s.x + x, p.s.x_lo + x, ti * S::SIDE, p.np),
+                      factor(p.s.x + x, p.s.x_lo + x, tj * S::SIDE, p.np), p.steps_n, buffers, acc))
+        return;
     _Float16* hi = p.s.o + o;
     _Float16* lo = p.s.o_lo + o;
     float* d = p.s.d + blockIdx.y * p.mp;
@@ -520,7 +634,9 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void square_kernel(OrthPar
     const _Float16* o_hi = p.s.o + o;
     const _Float16* o_lo = p.s.o_lo + o;
     Acc<S> acc;
-    products<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, buffers, acc);
+    if (!symmetric<S>(factor(o_hi, o_lo, ti * S::SIDE, p.mp), factor(o_hi, o_lo, tj * S::SIDE, p.mp), p.steps_m, buffers,
+                      acc))
+        return;
     _Float16* hi = p.s.b + o;
     _Float16* lo = p.s.b_lo + o;
     const float* d = p.s.d + blockIdx.y * p.mp;
@@ -904,6 +1020,12 @@ int32_t tile_side(int32_t batch, int32_t m, int32_t n, bool split_all)
     return tiles(128) >= 200 ? 128 : 64;
 }
 
+// Narrow tiles take the symmetric products where tiles of 64 would and each CU
+// has one narrow tile at most.  (The call with them and without, us: 701 x 1100
+// to binary32, 253 narrow tiles, 147 and 178, to bfloat16 108 and 120; 300 x 400
+// to binary32, 55 of them, 104 and 124; 900 x 900, 465 of them, 227 and 202.)
+constexpr int64_t kCus = 256;
+
 int32_t up_to(int32_t v, int32_t side) { return (v + side - 1) / side * side; }
 
 size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* base, Scratch* s)
@@ -1024,13 +1146,20 @@ hipError_t launch_orthogonalise(const sqn_batch& updates, int32_t steps, const f
         emit_kernel<<<dim3(1, p.m, updates.batch), kThreads, 0, stream>>>(p);
         return hipGetLastError();
     }
-    if (split_all)
-        return side == 128 ? run_steps<Shape<128, true>>(p, updates.batch, steps, stream)
-                           : run_steps<Shape<64, true>>(p, updates.batch, steps, stream);
+    const int64_t along = p.mp / Narrow<true>::SIDE;
+    const bool narrow = updates.batch * (along * (along + 1) / 2) <= kCus;
+    if (split_all) {
+        if (side == 128)
+            return run_steps<Shape<128, true>>(p, updates.batch, steps, stream);
+        return narrow ? run_steps<Shape<64, true>, Narrow<true>>(p, updates.batch, steps, stream)
+                      : run_steps<Shape<64, true>>(p, updates.batch, steps, stream);
+    }
     if (side == 256)
         return run_steps<Shape<256, false>>(p, updates.batch, steps, stream);
-    return side == 128 ? run_steps<Shape<128, false>>(p, updates.batch, steps, stream)
-                       : run_steps<Shape<64, false>>(p, updates.batch, steps, stream);
+    if (side == 128)
+        return run_steps<Shape<128, false>>(p, updates.batch, steps, stream);
+    return narrow ? run_steps<Shape<64, false>, Narrow<false>>(p, updates.batch, steps, stream)
+                  : run_steps<Shape<64, false>>(p, updates.batch, steps, stream);
 }
 
 }  // namespace sqn

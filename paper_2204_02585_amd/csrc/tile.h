@@ -72,6 +72,24 @@ __device__ __forceinline__ void landed()
     asm volatile("" ::: "memory");
 }
 
+// This wave's loads into LDS but the LATER newest have landed, for itself.
+template <int LATER>
+__device__ __forceinline__ void landed_own()
+{
+    static_assert(LATER < 64, "vmcnt has six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((LATER & 15) | 0xf70 | (LATER >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
+
+// This wave's reads of LDS are in registers: what they read may be loaded over.
+__device__ __forceinline__ void reads_done()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+}
+
 // A kernel's LDS for the steps of shape S: arrays of their own, so that reads of
 // one do not wait for loads into another.
 #define BUFFERS_IN_LDS(S)                                                            \

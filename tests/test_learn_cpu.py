@@ -184,6 +184,9 @@ out["g1023"] = names(gradient(200000, 1023, 8))      # ten bits hold the mark of
 out["g1024"] = names(gradient(200000, 1024, 8))
 for m, n, o in ((128, 256, BF16), (256, 128, BF16), (129, 200, BF16), (128, 257, BF16), (128, 128, F32), (100, 129, F16)):
     out["o%d_%d_%d" % (m, n, o)] = names(orth(batch(2, m, n), batch(2, m, n, o), steps=2))
+for b, m, n, o in ((1, 704, 1100, F32), (1, 705, 1100, F32), (1, 704, 1100, BF16), (7, 200, 200, BF16), (8, 200, 200, BF16)):
+    assert orth(batch(b, m, n), batch(b, m, n, o), steps=1) == 0
+    out["n%d_%d_%d" % (b, m, o)] = ["Narrow" in l for l in launches()[2:]]
 for p, u, c in ((16, 300, 999), (17, 300, 999), (17, 256, 512), (17, 256, 513), (17, 257, 512), (17, 256, 7)):
     out["l%d_%d_%d" % (p, u, c)] = names(layer(p, u, c))
 out["p16"], out["p17"] = names(product(16, 9, 100)), names(product(17, 9, 100))
@@ -204,6 +207,10 @@ print(json.dumps([out, spaces]))
         assert out[name] == ["small"], (name, out[name])
     for name in ("o129_200_2", "o128_257_2", "o100_129_1"):
         assert out[name] == tiles, (name, out[name])
+    for name in ("n1_704_0", "n1_704_2", "n7_200_2"):     # at most 256 narrow tiles, symmetric products only
+        assert out[name] == [True, True, False], (name, out[name])
+    for name in ("n1_705_0", "n8_200_2"):
+        assert out[name] == [False] * 3, (name, out[name])
     assert out["l16_300_999"] == ["few"] and out["l17_300_999"] == ["quantise_packed", "product"]
     assert out["l17_256_512"] == ["layer"]
     for name in ("l17_256_513", "l17_257_512", "l17_256_7"):
