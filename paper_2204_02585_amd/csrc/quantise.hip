@@ -668,17 +668,24 @@ bool is_layer(int64_t units, int64_t cols) { return units <= kLayerUnits && cols
 
 // ---- products of few points
 //
-// Up to kFew points (one token's activations among them) the weights' bytes are
+// For few points (one token's activations among them) the weights' bytes are
 // all that takes time, and a launch of its own for the activations' blocks
 // would take longer than the product.  A workgroup computes 16 units of all
-// points on v_mfma_scale_f32_16x16x128_f8f6f4; its waves share the sum and add
-// up in LDS, in the order of the waves.  Every wave puts the points' elements
-// of its stretch into blocks by itself.  4096 x 4096 of one point: 8.9 MB of
-// weights from the caches.
+// points, or 32 or 64 where there are many units, on
+// v_mfma_scale_f32_16x16x128_f8f6f4; its waves share the sum and add up in LDS,
+// in the order of the waves.  Every wave puts the points' elements of its
+// stretch into blocks by itself, which costs it more instructions than its
+// products: hence more units a workgroup (one point of 8192 by 8192 units 12.9
+// us a call, 18.1 with 16), and tiles for many elements (16 points of 16384
+// binary32 by 4096 units 24 us, 39 here; of 4096 binary16 14.0 and 10.2).
 
 constexpr uint32_t kFew = 16;
-constexpr int kFewAhead = 2;         // steps whose weights are under way together
+bool is_few(int64_t points, int64_t cols) { return points <= 4 || (points <= kFew && points * cols <= 65536); }
+// Steps whose weights are under way together: as many as the registers take.
+template <typename T, int UNITS>
+constexpr int kFewAhead = sizeof(T) == 4 || UNITS == 4 ? 1 : 2;
 constexpr int kFewMaxWaves = 16;
+constexpr uint32_t kFewGroups = 256;    // of 16 units: a workgroup takes more where there are more
 
 struct FewParams {
     const uint8_t *w, *w_scales;
@@ -757,25 +764,35 @@ __device__ __forceinline__ Operand encode_block(Elements<T> e, const T* row, uin
     return o;
 }
 
-template <typename T>
+template <typename T, int UNITS>
 __global__ __launch_bounds__(64 * kFewMaxWaves) void few_kernel(FewParams p)
 {
-    __shared__ float4v sums[kFewMaxWaves][64];
+    constexpr int AHEAD = kFewAhead<T, UNITS>;
+    __shared__ float4v sums[kFewMaxWaves][UNITS][64];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const uint32_t row = lane & 15, unit = min(blockIdx.x * 16 + row, p.units - 1);
+    const uint32_t row = lane & 15;
+    uint32_t unit[UNITS];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+        unit[u] = min((blockIdx.x * UNITS + u) * 16 + row, p.units - 1);
     const bool there = row < p.points;
     const uint32_t first = wave * p.steps, last = min(first + p.steps, (p.blocks + 3) / 4);
-    float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t k = first; k < last; k += kFewAhead) {
-        Operand w[kFewAhead], x[kFewAhead];
-        Elements<std::conditional_t<std::is_same<T, Blocks>::value, float, T>> e[kFewAhead];
+    float4v acc[UNITS];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+        acc[u] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t k = first; k < last; k += AHEAD) {
+        Operand w[AHEAD][UNITS], x[AHEAD];
+        Elements<std::conditional_t<std::is_same<T, Blocks>::value, float, T>> e[AHEAD];
         const T* row_x = nullptr;
         if constexpr (!std::is_same<T, Blocks>::value)
             row_x = static_cast<const T*>(p.x) + (there ? row : 0) * p.x_stride;
 #pragma unroll
-        for (int a = 0; a < kFewAhead; ++a) {
+        for (int a = 0; a < AHEAD; ++a) {
             const uint32_t block = 4 * (k + a) + (lane >> 4);
-            w[a] = load_block(p.w, p.w_scales, unit, block, p.blocks, k + a < last);
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u)
+                w[a][u] = load_block(p.w, p.w_scales, unit[u], block, p.blocks, k + a < last);
             if constexpr (std::is_same<T, Blocks>::value)
                 x[a] = load_block(static_cast<const uint8_t*>(p.x), p.x_scales, there ? row : 0, block, p.blocks,
                                   there && k + a < last);
@@ -783,40 +800,49 @@ __global__ __launch_bounds__(64 * kFewMaxWaves) void few_kernel(FewParams p)
                 e[a] = load_elements(row_x, block, p.cols);
         }
 #pragma unroll
-        for (int a = 0; a < kFewAhead; ++a) {
+        for (int a = 0; a < AHEAD; ++a) {
             if constexpr (!std::is_same<T, Blocks>::value)
                 x[a] = encode_block(e[a], row_x, 4 * (k + a) + (lane >> 4), p.cols, there && k + a < last);
-            const int8v w8 = __builtin_shufflevector(w[a].codes, w[a].codes, 0, 1, 2, 3, -1, -1, -1, -1);
             const int8v x8 = __builtin_shufflevector(x[a].codes, x[a].codes, 0, 1, 2, 3, -1, -1, -1, -1);
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, acc, 4, 4, 0, w[a].scale, 0, x[a].scale);
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const int4v c = w[a][u].codes;
+                const int8v w8 = __builtin_shufflevector(c, c, 0, 1, 2, 3, -1, -1, -1, -1);
+                acc[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, x8, acc[u], 4, 4, 0, w[a][u].scale, 0,
+                                                                          x[a].scale);
+            }
         }
     }
-    sums[wave][lane] = acc;
-    __syncthreads();
-    if (wave > 0)
-        return;
-    for (uint32_t k = 1; k < waves; ++k)
-        acc += sums[k][lane];
-    // element q: unit 4 (lane / 16) + q of point lane % 16
-    if (!there)
-        return;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const uint32_t u = blockIdx.x * 16 + 4 * (lane >> 4) + q;
-        if (u >= p.units)
-            break;
-        float v = acc[q];
-        if (p.bias)
-            v += p.bias[u];
-        if (p.relu)
-            v = v < 0.0f ? 0.0f : v;
-        const int64_t at = row * p.out_stride + u;
-        if (p.dtype == SQN_F32)
-            static_cast<float*>(p.out)[at] = v;
-        else if (p.dtype == SQN_F16)
-            static_cast<_Float16*>(p.out)[at] = static_cast<_Float16>(v);
-        else
-            static_cast<__bf16*>(p.out)[at] = static_cast<__bf16>(v);
+    for (int u = 0; u < UNITS; ++u)
+        sums[wave][u][lane] = acc[u];
+    __syncthreads();
+    // a wave for each 16 units, or one after another where there are fewer
+    for (uint32_t g = wave; g < UNITS; g += waves) {
+        float4v sum = sums[0][g][lane];
+        for (uint32_t k = 1; k < waves; ++k)
+            sum += sums[k][g][lane];
+        // element q: unit 4 (lane / 16) + q of point lane % 16
+        if (!there)
+            continue;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t u = (blockIdx.x * UNITS + g) * 16 + 4 * (lane >> 4) + q;
+            if (u >= p.units)
+                break;
+            float v = sum[q];
+            if (p.bias)
+                v += p.bias[u];
+            if (p.relu)
+                v = v < 0.0f ? 0.0f : v;
+            const int64_t at = row * p.out_stride + u;
+            if (p.dtype == SQN_F32)
+                static_cast<float*>(p.out)[at] = v;
+            else if (p.dtype == SQN_F16)
+                static_cast<_Float16*>(p.out)[at] = static_cast<_Float16>(v);
+            else
+                static_cast<__bf16*>(p.out)[at] = static_cast<__bf16>(v);
+        }
     }
 }
 
@@ -839,13 +865,20 @@ hipError_t launch_few(const void* x, const uint8_t* x_scales, int64_t x_stride, 
     p.blocks = static_cast<uint32_t>(quant_blocks(w.cols));
     p.relu = relu ? 1 : 0;
     p.dtype = out.dtype;
-    // a wave takes a batch of steps or more, unless that leaves CUs with little
     const uint32_t groups = (p.units + 15) / 16, steps = (p.blocks + 3) / 4;
+    const uint32_t each = groups >= 4 * kFewGroups ? 4 : groups >= 2 * kFewGroups ? 2 : 1;
+    const uint32_t grid = (groups + each - 1) / each;
+    // a wave takes a batch of steps or more, unless that leaves CUs with little
     uint32_t waves = 1;
-    while (waves < kFewMaxWaves && waves < steps && (groups * waves < 2048 || steps > waves * kFewAhead))
+    while (waves < kFewMaxWaves && waves < steps && (grid * waves < 2048 || steps > 2 * waves))
         waves *= 2;
     p.steps = (steps + waves - 1) / waves;
-    few_kernel<T><<<groups, 64 * waves, 0, stream>>>(p);
+    if (each == 4)
+        few_kernel<T, 4><<<grid, 64 * waves, 0, stream>>>(p);
+    else if (each == 2)
+        few_kernel<T, 2><<<grid, 64 * waves, 0, stream>>>(p);
+    else
+        few_kernel<T, 1><<<grid, 64 * waves, 0, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -973,7 +1006,7 @@ hipError_t launch_quantised_values(const sqn_quantised& x, const sqn_matrix& out
 hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised& w, const float* bias, bool relu,
                                     const sqn_matrix& out, void* workspace, hipStream_t stream)
 {
-    if (x.rows <= kFew)
+    if (is_few(x.rows, x.cols))
         return launch_few<Blocks>(x.codes, static_cast<const uint8_t*>(x.scales), 0, x.rows, w, bias, relu, out, stream);
     const ProductScratch t(x.rows, w.rows, x.cols, workspace);
     const PackParams pw = pack_of(w, t.w_packed);
@@ -991,7 +1024,7 @@ hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised&
 
 size_t quantised_product_bytes(int64_t points, int64_t units, int64_t cols)
 {
-    return points <= kFew ? 0 : ProductScratch(points, units, cols, nullptr).bytes;
+    return is_few(points, cols) ? 0 : ProductScratch(points, units, cols, nullptr).bytes;
 }
 
 size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols)
@@ -1002,7 +1035,7 @@ size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols)
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
                                   const sqn_matrix& out, void* workspace, hipStream_t stream)
 {
-    if (x.rows <= kFew) {
+    if (is_few(x.rows, x.cols)) {
         if (x.dtype == SQN_F32)
             return launch_few<float>(x.data, nullptr, x.row_stride, x.rows, w, bias, relu, out, stream);
         if (x.dtype == SQN_F16)

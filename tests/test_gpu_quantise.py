@@ -123,6 +123,14 @@ def test_larger_products(learn, points, units, cols):
         _check_product(learn, x, w, _randn(5, units), k == 0, dtype)
 
 
+@pytest.mark.parametrize("points,units,cols", [(1, 8192, 300), (16, 8215, 1000), (4, 16384, 513), (9, 16431, 70), (2, 17000, 32)])
+def test_few_points_by_many_units(learn, points, units, cols):
+    """Workgroups of 32 and 64 units, the last ones not full, and fewer waves than
+    groups of units."""
+    for k, dtype in enumerate(DTYPES):
+        _check_product(learn, _randn(1, points, cols, dtype=dtype), _randn(3, units, cols), _randn(5, units), k == 1, dtype)
+
+
 def test_product_scales_reach_far(learn):
     """Scales from the smallest to the largest that the sums can hold, in one
     product: the scale of every block is the one that is applied."""

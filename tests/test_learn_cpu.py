@@ -189,6 +189,8 @@ for b, m, n, o in ((1, 704, 1100, F32), (1, 705, 1100, F32), (1, 704, 1100, BF16
     out["n%d_%d_%d" % (b, m, o)] = ["Narrow" in l for l in launches()[2:]]
 for p, u, c in ((16, 300, 999), (17, 300, 999), (17, 256, 512), (17, 256, 513), (17, 257, 512), (17, 256, 7)):
     out["l%d_%d_%d" % (p, u, c)] = names(layer(p, u, c))
+for p, c in ((4, 1 << 20), (5, 13107), (5, 13108), (16, 4096), (16, 4097)):
+    out["f%d_%d" % (p, c)] = names(layer(p, 9, c))
 out["p16"], out["p17"] = names(product(16, 9, 100)), names(product(17, 9, 100))
 spaces = [lib.sqn_lookup_gradient_workspace(256, 90, 8), lib.sqn_orthogonalise_workspace(2, 128, 256, BF16),
           lib.sqn_quantised_layer_workspace(16, 300, 999), lib.sqn_quantised_layer_workspace(17, 256, 512)]
@@ -211,6 +213,10 @@ print(json.dumps([out, spaces]))
         assert out[name] == [True, True, False], (name, out[name])
     for name in ("n1_705_0", "n8_200_2"):
         assert out[name] == [False] * 3, (name, out[name])
+    for name in ("f4_1048576", "f5_13107", "f16_4096"):
+        assert out[name] == ["few"], (name, out[name])
+    for name in ("f5_13108", "f16_4097"):
+        assert out[name] == ["quantise_packed", "product"], (name, out[name])
     assert out["l16_300_999"] == ["few"] and out["l17_300_999"] == ["quantise_packed", "product"]
     assert out["l17_256_512"] == ["layer"]
     for name in ("l17_256_513", "l17_257_512", "l17_256_7"):
