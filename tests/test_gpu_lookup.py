@@ -130,6 +130,18 @@ def test_gradient_of_many_indices(learn):
     _check_gradient(learn, _randn(9, 1_300_003, 4, dtype=torch.float16), ids, 50021)
 
 
+@pytest.mark.parametrize("count", [300, 900, 3000, 8000, 20000, 60000])
+@pytest.mark.parametrize("rows,first,some", [(300_000, 5000, 3000), (300_000, 299_000, 1000), (70_001, 1536, 512), (1 << 25, 1 << 24, 1 << 15)])
+def test_gradient_of_rows_close_together(learn, rows, first, some, count):
+    """All indices in one bucket of the sort, in one or two passes, in LDS and past
+    what it holds; marks of outside indices beside them."""
+    ids = first + _ids(count, some, (count,), torch.int64, outside=0.0)
+    ids[::9] = -1
+    ids[1::9] = rows
+    cols = 2 if rows > 1 << 20 else 12
+    _check_gradient(learn, _randn(count, count, cols), ids, rows, scale=0.5)
+
+
 def test_gradient_of_long_stretches(learn):
     """Stretches of 2^16 keys, all of one digit in the first ones: a count that
     16 bits do not hold."""
