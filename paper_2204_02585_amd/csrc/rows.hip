@@ -392,12 +392,13 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
 // into 30,000 rows the sort alone took 39 us in one workgroup.)
 
 constexpr uint32_t kPositionBits = 17;
-constexpr uint32_t kMaxLow = 32 - kPositionBits, kMaxBuckets = 1024;
+constexpr uint32_t kMaxLow = 32 - kPositionBits, kMaxBuckets = 512;
 // Indices for each pass that the other sort takes.  (The call with one against
 // the other, us: 33,000 into 700 rows 29 and 31, 66,000 40 and 31; 66,000 into
-// 30,000 rows 38 and 51, 131,000 56 and 54; 66,000 into 2^20 47 and 71.)
+// 30,000 rows 38 and 51, 131,000 56 and 54; 100,000 into 2^23 53 and 66, into
+// 2^25, which would take 1024 buckets, 134 and 85.)
 constexpr uint32_t kBucketPass = 40960;
-static_assert(3 * kBucketPass <= 1u << kPositionBits, "up to 2^25 rows take three passes");
+static_assert(3 * kBucketPass <= 1u << kPositionBits, "up to 2^24 rows take three passes");
 // Half of a CU's LDS, for a second workgroup that clears: indices that a wave can
 // keep, and bits of a pass.
 constexpr uint32_t kSegment = 512;

@@ -131,7 +131,8 @@ def test_gradient_of_many_indices(learn):
 
 
 @pytest.mark.parametrize("count", [300, 900, 3000, 8000, 20000, 60000])
-@pytest.mark.parametrize("rows,first,some", [(300_000, 5000, 3000), (300_000, 299_000, 1000), (70_001, 1536, 512), (1 << 25, 1 << 24, 1 << 15)])
+@pytest.mark.parametrize("rows,first,some", [(300_000, 5000, 3000), (300_000, 299_000, 1000), (70_001, 1536, 512), (1 << 25, 1 << 24, 1 << 15),
+                                             (1 << 24, 1 << 23, 1 << 15)])
 def test_gradient_of_rows_close_together(learn, rows, first, some, count):
     """All indices in one bucket of the sort, in one or two passes, in LDS and past
     what it holds; marks of outside indices beside them."""
