@@ -5,9 +5,10 @@
 //
 // Both move bytes and compute next to nothing.  The gradient's sums must not
 // depend on the order in which the GPU gets to the rows, so the positions are
-// sorted by index (a stable radix sort), cut into tiles of the sorted order,
-// and each tile sums its runs of equal indices; runs that cross tiles leave
-// partial sums that a second kernel joins in tile order.
+// sorted by index (keeping their order where it is the same: by radix passes, or
+// of fewer by buckets of rows), cut into tiles of the sorted order, and each
+// tile sums its runs of equal indices; runs that cross tiles leave partial sums
+// that a second kernel joins in tile order.  Very few indices take one launch.
 #include <type_traits>
 
 #include "learn.h"
