@@ -378,6 +378,8 @@ void sqn_destroy_networks(sqn_networks* nets);
  * (aligned to 256 bytes, NULL where it is none; its contents need not be set
  * and are left unspecified); it must stay valid until the stream has finished
  * the call.
+ * All memory and the stream must belong to the current device; what lies on
+ * another is refused (SQN_ERR_INVALID_ARG).
  * Outputs must not overlap inputs except where stated. */
 
 /* A matrix in device memory: element (i, j) of `dtype` at data +

@@ -8,7 +8,6 @@
 
 namespace {
 
-using sqn::check_device_range;
 using sqn::element_size;
 using sqn::fail;
 
@@ -22,6 +21,57 @@ constexpr int64_t kMaxStride = int64_t{1} << 40;
 constexpr int32_t kMaxSteps = 64;
 
 bool valid_dtype(int32_t dt) { return dt == SQN_F32 || dt == SQN_F16 || dt == SQN_BF16; }
+
+// Whether the process sees more than one device: of one, nothing lies on
+// another, and the queries below (0.5 us of a lookup's 8.8 us call) are left out.
+bool several_devices()
+{
+    static const bool several = [] {
+        int count = 0;
+        if (hipGetDeviceCount(&count) == hipSuccess)
+            return count > 1;
+        (void)hipGetLastError();
+        return false;
+    }();
+    return several;
+}
+
+// The memory is there, and the current device's own: a launch goes to that
+// device, and nothing orders it with another's streams.
+sqn_status check_memory(const void* p, size_t bytes, const char* what)
+{
+    const sqn_status s = sqn::check_device_range(p, bytes, what);
+    if (s != SQN_OK || !several_devices())
+        return s;
+    int current = 0, device = 0;
+    if (hipGetDevice(&current) != hipSuccess)
+        return fail(SQN_ERR_DEVICE, "hipGetDevice failed");
+    if (hipPointerGetAttribute(&device, HIP_POINTER_ATTRIBUTE_DEVICE_ORDINAL, const_cast<void*>(p)) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(SQN_ERR_INVALID_ARG, "%s (%p): its device is not known", what, p);
+    }
+    if (device != current)
+        return fail(SQN_ERR_INVALID_ARG, "%s lives on device %d, current device is %d", what, device, current);
+    return SQN_OK;
+}
+
+sqn_status check_stream(void* stream)
+{
+    if (!stream || stream == hipStreamPerThread || !several_devices())
+        return SQN_OK;                // those two are the current device's
+    int current = 0;
+    hipDevice_t device = 0;
+    if (hipGetDevice(&current) != hipSuccess)
+        return fail(SQN_ERR_DEVICE, "hipGetDevice failed");
+    if (hipStreamGetDevice(static_cast<hipStream_t>(stream), &device) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(SQN_ERR_INVALID_ARG, "stream (%p): its device is not known", stream);
+    }
+    if (device != current)
+        return fail(SQN_ERR_INVALID_ARG, "stream belongs to device %d, current device is %d", static_cast<int>(device),
+                    current);
+    return SQN_OK;
+}
 
 // The matrix's description, then that its memory is there.
 sqn_status check_matrix(const sqn_matrix* x, bool written, const char* what)
@@ -46,7 +96,7 @@ sqn_status check_matrix(const sqn_matrix* x, bool written, const char* what)
         return fail(SQN_ERR_INVALID_ARG, "%s spans more than 2^63 bytes", what);
     if (reinterpret_cast<uintptr_t>(x->data) % element_size(x->dtype))
         return fail(SQN_ERR_INVALID_ARG, "%s (%p) is not aligned to its elements", what, x->data);
-    return check_device_range(x->data, static_cast<size_t>(bytes), what);
+    return check_memory(x->data, static_cast<size_t>(bytes), what);
 }
 
 sqn_status check_ids(const void* ids, int32_t type, int64_t n)
@@ -58,7 +108,7 @@ sqn_status check_ids(const void* ids, int32_t type, int64_t n)
     const size_t size = type == SQN_I64 ? 8 : 4;
     if (reinterpret_cast<uintptr_t>(ids) % size)
         return fail(SQN_ERR_INVALID_ARG, "ids (%p) is not aligned to its elements", ids);
-    return check_device_range(ids, static_cast<size_t>(n) * size, "ids");
+    return check_memory(ids, static_cast<size_t>(n) * size, "ids");
 }
 
 sqn_status check_workspace(const void* workspace, size_t bytes, size_t need)
@@ -69,7 +119,7 @@ sqn_status check_workspace(const void* workspace, size_t bytes, size_t need)
         return fail(SQN_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", bytes, need);
     if (reinterpret_cast<uintptr_t>(workspace) % 256)
         return fail(SQN_ERR_INVALID_ARG, "workspace (%p) is not aligned to 256 bytes", workspace);
-    return check_device_range(workspace, need, "workspace");
+    return check_memory(workspace, need, "workspace");
 }
 
 // The batch's description and the elements it spans.
@@ -96,7 +146,7 @@ sqn_status check_batch(const sqn_batch* x, const char* what)
         return fail(SQN_ERR_INVALID_ARG, "%s spans more than 2^63 bytes", what);
     if (reinterpret_cast<uintptr_t>(x->data) % element_size(x->dtype))
         return fail(SQN_ERR_INVALID_ARG, "%s (%p) is not aligned to its elements", what, x->data);
-    return check_device_range(x->data, static_cast<size_t>(bytes), what);
+    return check_memory(x->data, static_cast<size_t>(bytes), what);
 }
 
 // No two elements of a written batch at one place: each axis, from the one
@@ -184,10 +234,10 @@ sqn_status check_quantised(const sqn_quantised* x, const char* what)
     if (reinterpret_cast<uintptr_t>(x->codes) % 16)
         return fail(SQN_ERR_INVALID_ARG, "%s: codes (%p) are not aligned to 16 bytes", what, x->codes);
     const size_t blocks = static_cast<size_t>(x->rows) * sqn::quant_blocks(x->cols);
-    sqn_status s = check_device_range(x->codes, 16 * blocks, what);
+    sqn_status s = check_memory(x->codes, 16 * blocks, what);
     if (s != SQN_OK)
         return s;
-    return check_device_range(x->scales, blocks, what);
+    return check_memory(x->scales, blocks, what);
 }
 
 // Everything of a product but its first factor, [points][cols].
@@ -215,7 +265,7 @@ sqn_status check_layer(int64_t points, int64_t cols, const sqn_quantised* w, con
     if (bias) {
         if (reinterpret_cast<uintptr_t>(bias) % 4)
             return fail(SQN_ERR_INVALID_ARG, "bias (%p) is not aligned to its elements", static_cast<const void*>(bias));
-        return check_device_range(bias, static_cast<size_t>(w->rows) * 4, "bias");
+        return check_memory(bias, static_cast<size_t>(w->rows) * 4, "bias");
     }
     return SQN_OK;
 }
@@ -237,8 +287,10 @@ extern "C" {
 sqn_status sqn_lookup(const sqn_matrix* table, const void* ids, int32_t ids_type, float scale, const sqn_matrix* out,
                       void* stream)
 {
-    sqn_status s = check_matrix(table, false, "table");
+    sqn_status s = check_stream(stream);
     if (s != SQN_OK)
+        return s;
+    if ((s = check_matrix(table, false, "table")) != SQN_OK)
         return s;
     if ((s = check_matrix(out, true, "out")) != SQN_OK)
         return s;
@@ -263,8 +315,10 @@ sqn_status sqn_lookup_gradient(const sqn_matrix* grad, const void* ids, int32_t 
                                int32_t accumulate, const sqn_matrix* table_grad, void* workspace, size_t workspace_bytes,
                                void* stream)
 {
-    sqn_status s = check_matrix(grad, false, "grad");
+    sqn_status s = check_stream(stream);
     if (s != SQN_OK)
+        return s;
+    if ((s = check_matrix(grad, false, "grad")) != SQN_OK)
         return s;
     if ((s = check_matrix(table_grad, true, "table_grad")) != SQN_OK)
         return s;
@@ -302,6 +356,8 @@ sqn_status sqn_orthogonalise(const sqn_batch* updates, int32_t steps, const floa
     sqn_status s = check_coefficients(coefficients, steps);
     if (s != SQN_OK)
         return s;
+    if ((s = check_stream(stream)) != SQN_OK)
+        return s;
     if ((s = check_batch(updates, "updates")) != SQN_OK)
         return s;
     if ((s = check_batch(out, "out")) != SQN_OK)
@@ -324,8 +380,10 @@ sqn_status sqn_orthogonalise(const sqn_batch* updates, int32_t steps, const floa
 
 sqn_status sqn_quantise(const sqn_matrix* x, const sqn_quantised* out, void* stream)
 {
-    sqn_status s = check_matrix(x, false, "x");
+    sqn_status s = check_stream(stream);
     if (s != SQN_OK)
+        return s;
+    if ((s = check_matrix(x, false, "x")) != SQN_OK)
         return s;
     if ((s = check_quantised(out, "out")) != SQN_OK)
         return s;
@@ -338,8 +396,10 @@ sqn_status sqn_quantise(const sqn_matrix* x, const sqn_quantised* out, void* str
 
 sqn_status sqn_quantised_values(const sqn_quantised* x, const sqn_matrix* out, void* stream)
 {
-    sqn_status s = check_quantised(x, "x");
+    sqn_status s = check_stream(stream);
     if (s != SQN_OK)
+        return s;
+    if ((s = check_quantised(x, "x")) != SQN_OK)
         return s;
     if ((s = check_matrix(out, true, "out")) != SQN_OK)
         return s;
@@ -360,8 +420,10 @@ size_t sqn_quantised_product_workspace(int64_t points, int64_t units, int64_t co
 sqn_status sqn_quantised_product(const sqn_quantised* x, const sqn_quantised* w, const float* bias, int32_t relu,
                                  const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream)
 {
-    sqn_status s = check_quantised(x, "x");
+    sqn_status s = check_stream(stream);
     if (s != SQN_OK)
+        return s;
+    if ((s = check_quantised(x, "x")) != SQN_OK)
         return s;
     if ((s = check_layer(x->rows, x->cols, w, bias, relu, out)) != SQN_OK)
         return s;
@@ -385,8 +447,10 @@ size_t sqn_quantised_layer_workspace(int64_t points, int64_t units, int64_t cols
 sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, const float* bias, int32_t relu,
                                const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream)
 {
-    sqn_status s = check_matrix(x, false, "x");
+    sqn_status s = check_stream(stream);
     if (s != SQN_OK)
+        return s;
+    if ((s = check_matrix(x, false, "x")) != SQN_OK)
         return s;
     if ((s = check_layer(x->rows, x->cols, w, bias, relu, out)) != SQN_OK)
         return s;

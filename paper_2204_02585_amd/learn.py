@@ -6,7 +6,9 @@ gradient, updates orthogonalised by Newton-Schulz products, and layers held in
 Like `binding`, argument marshalling only: every value is computed by the
 HIP library.  Calls run on torch's current stream unless `stream` is given,
 which then waits for the work queued on the current stream; scratch and
-outputs come from torch's allocator.
+outputs come from torch's allocator.  Tensors and `stream` must belong to
+torch's current device (`with torch.cuda.device(x.device):`); a call on
+another's is refused.
 """
 from __future__ import annotations
 
