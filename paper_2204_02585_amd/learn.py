@@ -16,6 +16,7 @@ import ctypes
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 from .binding import Matrix, _check, _current_stream, _order_after_current, lib
@@ -89,6 +90,19 @@ def _on(stream, *tensors) -> int:
     return stream.cuda_stream
 
 
+def _tangent(t: torch.Tensor) -> Optional[torch.Tensor]:
+    """The tangent of a dual tensor of forward-mode differentiation, None of others."""
+    if getattr(forward_ad, "_current_level", 0) < 0:        # none is open: spares a call the look
+        return None
+    return forward_ad.unpack_dual(t).tangent
+
+
+def _no_tangent(what: str, *tensors) -> None:
+    """A raw pointer would drop it without a word."""
+    if any(t is not None and _tangent(t) is not None for t in tensors):
+        raise RuntimeError(f"{what} has no forward-mode derivative")
+
+
 # ---------------------------------------------------------------- rows of a table
 
 def _ids(ids: torch.Tensor, beside: torch.Tensor) -> torch.Tensor:
@@ -120,6 +134,7 @@ class _Lookup(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, ids, scale):
         ctx.save_for_backward(ids)
+        ctx.save_for_forward(ids)
         ctx.rows, ctx.scale, ctx.dtype = table.shape[0], scale, table.dtype
         return _lookup(table.detach(), ids, scale, None, None)
 
@@ -129,14 +144,23 @@ class _Lookup(torch.autograd.Function):
         (ids,) = ctx.saved_tensors
         return lookup_gradient(grad, ids, ctx.rows, scale=ctx.scale, dtype=ctx.dtype), None, None
 
+    @staticmethod
+    def jvp(ctx, table, _ids, _scale):
+        (ids,) = ctx.saved_tensors
+        return lookup(table, ids, scale=ctx.scale)
+
 
 def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
            stream=None) -> torch.Tensor:
     """sqn_lookup: scale * table[ids], [*ids.shape, D]; an index outside the
     table (a padding mark) gives zeros.  Differentiable in a table that
-    requires a gradient (without `out` and `stream`), by lookup_gradient."""
-    if out is None and stream is None and table.requires_grad and torch.is_grad_enabled():
-        return _Lookup.apply(table, ids, float(scale))
+    requires a gradient (without `out` and `stream`), by lookup_gradient, and
+    in forward mode."""
+    if out is None and stream is None:
+        if (table.requires_grad and torch.is_grad_enabled()) or _tangent(table) is not None:
+            return _Lookup.apply(table, ids, float(scale))
+    else:
+        _no_tangent("lookup with out or stream", table)
     return _lookup(table, ids, float(scale), out, stream)
 
 
@@ -145,7 +169,15 @@ def lookup_gradient(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: flo
                     dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """sqn_lookup_gradient: the gradient [rows, D] of lookup's table, from grad
     [*ids.shape, D].  `dtype` (grad's own by default) is the result's;
-    `accumulate` adds to `out` instead of writing all of it."""
+    `accumulate` adds to `out` instead of writing all of it.  It is linear in
+    grad, and so are its forward-mode derivatives (without `out` and `stream`);
+    no gradient passes back through it."""
+    tangent = _tangent(grad)
+    if tangent is not None:
+        if out is not None or stream is not None:
+            _no_tangent("lookup_gradient with out or stream", grad)
+        both = (forward_ad.unpack_dual(grad).primal, tangent)
+        return forward_ad.make_dual(*(lookup_gradient(g, ids, rows, scale, dtype=dtype or grad.dtype) for g in both))
     _on_gpu(grad, "grad")
     if tuple(grad.shape[:-1]) != tuple(ids.shape) or grad.dim() == 0:
         raise ValueError(f"grad of shape {tuple(grad.shape)} does not go with ids of shape {tuple(ids.shape)}")
@@ -175,7 +207,9 @@ def orthogonalise(updates: torch.Tensor, steps: int = 5, coefficients=MUON, eps:
                   dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """sqn_orthogonalise: [m, n] or a batch [B, m, n] of updates, any strides,
     orthogonalised by `steps` Newton-Schulz products.  A bfloat16 result
-    takes one product per factor pair, a float16 or float32 one three."""
+    takes one product per factor pair, a float16 or float32 one three.  No
+    gradient passes through it."""
+    _no_tangent("orthogonalise", updates)
     _on_gpu(updates, "updates")
     if updates.dim() not in (2, 3):
         raise ValueError(f"updates must be [m, n] or [B, m, n], got shape {tuple(updates.shape)}")
@@ -238,7 +272,8 @@ class Quantised:
 
 
 def quantise(x: torch.Tensor, stream=None) -> Quantised:
-    """sqn_quantise: x [rows, cols] in 4-bit blocks along its rows."""
+    """sqn_quantise: x [rows, cols] in 4-bit blocks along its rows.  Codes and
+    scales are whole numbers: no gradient passes through them."""
     _on_gpu(x, "x")
     if x.dim() != 2 or x.shape[1] < 1:
         raise ValueError(f"x must be a matrix, got shape {tuple(x.shape)}")
@@ -262,6 +297,7 @@ def product(x, w: Quantised, bias: Optional[torch.Tensor] = None, relu: bool = F
     blocks = isinstance(x, Quantised)
     if not isinstance(w, Quantised):
         raise TypeError("w must be Quantised")
+    _no_tangent("product", None if blocks else x, bias)
     _on_gpu(x.codes if blocks else x, "x", w.codes)
     shape = x.shape
     if len(shape) < 1 or shape[-1] != w.cols:
