@@ -142,6 +142,8 @@ class _Lookup(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         (ids,) = ctx.saved_tensors
+        if ctx.rows == 0:             # every index was outside; the library's gradient has a row
+            return grad.new_zeros((0, grad.shape[-1]), dtype=ctx.dtype), None, None
         return lookup_gradient(grad, ids, ctx.rows, scale=ctx.scale, dtype=ctx.dtype), None, None
 
     @staticmethod

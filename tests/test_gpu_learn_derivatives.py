@@ -86,3 +86,13 @@ def test_lost_tangents_are_refused(learn):
         # tensors without a tangent are taken as outside of a level
         assert learn.product(x, w, bias=bias).shape == (6, 7)
         assert learn.orthogonalise(x).shape == (6, 40)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_backward_of_a_table_without_rows(learn, dtype):
+    """Its lookup gives zeros for every index, and its gradient has no rows either."""
+    table = torch.empty((0, 7), dtype=dtype, device="cuda", requires_grad=True)
+    rows = learn.lookup(table, IDS.cuda())
+    assert torch.equal(rows, torch.zeros((2, 3, 7), dtype=dtype, device="cuda"))
+    rows.sum().backward()
+    assert table.grad.shape == (0, 7) and table.grad.dtype == dtype
