@@ -399,6 +399,10 @@ constexpr uint32_t kMaxLow = 32 - kPositionBits, kMaxBuckets = 512;
 // 30,000 rows 38 and 51, 131,000 56 and 54; 100,000 into 2^23 53 and 66, into
 // 2^25, which would take 1024 buckets, 134 and 85.)
 constexpr uint32_t kBucketPass = 40960;
+// ... and for each bucket, half of what LDS holds: few rows have few buckets, a
+// workgroup each.  (20,000 into 5 rows 50 and 26, into 33 24 and 24; 40,000 into 5
+// rows 79 and 28, into 64 27 and 25; 4,000 into 5 rows 18 and 22.)
+constexpr uint32_t kBucketShare = 4096;
 static_assert(3 * kBucketPass <= 1u << kPositionBits, "up to 2^24 rows take three passes");
 // Half of a CU's LDS, for a second workgroup that clears: indices that a wave can
 // keep, and bits of a pass.
@@ -938,7 +942,7 @@ Plan plan_of(int64_t n, int64_t rows, int64_t cols)
     // 64 to 128 buckets, so that a CU has one, and others clear
     q.low = bits <= 10 ? 3 : bits - 7 < kMaxLow ? bits - 7 : kMaxLow;
     q.buckets = static_cast<uint32_t>((rows + (int64_t{1} << q.low) - 1) >> q.low);
-    if (n > int64_t{kBucketPass} * q.passes || q.buckets > kMaxBuckets)
+    if (n > int64_t{kBucketPass} * q.passes || n > int64_t{kBucketShare} * q.buckets || q.buckets > kMaxBuckets)
         q.buckets = 0;
     const int64_t steps = (n + kPlaceStep - 1) / kPlaceStep;
     q.stretch = static_cast<uint32_t>((steps + kMaxStretches - 1) / kMaxStretches * kPlaceStep);
