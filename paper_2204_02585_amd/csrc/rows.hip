@@ -384,24 +384,32 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortParams p)
 
 // ---- gradient: sorting in one launch
 //
-// A workgroup a bucket of 2^low rows: it reads all indices, keeps those of its
-// bucket in their order and counts those of the buckets before, which is where
-// its own go.  Those that it keeps fit LDS, as the row in the bucket and the
-// position in one word, and are sorted there by the row's bits; more than that
-// (many indices on few rows) go through global memory in steps.  A further
-// workgroup writes the marks of indices outside the table.  (Of 16,000 indices
-// into 30,000 rows the sort alone took 39 us in one workgroup.)
+// A workgroup a bucket of rows: it reads all indices, keeps those of its bucket in
+// their order and counts those of the buckets before, which is where its own go.
+// Those that it keeps fit LDS, as the row in the bucket and the position in one
+// word, and are sorted there by the row's bits.  Where they do not, a row that
+// most of them name goes first, already in order, and the rest is sorted; several
+// such rows in one bucket go through global memory in steps.  A further workgroup
+// writes the marks of indices outside the table.  (Of 16,000 indices into 30,000
+// rows the sort alone took 39 us in one workgroup.)
+//
+// Equal indices have to lie together, their rows need no order: a row's bucket
+// mixes all digits of its index, so that neither rows close together (a vocabulary
+// in the order of its words' frequency) nor rows at some stride (a column of
+// texels) are in one bucket.
 
 constexpr uint32_t kPositionBits = 17;
 constexpr uint32_t kMaxLow = 32 - kPositionBits, kMaxBuckets = 512;
 // Indices for each pass that the other sort takes.  (The call with one against
-// the other, us: 33,000 into 700 rows 29 and 31, 66,000 40 and 31; 66,000 into
-// 30,000 rows 38 and 51, 131,000 56 and 54; 100,000 into 2^23 53 and 66, into
-// 2^25, which would take 1024 buckets, 134 and 85.)
+// the other, us: 33,000 into 700 rows 21 and 25, 66,000 29 and 28; 66,000 into
+// 30,000 rows 34 and 50, 131,000 46 and 51; 100,000 into 2^23 57 and 75, into
+// 2^25, which would take 1024 buckets, 227 and 138.  With half of the indices on
+// one row, 20,000 into 30,000 rows 40 and 50, 80,000 89 and 69, 120,000 into 2^20
+// 129 and 108; with all of them 41 and 55, 105 and 86, 152 and 129.)
 constexpr uint32_t kBucketPass = 40960;
 // ... and for each bucket, half of what LDS holds: few rows have few buckets, a
-// workgroup each.  (20,000 into 5 rows 50 and 26, into 33 24 and 24; 40,000 into 5
-// rows 79 and 28, into 64 27 and 25; 4,000 into 5 rows 18 and 22.)
+// workgroup each.  (20,000 into 5 rows 57 and 26, into 33 21 and 24; 40,000 into 5
+// rows 90 and 28, into 64 27 and 25; 4,000 into 5 rows 18 and 21.)
 constexpr uint32_t kBucketShare = 4096;
 static_assert(3 * kBucketPass <= 1u << kPositionBits, "up to 2^24 rows take three passes");
 // Half of a CU's LDS, for a second workgroup that clears: indices that a wave can
@@ -415,34 +423,65 @@ struct BucketParams {
     const void* ids;
     Pair *out, *spare;
     uint32_t n, rows;
-    uint32_t low, buckets;
+    uint32_t high, low, buckets;       // digits of an index, low that of the row in its bucket; buckets = 2^high
     int passes;                        // over the bits of the row in the bucket
     Clear clear;
 };
 
-// emit(key, i) for the wave's indices in their order, by all lanes; the key
-// ~0 is none.
+// The bucket of an index inside the table; and back, with the row in the bucket,
+// which is the index without its lowest digit.
+__device__ __forceinline__ uint32_t bucket_of(const BucketParams& p, uint32_t key)
+{
+    return ((key ^ key >> p.high) + (key >> 2 * p.high)) & (p.buckets - 1);
+}
+
+__device__ __forceinline__ uint32_t key_of(const BucketParams& p, uint32_t bucket, uint32_t row)
+{
+    return row << p.high | (((bucket - (row >> p.high)) ^ row) & (p.buckets - 1));
+}
+
+// Set lanes of a mask below this one, and `base`.
+__device__ __forceinline__ uint32_t lanes_below(uint64_t mask, uint32_t base)
+{
+    return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
+                                     __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), base));
+}
+
+// emit(inside, key, i) for the wave's indices in their order, by all lanes;
+// `inside` is false of those outside the table and past the wave's last.  A
+// thread's instructions per index are what the scan takes (80,000 indices: six
+// more, 3 us), so whole batches look at no end.
 template <typename I, typename E>
 __device__ __forceinline__ void scan_ids(const BucketParams& p, E emit)
 {
     const uint32_t span = (p.n + 64 * kWaves - 1) / (64 * kWaves) * 64;
     const uint32_t lane = threadIdx.x & 63, first = (threadIdx.x >> 6) * span, last = min(p.n, first + span);
-    for (uint32_t i = first; i < last; i += 64 * kScanAhead) {
-        uint32_t key[kScanAhead];
+    const I* ids = static_cast<const I*>(p.ids);
+    auto batch = [&](uint32_t i, auto whole) {
+        constexpr bool all = decltype(whole)::value;
+        I id[kScanAhead];
 #pragma unroll
         for (int a = 0; a < kScanAhead; ++a)
-            key[a] = key_at<I>(p.ids, min(i + 64 * a + lane, p.n - 1), p.rows);
+            id[a] = all ? (ids + i + lane)[64 * a] : ids[min(i + 64 * a + lane, p.n - 1)];
 #pragma unroll
-        for (int a = 0; a < kScanAhead; ++a)
-            emit(i + 64 * a + lane < last ? key[a] : ~0u, i + 64 * a + lane);
-    }
+        for (int a = 0; a < kScanAhead; ++a) {
+            // rows < 2^31: a negative index is outside as an unsigned one of its own size
+            const bool inside = static_cast<std::make_unsigned_t<I>>(id[a]) < p.rows;
+            emit(inside && (all || i + 64 * a + lane < last), static_cast<uint32_t>(id[a]), i + 64 * a + lane);
+        }
+    };
+    uint32_t i = first;
+    for (; i + 64 * kScanAhead <= last; i += 64 * kScanAhead)
+        batch(i, std::true_type());
+    for (; i < last; i += 64 * kScanAhead)
+        batch(i, std::false_type());
 }
 
 __device__ __forceinline__ int shift_of(const BucketParams& p, int pass) { return p.low * pass / p.passes; }
 
 // The m kept words of `list`, in order, to out[start..].
 template <int KEYS>
-__device__ __forceinline__ void sort_list(const BucketParams& p, uint32_t first, uint32_t m, uint32_t start,
+__device__ __forceinline__ void sort_list(const BucketParams& p, uint32_t bucket, uint32_t m, uint32_t start,
                                           uint32_t (*seen)[kBucketBins], uint32_t* list, uint32_t* wave_sums)
 {
     const uint32_t tid = threadIdx.x, wave = tid >> 6;
@@ -489,7 +528,25 @@ __device__ __forceinline__ void sort_list(const BucketParams& p, uint32_t first,
 #pragma unroll
     for (int k = 0; k < KEYS; ++k)
         if (number_of<KEYS>(k) < m)
-            p.out[start + to[k]] = Pair{first + (v[k] >> kPositionBits), v[k] & ((1u << kPositionBits) - 1)};
+            p.out[start + to[k]] = Pair{key_of(p, bucket, v[k] >> kPositionBits), v[k] & ((1u << kPositionBits) - 1)};
+}
+
+// The row in the bucket that most of 64 kept words name, from all waves' parts of
+// `list`; the same in every wave.
+__device__ __forceinline__ uint32_t frequent_row(const uint32_t* list, const uint32_t* kept_by)
+{
+    static_assert(kWaves == 16, "four words of every wave's");
+    const uint32_t lane = threadIdx.x & 63, wave = lane & (kWaves - 1), kept = min(kept_by[wave], kSegment);
+    const uint32_t row = kept ? list[wave * kSegment + (lane / kWaves) * kept / 4] >> kPositionBits : ~0u;
+    uint32_t found = ~0u, most = 0;
+    for (int s = 0; s < 64; ++s) {
+        const uint32_t at = __shfl(row, s), count = static_cast<uint32_t>(__popcll(__ballot(row == at)));
+        if (at != ~0u && count > most) {
+            most = count;
+            found = at;
+        }
+    }
+    return found;
 }
 
 template <typename I>
@@ -504,18 +561,18 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(BucketParams p)
     __shared__ uint32_t wave_sums[kWaves], kept_by[kWaves], before_by[kWaves];
     static_assert(sizeof(list) <= sizeof(seen), "the list moves there and back");
     const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const uint64_t below = (uint64_t{1} << lane) - 1;
-    const bool marks = blockIdx.x == p.buckets;
-    const uint32_t first = marks ? p.rows : blockIdx.x << p.low, count = marks ? 0 : min(1u << p.low, p.rows - first);
+    const uint32_t bucket = blockIdx.x;
+    const bool marks = bucket == p.buckets;
 
     uint32_t kept = 0, before = 0;
-    scan_ids<I>(p, [&](uint32_t key, uint32_t i) {
-        const bool mine = key - first < count;
+    scan_ids<I>(p, [&](bool inside, uint32_t key, uint32_t i) {
+        const uint32_t of = bucket_of(p, key);
+        const bool mine = inside && of == bucket;       // none of the marks'
         const uint64_t all = __ballot(mine);
-        before += __popcll(__ballot(key < first));
-        const uint32_t at = kept + __popcll(all & below);
+        before += __popcll(__ballot(inside && of < bucket));
+        const uint32_t at = lanes_below(all, kept);
         if (mine && at < kSegment)
-            list[wave * kSegment + at] = (key - first) << kPositionBits | i;
+            list[wave * kSegment + at] = key >> p.high << kPositionBits | i;
         kept += __popcll(all);
     });
     if (lane == 0) {
@@ -539,6 +596,52 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(BucketParams p)
     }
     if (m == 0)
         return;
+    if (!fits) {
+        // without the row that most of them name
+        const uint32_t hot = frequent_row(list, kept_by);
+        uint32_t equal = 0, rest = 0;
+        __syncthreads();
+        scan_ids<I>(p, [&](bool inside, uint32_t key, uint32_t i) {
+            const bool mine = inside && bucket_of(p, key) == bucket;
+            equal += __popcll(__ballot(mine && key >> p.high == hot));
+            const bool other = mine && key >> p.high != hot;
+            const uint64_t all = __ballot(other);
+            const uint32_t at = lanes_below(all, rest);
+            if (other && at < kSegment)
+                list[wave * kSegment + at] = key >> p.high << kPositionBits | i;
+            rest += __popcll(all);
+        });
+        if (lane == 0) {
+            kept_by[wave] = rest;
+            before_by[wave] = equal;
+        }
+        __syncthreads();
+        uint32_t equals = 0, rests = 0, equal_at = start, rest_at = 0;
+        fits = true;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) {
+            equal_at += w < wave ? before_by[w] : 0;
+            rest_at += w < wave ? kept_by[w] : 0;
+            equals += before_by[w];
+            rests += kept_by[w];
+            fits = fits && kept_by[w] <= kSegment;
+        }
+        if (fits) {
+            scan_ids<I>(p, [&](bool inside, uint32_t key, uint32_t i) {
+                const bool mine = inside && bucket_of(p, key) == bucket && key >> p.high == hot;
+                const uint64_t all = __ballot(mine);
+                if (mine)
+                    p.out[lanes_below(all, equal_at)] = Pair{key, i};
+                equal_at += __popcll(all);
+            });
+            kept = rest;
+            offset = rest_at;
+            m = rests;
+            start += equals;
+            if (m == 0)
+                return;
+        }
+    }
     if (fits) {
         uint32_t* whole = &seen[0][0];
         for (uint32_t i = lane; i < kept; i += 64)
@@ -548,21 +651,21 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(BucketParams p)
             list[i] = whole[i];
         __syncthreads();
         if (m <= kSortThreads)
-            sort_list<1>(p, first, m, start, seen, list, wave_sums);
+            sort_list<1>(p, bucket, m, start, seen, list, wave_sums);
         else if (m <= 4 * kSortThreads)
-            sort_list<4>(p, first, m, start, seen, list, wave_sums);
+            sort_list<4>(p, bucket, m, start, seen, list, wave_sums);
         else
-            sort_list<8>(p, first, m, start, seen, list, wave_sums);
+            sort_list<8>(p, bucket, m, start, seen, list, wave_sums);
         return;
     }
 
     // more than LDS holds: to global memory in order, then pass by pass
     Pair *from = (p.passes & 1 ? p.spare : p.out) + start, *to = (p.passes & 1 ? p.out : p.spare) + start;
-    scan_ids<I>(p, [&](uint32_t key, uint32_t i) {
-        const bool mine = key - first < count;
+    scan_ids<I>(p, [&](bool inside, uint32_t key, uint32_t i) {
+        const bool mine = inside && bucket_of(p, key) == bucket;
         const uint64_t all = __ballot(mine);
         if (mine)
-            from[offset + __popcll(all & below)] = Pair{key, i};
+            from[lanes_below(all, offset)] = Pair{key, i};
         offset += __popcll(all);
     });
     for (int pass = 0; pass < p.passes; ++pass) {
@@ -572,16 +675,16 @@ __global__ __launch_bounds__(kSortThreads) void bucket_kernel(BucketParams p)
             list[tid] = 0;
         __syncthreads();
         for (uint32_t i = tid; i < m; i += kSortThreads)
-            atomicAdd(&list[(from[i].key - first) >> shift & (bins - 1)], 1u);
+            atomicAdd(&list[from[i].key >> p.high >> shift & (bins - 1)], 1u);
         __syncthreads();
         uint32_t base = exclusive_sum(tid < bins ? list[tid] : 0, wave_sums);
         for (uint32_t step = 0; step < m; step += kPlaceStep) {
             Pair pair[kPlaceKeys];
             uint32_t rank[kPlaceKeys];
-            auto digit = [&](int k) { return (pair[k].key - first) >> shift & (bins - 1); };
+            auto digit = [&](int k) { return pair[k].key >> p.high >> shift & (bins - 1); };
 #pragma unroll
             for (int k = 0; k < kPlaceKeys; ++k)
-                pair[k] = number_of<kPlaceKeys>(k) < m - step ? from[step + number_of<kPlaceKeys>(k)] : Pair{first, 0};
+                pair[k] = number_of<kPlaceKeys>(k) < m - step ? from[step + number_of<kPlaceKeys>(k)] : Pair{0, 0};
             if (tid < bins) {
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w)
@@ -925,7 +1028,7 @@ constexpr int64_t kShortLanes = 1 << 17;
 
 struct Plan {
     uint32_t passes, bits, stretch, stretches, tile, tiles;
-    uint32_t low, buckets;              // 0 where the sort goes by digits
+    uint32_t high, low, buckets;        // buckets is 0 where the sort goes by digits
     size_t pairs[2], counts, head, tail, bytes;
 };
 
@@ -939,9 +1042,13 @@ Plan plan_of(int64_t n, int64_t rows, int64_t cols)
         ++bits;                          // the largest key is `rows`
     q.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     q.bits = bits < 2 ? 2 : bits;        // counts are read by fours
-    // 64 to 128 buckets, so that a CU has one, and others clear
-    q.low = bits <= 10 ? 3 : bits - 7 < kMaxLow ? bits - 7 : kMaxLow;
-    q.buckets = static_cast<uint32_t>((rows + (int64_t{1} << q.low) - 1) >> q.low);
+    // of indices inside the table; 128 buckets, so that a CU has one, and others clear
+    uint32_t inside = 1;
+    while (((rows - 1) >> inside) > 0)
+        ++inside;
+    q.low = inside <= 10 ? 3 : inside - 7 < kMaxLow ? inside - 7 : kMaxLow;
+    q.high = inside > q.low ? inside - q.low : 0;
+    q.buckets = 1u << q.high;
     if (n > int64_t{kBucketPass} * q.passes || n > int64_t{kBucketShare} * q.buckets || q.buckets > kMaxBuckets)
         q.buckets = 0;
     const int64_t steps = (n + kPlaceStep - 1) / kPlaceStep;
@@ -1139,7 +1246,8 @@ hipError_t launch_lookup_gradient(const sqn_matrix& grad, const void* ids, bool 
     };
     if (q.buckets) {
         const dim3 all = grid();
-        const BucketParams b{ids, pairs[0], pairs[1], s.n, s.rows, q.low, q.buckets, (static_cast<int>(q.low) + kBucketBits - 1) / kBucketBits, c};
+        const BucketParams b{ids, pairs[0], pairs[1], s.n, s.rows, q.high, q.low, q.buckets,
+                             (static_cast<int>(q.low) + kBucketBits - 1) / kBucketBits, c};
         if (ids64)
             bucket_kernel<int64_t><<<all, kSortThreads, 0, stream>>>(b);
         else
