@@ -1011,13 +1011,24 @@ hipError_t launch_small(const OrthParams& p, int32_t batch, int32_t steps, bool 
     return hipGetLastError();
 }
 
-// Side of the tiles of a batch of matrices.
+int32_t up_to(int32_t v, int32_t side) { return (v + side - 1) / side * side; }
+
+// Side of the tiles of a batch of matrices: the largest whose tiles fill the chip
+// and whose rows and columns past the matrix add at most half to the products
+// that tiles of 64 take, and to their scratch.  (Larger tiles and those of 64, us
+// to bfloat16: 64 of 390 x 390 534 and 736, products 1.49 times as large; 24 of 520
+// x 520 470 and 500, 1.37; 16 of 257 x 900 244 and 213, 1.54; 24 of 130 x 1300 293
+// and 199, 1.86; 1000 of 16 x 4096 14,560 and 4,629, with 8.7 and 2.1 GB.)
 int32_t tile_side(int32_t batch, int32_t m, int32_t n, bool split_all)
 {
-    auto tiles = [&](int64_t side) { return batch * ((m + side - 1) / side) * ((n + side - 1) / side); };
-    if (!split_all && tiles(256) >= 200)
+    auto taken = [&](int32_t side) {
+        const int64_t mp = up_to(m, side), np = up_to(n, side);
+        return batch * (mp / side) * (np / side) >= 200
+               && 2 * mp * mp * np <= 3 * int64_t{up_to(m, 64)} * up_to(m, 64) * up_to(n, 64);
+    };
+    if (!split_all && taken(256))
         return 256;
-    return tiles(128) >= 200 ? 128 : 64;
+    return taken(128) ? 128 : 64;
 }
 
 // Narrow tiles take the symmetric products where tiles of 64 would and each CU
@@ -1025,8 +1036,6 @@ int32_t tile_side(int32_t batch, int32_t m, int32_t n, bool split_all)
 // to binary32, 253 narrow tiles, 147 and 178, to bfloat16 108 and 120; 300 x 400
 // to binary32, 55 of them, 104 and 124; 900 x 900, 465 of them, 227 and 202.)
 constexpr int64_t kCus = 256;
-
-int32_t up_to(int32_t v, int32_t side) { return (v + side - 1) / side * side; }
 
 size_t layout(int32_t batch, int32_t rows, int32_t cols, bool split_all, char* base, Scratch* s)
 {
