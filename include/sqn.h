@@ -438,7 +438,9 @@ typedef struct {
  * s -> a s + b s^3 + c s^5 each step, near 1 in the end.  Sums are binary32.
  * For a bfloat16 output the products take binary16 factors, the diagonals
  * of A and b A + c A A kept apart in binary32 and X in 22 bits or more; for
- * binary16 and binary32 outputs every factor has 22 bits and X 24.
+ * binary16 and binary32 outputs every factor has 22 bits and X 24.  (The
+ * error in the 2-norm, of Gaussian updates, sides 128 to 4096: a bfloat16 result
+ * 1.7e-3 to 1.9e-3, of which 1.66e-3 is its own rounding; a binary32 one 4e-7.)
  *   coefficients: host, finite; refused where the steps could take a singular
  *                 value past 2 or b s^2 + c s^4 past 16 in magnitude, the
  *                 range the binary16 factors are scaled for;

@@ -17,7 +17,7 @@
 // and B = b A + c A A are near 1 and -2.7 while the rest is near 0: they are
 // kept in binary32 and applied in the epilogues, (A A)_ij = (O O)_ij +
 // (d_i + d_j) O_ij + [i = j] d_i^2 with O = A - diag(d) (the error of a
-// 256 x 256 update falls from 1.4e-3 to 6e-4 of its norm).  And updates of low
+// 256 x 256 update falls from 1.7e-3 to 7.5e-4 of its norm).  And updates of low
 // rank have singular values that one rounding of X would bury: X is kept as
 // hi + lo, two binary16, and a X takes both.  What is left is less than the
 // rounding of a bfloat16 result (1.7e-3).  For binary16 and binary32 results

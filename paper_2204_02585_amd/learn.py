@@ -209,8 +209,12 @@ def orthogonalise(updates: torch.Tensor, steps: int = 5, coefficients=MUON, eps:
                   dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """sqn_orthogonalise: [m, n] or a batch [B, m, n] of updates, any strides,
     orthogonalised by `steps` Newton-Schulz products.  A bfloat16 result
-    takes one product per factor pair, a float16 or float32 one three.  No
-    gradient passes through it."""
+    takes one product per factor pair, a float16 or float32 one three.  The
+    first is off by 1.1 times its rounding (Gaussian updates: 1.83e-3 of the
+    norm, 1.66e-3 the rounding alone); `dtype=torch.float32` and then
+    `.to(torch.bfloat16)` has the rounding alone, in 1.4 to 3.1 times the
+    time.  The same coefficients apply to every step.  No gradient passes
+    through it."""
     _no_tangent("orthogonalise", updates)
     _on_gpu(updates, "updates")
     if updates.dim() not in (2, 3):
