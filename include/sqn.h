@@ -404,7 +404,8 @@ sqn_status sqn_lookup(const sqn_matrix* table, const void* ids, int32_t ids_type
                       const sqn_matrix* out, void* stream);
 
 /* The gradient of sqn_lookup's table: with g[v] the sum of grad[t] over the t
- * with ids[t] = v in binary32 (in an order that the indices alone fix),
+ * with ids[t] = v in binary32 (in an order that the indices, the shapes and
+ * the types fix),
  *   table_grad[v] = scale * g[v]                       (accumulate = 0), or
  *   table_grad[v] = table_grad[v] + scale * g[v]       (accumulate = 1; rows
  *                   without an index are neither read nor written),

@@ -55,3 +55,21 @@ print(json.dumps(out))
 """, [(1, 4096, 4096, 2), (1, 4096, 4096, 0), (64, 390, 390, 2), (24, 520, 520, 2), (64, 200, 300, 0), (24, 130, 1300, 2), (1000, 16, 4096, 2)])
     for name, side in zip(got, (256, 128, 256, 128, 128, 64, 64)):
         assert f"ILi{side}E" in name, (name, side)
+
+
+def test_many_points_by_several_tiles_of_units():
+    """The ends of the range of products, each within it: as many tiles of 64 x 64 as
+    a product may have, and one more."""
+    cases = [(1 << 26, 500, 100), (1 << 26, 512, 33), ((1 << 23) // 5 * 64, 300, 100), (1 << 29, 64, 40), (32768, 1 << 20, 40), (17, 1 << 20, 1),
+             (185_000, 185_000, 64)]
+    got = fake_hip.run(SETUP + """
+out = []
+fake.fake_reset()
+for points, units, cols in DATA:
+    out.append([layer(points, units, cols), len(launches()), product(points, units, cols), len(launches())])
+print(json.dumps([out, layer((1 << 26) + 1, 512, 100), product((1 << 26) + 1, 512, 100), len(launches())]))
+""", cases)
+    assert all(-(-p // 64) * -(-u // 64) <= 1 << 23 for p, u, _ in cases)
+    for case, (status, launched, status_blocks, launched_blocks) in zip(cases, got[0]):
+        assert status == status_blocks == 0 and launched > 0 and launched_blocks > 0, case
+    assert got[1] == got[2] == 4 and got[3] == 0
