@@ -664,6 +664,10 @@ hipError_t launch_layer(const sqn_matrix& x, const sqn_quantised& w, const float
     return hipGetLastError();
 }
 
+// All 256 units are multiplied, fewer as copies of the last.  (A call so and in
+// tiles, us: 65,536 points of 256 elements by 256 units 23.7 and 23.6, by 128 22.6
+// and 23.5, by 3 19.5 and 23.8; 1000 points 10 and 15; 2^20 points of 256 by 256 300
+// and 330, of 32 by 3 286 and 260.)
 bool is_layer(int64_t units, int64_t cols) { return units <= kLayerUnits && cols >= 8 && quant_blocks(cols) <= 16; }
 
 // ---- products of few points
