@@ -501,6 +501,81 @@ sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, cons
                                const sqn_matrix* out, void* workspace, size_t workspace_bytes, void* stream);
 size_t sqn_quantised_layer_workspace(int64_t points, int64_t units, int64_t cols);
 
+/* A mask of dropout, made from a counter and never stored.  Element (row, col)
+ * of a matrix of `cols` columns takes 32 bits of
+ *   word(row, col / 2) = mix(mix(seed + *step) + (row ceil(cols / 2) + col / 2 + 1) G),
+ * the low half for an even col, with mix and G = 0x9E3779B97F4A7C15 those of
+ * SplitMix64, all modulo 2^64: it is dropped (0, whatever it was) where they
+ * are below round(p 2^32), else multiplied by 1 / (1 - p) in binary32.  The
+ * same p, seed, step and columns give the same mask in every call here. */
+typedef struct {
+    double p;                 /* in [0, 1]; 0 keeps everything as it is, 1 drops it */
+    uint64_t seed;
+    const void* step;         /* device, one uint64 (8-byte aligned) read by the   */
+                              /* call's kernels and added to the seed, so that a   */
+                              /* captured graph need not repeat its mask; or NULL  */
+} sqn_dropout_mask;
+
+/* Dropout: out = D(x), or D(x) + residual, in binary32 and rounded once; with
+ * the same mask and no residual it is its own gradient.
+ *   residual: x's rows, cols and dtype, or NULL;
+ *   out:      x's rows, cols and dtype; may be x's or the residual's own memory
+ *             if the layout is the same.
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
+sqn_status sqn_dropout(const sqn_matrix* x, const sqn_dropout_mask* mask, const sqn_matrix* residual, const sqn_matrix* out,
+                       void* stream);
+
+/* max(0, z) (a NaN stays); z Phi(z), Phi the normal distribution's share below z;
+ * z / (1 + exp(-z)). */
+typedef enum { SQN_ACT_NONE = 0, SQN_ACT_RELU = 1, SQN_ACT_GELU = 2, SQN_ACT_SILU = 3 } sqn_activation;
+
+/* What a layer does with its sums, every part optional (zeros: none). */
+typedef struct {
+    const void* bias;                   /* device, [units] of bias_dtype, or NULL       */
+    int32_t bias_dtype;                 /* SQN_F32 or x's                               */
+    int32_t activation;                 /* sqn_activation                               */
+    const sqn_dropout_mask* dropout;    /* host, or NULL                                */
+    const sqn_matrix* residual;         /* [points][units] of out's dtype, or NULL      */
+    const sqn_matrix* pre;              /* out: z, [points][units] of x's dtype, as     */
+                                        /* sqn_layer_gradient takes it, or NULL         */
+} sqn_epilogue;
+
+/* A layer: z = x w^T + bias, out = D(act(z)) + residual, [points][units], with
+ * x [points][cols] and w [units][cols] of one dtype.  Products and sums in
+ * binary32, z included; rounded once to out's dtype (x's or SQN_F32).
+ * points >= 0, units >= 1.
+ *   epilogue:  or NULL for none of it;
+ *   out:       may be the residual's own memory if the layout is the same;
+ *   workspace: sqn_layer_workspace(x, w) bytes, for these sizes, strides and
+ *              alignments (copies of factors that do not lie on 16-byte
+ *              boundaries, sums in parts).
+ * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_UNSUPPORTED (more than 2^23 tiles of
+ * 64 x 64 in out), SQN_ERR_DEVICE. */
+sqn_status sqn_layer(const sqn_matrix* x, const sqn_matrix* w, const sqn_epilogue* epilogue, const sqn_matrix* out,
+                     void* workspace, size_t workspace_bytes, void* stream);
+size_t sqn_layer_workspace(const sqn_matrix* x, const sqn_matrix* w);
+
+/* The gradients of sqn_layer from grad, that of its output:
+ *   dz = D(grad) act'(z),  grad_x = dz w,  grad_w = dz^T x,  grad_bias = sum of dz's rows
+ * (the residual's is grad itself).  Sums are binary32, in an order that the
+ * arguments fix; act'(0) of max(0, z) is 0.  For products of binary16 and
+ * bfloat16 factors dz is rounded to x's dtype, before its share 1 / (1 - p);
+ * grad_bias sums it unrounded.
+ *   grad:      [points][units] of x's dtype or SQN_F32;
+ *   pre:       [points][units] of x's dtype, the z that sqn_layer wrote; NULL
+ *              and only then for SQN_ACT_NONE;
+ *   mask:      the layer's, or NULL;
+ *   grad_x:    [points][cols] of x's dtype, or NULL;
+ *   grad_w:    [units][cols] of w's dtype, or NULL;
+ *   grad_bias: device, [units] of bias_dtype (SQN_F32 or x's), or NULL;
+ *   workspace: sqn_layer_gradient_workspace bytes for the same arguments.
+ * Errors: those of sqn_layer (tiles of grad_x and grad_w). */
+sqn_status sqn_layer_gradient(const sqn_matrix* grad, const sqn_matrix* x, const sqn_matrix* w, const sqn_matrix* pre,
+                              int32_t activation, const sqn_dropout_mask* mask, const sqn_matrix* grad_x, const sqn_matrix* grad_w,
+                              void* grad_bias, int32_t bias_dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t sqn_layer_gradient_workspace(const sqn_matrix* grad, const sqn_matrix* x, const sqn_matrix* w, int32_t activation,
+                                    const sqn_dropout_mask* mask, int32_t for_x, int32_t for_w, int32_t for_bias);
+
 /* Ray space of later renders with this handle.  ndc_near = 0 (the default):
  * world rays as above.  ndc_near > 0: forward-facing captures (the LLFF
  * scenes the paper evaluates, Sec. 4), marched as in NeRF in the normalized

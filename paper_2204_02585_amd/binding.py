@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_PKG, "libsqn.so")
 SQN_OK, SQN_ERR_INVALID_ARG, SQN_ERR_OUT_OF_MEMORY, SQN_ERR_DEVICE, SQN_ERR_UNSUPPORTED = range(5)
 SQN_F32, SQN_F16, SQN_BF16 = 0, 1, 2
 SQN_I32, SQN_I64 = 0, 1
+SQN_ACT_NONE, SQN_ACT_RELU, SQN_ACT_GELU, SQN_ACT_SILU = range(4)
 
 EXPORTS = ("sqn_create_caches", "sqn_create_linear_caches", "sqn_recreate_caches", "sqn_render", "sqn_render_stats",
            "sqn_set_lanes_per_ray", "sqn_tune_lanes_per_ray", "sqn_set_centre_block",
@@ -26,7 +27,8 @@ EXPORTS = ("sqn_create_caches", "sqn_create_linear_caches", "sqn_recreate_caches
            "sqn_generate_caches", "sqn_networks_device_bytes", "sqn_destroy_networks",
            "sqn_lookup", "sqn_lookup_gradient", "sqn_lookup_gradient_workspace", "sqn_orthogonalise",
            "sqn_orthogonalise_workspace", "sqn_quantise", "sqn_quantised_values", "sqn_quantised_product", "sqn_quantised_product_workspace",
-           "sqn_quantised_layer", "sqn_quantised_layer_workspace")
+           "sqn_quantised_layer", "sqn_quantised_layer_workspace", "sqn_dropout", "sqn_layer", "sqn_layer_workspace", "sqn_layer_gradient",
+           "sqn_layer_gradient_workspace")
 
 
 class CacheDesc(ctypes.Structure):
@@ -72,6 +74,16 @@ class Batch(ctypes.Structure):
 class QuantisedMatrix(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
                 ("cols", ctypes.c_int64)]
+
+
+class DropoutMask(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class Epilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("dropout", ctypes.POINTER(DropoutMask)), ("residual", ctypes.POINTER(Matrix)),
+                ("pre", ctypes.POINTER(Matrix))]
 
 
 class SqnError(RuntimeError):
@@ -129,6 +141,7 @@ def _load() -> ctypes.CDLL:
     lib.sqn_destroy.argtypes = [vp]
     i64, size = ctypes.c_int64, ctypes.c_size_t
     mat, quant, batch = ctypes.POINTER(Matrix), ctypes.POINTER(QuantisedMatrix), ctypes.POINTER(Batch)
+    mask, epilogue = ctypes.POINTER(DropoutMask), ctypes.POINTER(Epilogue)
     for name, result, args in (
             ("sqn_lookup", ctypes.c_int, [mat, vp, i32, f32, mat, vp]),
             ("sqn_lookup_gradient", ctypes.c_int, [mat, vp, i32, f32, i32, mat, vp, size, vp]),
@@ -140,7 +153,12 @@ def _load() -> ctypes.CDLL:
             ("sqn_quantised_product", ctypes.c_int, [quant, quant, vp, i32, mat, vp, size, vp]),
             ("sqn_quantised_product_workspace", size, [i64, i64, i64]),
             ("sqn_quantised_layer", ctypes.c_int, [mat, quant, vp, i32, mat, vp, size, vp]),
-            ("sqn_quantised_layer_workspace", size, [i64, i64, i64])):
+            ("sqn_quantised_layer_workspace", size, [i64, i64, i64]),
+            ("sqn_dropout", ctypes.c_int, [mat, mask, mat, mat, vp]),
+            ("sqn_layer", ctypes.c_int, [mat, mat, epilogue, mat, vp, size, vp]),
+            ("sqn_layer_workspace", size, [mat, mat]),
+            ("sqn_layer_gradient", ctypes.c_int, [mat, mat, mat, mat, i32, mask, mat, mat, vp, i32, vp, size, vp]),
+            ("sqn_layer_gradient_workspace", size, [mat, mat, mat, i32, mask, i32, i32, i32])):
         call = getattr(lib, name)
         call.restype, call.argtypes = result, args
     lib.sqn_status_string.restype = ctypes.c_char_p

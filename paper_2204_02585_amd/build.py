@@ -11,7 +11,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_PATH = os.path.join(PKG, "libsqn.so")
 SOURCES = [os.path.join(CSRC, "api.hip"), os.path.join(CSRC, "render.hip"),
            os.path.join(CSRC, "prepare.hip"), os.path.join(CSRC, "generate.hip"),
-           os.path.join(CSRC, "rows.hip"), os.path.join(CSRC, "orthogonal.hip"), os.path.join(CSRC, "quantise.hip")]
+           os.path.join(CSRC, "rows.hip"), os.path.join(CSRC, "orthogonal.hip"), os.path.join(CSRC, "quantise.hip"),
+           os.path.join(CSRC, "layer.hip"), os.path.join(CSRC, "dropout.hip")]
 # parts of libsqn.so without device code
 HOST_SOURCES = [os.path.join(CSRC, "learn_api.hip")]
 # memory-level ceilings for the benchmark's roofline (not part of the render ABI)

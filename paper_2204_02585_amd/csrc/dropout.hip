@@ -1,0 +1,118 @@
+// Dropout with a mask that is made in place: out = D(x) [+ residual].
+//
+// Bound by its bytes: an element is read and written once, and 20 integer
+// operations make its share of a word.
+#include <algorithm>
+
+#include "learn.h"
+#include "mask.h"
+#include "numeric.h"
+
+namespace sqn {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint32_t kMaxGroups = 1u << 23;     // of a launch; a thread takes more runs past them
+
+struct DropoutParams {
+    const void *x, *residual;
+    void* out;
+    int64_t x_stride, residual_stride, out_stride;    // elements
+    uint64_t runs;                                    // rows * per_row
+    uint32_t per_row, cols;                           // runs in a row
+    Mask mask;
+};
+
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutParams p)
+{
+    const uint64_t key = p.mask.on ? mask_key(p.mask) : 0;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.runs;
+         i += static_cast<uint64_t>(gridDim.x) * kThreads) {
+        // the 64-bit division is left to matrices of 2^32 runs or more
+        const uint32_t row = p.runs >> 32 ? static_cast<uint32_t>(i / p.per_row) : static_cast<uint32_t>(i) / p.per_row;
+        const uint32_t col = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * p.per_row) * V;
+        const T* x = static_cast<const T*>(p.x) + row * p.x_stride + col;
+        const T* residual = static_cast<const T*>(p.residual) + row * p.residual_stride + col;
+        T* out = static_cast<T*>(p.out) + row * p.out_stride + col;
+        float v[V], r[V];
+        const bool whole = col + V <= p.cols;
+        if (whole) {
+            load_run<T, V>(x, v);
+            if (p.residual)
+                load_run<T, V>(residual, r);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                v[k] = col + k < p.cols ? to_f32(x[k]) : 0.0f;
+                r[k] = p.residual && col + k < p.cols ? to_f32(residual[k]) : 0.0f;
+            }
+        }
+        if (p.mask.on)
+            apply_mask<V>(p.mask, key, row, col, p.mask.scale, v);
+        if (p.residual)
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                v[k] += r[k];
+        if (whole) {
+            store_run<T, V>(out, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (col + k < p.cols)
+                    out[k] = from_f32<T>(v[k]);
+        }
+    }
+}
+
+template <typename T>
+void launch_type(DropoutParams& p, int64_t rows, hipStream_t stream)
+{
+    constexpr int V = 16 / sizeof(T);
+    p.per_row = (p.cols + V - 1) / V;
+    p.runs = static_cast<uint64_t>(rows) * p.per_row;
+    const uint64_t groups = std::min((p.runs + kThreads - 1) / kThreads, static_cast<uint64_t>(kMaxGroups));
+    dropout_kernel<T, V><<<static_cast<uint32_t>(groups), kThreads, 0, stream>>>(p);
+}
+
+}  // namespace
+
+Mask mask_of(const sqn_dropout_mask* mask, int64_t cols)
+{
+    Mask m{};
+    m.pairs = static_cast<uint64_t>(cols + 1) / 2;
+    m.scale = 1.0f;
+    if (!mask || mask->p == 0.0)
+        return m;
+    const uint64_t bound = static_cast<uint64_t>(mask->p * 4294967296.0 + 0.5);
+    m.on = 1;
+    m.seed = mask->seed;
+    m.step = static_cast<const uint64_t*>(mask->step);
+    m.all = bound >> 32 ? 1 : 0;
+    m.bound = static_cast<uint32_t>(bound);
+    m.scale = m.all ? 0.0f : static_cast<float>(1.0 / (1.0 - mask->p));
+    return m;
+}
+
+hipError_t launch_dropout(const sqn_matrix& x, const sqn_dropout_mask& mask, const sqn_matrix* residual,
+                          const sqn_matrix& out, hipStream_t stream)
+{
+    DropoutParams p{};
+    p.x = x.data;
+    p.x_stride = x.row_stride;
+    p.residual = residual ? residual->data : nullptr;
+    p.residual_stride = residual ? residual->row_stride : 0;
+    p.out = out.data;
+    p.out_stride = out.row_stride;
+    p.cols = static_cast<uint32_t>(x.cols);
+    p.mask = mask_of(&mask, x.cols);
+    if (x.dtype == SQN_F32)
+        launch_type<float>(p, x.rows, stream);
+    else if (x.dtype == SQN_F16)
+        launch_type<_Float16>(p, x.rows, stream);
+    else
+        launch_type<__bf16>(p, x.rows, stream);
+    return hipGetLastError();
+}
+
+}  // namespace sqn

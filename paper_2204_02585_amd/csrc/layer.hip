@@ -1,0 +1,886 @@
+// A layer while it is trained and asked, and its gradient:
+//
+//   z = x w^T + b,  y = D(act(z)) + residual
+//   dz = D(dy) act'(z),  dx = dz w,  dw = dz^T x,  db = sum of dz's rows
+//
+// All three products are C = P Q^T, stored with the rows of P along the memory of
+// C's rows: P = w, Q = x;  P = w^T, Q = dz;  P = x^T, Q = dz^T.  A factor whose
+// rows are contiguous along the sum ("along") or across it ("across") is read as
+// it lies in memory: the tiles of tile.h, whose steps bring 128 bytes of the sum
+// of every row, or as many elements of the sum across, and the LDS reads that
+// turn 16-bit elements on their way to the registers.  Nothing is transposed in
+// memory.
+#include <math.h>
+#include <algorithm>
+#include <type_traits>
+
+#include "learn.h"
+#include "mask.h"
+#include "numeric.h"
+#include "sqn_internal.h"
+#include "tile.h"
+
+namespace sqn {
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v lds_short4;
+
+constexpr int kThreads = 256;
+
+// what steps past a sum's end bring
+__device__ const uint4 zeros = {0, 0, 0, 0};
+
+// ---- what a product's sums go through on their way out
+
+struct Finish {
+    const void* bias;            // [units] or null
+    const void* residual;        // of the output's type, or null
+    void* pre;                   // z of the factors' type, or null
+    void* out;
+    int64_t residual_stride, pre_stride, out_stride;      // elements
+    uint32_t bias_f32, act, units;
+    float scale;                 // of a gradient's product
+    Mask mask;
+};
+
+__device__ __forceinline__ float activate(float z, uint32_t act)
+{
+    if (act == SQN_ACT_RELU)
+        return z < 0.0f ? 0.0f : z;
+    // erfc, not 1 + erf: below zero the sum would cancel
+    if (act == SQN_ACT_GELU)
+        return 0.5f * z * erfcf(z * -0.70710678f);
+    if (act == SQN_ACT_SILU)
+        return z / (1.0f + expf(-z));
+    return z;
+}
+
+__device__ __forceinline__ float slope(float z, uint32_t act)
+{
+    if (act == SQN_ACT_RELU)
+        return z <= 0.0f ? 0.0f : 1.0f;
+    if (act == SQN_ACT_GELU)
+        return 0.5f * erfcf(z * -0.70710678f) + z * expf(-0.5f * z * z) * 0.39894228f;
+    const float s = 1.0f / (1.0f + expf(-z));
+    return s * (1.0f + z * (1.0f - s));
+}
+
+// A run of V elements of which `left` are inside the row.
+template <typename T, int V>
+__device__ __forceinline__ void load_inside(const T* p, uint32_t left, float (&v)[V])
+{
+    if (left >= V) {
+        load_run<T, V>(p, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] = k < static_cast<int>(left) ? to_f32(p[k]) : 0.0f;
+    }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_values(T* p, uint32_t left, const float (&v)[V])
+{
+    if (left >= V) {
+        store_run<T, V>(p, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (k < static_cast<int>(left))
+                p[k] = from_f32<T>(v[k]);
+    }
+}
+
+// Elements unit..unit + V of row `row` of an output of type T, from factors of
+// type X; all of a layer's epilogue, or a gradient's scale.
+template <typename X, typename T, bool LAYER, int V>
+__device__ __forceinline__ void finish(const Finish& f, uint64_t key, uint64_t row, uint32_t unit, float (&v)[V])
+{
+    const uint32_t left = f.units - unit;
+    if constexpr (LAYER) {
+        float r[V];
+        if (f.bias) {
+            if (f.bias_f32)
+                load_inside<float, V>(static_cast<const float*>(f.bias) + unit, left, r);
+            else
+                load_inside<X, V>(static_cast<const X*>(f.bias) + unit, left, r);
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                v[k] += r[k];
+        }
+        if (f.pre)
+            store_values<X, V>(static_cast<X*>(f.pre) + row * f.pre_stride + unit, left, v);
+        if (f.act)
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                v[k] = activate(v[k], f.act);
+        if (f.mask.on)
+            apply_mask<V>(f.mask, key, row, unit, f.mask.scale, v);
+        if (f.residual) {
+            load_inside<T, V>(static_cast<const T*>(f.residual) + row * f.residual_stride + unit, left, r);
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                v[k] += r[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] *= f.scale;
+    }
+    store_values<T, V>(static_cast<T*>(f.out) + row * f.out_stride + unit, left, v);
+}
+
+// ---- factors
+
+struct Operand {
+    const char* data;            // 16-byte aligned
+    uint64_t pitch;              // bytes from row to row in memory, a multiple of 16
+    uint32_t rows;               // of the factor: along, rows in memory; across, elements of one, in whole 16 bytes
+    uint32_t valid;              // of the sum: along, bytes of a row, whole 16; across, rows in memory
+};
+
+template <typename X>
+struct Elements {
+    static constexpr uint32_t STEP = kStepBytes / sizeof(X);     // of the sum
+    static constexpr uint32_t PIECE = kSlot / sizeof(X);
+};
+
+// The slots of a row of an across factor in LDS are permuted by its place in the
+// step, so that the lanes that LDS serves together reach all banks once: 16
+// lanes of a turning read take four rows, 32 consecutive bytes of each.
+template <typename X, int SIDE>
+__device__ __forceinline__ uint32_t across_key(uint32_t k)
+{
+    if constexpr (sizeof(X) == 4)
+        return 8 * (k >> 4 & 1);
+    else
+        return SIDE >= 128 ? 4 * (k & 3) : 4 * (k >> 1 & 1);
+}
+
+// What a lane brings of a factor's steps.
+template <typename X, int SIDE, int WAVES, bool ACROSS>
+struct Bringer {
+    static constexpr int COUNT = SIDE * static_cast<int>(kStepBytes) / (1024 * WAVES);
+    static constexpr uint32_t SLOTS = SIDE * sizeof(X) / kSlot;  // of a row across
+    static constexpr uint32_t LINES = 64 / (SLOTS < 64 ? SLOTS : 64);            // of an instruction, across
+    const char* from;
+    uint32_t at[COUNT], place[COUNT];
+    uint32_t valid;
+    uint64_t on;                 // bytes from step to step
+
+    __device__ __forceinline__ Bringer(const Operand& o, uint32_t row0)
+    {
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        valid = o.valid;
+        if constexpr (ACROSS) {
+            static_assert(SLOTS <= 64, "a row of a step is one instruction's at most");
+            from = o.data + static_cast<uint64_t>(row0) * sizeof(X);
+            on = o.pitch * Elements<X>::STEP;
+            const uint32_t last = (o.rows - row0) / Elements<X>::PIECE - 1;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const uint32_t k = (WAVES * i + wave) * LINES + lane / SLOTS;
+                const uint32_t piece = min(lane % SLOTS ^ across_key<X, SIDE>(k), last);
+                place[i] = k;
+                at[i] = k * static_cast<uint32_t>(o.pitch) + piece * kSlot;
+            }
+        } else {
+            from = o.data + row0 * o.pitch;
+            on = kStepBytes;
+            const uint32_t piece = brought_piece(lane, wave) * kSlot;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const uint32_t row = 8 * (WAVES * i + wave) + (lane >> 3);
+                place[i] = piece;
+                at[i] = min(row, o.rows - 1 - row0) * static_cast<uint32_t>(o.pitch) + piece;
+            }
+        }
+    }
+
+    // pieces past the sum's end are zeros
+    __device__ __forceinline__ void bring_step(uint32_t step, char* to) const
+    {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const char* base = from + step * on;
+        const uint32_t left = valid - step * (ACROSS ? Elements<X>::STEP : kStepBytes);
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+            bring(place[i] < left ? base + at[i] : reinterpret_cast<const char*>(&zeros), to + (WAVES * i + wave) * 1024);
+    }
+};
+
+// A lane's 16 bytes of a block of 32 rows at one depth: eight elements of the sum
+// (four of binary32) of row lane % 32, places 32 g + 8 o (16 g + 4 o) on, g =
+// lane / 32, of the step.
+template <typename X, int SIDE, bool ACROSS, int F>
+struct Reader {
+    uint32_t at[F];
+
+    __device__ __forceinline__ explicit Reader(uint32_t first)
+    {
+        const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < F; ++s) {
+            const uint32_t row = first + 32 * s;
+            if constexpr (!ACROSS) {
+                at[s] = row * kStepBytes;
+            } else if constexpr (sizeof(X) == 4) {
+                const uint32_t r = row + (lane & 31), k = 16 * half;
+                at[s] = k * SIDE * 4 + ((r >> 2) ^ across_key<X, SIDE>(k)) * kSlot + (r & 3) * 4;
+            } else {
+                // lane 4 a + b of 16 takes elements 4 b .. 4 b + 3 of row a, and gets
+                // element 4 a + b of the four rows
+                const uint32_t k = 32 * half + (lane >> 2 & 3);
+                const uint32_t piece = row / 8 + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                at[s] = k * SIDE * 2 + (piece ^ across_key<X, SIDE>(k)) * kSlot + (lane & 1) * 8;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void read(uint4 (&f)[F], const char* buffer, uint32_t o) const
+    {
+        const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+        for (int s = 0; s < F; ++s) {
+            if constexpr (!ACROSS) {
+                f[s] = *reinterpret_cast<const uint4*>(buffer + at[s] + piece_at(lane, o));
+            } else if constexpr (sizeof(X) == 4) {
+                const char* p = buffer + at[s] + 4 * o * SIDE * 4;
+                auto word = [&](int k) { return *reinterpret_cast<const uint32_t*>(p + k * SIDE * 4); };
+                f[s] = uint4{word(0), word(1), word(2), word(3)};
+            } else {
+                // places 8 o and 8 o + 4 on: rows a of each four keep their key
+                const char* p = buffer + at[s] + 8 * o * SIDE * 2;
+                short4v e[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    e[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p + 4 * k * SIDE * 2));
+                __builtin_memcpy(&f[s], e, 16);
+            }
+        }
+    }
+};
+
+template <typename X>
+__device__ __forceinline__ float16v multiply(const uint4& a, const uint4& b, float16v acc)
+{
+    if constexpr (sizeof(X) == 4) {
+        float4v u, v;
+        __builtin_memcpy(&u, &a, 16);
+        __builtin_memcpy(&v, &b, 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(u[k], v[k], acc, 0, 0, 0);
+        return acc;
+    } else if constexpr (std::is_same_v<X, __bf16>) {
+        bhalf8 u, v;
+        __builtin_memcpy(&u, &a, 16);
+        __builtin_memcpy(&v, &b, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(u, v, acc, 0, 0, 0);
+    } else {
+        half8 u, v;
+        __builtin_memcpy(&u, &a, 16);
+        __builtin_memcpy(&v, &b, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(u, v, acc, 0, 0, 0);
+    }
+}
+
+// ---- tiles
+
+// A workgroup's tile: SIDE x SIDE of C by 2 x 2 waves.  The wide accumulators of
+// the largest tile (128 x 128 a wave, one wave a SIMD) halve what the products
+// read from LDS: with eight waves of 128 x 64 reads and loads took all of its
+// cycles.
+template <int SIDE_>
+struct Shape {
+    static constexpr int SIDE = SIDE_;
+    static constexpr int WAVES = 4, THREADS = 64 * WAVES;
+    static constexpr int F = SIDE / 64;                          // blocks of a wave, either way
+    static constexpr int ROWS = SIDE * static_cast<int>(kStepBytes);
+    static constexpr int BUFFER = 2 * ROWS;
+    static constexpr int LOADS = BUFFER / (1024 * WAVES);
+    static constexpr int BUFFERS = SIDE == 64 ? 4 : 2;
+    static constexpr int PER_SIMD = SIDE == 256 ? 1 : 2;         // waves
+};
+
+struct ProductParams {
+    Operand p, q;
+    uint32_t rows;               // of C
+    uint32_t tiles_p, tiles_q;   // of C
+    uint32_t steps, part_steps;  // of the sum, of a part of it
+    uint32_t parts;              // 1: the sums are finished here
+    float* partial;              // [parts][rows][partial_pitch]
+    uint32_t partial_pitch;
+    Finish f;
+};
+
+template <typename S>
+struct Fragments {
+    uint4 p[S::F], q[S::F];
+};
+
+// Workgroups that follow each other go to the eight XCDs in turn: each takes a
+// run of tiles, in columns of 8 tiles of Q, so that what its CUs work on at a time
+// shares rows of both factors in the XCD's cache.
+__device__ __forceinline__ void tile_of(uint32_t group, uint32_t tiles_p, uint32_t tiles_q, uint32_t& tp, uint32_t& tq)
+{
+    constexpr uint32_t kXcds = 8, kBand = 8;
+    const uint32_t all = tiles_p * tiles_q, each = all / kXcds, more = all % kXcds;
+    const uint32_t xcd = group % kXcds, nth = group / kXcds;
+    const uint32_t t = xcd * each + min(xcd, more) + nth;
+    const uint32_t band = t / (kBand * tiles_p), in_band = t - band * kBand * tiles_p;
+    const uint32_t width = min(kBand, tiles_q - band * kBand);
+    tp = in_band / width;
+    tq = band * kBand + in_band - tp * width;
+}
+
+template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
+__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductParams p)
+{
+    BUFFERS_IN_LDS(S)
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tiles = p.tiles_p * p.tiles_q;
+    const uint32_t part = blockIdx.x / tiles;
+    uint32_t tp, tq;
+    tile_of(blockIdx.x - part * tiles, p.tiles_p, p.tiles_q, tp, tq);
+    const uint32_t p0 = tp * S::SIDE, q0 = tq * S::SIDE;
+    const Bringer<X, S::SIDE, S::WAVES, PA> bring_p(p.p, p0);
+    const Bringer<X, S::SIDE, S::WAVES, QA> bring_q(p.q, q0);
+    const uint32_t wave_p = (wave & 1) * (S::SIDE / 2), wave_q = (wave >> 1) * (S::SIDE / 2);
+    const Reader<X, S::SIDE, PA, S::F> read_p(wave_p);
+    const Reader<X, S::SIDE, QA, S::F> read_q(wave_q);
+    float16v acc[S::F][S::F];
+#pragma unroll
+    for (int s = 0; s < S::F; ++s)
+#pragma unroll
+        for (int t = 0; t < S::F; ++t)
+            acc[s][t] = float16v{};
+    const uint32_t first = part * p.part_steps, count = min(p.part_steps, p.steps - first);
+    pipeline<S::LOADS, Fragments<S>>(
+        count, buffers, [](uint32_t, int) {},
+        [&](uint32_t k, char* buffer) {
+            bring_p.bring_step(first + k, buffer);
+            bring_q.bring_step(first + k, buffer + S::ROWS);
+            // the loads stay ahead of the products that hide them
+            __builtin_amdgcn_sched_barrier(0);
+        },
+        [&](Fragments<S>& f, const char* buffer, uint32_t o) {
+            read_p.read(f.p, buffer, o);
+            read_q.read(f.q, buffer + S::ROWS, o);
+        },
+        [&](const Fragments<S>& f, int) {
+#pragma unroll
+            for (int s = 0; s < S::F; ++s)
+#pragma unroll
+                for (int t = 0; t < S::F; ++t)
+                    acc[s][t] = multiply<X>(f.p[s], f.q[t], acc[s][t]);
+        });
+    // out through LDS in binary32, a column of blocks at a time, so that a lane
+    // finishes a run of a row
+    constexpr int V = 16 / sizeof(T);
+    constexpr uint32_t PITCH = S::F * 32 * 4, PIECES = PITCH / 16;
+    char* own = own_part<S::F, S::BUFFER>(buffers[0], buffers[1], wave);
+    const uint32_t half = lane >> 5, mine = lane & 31;
+    const uint64_t key = LAYER && p.f.mask.on ? mask_key(p.f.mask) : 0;
+    auto slot = [](uint32_t column, uint32_t piece) { return column * PITCH + (piece ^ (column & (PIECES - 1))) * 16; };
+#pragma unroll
+    for (int t = 0; t < S::F; ++t) {
+#pragma unroll
+        for (int s = 0; s < S::F; ++s)
+#pragma unroll
+            for (uint32_t g = 0; g < 4; ++g)
+                *reinterpret_cast<float4v*>(own + slot(mine, 8 * s + 2 * g + half))
+                    = float4v{acc[s][t][4 * g], acc[s][t][4 * g + 1], acc[s][t][4 * g + 2], acc[s][t][4 * g + 3]};
+        wave_fence();
+        if (p.parts > 1) {
+#pragma unroll 2
+            for (uint32_t i = 0; i < PIECES / 2; ++i) {
+                const uint32_t column = (64 * i + lane) / PIECES, piece = lane & (PIECES - 1);
+                const uint32_t row = q0 + wave_q + 32 * t + column, unit = p0 + wave_p + 4 * piece;
+                if (row < p.rows && unit < p.partial_pitch)
+                    *reinterpret_cast<float4v*>(p.partial + (static_cast<uint64_t>(part) * p.rows + row) * p.partial_pitch + unit)
+                        = *reinterpret_cast<const float4v*>(own + slot(column, piece));
+            }
+        } else {
+#pragma unroll 2
+            for (uint32_t i = 0; i < PIECES * 2 / V; ++i) {
+                constexpr uint32_t RUNS = PIECES * 4 / V;
+                const uint32_t column = (64 * i + lane) / RUNS, run = lane & (RUNS - 1);
+                const uint32_t row = q0 + wave_q + 32 * t + column, unit = p0 + wave_p + V * run;
+                float v[V];
+#pragma unroll
+                for (int k = 0; k < V / 4; ++k) {
+                    const float4v e = *reinterpret_cast<const float4v*>(own + slot(column, V / 4 * run + k));
+                    __builtin_memcpy(v + 4 * k, &e, 16);
+                }
+                if (row < p.rows && unit < p.f.units)
+                    finish<X, T, LAYER, V>(p.f, key, row, unit, v);
+            }
+        }
+        wave_fence();
+    }
+}
+
+// The parts of the sums added up, in their order, and finished; zeros of no parts.
+struct PartsParams {
+    const float* partial;
+    uint64_t rows, runs;         // runs: rows * per_row
+    uint32_t parts, pitch, per_row;
+    Finish f;
+};
+
+template <typename X, typename T, bool LAYER>
+__global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
+{
+    constexpr int V = 4;
+    const uint64_t key = LAYER && p.f.mask.on ? mask_key(p.f.mask) : 0;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.runs;
+         i += static_cast<uint64_t>(gridDim.x) * kThreads) {
+        const uint64_t row = i / p.per_row;
+        const uint32_t unit = static_cast<uint32_t>(i - row * p.per_row) * V;
+        float v[V] = {};
+#pragma unroll 4
+        for (uint32_t k = 0; k < p.parts; ++k) {
+            const float4v e = *reinterpret_cast<const float4v*>(p.partial + (k * p.rows + row) * p.pitch + unit);
+#pragma unroll
+            for (int r = 0; r < V; ++r)
+                v[r] += e[r];
+        }
+        finish<X, T, LAYER, V>(p.f, key, row, unit, v);
+    }
+}
+
+// ---- factors that do not lie on 16-byte boundaries, copied to where they do
+
+struct PackParams {
+    const void* from;
+    char* to;
+    int64_t stride;              // elements
+    uint64_t pieces;             // rows * per_row
+    uint32_t cols, per_row;      // pieces of 16 bytes in a row, zeros past its end
+};
+
+template <typename U>
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackParams p)
+{
+    constexpr uint32_t N = 16 / sizeof(U);
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.pieces;
+         i += static_cast<uint64_t>(gridDim.x) * kThreads) {
+        const uint64_t row = p.pieces >> 32 ? i / p.per_row : static_cast<uint32_t>(i) / p.per_row;
+        const uint32_t col = static_cast<uint32_t>(i - row * p.per_row) * N;
+        const U* from = static_cast<const U*>(p.from) + row * p.stride + col;
+        U e[N];
+        if (col + N <= p.cols) {
+            const Run<U, N> r = *reinterpret_cast<const Run<U, N>*>(from);
+            __builtin_memcpy(e, &r, 16);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < N; ++k)
+                e[k] = col + k < p.cols ? from[k] : U{0};
+        }
+        uint4 piece;
+        __builtin_memcpy(&piece, e, 16);
+        *reinterpret_cast<uint4*>(p.to + i * 16) = piece;
+    }
+}
+
+// ---- the gradient before a layer's activation, and its sums
+
+struct SlopeParams {
+    const void *grad, *pre;      // pre: null without an activation
+    void* dz;                    // [points][pitch] of the factors' type, zeros past the units, or null
+    float* sums;                 // [groups down][units] or null
+    int64_t grad_stride, pre_stride;
+    uint32_t points, units, pitch, rows, act;     // rows: of a workgroup
+    uint32_t across;             // threads along a row: a power of two
+    Mask mask;                   // its scale is applied to the products and sums: dz stays in a binary16's range
+};
+
+template <typename X, typename G>
+__global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
+{
+    constexpr int V = 8;
+    __shared__ float part[kThreads][V + 1];
+    const uint32_t tx = threadIdx.x & (p.across - 1), ty = threadIdx.x / p.across, down = kThreads / p.across;
+    const uint32_t unit = (blockIdx.x * p.across + tx) * V;
+    const uint64_t row0 = static_cast<uint64_t>(blockIdx.y) * p.rows;
+    const uint64_t end = min(row0 + p.rows, static_cast<uint64_t>(p.points));
+    const uint64_t key = p.mask.on ? mask_key(p.mask) : 0;
+    const uint32_t left = unit < p.units ? p.units - unit : 0;
+    float sum[V] = {};
+    if (unit < p.pitch)
+        for (uint64_t row = row0 + ty; row < end; row += down) {
+            float v[V], z[V];
+            load_inside<G, V>(static_cast<const G*>(p.grad) + row * p.grad_stride + unit, left, v);
+            if (p.pre)
+                load_inside<X, V>(static_cast<const X*>(p.pre) + row * p.pre_stride + unit, left, z);
+            if (p.mask.on)
+                apply_mask<V>(p.mask, key, row, unit, 1.0f, v);
+            if (p.pre)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    v[k] *= slope(z[k], p.act);
+            if (p.dz)
+                store_values<X, V>(static_cast<X*>(p.dz) + row * p.pitch + unit, p.pitch - unit, v);
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                sum[k] += v[k];
+        }
+    if (!p.sums)
+        return;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        part[threadIdx.x][k] = sum[k];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < p.across * V; c += kThreads) {
+        float total = 0.0f;
+        for (uint32_t k = 0; k < down; ++k)
+            total += part[k * p.across + c / V][c % V];
+        const uint32_t u = blockIdx.x * p.across * V + c;
+        if (u < p.units)
+            p.sums[static_cast<uint64_t>(blockIdx.y) * p.units + u] = total;
+    }
+}
+
+// The workgroups' sums added up: 32 units a workgroup, eight threads each.
+__global__ __launch_bounds__(kThreads) void bias_kernel(const float* sums, uint32_t groups, uint32_t units, float scale, void* out,
+                                                        int32_t dtype)
+{
+    __shared__ float part[8][32];
+    const uint32_t tx = threadIdx.x & 31, ty = threadIdx.x >> 5, u = blockIdx.x * 32 + tx;
+    float total = 0.0f;
+    if (u < units)
+        for (uint32_t k = ty; k < groups; k += 8)
+            total += sums[static_cast<uint64_t>(k) * units + u];
+    part[ty][tx] = total;
+    __syncthreads();
+    if (ty || u >= units)
+        return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k)
+        total += part[k][tx];
+    total *= scale;
+    if (dtype == SQN_F32)
+        static_cast<float*>(out)[u] = total;
+    else if (dtype == SQN_F16)
+        static_cast<_Float16*>(out)[u] = from_f32<_Float16>(total);
+    else
+        static_cast<__bf16*>(out)[u] = from_f32<__bf16>(total);
+}
+
+// ---- choices
+
+constexpr int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// A matrix whose pieces can be brought as they lie: on 16-byte boundaries in whole
+// pieces, a tile's rows within 32-bit offsets.
+bool in_place(const sqn_matrix& m)
+{
+    const int64_t size = static_cast<int64_t>(element_size(m.dtype));
+    return reinterpret_cast<uintptr_t>(m.data) % kSlot == 0 && m.row_stride * size % kSlot == 0 && m.cols * size % kSlot == 0
+        && m.row_stride * size < (int64_t{1} << 23);
+}
+
+int64_t packed_cols(const sqn_matrix& m) { return round_up(m.cols, kSlot / static_cast<int64_t>(element_size(m.dtype))); }
+
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+size_t pack_bytes(const sqn_matrix& m)
+{
+    return in_place(m) ? 0 : aligned(static_cast<size_t>(m.rows) * packed_cols(m) * element_size(m.dtype));
+}
+
+// What a launch moves at most in one go; threads take more past it.
+constexpr uint64_t kMaxGroups = 1u << 22;
+
+uint32_t groups_of(uint64_t items)
+{
+    return static_cast<uint32_t>(std::min((items + kThreads - 1) / kThreads, kMaxGroups));
+}
+
+// The matrix, or a copy of it at `to`, whose rows are filled up.
+sqn_matrix packed(const sqn_matrix& m, char*& to, hipStream_t stream)
+{
+    if (in_place(m))
+        return m;
+    sqn_matrix c = m;
+    c.data = to;
+    c.cols = c.row_stride = packed_cols(m);
+    to += pack_bytes(m);
+    if (m.rows == 0)
+        return c;
+    PackParams p;
+    p.from = m.data;
+    p.to = static_cast<char*>(c.data);
+    p.stride = m.row_stride;
+    p.cols = static_cast<uint32_t>(m.cols);
+    p.per_row = static_cast<uint32_t>(c.cols * static_cast<int64_t>(element_size(m.dtype)) / kSlot);
+    p.pieces = static_cast<uint64_t>(m.rows) * p.per_row;
+    if (m.dtype == SQN_F32)
+        pack_kernel<uint32_t><<<groups_of(p.pieces), kThreads, 0, stream>>>(p);
+    else
+        pack_kernel<uint16_t><<<groups_of(p.pieces), kThreads, 0, stream>>>(p);
+    return c;
+}
+
+Operand along(const sqn_matrix& m)
+{
+    const int64_t size = static_cast<int64_t>(element_size(m.dtype));
+    return {static_cast<const char*>(m.data), static_cast<uint64_t>(m.row_stride * size), static_cast<uint32_t>(m.rows),
+            static_cast<uint32_t>(m.cols * size)};
+}
+
+Operand across(const sqn_matrix& m)
+{
+    const int64_t size = static_cast<int64_t>(element_size(m.dtype));
+    return {static_cast<const char*>(m.data), static_cast<uint64_t>(m.row_stride * size), static_cast<uint32_t>(m.cols),
+            static_cast<uint32_t>(m.rows)};
+}
+
+// Tiles and parts of a product's sum.
+struct Plan {
+    int64_t side;
+    int64_t steps, part_steps, parts;
+    size_t bytes;                // of the parts' sums
+};
+
+int64_t tiles_of(int64_t rows_p, int64_t rows_q, int64_t side) { return (rows_p + side - 1) / side * ((rows_q + side - 1) / side); }
+
+// A larger tile is taken where there are enough of it for most of the CUs; a
+// product of few tiles is split along its sum.
+Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
+{
+    Plan r{};
+    const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
+    r.steps = (sum + step - 1) / step;
+    r.parts = 1;
+    if (tiles_of(rows_p, rows_q, 256) >= 200) {
+        r.side = 256;
+    } else if (tiles_of(rows_p, rows_q, 128) >= 200) {
+        r.side = 128;
+    } else {
+        r.side = std::min(rows_p, rows_q) > 64 && r.steps >= 64 ? 128 : 64;
+        const int64_t tiles = std::max<int64_t>(1, tiles_of(rows_p, rows_q, r.side));
+        const int64_t most = std::max<int64_t>(1, r.steps / 8);
+        r.parts = std::max<int64_t>(1, std::min({most, 512 / tiles, int64_t{64}}));
+    }
+    r.part_steps = std::max<int64_t>(1, (r.steps + r.parts - 1) / r.parts);
+    r.parts = std::max<int64_t>(r.steps ? 1 : 0, (r.steps + r.part_steps - 1) / r.part_steps);
+    r.bytes = r.parts > 1 ? aligned(static_cast<size_t>(r.parts) * rows_q * round_up(rows_p, 4) * 4) : 0;
+    return r;
+}
+
+template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
+void launch_tiles(ProductParams& p, hipStream_t stream)
+{
+    p.tiles_p = (p.f.units + S::SIDE - 1) / S::SIDE;
+    p.tiles_q = (p.rows + S::SIDE - 1) / S::SIDE;
+    tile_kernel<S, X, T, LAYER, PA, QA><<<p.tiles_p * p.tiles_q * p.parts, S::THREADS, 0, stream>>>(p);
+}
+
+// `rows_q`: rows of C.  `partial` holds the plan's bytes.
+template <typename X, typename T, bool LAYER, bool PA, bool QA>
+void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t sum, const Finish& f, char* partial, int32_t dtype,
+                    hipStream_t stream)
+{
+    const Plan plan = plan_of(f.units, rows_q, sum, dtype);
+    ProductParams p{};
+    p.p = a;
+    p.q = b;
+    p.rows = static_cast<uint32_t>(rows_q);
+    p.steps = static_cast<uint32_t>(plan.steps);
+    p.part_steps = static_cast<uint32_t>(plan.part_steps);
+    p.parts = static_cast<uint32_t>(plan.parts);
+    p.partial = reinterpret_cast<float*>(partial);
+    p.partial_pitch = static_cast<uint32_t>(round_up(f.units, 4));
+    p.f = f;
+    if (plan.parts) {
+        if (plan.side == 256)
+            launch_tiles<Shape<256>, X, T, LAYER, PA, QA>(p, stream);
+        else if (plan.side == 128)
+            launch_tiles<Shape<128>, X, T, LAYER, PA, QA>(p, stream);
+        else
+            launch_tiles<Shape<64>, X, T, LAYER, PA, QA>(p, stream);
+    }
+    if (plan.parts == 1)
+        return;
+    PartsParams j{};
+    j.partial = p.partial;
+    j.rows = static_cast<uint64_t>(rows_q);
+    j.parts = p.parts;
+    j.pitch = p.partial_pitch;
+    j.per_row = j.pitch / 4;
+    j.runs = j.rows * j.per_row;
+    j.f = f;
+    parts_kernel<X, T, LAYER><<<groups_of(j.runs), kThreads, 0, stream>>>(j);
+}
+
+template <typename X, typename T>
+void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& f, char* work, hipStream_t stream)
+{
+    const sqn_matrix a = packed(w, work, stream), b = packed(x, work, stream);
+    launch_product<X, T, true, false, false>(along(a), along(b), x.rows, x.cols, f, work, x.dtype, stream);
+}
+
+// Workgroups of slope_kernel down the points, and the rows of one: the sums of
+// at most 512 groups are added up behind it.
+uint32_t slope_rows(int64_t points, int64_t units)
+{
+    const int64_t wide = (units + 255) / 256;
+    const int64_t groups = std::clamp<int64_t>(2048 / wide, 1, 512);
+    return static_cast<uint32_t>(std::max<int64_t>(32, (points + groups - 1) / groups));
+}
+
+// What a gradient keeps in its workspace, in this order.
+struct GradientScratch {
+    bool own_dz;                 // grad is dz as it lies otherwise
+    size_t dz, sums, x, w, partial;
+
+    GradientScratch(const sqn_matrix& grad, const sqn_matrix& x_, const sqn_matrix& w_, bool slopes, bool for_x, bool for_w, bool for_bias)
+    {
+        const int64_t points = x_.rows, units = w_.rows;
+        own_dz = (for_x || for_w) && (slopes || grad.dtype != x_.dtype || !in_place(grad));
+        const int64_t piece = kSlot / static_cast<int64_t>(element_size(x_.dtype));
+        dz = own_dz ? aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype)) : 0;
+        sums = 0;
+        if (for_bias && points) {
+            const int64_t rows = slope_rows(points, units);
+            sums = aligned(static_cast<size_t>((points + rows - 1) / rows) * units * 4);
+        }
+        x = for_w ? pack_bytes(x_) : 0;
+        w = for_x ? pack_bytes(w_) : 0;
+        partial = std::max(for_x ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
+                           for_w ? plan_of(x_.cols, units, points, x_.dtype).bytes : 0);
+    }
+
+    size_t bytes() const { return dz + sums + x + w + partial; }
+};
+
+template <typename X>
+hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre,
+                                 int32_t act, const sqn_dropout_mask* mask, const LayerGradients& to, void* workspace,
+                                 hipStream_t stream)
+{
+    const GradientScratch scratch(grad, x, w, pre || (mask && mask->p != 0.0), to.x, to.w, to.bias);
+    char* work = static_cast<char*>(workspace);
+    const int64_t points = x.rows, units = w.rows;
+    const Mask m = mask_of(mask, units);
+    sqn_matrix dz = grad;
+    char* const dz_at = work;
+    work += scratch.dz;
+    float* const sums = scratch.sums ? reinterpret_cast<float*>(work) : nullptr;
+    work += scratch.sums;
+    if (scratch.own_dz) {
+        dz.data = dz_at;
+        dz.dtype = x.dtype;
+        dz.cols = dz.row_stride = round_up(units, Elements<X>::PIECE);
+    }
+    uint32_t groups = 0;
+    if (points && (scratch.own_dz || sums)) {
+        SlopeParams p{};
+        p.grad = grad.data;
+        p.grad_stride = grad.row_stride;
+        p.pre = pre ? pre->data : nullptr;
+        p.pre_stride = pre ? pre->row_stride : 0;
+        p.dz = scratch.own_dz ? dz.data : nullptr;
+        p.sums = sums;
+        p.points = static_cast<uint32_t>(points);
+        p.units = static_cast<uint32_t>(units);
+        p.pitch = static_cast<uint32_t>(scratch.own_dz ? dz.cols : units);
+        p.rows = slope_rows(points, units);
+        p.act = static_cast<uint32_t>(act);
+        p.mask = m;
+        const uint32_t runs = (p.pitch + 7) / 8;
+        p.across = 1;
+        while (p.across < 32 && p.across < runs)
+            p.across *= 2;
+        groups = (p.points + p.rows - 1) / p.rows;
+        const dim3 grid((runs + p.across - 1) / p.across, groups);
+        if (grad.dtype == SQN_F32)
+            slope_kernel<X, float><<<grid, kThreads, 0, stream>>>(p);
+        else
+            slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
+    }
+    if (to.bias)
+        bias_kernel<<<static_cast<uint32_t>((units + 31) / 32), kThreads, 0, stream>>>(sums, groups, static_cast<uint32_t>(units), m.scale,
+                                                                                       to.bias, to.bias_dtype);
+    Finish f{};
+    f.scale = m.scale;
+    f.units = static_cast<uint32_t>(x.cols);
+    if (to.x && points) {
+        const sqn_matrix a = packed(w, work, stream);
+        f.out = to.x->data;
+        f.out_stride = to.x->row_stride;
+        launch_product<X, X, false, true, false>(across(a), along(dz), points, units, f, work + scratch.x, x.dtype, stream);
+    }
+    if (to.w) {
+        const sqn_matrix a = packed(x, work, stream);
+        f.out = to.w->data;
+        f.out_stride = to.w->row_stride;
+        launch_product<X, X, false, true, true>(across(a), across(dz), units, points, f, work, x.dtype, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t layer_bytes(const sqn_matrix& x, const sqn_matrix& w)
+{
+    return pack_bytes(x) + pack_bytes(w) + plan_of(w.rows, x.rows, x.cols, x.dtype).bytes;
+}
+
+hipError_t launch_layer(const sqn_matrix& x, const sqn_matrix& w, const sqn_epilogue& e, const sqn_matrix& out, void* workspace,
+                        hipStream_t stream)
+{
+    Finish f{};
+    f.bias = e.bias;
+    f.bias_f32 = e.bias_dtype == SQN_F32 ? 1 : 0;
+    f.act = static_cast<uint32_t>(e.activation);
+    f.units = static_cast<uint32_t>(w.rows);
+    f.mask = mask_of(e.dropout, w.rows);
+    if (e.residual) {
+        f.residual = e.residual->data;
+        f.residual_stride = e.residual->row_stride;
+    }
+    if (e.pre) {
+        f.pre = e.pre->data;
+        f.pre_stride = e.pre->row_stride;
+    }
+    f.out = out.data;
+    f.out_stride = out.row_stride;
+    char* work = static_cast<char*>(workspace);
+    if (x.dtype == SQN_F32)
+        launch_layer_typed<float, float>(x, w, f, work, stream);
+    else if (x.dtype == SQN_F16 && out.dtype == SQN_F32)
+        launch_layer_typed<_Float16, float>(x, w, f, work, stream);
+    else if (x.dtype == SQN_F16)
+        launch_layer_typed<_Float16, _Float16>(x, w, f, work, stream);
+    else if (out.dtype == SQN_F32)
+        launch_layer_typed<__bf16, float>(x, w, f, work, stream);
+    else
+        launch_layer_typed<__bf16, __bf16>(x, w, f, work, stream);
+    return hipGetLastError();
+}
+
+size_t layer_gradient_bytes(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, bool slopes, bool for_x, bool for_w,
+                            bool for_bias)
+{
+    return GradientScratch(grad, x, w, slopes, for_x, for_w, for_bias).bytes();
+}
+
+hipError_t launch_layer_gradient(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre,
+                                 int32_t act, const sqn_dropout_mask* mask, const LayerGradients& to, void* workspace,
+                                 hipStream_t stream)
+{
+    if (x.dtype == SQN_F32)
+        return launch_gradient_typed<float>(grad, x, w, pre, act, mask, to, workspace, stream);
+    if (x.dtype == SQN_F16)
+        return launch_gradient_typed<_Float16>(grad, x, w, pre, act, mask, to, workspace, stream);
+    return launch_gradient_typed<__bf16>(grad, x, w, pre, act, mask, to, workspace, stream);
+}
+
+}  // namespace sqn

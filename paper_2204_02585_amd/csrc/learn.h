@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mask.h"
 #include "sqn.h"
 
 namespace sqn {
@@ -37,5 +38,30 @@ hipError_t launch_quantised_product(const sqn_quantised& x, const sqn_quantised&
 size_t quantised_layer_bytes(int64_t points, int64_t units, int64_t cols);
 hipError_t launch_quantised_layer(const sqn_matrix& x, const sqn_quantised& w, const float* bias, bool relu,
                                   const sqn_matrix& out, void* workspace, hipStream_t stream);
+
+// ---- dropout.hip
+
+// The mask of a matrix of `cols` columns; null for none.
+Mask mask_of(const sqn_dropout_mask* mask, int64_t cols);
+hipError_t launch_dropout(const sqn_matrix& x, const sqn_dropout_mask& mask, const sqn_matrix* residual,
+                          const sqn_matrix& out, hipStream_t stream);
+
+// ---- layer.hip
+
+size_t layer_bytes(const sqn_matrix& x, const sqn_matrix& w);
+hipError_t launch_layer(const sqn_matrix& x, const sqn_matrix& w, const sqn_epilogue& epilogue, const sqn_matrix& out,
+                        void* workspace, hipStream_t stream);
+
+struct LayerGradients {
+    const sqn_matrix *x, *w;     // null where not wanted
+    void* bias;
+    int32_t bias_dtype;
+};
+// slopes: an activation or a mask stands between grad and dz.
+size_t layer_gradient_bytes(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, bool slopes, bool for_x, bool for_w,
+                            bool for_bias);
+hipError_t launch_layer_gradient(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre,
+                                 int32_t activation, const sqn_dropout_mask* mask, const LayerGradients& to, void* workspace,
+                                 hipStream_t stream);
 
 }  // namespace sqn

@@ -275,6 +275,91 @@ bool valid_layer(int64_t points, int64_t units, int64_t cols)
     return points >= 0 && points <= kMaxRows && units >= 1 && units <= kMaxRows && cols >= 1 && cols <= kMaxCols;
 }
 
+sqn_status check_mask(const sqn_dropout_mask* mask)
+{
+    if (!(mask->p >= 0.0 && mask->p <= 1.0))
+        return fail(SQN_ERR_INVALID_ARG, "p = %g outside [0, 1]", mask->p);
+    if (!mask->step)
+        return SQN_OK;
+    if (reinterpret_cast<uintptr_t>(mask->step) % 8)
+        return fail(SQN_ERR_INVALID_ARG, "step (%p) is not aligned to 8 bytes", mask->step);
+    return check_memory(mask->step, 8, "step");
+}
+
+// A matrix of the given sizes and type.
+sqn_status check_like(const sqn_matrix* x, int64_t rows, int64_t cols, int32_t dtype, bool written, const char* what)
+{
+    const sqn_status s = check_matrix(x, written, what);
+    if (s != SQN_OK)
+        return s;
+    if (x->rows != rows || x->cols != cols || x->dtype != dtype)
+        return fail(SQN_ERR_INVALID_ARG, "%s must be %lld x %lld of dtype %d, is %lld x %lld of %d", what,
+                    static_cast<long long>(rows), static_cast<long long>(cols), dtype, static_cast<long long>(x->rows),
+                    static_cast<long long>(x->cols), x->dtype);
+    return SQN_OK;
+}
+
+sqn_status check_bias(const void* bias, int32_t dtype, int64_t units, int32_t x_dtype, const char* what)
+{
+    if (!bias)
+        return SQN_OK;
+    if (dtype != SQN_F32 && dtype != x_dtype)
+        return fail(SQN_ERR_INVALID_ARG, "%s must be SQN_F32 or of x's dtype", what);
+    if (reinterpret_cast<uintptr_t>(bias) % element_size(dtype))
+        return fail(SQN_ERR_INVALID_ARG, "%s (%p) is not aligned to its elements", what, bias);
+    return check_memory(bias, static_cast<size_t>(units) * element_size(dtype), what);
+}
+
+// The factors of a layer.
+sqn_status check_factors(const sqn_matrix* x, const sqn_matrix* w)
+{
+    sqn_status s = check_matrix(x, false, "x");
+    if (s != SQN_OK)
+        return s;
+    if ((s = check_matrix(w, false, "w")) != SQN_OK)
+        return s;
+    if (w->dtype != x->dtype)
+        return fail(SQN_ERR_INVALID_ARG, "x and w must have one dtype");
+    if (w->cols != x->cols)
+        return fail(SQN_ERR_INVALID_ARG, "x has %lld columns, w %lld", static_cast<long long>(x->cols),
+                    static_cast<long long>(w->cols));
+    if (w->rows < 1 || w->rows > kMaxCols)
+        return fail(SQN_ERR_INVALID_ARG, "w has %lld rows, 1 to 2^20 make a layer", static_cast<long long>(w->rows));
+    return SQN_OK;
+}
+
+sqn_status check_tiles(int64_t rows, int64_t cols)
+{
+    if (((rows + 63) / 64) * ((cols + 63) / 64) > kMaxTiles)
+        return fail(SQN_ERR_UNSUPPORTED, "a product of %lld x %lld has more than 2^23 tiles of 64 x 64",
+                    static_cast<long long>(rows), static_cast<long long>(cols));
+    return SQN_OK;
+}
+
+sqn_status check_activation(int32_t activation)
+{
+    if (activation < SQN_ACT_NONE || activation > SQN_ACT_SILU)
+        return fail(SQN_ERR_INVALID_ARG, "activation must be SQN_ACT_NONE, SQN_ACT_RELU, SQN_ACT_GELU or SQN_ACT_SILU");
+    return SQN_OK;
+}
+
+// Descriptions that a workspace can be told for; nothing is read through them.
+bool plain_sizes(const sqn_matrix* x)
+{
+    return x && valid_dtype(x->dtype) && x->rows >= 0 && x->rows <= kMaxRows && x->cols >= 1 && x->cols <= kMaxCols
+        && x->row_stride >= 0 && x->row_stride <= kMaxStride;
+}
+
+bool plain_factors(const sqn_matrix* x, const sqn_matrix* w)
+{
+    return plain_sizes(x) && plain_sizes(w) && w->rows >= 1 && w->rows <= kMaxCols && w->cols == x->cols && w->dtype == x->dtype;
+}
+
+bool has_slopes(int32_t activation, const sqn_dropout_mask* mask)
+{
+    return activation != SQN_ACT_NONE || (mask && mask->p != 0.0);
+}
+
 sqn_status launched(hipError_t e, const char* what)
 {
     return e == hipSuccess ? SQN_OK : fail(SQN_ERR_DEVICE, "%s launch failed: %s", what, hipGetErrorString(e));
@@ -462,6 +547,120 @@ sqn_status sqn_quantised_layer(const sqn_matrix* x, const sqn_quantised* w, cons
     return launched(sqn::launch_quantised_layer(*x, *w, bias, relu != 0, *out, workspace,
                                                 static_cast<hipStream_t>(stream)),
                     "layer");
+}
+
+sqn_status sqn_dropout(const sqn_matrix* x, const sqn_dropout_mask* mask, const sqn_matrix* residual, const sqn_matrix* out,
+                       void* stream)
+{
+    sqn_status s = check_stream(stream);
+    if (s != SQN_OK)
+        return s;
+    if (!mask)
+        return fail(SQN_ERR_INVALID_ARG, "mask is NULL");
+    if ((s = check_mask(mask)) != SQN_OK)
+        return s;
+    if ((s = check_matrix(x, false, "x")) != SQN_OK)
+        return s;
+    if (residual && (s = check_like(residual, x->rows, x->cols, x->dtype, false, "residual")) != SQN_OK)
+        return s;
+    if ((s = check_like(out, x->rows, x->cols, x->dtype, true, "out")) != SQN_OK)
+        return s;
+    if (x->rows == 0)
+        return SQN_OK;
+    return launched(sqn::launch_dropout(*x, *mask, residual, *out, static_cast<hipStream_t>(stream)), "dropout");
+}
+
+size_t sqn_layer_workspace(const sqn_matrix* x, const sqn_matrix* w)
+{
+    return plain_factors(x, w) ? sqn::layer_bytes(*x, *w) : 0;
+}
+
+sqn_status sqn_layer(const sqn_matrix* x, const sqn_matrix* w, const sqn_epilogue* epilogue, const sqn_matrix* out,
+                     void* workspace, size_t workspace_bytes, void* stream)
+{
+    static const sqn_epilogue none{};
+    const sqn_epilogue& e = epilogue ? *epilogue : none;
+    sqn_status s = check_stream(stream);
+    if (s != SQN_OK)
+        return s;
+    if ((s = check_factors(x, w)) != SQN_OK)
+        return s;
+    if (!out)
+        return fail(SQN_ERR_INVALID_ARG, "out is NULL");
+    if (out->dtype != x->dtype && out->dtype != SQN_F32)
+        return fail(SQN_ERR_INVALID_ARG, "out must be SQN_F32 or of x's dtype");
+    if ((s = check_like(out, x->rows, w->rows, out->dtype, true, "out")) != SQN_OK)
+        return s;
+    if ((s = check_tiles(x->rows, w->rows)) != SQN_OK)
+        return s;
+    if ((s = check_activation(e.activation)) != SQN_OK)
+        return s;
+    if ((s = check_bias(e.bias, e.bias_dtype, w->rows, x->dtype, "bias")) != SQN_OK)
+        return s;
+    if (e.dropout && (s = check_mask(e.dropout)) != SQN_OK)
+        return s;
+    if (e.residual && (s = check_like(e.residual, x->rows, w->rows, out->dtype, false, "residual")) != SQN_OK)
+        return s;
+    if (e.pre && (s = check_like(e.pre, x->rows, w->rows, x->dtype, true, "pre")) != SQN_OK)
+        return s;
+    if (x->rows == 0)
+        return SQN_OK;
+    if ((s = check_workspace(workspace, workspace_bytes, sqn::layer_bytes(*x, *w))) != SQN_OK)
+        return s;
+    return launched(sqn::launch_layer(*x, *w, e, *out, workspace, static_cast<hipStream_t>(stream)), "layer");
+}
+
+size_t sqn_layer_gradient_workspace(const sqn_matrix* grad, const sqn_matrix* x, const sqn_matrix* w, int32_t activation,
+                                    const sqn_dropout_mask* mask, int32_t for_x, int32_t for_w, int32_t for_bias)
+{
+    if (!plain_sizes(grad) || !plain_factors(x, w))
+        return 0;
+    return sqn::layer_gradient_bytes(*grad, *x, *w, has_slopes(activation, mask), for_x != 0, for_w != 0, for_bias != 0);
+}
+
+sqn_status sqn_layer_gradient(const sqn_matrix* grad, const sqn_matrix* x, const sqn_matrix* w, const sqn_matrix* pre,
+                              int32_t activation, const sqn_dropout_mask* mask, const sqn_matrix* grad_x, const sqn_matrix* grad_w,
+                              void* grad_bias, int32_t bias_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    sqn_status s = check_stream(stream);
+    if (s != SQN_OK)
+        return s;
+    if ((s = check_factors(x, w)) != SQN_OK)
+        return s;
+    if (!grad)
+        return fail(SQN_ERR_INVALID_ARG, "grad is NULL");
+    if (grad->dtype != x->dtype && grad->dtype != SQN_F32)
+        return fail(SQN_ERR_INVALID_ARG, "grad must be SQN_F32 or of x's dtype");
+    if ((s = check_like(grad, x->rows, w->rows, grad->dtype, false, "grad")) != SQN_OK)
+        return s;
+    if ((s = check_activation(activation)) != SQN_OK)
+        return s;
+    if ((activation == SQN_ACT_NONE) != !pre)
+        return fail(SQN_ERR_INVALID_ARG, "pre goes with an activation, and an activation needs it");
+    if (pre && (s = check_like(pre, x->rows, w->rows, x->dtype, false, "pre")) != SQN_OK)
+        return s;
+    if (mask && (s = check_mask(mask)) != SQN_OK)
+        return s;
+    if (grad_x && (s = check_like(grad_x, x->rows, x->cols, x->dtype, true, "grad_x")) != SQN_OK)
+        return s;
+    if (grad_x && (s = check_tiles(x->rows, x->cols)) != SQN_OK)
+        return s;
+    if (grad_w && (s = check_like(grad_w, w->rows, w->cols, w->dtype, true, "grad_w")) != SQN_OK)
+        return s;
+    if (grad_w && (s = check_tiles(w->rows, w->cols)) != SQN_OK)
+        return s;
+    if ((s = check_bias(grad_bias, bias_dtype, w->rows, x->dtype, "grad_bias")) != SQN_OK)
+        return s;
+    if (!grad_x && !grad_w && !grad_bias)
+        return SQN_OK;
+    if ((s = check_workspace(workspace, workspace_bytes,
+                             sqn::layer_gradient_bytes(*grad, *x, *w, has_slopes(activation, mask), grad_x != nullptr,
+                                                       grad_w != nullptr, grad_bias != nullptr))) != SQN_OK)
+        return s;
+    const sqn::LayerGradients to = {grad_x, grad_w, grad_bias, bias_dtype};
+    return launched(sqn::launch_layer_gradient(*grad, *x, *w, pre, activation, mask, to, workspace,
+                                               static_cast<hipStream_t>(stream)),
+                    "layer gradient");
 }
 
 }  // extern "C"

@@ -25,6 +25,8 @@ BLOCK = 32                                      # elements of a 4-bit block
 MUON = (3.4445, -4.7750, 2.0315)                # the Muon optimiser's coefficients
 
 _CODES = {torch.float32: binding.SQN_F32, torch.float16: binding.SQN_F16, torch.bfloat16: binding.SQN_BF16}
+_ACTIVATIONS = {None: binding.SQN_ACT_NONE, "relu": binding.SQN_ACT_RELU, "gelu": binding.SQN_ACT_GELU,
+                "silu": binding.SQN_ACT_SILU}
 _IDS = {torch.int32: binding.SQN_I32, torch.int64: binding.SQN_I64}
 
 
@@ -332,3 +334,234 @@ def product(x, w: Quantised, bias: Optional[torch.Tensor] = None, relu: bool = F
     _check(lib.sqn_quantised_layer(_matrix(source, "x"), w._arg(), _ptr(bias), 1 if relu else 0, into, _ptr(work), size,
                                    _on(stream, source, w.codes, w.scales, bias, out, work)))
     return out
+
+
+# ---------------------------------------------------------------- dropout
+
+def _probability(p) -> float:
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must lie in [0, 1], got {p}")
+    return p
+
+
+def _mask(p: float, seed: int, step: Optional[torch.Tensor], beside: torch.Tensor) -> Optional[binding.DropoutMask]:
+    if step is not None:
+        if step.dtype != torch.int64 or step.numel() != 1:
+            raise ValueError(f"step must be an int64 tensor of one element, got {step.dtype} {tuple(step.shape)}")
+        _on_gpu(step, "step", beside)
+    return binding.DropoutMask(p, int(seed) & 0xFFFFFFFFFFFFFFFF, _ptr(step))
+
+
+def _beside(t: Optional[torch.Tensor], shape, dtype, beside: torch.Tensor, name: str) -> None:
+    if t is None:
+        return
+    _on_gpu(t, name, beside)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _wants_gradient(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _dropout(x, p, seed, step, residual, out, stream):
+    _on_gpu(x, "x")
+    if x.dim() == 0:
+        raise ValueError("x must have a dimension")
+    _beside(residual, x.shape, x.dtype, x, "residual")
+    mask = _mask(p, seed, step, x)
+    out = _out(out, x.shape, x.dtype, x)
+    if out.numel() == 0:
+        return out
+    source, more = _rows(x), None if residual is None else _rows(residual)
+    _check(lib.sqn_dropout(_matrix(source, "x"), mask, None if more is None else _matrix(more, "residual"),
+                           _matrix(_rows(out), "out"), _on(stream, source, more, step, out)))
+    return out
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, step, p, seed):
+        # saved, so that a step that is changed before the backward pass is noticed
+        ctx.save_for_backward(step)
+        ctx.save_for_forward(step)
+        ctx.p, ctx.seed = p, seed
+        return _dropout(x.detach(), p, seed, step, None if residual is None else residual.detach(), None, None)
+
+    @staticmethod
+    def backward(ctx, grad):
+        (step,) = ctx.saved_tensors
+        grad_x = dropout(grad, ctx.p, ctx.seed, step) if ctx.needs_input_grad[0] else None
+        return grad_x, grad if ctx.needs_input_grad[1] else None, None, None, None
+
+    @staticmethod
+    def jvp(ctx, x, residual, _step, _p, _seed):
+        (step,) = ctx.saved_tensors
+        if x is None:
+            return residual
+        return dropout(x, ctx.p, ctx.seed, step, residual)
+
+
+def dropout(x: torch.Tensor, p: float, seed: int = 0, step: Optional[torch.Tensor] = None,
+            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sqn_dropout: x [..., cols] with a share p of its elements zeros and the
+    rest times 1 / (1 - p), plus `residual` if there is one.  The mask is made
+    from `seed` (an int) plus `step` (an int64 tensor of one element on the
+    device, for captured graphs; None: nothing) and each element's place; it is
+    never stored, and the same arguments give the same mask.  `out` may be x or
+    the residual.  Differentiable in x and the residual (without `out` and
+    `stream`), also twice, and in forward mode; the gradient makes the mask
+    again, so `step` must hold its value until then."""
+    p = _probability(p)
+    if out is None and stream is None:
+        if (_wants_gradient(x, residual) or _tangent(x) is not None
+                or (residual is not None and _tangent(residual) is not None)):
+            return _Dropout.apply(x, residual, step, p, int(seed))
+    else:
+        _no_tangent("dropout with out or stream", x, residual)
+    return _dropout(x, p, seed, step, residual, out, stream)
+
+
+# ---------------------------------------------------------------- layers
+
+def _activation(name) -> int:
+    if name not in _ACTIVATIONS:
+        raise ValueError(f"activation must be None, 'relu', 'gelu' or 'silu', got {name!r}")
+    return _ACTIVATIONS[name]
+
+
+def _factors(x: torch.Tensor, w: torch.Tensor) -> None:
+    _on_gpu(x, "x")
+    _on_gpu(w, "w", x)
+    if w.dim() != 2 or x.dim() == 0 or x.shape[-1] != w.shape[1]:
+        raise ValueError(f"x [..., cols] and w [units, cols] are needed, got {tuple(x.shape)} and {tuple(w.shape)}")
+    if w.numel() == 0:
+        raise ValueError(f"w must have units and columns, got {tuple(w.shape)}")
+    if x.dtype != w.dtype:
+        raise TypeError(f"x and w must have one dtype, got {x.dtype} and {w.dtype}")
+
+
+def _bias(bias: Optional[torch.Tensor], w: torch.Tensor) -> Optional[torch.Tensor]:
+    if bias is None:
+        return None
+    _on_gpu(bias, "bias", w)
+    if bias.dtype not in (torch.float32, w.dtype) or tuple(bias.shape) != (w.shape[0],):
+        raise ValueError(f"bias must be a float32 or {w.dtype} tensor of shape {(w.shape[0],)}, got {bias.dtype} {tuple(bias.shape)}")
+    return bias if bias.is_contiguous() else bias.contiguous()
+
+
+def _layer(x, w, bias, activation, residual, p, seed, step, dtype, out, pre, stream):
+    _factors(x, w)
+    act = _activation(activation)
+    bias = _bias(bias, w)
+    shape = (*x.shape[:-1], w.shape[0])
+    if dtype is None:
+        dtype = x.dtype if out is None else out.dtype
+    if dtype not in (x.dtype, torch.float32):
+        raise TypeError(f"dtype must be float32 or x's {x.dtype}, got {dtype}")
+    _beside(residual, shape, dtype, x, "residual")
+    if pre is not None:
+        _out(pre, shape, x.dtype, x, "pre")
+    mask = _mask(p, seed, step, x)
+    out = _out(out, shape, dtype, x)
+    if out.numel() == 0:
+        return out
+    a, b = _rows(x), _rows(w)
+    more = None if residual is None else _rows(residual)
+    source, weights = _matrix(a, "x"), _matrix(b, "w")
+    epilogue = binding.Epilogue(_ptr(bias), 0 if bias is None else _CODES[bias.dtype], act)
+    if p:
+        epilogue.dropout = ctypes.pointer(mask)
+    if more is not None:
+        epilogue.residual = ctypes.pointer(_matrix(more, "residual"))
+    if pre is not None:
+        epilogue.pre = ctypes.pointer(_matrix(_rows(pre), "pre"))
+    size = lib.sqn_layer_workspace(source, weights)
+    work = _workspace(size, x)
+    _check(lib.sqn_layer(source, weights, epilogue, _matrix(_rows(out), "out"), _ptr(work), size,
+                         _on(stream, a, b, bias, more, pre, step, out, work)))
+    return out
+
+
+class _Layer(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, residual, step, activation, p, seed, dtype):
+        plain = [None if t is None else t.detach() for t in (x, w, bias, residual)]
+        pre = None
+        if activation is not None and any(ctx.needs_input_grad[:3]):
+            _factors(x, w)
+            pre = _out(None, (*x.shape[:-1], w.shape[0]), x.dtype, plain[0])
+        ctx.save_for_backward(x, w, pre, step)
+        ctx.options = activation, p, seed
+        ctx.bias = None if bias is None else bias.dtype
+        ctx.residual = None if residual is None else residual.dtype
+        return _layer(*plain[:3], activation, plain[3], p, seed, step, dtype, None, pre, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, w, pre, step = ctx.saved_tensors
+        activation, p, seed = ctx.options
+        for_x, for_w, for_bias, for_residual = ctx.needs_input_grad[:4]
+        grads = (None, None, None)
+        if for_x or for_w or for_bias:
+            grads = layer_gradient(grad, x, w, pre, activation, p, seed, step, for_x=for_x, for_w=for_w,
+                                   for_bias=for_bias, bias_dtype=ctx.bias or torch.float32)
+        return (*grads, grad if for_residual else None, None, None, None, None, None)
+
+
+def layer(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Optional[str] = None,
+          residual: Optional[torch.Tensor] = None, dropout: float = 0.0, seed: int = 0,
+          step: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+          out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sqn_layer: D(act(x w^T + bias)) + residual, [..., units], of x [..., cols]
+    and w [units, cols] (one dtype), bias [units] (float32 or theirs), residual
+    [..., units] of the result's dtype, which is x's or float32.  `activation`
+    is None, "relu", "gelu" (with the normal distribution itself) or "silu"; D
+    is the mask of `dropout`(..., p=dropout, seed=seed, step=step).  Sums and the
+    epilogue are float32, rounded once.  Differentiable in x, w, bias and
+    residual (without `out`, `pre` and `stream`), by layer_gradient, which takes
+    what `pre` holds: x w^T + bias in x's dtype.  No forward-mode derivative."""
+    p = _probability(dropout)
+    _no_tangent("layer", x, w, bias, residual)
+    if out is None and pre is None and stream is None and _wants_gradient(x, w, bias, residual):
+        return _Layer.apply(x, w, bias, residual, step, activation, p, int(seed), dtype)
+    return _layer(x, w, bias, activation, residual, p, seed, step, dtype, out, pre, stream)
+
+
+def layer_gradient(grad: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre: Optional[torch.Tensor] = None,
+                   activation: Optional[str] = None, dropout: float = 0.0, seed: int = 0,
+                   step: Optional[torch.Tensor] = None, for_x: bool = True, for_w: bool = True, for_bias: bool = True,
+                   bias_dtype: torch.dtype = torch.float32, stream=None):
+    """sqn_layer_gradient: the gradients (of x, of w, of the bias) of layer from
+    grad [..., units], that of its result (x's dtype or float32); None where one
+    is not wanted.  `pre` is what layer wrote there, needed with an activation
+    and only then; the residual's gradient is grad.  No gradient passes through
+    it."""
+    p = _probability(dropout)
+    _no_tangent("layer_gradient", grad, x, w, pre)
+    _factors(x, w)
+    act = _activation(activation)
+    shape = (*x.shape[:-1], w.shape[0])
+    _on_gpu(grad, "grad", x)
+    if tuple(grad.shape) != shape or grad.dtype not in (x.dtype, torch.float32):
+        raise ValueError(f"grad must be a float32 or {x.dtype} tensor of shape {shape}, got {grad.dtype} {tuple(grad.shape)}")
+    if (pre is None) != (act == 0):
+        raise ValueError("pre goes with an activation, and an activation needs it")
+    _beside(pre, shape, x.dtype, x, "pre")
+    if bias_dtype not in (torch.float32, x.dtype):
+        raise TypeError(f"bias_dtype must be float32 or x's {x.dtype}, got {bias_dtype}")
+    mask = _mask(p, seed, step, x)
+    grad_x = _out(None, x.shape, x.dtype, x) if for_x else None
+    grad_w = _out(None, w.shape, w.dtype, x) if for_w else None
+    grad_bias = _out(None, (w.shape[0],), bias_dtype, x) if for_bias else None
+    g, a, b, z = _rows(grad), _rows(x), _rows(w), None if pre is None else _rows(pre)
+    args = (_matrix(g, "grad"), _matrix(a, "x"), _matrix(b, "w"))
+    size = lib.sqn_layer_gradient_workspace(*args, act, mask, for_x, for_w, for_bias)
+    work = _workspace(size, x)
+    _check(lib.sqn_layer_gradient(*args, None if z is None else _matrix(z, "pre"), act, mask,
+                                  _matrix(_rows(grad_x), "grad_x") if for_x else None,
+                                  _matrix(grad_w, "grad_w") if for_w else None, _ptr(grad_bias), _CODES[bias_dtype],
+                                  _ptr(work), size, _on(stream, g, a, b, z, step, grad_x, grad_w, grad_bias, work)))
+    return grad_x, grad_w, grad_bias

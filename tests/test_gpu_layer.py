@@ -1,0 +1,201 @@
+"""Layers against their plain form in 64 bits (tests/layer_util.py): sizes around
+the tiles' and the steps' ends, types, layouts, epilogues, non-finite values."""
+import numpy as np
+import pytest
+import torch
+
+from tests import layer_util as U
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+ACTS = [None, "relu", "gelu", "silu"]
+#        points, cols, units
+SIZES = [(1, 1, 1), (1, 7, 3), (2, 8, 8), (5, 42, 50), (16, 64, 64), (17, 64, 64), (1, 4096, 520), (3, 2051, 257), (33, 100, 129),
+         (64, 128, 64), (130, 1000, 70), (257, 513, 255), (300, 72, 136), (1000, 24, 16), (65, 4096, 130), (2000, 40, 1032)]
+
+
+def draw(shape, dtype, gen, spread=1.0):
+    return (spread * torch.randn(shape, generator=gen)).to(dtype).cuda()
+
+
+def inputs(points, cols, units, dtype, out=None, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    return (draw((points, cols), dtype, gen), draw((units, cols), dtype, gen, (2.0 / cols) ** 0.5), draw((units,), torch.float32, gen),
+            draw((points, units), out or dtype, gen))
+
+
+def check(y, x, w, bias=None, activation=None, residual=None, dropout=0.0, seed=0, pre=None, what=""):
+    want, off, z, off_z = U.layer(x.reshape(-1, x.shape[-1]), w, bias, activation, None if residual is None else
+                                  residual.reshape(-1, residual.shape[-1]), dropout, seed, y.dtype)
+    U.assert_within(y.reshape(-1, y.shape[-1]), want, off, what)
+    if pre is not None:
+        U.assert_within(pre, z, off_z, (what, "pre"))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", SIZES)
+def test_values(dtype, size):
+    from paper_2204_02585_amd import learn
+    x, w, bias, residual = inputs(*size, dtype)
+    check(learn.layer(x, w), x, w)
+    k = SIZES.index(size) % 4
+    for activation in (ACTS[k], ACTS[(k + 1) % 4]):
+        pre = torch.empty_like(residual)
+        y = learn.layer(x, w, bias, activation, residual, dropout=0.3, seed=7, pre=pre)
+        check(y, x, w, bias, activation, residual, 0.3, 7, pre, activation)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("activation", ACTS)
+def test_epilogues(dtype, activation):
+    from paper_2204_02585_amd import learn
+    for size in ((9, 64, 61), (200, 96, 72)):
+        for out in {dtype, torch.float32}:
+            x, w, bias, residual = inputs(*size, dtype, out)
+            for b in (None, bias, bias.to(dtype)):
+                for r in (None, residual):
+                    for p in (0.0, 0.5):
+                        y = learn.layer(x, w, b, activation, r, dropout=p, seed=3, dtype=out)
+                        assert y.dtype == out
+                        check(y, x, w, b, activation, r, p, 3, what=(size, out, b is None, r is None, p))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_tiles(dtype):
+    """Tiles of 128 and of 256, ragged at every end; all values against a product
+    in 64 bits on the GPU."""
+    from paper_2204_02585_amd import learn
+    for size in ((2100, 330, 1700), (3700, 200, 3900)):
+        x, w, bias, _ = inputs(*size, dtype)
+        y = learn.layer(x, w, bias, "relu")
+        x64, w64 = x.double(), w.double()
+        z = x64 @ w64.t() + bias.double()
+        off = 2 * U.F32 * (size[1] + 8) * (x64.abs() @ w64.abs().t() + bias.double().abs())
+        want = z.clamp(min=0)
+        bound = off + U.UNIT[dtype] * (want + off) + U.UNIT[dtype] * U.TINY[dtype]
+        assert ((y.double() - want).abs() <= bound).all(), size
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layouts(dtype):
+    """Slices off the 16-byte boundaries with NaN around them, transposed and
+    broadcast factors, more dimensions, results inside a larger tensor whose rest
+    stays as it was."""
+    from paper_2204_02585_amd import learn
+    gen = torch.Generator().manual_seed(5)
+    for (points, cols, units), (row, col) in (((70, 90, 40), (1, 3)), ((70, 96, 40), (2, 8)), ((3, 130, 24), (1, 1)), ((150, 64, 128), (0, 16))):
+        def inside(rows, columns):
+            big = torch.full((rows + 3, columns + 24), float("nan"), dtype=dtype, device="cuda")
+            part = big[row:row + rows, col:col + columns]
+            part.copy_(draw((rows, columns), dtype, gen))
+            return part
+        x, w, residual = inside(points, cols), inside(units, cols), inside(points, units)
+        out = torch.full((points + 5, units + 9), 7.0, dtype=dtype, device="cuda")
+        pre = out.clone()
+        y, z = out[2:2 + points, 3:3 + units], pre[1:1 + points, 4:4 + units]
+        learn.layer(x, w, None, "silu", residual, out=y, pre=z)
+        check(y, x, w, None, "silu", residual, pre=z, what=(points, cols, units))
+        y[:], z[:] = 7.0, 7.0
+        assert (out == 7.0).all() and (pre == 7.0).all()
+    x, w = draw((31, 48), dtype, gen), draw((48, 20), dtype, gen)
+    check(learn.layer(x, w.t()), x, w.t())
+    check(learn.layer(x.t(), draw((9, 31), dtype, gen)[:0].new_ones((9, 31))), x.t(), torch.ones((9, 31), dtype=dtype))
+    broad = x[:1].expand(31, 48)
+    check(learn.layer(broad, w.t(), None, None, x[:, :20]), broad, w.t(), None, None, x[:, :20])
+    cube = draw((3, 4, 5, 48), dtype, gen)
+    y = learn.layer(cube, w.t())
+    assert y.shape == (3, 4, 5, 20)
+    check(y, cube, w.t())
+    line = draw((48,), dtype, gen)
+    assert learn.layer(line, w.t()).shape == (20,)
+    check(learn.layer(line, w.t()), line[None], w.t())
+    r = draw((31, 20), dtype, gen)
+    want = learn.layer(x, w.t(), None, "relu", r)
+    assert torch.equal(learn.layer(x, w.t(), None, "relu", r, out=r), want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(2, 100, 40), (40, 100, 40), (40, 4096, 70)])
+def test_not_finite(dtype, size):
+    """A NaN or an infinity stays in its row, and products with zeros beside the
+    sum's end make none."""
+    from paper_2204_02585_amd import learn
+    x, w, bias, _ = inputs(*size, dtype)
+    clean = learn.layer(x, w, bias, "relu")
+    x2 = x.clone()
+    x2[0, 5] = float("nan")
+    x2[1, 7] = float("inf")
+    w2 = w.clone()
+    w2[:, 7] = w2[:, 7].abs() + 1
+    y = learn.layer(x2, w2, bias, "relu")
+    assert y[0].isnan().all()
+    assert (y[1] == float("inf")).all()
+    w3 = w.clone()
+    w3[3, 0] = float("inf")
+    y = learn.layer(x, w3, bias)
+    keep = [k for k in range(size[2]) if k != 3]
+    assert not torch.isfinite(y[:, 3]).any()
+    assert torch.equal(torch.relu(y[:, keep]), clean[:, keep])
+
+
+def test_large_values():
+    """Sums past binary16's largest value are infinite in it and not in binary32."""
+    from paper_2204_02585_amd import learn
+    x = torch.full((20, 64), 100.0, dtype=torch.float16, device="cuda")
+    w = torch.full((16, 64), 100.0, dtype=torch.float16, device="cuda")
+    assert (learn.layer(x, w) == float("inf")).all()
+    assert (learn.layer(x, w, dtype=torch.float32) == 640000.0).all()
+
+
+def test_same_bits_every_time():
+    from paper_2204_02585_amd import learn
+    for size in ((100, 4096, 200), (2, 3000, 100)):
+        x, w, bias, residual = inputs(*size, torch.bfloat16)
+        first = learn.layer(x, w, bias, "gelu", residual, dropout=0.1)
+        for _ in range(3):
+            assert torch.equal(learn.layer(x, w, bias, "gelu", residual, dropout=0.1), first)
+
+
+def test_empty():
+    from paper_2204_02585_amd import learn
+    w = torch.zeros((8, 16), device="cuda")
+    assert learn.layer(torch.zeros((0, 16), device="cuda"), w, activation="relu").shape == (0, 8)
+    assert learn.layer(torch.zeros((3, 0, 16), device="cuda"), w).shape == (3, 0, 8)
+
+
+def test_another_stream():
+    from paper_2204_02585_amd import learn
+    x, w, bias, _ = inputs(300, 2049, 100, torch.float32)
+    side = torch.cuda.Stream()
+    y = learn.layer(x * 2, w, bias, "relu", stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    check(y, x * 2, w, bias, "relu")
+
+
+def test_refusals():
+    from paper_2204_02585_amd import learn
+    x, w, bias, residual = inputs(4, 8, 6, torch.float32)
+    for call, kind, word in ((lambda: learn.layer(x.cpu(), w), ValueError, "x must live"),
+                             (lambda: learn.layer(x, w.cpu()), ValueError, "w must live"),
+                             (lambda: learn.layer(x, w.half()), TypeError, "one dtype"),
+                             (lambda: learn.layer(x.double(), w.double()), TypeError, "float32, float16"),
+                             (lambda: learn.layer(x, w[:, :7]), ValueError, "cols"),
+                             (lambda: learn.layer(x, w[0]), ValueError, "cols"),
+                             (lambda: learn.layer(x, w[:0]), ValueError, "units"),
+                             (lambda: learn.layer(x[:, :0], w[:, :0]), ValueError, "columns"),
+                             (lambda: learn.layer(x, w, bias[:5]), ValueError, "bias must"),
+                             (lambda: learn.layer(x, w, bias.half()), ValueError, "bias must"),
+                             (lambda: learn.layer(x, w, bias, "tanh"), ValueError, "activation"),
+                             (lambda: learn.layer(x, w, residual=residual[:3]), ValueError, "residual"),
+                             (lambda: learn.layer(x, w, residual=residual.half()), ValueError, "residual"),
+                             (lambda: learn.layer(x, w, dtype=torch.float16), TypeError, "dtype must"),
+                             (lambda: learn.layer(x.half(), w.half(), dtype=torch.bfloat16), TypeError, "dtype must"),
+                             (lambda: learn.layer(x, w, dropout=1.5), ValueError, "p must"),
+                             (lambda: learn.layer(x, w, out=residual.t()), ValueError, "out must"),
+                             (lambda: learn.layer(x, w, pre=residual.half()), ValueError, "pre must")):
+        with pytest.raises(kind, match=word):
+            call()
+    from torch.autograd import forward_ad
+    with forward_ad.dual_level(), pytest.raises(RuntimeError, match="forward-mode"):
+        learn.layer(forward_ad.make_dual(x, x), w)
