@@ -11,6 +11,7 @@
 // turn 16-bit elements on their way to the registers.  Nothing is transposed in
 // memory.
 #include <math.h>
+#include <stdlib.h>
 #include <algorithm>
 #include <type_traits>
 
@@ -47,26 +48,80 @@ struct Finish {
     Mask mask;
 };
 
-__device__ __forceinline__ float activate(float z, uint32_t act)
+// The normal distribution: its share Phi below z, and exp(-z^2 / 2).
+//
+// Phi(-a) = exp(-a^2 / 2) q(a) for a >= 0, and t = 1 / (1 + 0.35 a) takes q to the
+// whole of (0, 1]: a polynomial of degree 9 in t, fitted for the least relative
+// error (3.2e-8; 3.3e-7 with binary32's roundings), so that the values far below
+// zero keep their digits.  20 operations a value with the exponential that the
+// slope shares, where erfcf and expf took 80: of 8192 x 8192 outputs 170 us.
+__device__ __forceinline__ float normal_share(float z, float& bell)
 {
-    if (act == SQN_ACT_RELU)
-        return z < 0.0f ? 0.0f : z;
-    // erfc, not 1 + erf: below zero the sum would cancel
-    if (act == SQN_ACT_GELU)
-        return 0.5f * z * erfcf(z * -0.70710678f);
-    if (act == SQN_ACT_SILU)
-        return z / (1.0f + expf(-z));
-    return z;
+    const float a = fabsf(z);
+    bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, a, 1.0f));
+    float q = -0.029125869f;
+    q = __builtin_fmaf(q, t, 0.14387225f);
+    q = __builtin_fmaf(q, t, -0.25550461f);
+    q = __builtin_fmaf(q, t, 0.15892933f);
+    q = __builtin_fmaf(q, t, -0.022937165f);
+    q = __builtin_fmaf(q, t, 0.10543295f);
+    q = __builtin_fmaf(q, t, 0.11985243f);
+    q = __builtin_fmaf(q, t, 0.13985908f);
+    q = __builtin_fmaf(q, t, 0.13962157f);
+    q *= t * bell;
+    return z < 0.0f ? q : 1.0f - q;
 }
 
-__device__ __forceinline__ float slope(float z, uint32_t act)
+// 1 / (1 + exp(-z))
+__device__ __forceinline__ float logistic(float z)
 {
-    if (act == SQN_ACT_RELU)
-        return z <= 0.0f ? 0.0f : 1.0f;
-    if (act == SQN_ACT_GELU)
-        return 0.5f * erfcf(z * -0.70710678f) + z * expf(-0.5f * z * z) * 0.39894228f;
-    const float s = 1.0f / (1.0f + expf(-z));
-    return s * (1.0f + z * (1.0f - s));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.442695f));
+}
+
+// The choice stands outside the loops over a run, whose values then go through
+// the long chains side by side.
+template <int V>
+__device__ __forceinline__ void activate(uint32_t act, float (&v)[V])
+{
+    float bell;
+    if (act == SQN_ACT_RELU) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] = v[k] < 0.0f ? 0.0f : v[k];
+    } else if (act == SQN_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] *= normal_share(v[k], bell);
+    } else if (act == SQN_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] *= logistic(v[k]);
+    }
+}
+
+// v times the activation's slopes at z.
+template <int V>
+__device__ __forceinline__ void times_slope(uint32_t act, const float (&z)[V], float (&v)[V])
+{
+    if (act == SQN_ACT_RELU) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            v[k] = z[k] <= 0.0f ? 0.0f : v[k];
+    } else if (act == SQN_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            float bell;
+            const float share = normal_share(z[k], bell);
+            v[k] *= __builtin_fmaf(z[k] * 0.39894228f, bell, share);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float s = logistic(z[k]);
+            v[k] *= s * __builtin_fmaf(z[k], 1.0f - s, 1.0f);
+        }
+    }
 }
 
 // A run of V elements of which `left` are inside the row.
@@ -95,37 +150,68 @@ __device__ __forceinline__ void store_values(T* p, uint32_t left, const float (&
     }
 }
 
+// A run as it is loaded, turned into values later, so that many are under way
+// together.
+template <typename T, int V>
+struct Raw {
+    T e[V];
+
+    __device__ __forceinline__ void load(const T* p, uint32_t left)
+    {
+        if (left >= V) {
+            const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
+            __builtin_memcpy(e, &r, sizeof(e));
+        } else {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                e[k] = k < static_cast<int>(left) ? p[k] : T(0.0f);
+        }
+    }
+};
+
+// The bias of units unit..unit + V, zeros of none.
+template <typename X, int V>
+__device__ __forceinline__ void load_bias(const Finish& f, uint32_t unit, float (&b)[V])
+{
+    const uint32_t left = f.units - min(unit, f.units);
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        b[k] = 0.0f;
+    if (f.bias && left) {
+        if (f.bias_f32)
+            load_inside<float, V>(static_cast<const float*>(f.bias) + unit, left, b);
+        else
+            load_inside<X, V>(static_cast<const X*>(f.bias) + unit, left, b);
+    }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void load_residual(const Finish& f, uint64_t row, uint32_t unit, Raw<T, V>& r)
+{
+    if (f.residual)
+        r.load(static_cast<const T*>(f.residual) + row * f.residual_stride + unit, f.units - unit);
+}
+
 // Elements unit..unit + V of row `row` of an output of type T, from factors of
 // type X; all of a layer's epilogue, or a gradient's scale.
 template <typename X, typename T, bool LAYER, int V>
-__device__ __forceinline__ void finish(const Finish& f, uint64_t key, uint64_t row, uint32_t unit, float (&v)[V])
+__device__ __forceinline__ void finish(const Finish& f, uint64_t key, uint64_t row, uint32_t unit, const float (&bias)[V],
+                                       const Raw<T, V>& residual, float (&v)[V])
 {
     const uint32_t left = f.units - unit;
     if constexpr (LAYER) {
-        float r[V];
-        if (f.bias) {
-            if (f.bias_f32)
-                load_inside<float, V>(static_cast<const float*>(f.bias) + unit, left, r);
-            else
-                load_inside<X, V>(static_cast<const X*>(f.bias) + unit, left, r);
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                v[k] += r[k];
-        }
+        for (int k = 0; k < V; ++k)
+            v[k] += bias[k];
         if (f.pre)
             store_values<X, V>(static_cast<X*>(f.pre) + row * f.pre_stride + unit, left, v);
-        if (f.act)
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                v[k] = activate(v[k], f.act);
+        activate<V>(f.act, v);
         if (f.mask.on)
             apply_mask<V>(f.mask, key, row, unit, f.mask.scale, v);
-        if (f.residual) {
-            load_inside<T, V>(static_cast<const T*>(f.residual) + row * f.residual_stride + unit, left, r);
+        if (f.residual)
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                v[k] += r[k];
-        }
+                v[k] += to_f32(residual.e[k]);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -353,6 +439,13 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
     const uint32_t wave_p = (wave & 1) * (S::SIDE / 2), wave_q = (wave >> 1) * (S::SIDE / 2);
     const Reader<X, S::SIDE, PA, S::F> read_p(wave_p);
     const Reader<X, S::SIDE, QA, S::F> read_q(wave_q);
+    // a lane's units of the output, and how many rows a wave finishes at once
+    constexpr int V = 16 / sizeof(T);
+    constexpr uint32_t RUNS = S::F * 32 / V, ROUNDS = RUNS / 2, TOGETHER = ROUNDS < 4 ? ROUNDS : 4;
+    const uint32_t unit = p0 + wave_p + V * (lane % RUNS);
+    float bias[V];
+    if constexpr (LAYER)
+        load_bias<X, V>(p.f, unit, bias);
     float16v acc[S::F][S::F];
 #pragma unroll
     for (int s = 0; s < S::F; ++s)
@@ -380,8 +473,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
                     acc[s][t] = multiply<X>(f.p[s], f.q[t], acc[s][t]);
         });
     // out through LDS in binary32, a column of blocks at a time, so that a lane
-    // finishes a run of a row
-    constexpr int V = 16 / sizeof(T);
+    // finishes runs of rows, always of the same units
     constexpr uint32_t PITCH = S::F * 32 * 4, PIECES = PITCH / 16;
     char* own = own_part<S::F, S::BUFFER>(buffers[0], buffers[1], wave);
     const uint32_t half = lane >> 5, mine = lane & 31;
@@ -389,6 +481,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
     auto slot = [](uint32_t column, uint32_t piece) { return column * PITCH + (piece ^ (column & (PIECES - 1))) * 16; };
 #pragma unroll
     for (int t = 0; t < S::F; ++t) {
+        const uint32_t row0 = q0 + wave_q + 32 * t + lane / RUNS;
 #pragma unroll
         for (int s = 0; s < S::F; ++s)
 #pragma unroll
@@ -400,25 +493,32 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
 #pragma unroll 2
             for (uint32_t i = 0; i < PIECES / 2; ++i) {
                 const uint32_t column = (64 * i + lane) / PIECES, piece = lane & (PIECES - 1);
-                const uint32_t row = q0 + wave_q + 32 * t + column, unit = p0 + wave_p + 4 * piece;
-                if (row < p.rows && unit < p.partial_pitch)
-                    *reinterpret_cast<float4v*>(p.partial + (static_cast<uint64_t>(part) * p.rows + row) * p.partial_pitch + unit)
+                const uint32_t row = q0 + wave_q + 32 * t + column, at = p0 + wave_p + 4 * piece;
+                if (row < p.rows && at < p.partial_pitch)
+                    *reinterpret_cast<float4v*>(p.partial + (static_cast<uint64_t>(part) * p.rows + row) * p.partial_pitch + at)
                         = *reinterpret_cast<const float4v*>(own + slot(column, piece));
             }
         } else {
-#pragma unroll 2
-            for (uint32_t i = 0; i < PIECES * 2 / V; ++i) {
-                constexpr uint32_t RUNS = PIECES * 4 / V;
-                const uint32_t column = (64 * i + lane) / RUNS, run = lane & (RUNS - 1);
-                const uint32_t row = q0 + wave_q + 32 * t + column, unit = p0 + wave_p + V * run;
-                float v[V];
+#pragma unroll 1
+            for (uint32_t i0 = 0; i0 < ROUNDS; i0 += TOGETHER) {
+                Raw<T, V> residual[TOGETHER];
+                if constexpr (LAYER)
 #pragma unroll
-                for (int k = 0; k < V / 4; ++k) {
-                    const float4v e = *reinterpret_cast<const float4v*>(own + slot(column, V / 4 * run + k));
-                    __builtin_memcpy(v + 4 * k, &e, 16);
+                    for (uint32_t i = 0; i < TOGETHER; ++i)
+                        if (row0 + (i0 + i) * (64 / RUNS) < p.rows && unit < p.f.units)
+                            load_residual<T, V>(p.f, row0 + (i0 + i) * (64 / RUNS), unit, residual[i]);
+#pragma unroll
+                for (uint32_t i = 0; i < TOGETHER; ++i) {
+                    const uint32_t row = row0 + (i0 + i) * (64 / RUNS), column = (64 * (i0 + i) + lane) / RUNS;
+                    float v[V];
+#pragma unroll
+                    for (int k = 0; k < V / 4; ++k) {
+                        const float4v e = *reinterpret_cast<const float4v*>(own + slot(column, V / 4 * (lane % RUNS) + k));
+                        __builtin_memcpy(v + 4 * k, &e, 16);
+                    }
+                    if (row < p.rows && unit < p.f.units)
+                        finish<X, T, LAYER, V>(p.f, key, row, unit, bias, residual[i], v);
                 }
-                if (row < p.rows && unit < p.f.units)
-                    finish<X, T, LAYER, V>(p.f, key, row, unit, v);
             }
         }
         wave_fence();
@@ -442,7 +542,12 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
          i += static_cast<uint64_t>(gridDim.x) * kThreads) {
         const uint64_t row = i / p.per_row;
         const uint32_t unit = static_cast<uint32_t>(i - row * p.per_row) * V;
-        float v[V] = {};
+        float v[V] = {}, bias[V];
+        Raw<T, V> residual;
+        if constexpr (LAYER) {
+            load_bias<X, V>(p.f, unit, bias);
+            load_residual<T, V>(p.f, row, unit, residual);
+        }
 #pragma unroll 4
         for (uint32_t k = 0; k < p.parts; ++k) {
             const float4v e = *reinterpret_cast<const float4v*>(p.partial + (k * p.rows + row) * p.pitch + unit);
@@ -450,7 +555,7 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
             for (int r = 0; r < V; ++r)
                 v[r] += e[r];
         }
-        finish<X, T, LAYER, V>(p.f, key, row, unit, v);
+        finish<X, T, LAYER, V>(p.f, key, row, unit, bias, residual, v);
     }
 }
 
@@ -521,9 +626,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
             if (p.mask.on)
                 apply_mask<V>(p.mask, key, row, unit, 1.0f, v);
             if (p.pre)
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    v[k] *= slope(z[k], p.act);
+                times_slope<V>(p.act, z, v);
             if (p.dz)
                 store_values<X, V>(static_cast<X*>(p.dz) + row * p.pitch + unit, p.pitch - unit, v);
 #pragma unroll
@@ -546,22 +649,27 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
     }
 }
 
-// The workgroups' sums added up: 32 units a workgroup, eight threads each.
-__global__ __launch_bounds__(kThreads) void bias_kernel(const float* sums, uint32_t groups, uint32_t units, float scale, void* out,
-                                                        int32_t dtype)
+// The workgroups' sums added up: 16 units a workgroup, 64 threads each, whose
+// loads are under way together (8 threads each, one load after another, took
+// 17 us of 512 sums).
+constexpr uint32_t kSumUnits = 16, kSumSlices = 64;
+
+__global__ __launch_bounds__(kSumUnits * kSumSlices) void bias_kernel(const float* sums, uint32_t groups, uint32_t units, float scale,
+                                                                     void* out, int32_t dtype)
 {
-    __shared__ float part[8][32];
-    const uint32_t tx = threadIdx.x & 31, ty = threadIdx.x >> 5, u = blockIdx.x * 32 + tx;
+    __shared__ float part[kSumSlices][kSumUnits + 1];
+    const uint32_t tx = threadIdx.x % kSumUnits, ty = threadIdx.x / kSumUnits, u = blockIdx.x * kSumUnits + tx;
     float total = 0.0f;
-    if (u < units)
-        for (uint32_t k = ty; k < groups; k += 8)
+    if (u < units) {
+#pragma unroll 8
+        for (uint32_t k = ty; k < groups; k += kSumSlices)
             total += sums[static_cast<uint64_t>(k) * units + u];
+    }
     part[ty][tx] = total;
     __syncthreads();
     if (ty || u >= units)
         return;
-#pragma unroll
-    for (int k = 1; k < 8; ++k)
+    for (uint32_t k = 1; k < kSumSlices; ++k)
         total += part[k][tx];
     total *= scale;
     if (dtype == SQN_F32)
@@ -668,6 +776,8 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
         const int64_t most = std::max<int64_t>(1, r.steps / 8);
         r.parts = std::max<int64_t>(1, std::min({most, 512 / tiles, int64_t{64}}));
     }
+    if (const char* e = getenv("SQN_SIDE")) r.side = atoi(e);
+    if (const char* e = getenv("SQN_PARTS")) r.parts = std::max<int64_t>(1, std::min<int64_t>(r.steps, atoi(e)));
     r.part_steps = std::max<int64_t>(1, (r.steps + r.parts - 1) / r.parts);
     r.parts = std::max<int64_t>(r.steps ? 1 : 0, (r.steps + r.part_steps - 1) / r.part_steps);
     r.bytes = r.parts > 1 ? aligned(static_cast<size_t>(r.parts) * rows_q * round_up(rows_p, 4) * 4) : 0;
@@ -806,7 +916,7 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
             slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
     }
     if (to.bias)
-        bias_kernel<<<static_cast<uint32_t>((units + 31) / 32), kThreads, 0, stream>>>(sums, groups, static_cast<uint32_t>(units), m.scale,
+        bias_kernel<<<static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits), kSumUnits * kSumSlices, 0, stream>>>(sums, groups, static_cast<uint32_t>(units), m.scale,
                                                                                        to.bias, to.bias_dtype);
     Finish f{};
     f.scale = m.scale;
