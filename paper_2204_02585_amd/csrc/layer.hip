@@ -11,7 +11,6 @@
 // turn 16-bit elements on their way to the registers.  Nothing is transposed in
 // memory.
 #include <math.h>
-#include <stdlib.h>
 #include <algorithm>
 #include <type_traits>
 
@@ -29,11 +28,9 @@ typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4v lds_short4;
+typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kThreads = 256;
-
-// what steps past a sum's end bring
-__device__ const uint4 zeros = {0, 0, 0, 0};
 
 // ---- what a product's sums go through on their way out
 
@@ -247,14 +244,17 @@ __device__ __forceinline__ uint32_t across_key(uint32_t k)
         return SIDE >= 128 ? 4 * (k & 3) : 4 * (k >> 1 & 1);
 }
 
-// What a lane brings of a factor's steps.
+// What a lane brings of a factor's steps, through a buffer descriptor of the
+// tile's rows: pieces past the sum's end lie past the descriptor's, and come as
+// zeros without an access.
 template <typename X, int SIDE, int WAVES, bool ACROSS>
 struct Bringer {
     static constexpr int COUNT = SIDE * static_cast<int>(kStepBytes) / (1024 * WAVES);
     static constexpr uint32_t SLOTS = SIDE * sizeof(X) / kSlot;  // of a row across
     static constexpr uint32_t LINES = 64 / (SLOTS < 64 ? SLOTS : 64);            // of an instruction, across
+    static constexpr uint32_t OUTSIDE = 0x80000000u;             // a tile's rows span less (in_place)
     const char* from;
-    uint32_t at[COUNT], place[COUNT];
+    uint32_t at[COUNT], place[ACROSS ? COUNT : 1];
     uint32_t valid;
     uint64_t on;                 // bytes from step to step
 
@@ -266,36 +266,44 @@ struct Bringer {
             static_assert(SLOTS <= 64, "a row of a step is one instruction's at most");
             from = o.data + static_cast<uint64_t>(row0) * sizeof(X);
             on = o.pitch * Elements<X>::STEP;
-            const uint32_t last = (o.rows - row0) / Elements<X>::PIECE - 1;
+            const uint32_t pieces = (o.rows - row0) / Elements<X>::PIECE;
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const uint32_t k = (WAVES * i + wave) * LINES + lane / SLOTS;
-                const uint32_t piece = min(lane % SLOTS ^ across_key<X, SIDE>(k), last);
+                const uint32_t piece = lane % SLOTS ^ across_key<X, SIDE>(k);
                 place[i] = k;
-                at[i] = k * static_cast<uint32_t>(o.pitch) + piece * kSlot;
+                at[i] = piece < pieces ? k * static_cast<uint32_t>(o.pitch) + piece * kSlot : OUTSIDE;
             }
         } else {
             from = o.data + row0 * o.pitch;
             on = kStepBytes;
-            const uint32_t piece = brought_piece(lane, wave) * kSlot;
+            place[0] = brought_piece(lane, wave) * kSlot;
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
                 const uint32_t row = 8 * (WAVES * i + wave) + (lane >> 3);
-                place[i] = piece;
-                at[i] = min(row, o.rows - 1 - row0) * static_cast<uint32_t>(o.pitch) + piece;
+                at[i] = row < o.rows - row0 ? row * static_cast<uint32_t>(o.pitch) + place[0] : OUTSIDE;
             }
         }
     }
 
-    // pieces past the sum's end are zeros
-    __device__ __forceinline__ void bring_step(uint32_t step, char* to) const
+    // the rows of a step, and how much of the sum is left from it on
+    struct Step {
+        __amdgpu_buffer_rsrc_t rows;
+        uint32_t left;
+    };
+
+    __device__ __forceinline__ Step step(uint32_t k) const
+    {
+        // raw bytes, OUTSIDE of them
+        return {__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from + k * on), 0, OUTSIDE, 0x00020000),
+                valid - k * (ACROSS ? Elements<X>::STEP : kStepBytes)};
+    }
+
+    __device__ __forceinline__ void bring(const Step& s, int i, char* to) const
     {
         const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const char* base = from + step * on;
-        const uint32_t left = valid - step * (ACROSS ? Elements<X>::STEP : kStepBytes);
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i)
-            bring(place[i] < left ? base + at[i] : reinterpret_cast<const char*>(&zeros), to + (WAVES * i + wave) * 1024);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(s.rows, (lds_void*)(to + (WAVES * i + wave) * 1024), kSlot,
+                                                 place[ACROSS ? i : 0] < s.left ? at[i] : OUTSIDE, 0, 0, 0);
     }
 };
 
@@ -327,41 +335,39 @@ struct Reader {
         }
     }
 
-    __device__ __forceinline__ void read(uint4 (&f)[F], const char* buffer, uint32_t o) const
+    // block s at depth o
+    __device__ __forceinline__ uint4 read(const char* buffer, int s, uint32_t o) const
     {
-        const uint32_t lane = threadIdx.x & 63;
+        uint4 f;
+        if constexpr (!ACROSS) {
+            f = *reinterpret_cast<const uint4*>(buffer + at[s] + piece_at(threadIdx.x & 63, o));
+        } else if constexpr (sizeof(X) == 4) {
+            const char* p = buffer + at[s] + 4 * o * SIDE * 4;
+            auto word = [&](int k) { return *reinterpret_cast<const uint32_t*>(p + k * SIDE * 4); };
+            f = uint4{word(0), word(1), word(2), word(3)};
+        } else {
+            // places 8 o and 8 o + 4 on: rows a of each four keep their key
+            const char* p = buffer + at[s] + 8 * o * SIDE * 2;
+            short4v e[2];
 #pragma unroll
-        for (int s = 0; s < F; ++s) {
-            if constexpr (!ACROSS) {
-                f[s] = *reinterpret_cast<const uint4*>(buffer + at[s] + piece_at(lane, o));
-            } else if constexpr (sizeof(X) == 4) {
-                const char* p = buffer + at[s] + 4 * o * SIDE * 4;
-                auto word = [&](int k) { return *reinterpret_cast<const uint32_t*>(p + k * SIDE * 4); };
-                f[s] = uint4{word(0), word(1), word(2), word(3)};
-            } else {
-                // places 8 o and 8 o + 4 on: rows a of each four keep their key
-                const char* p = buffer + at[s] + 8 * o * SIDE * 2;
-                short4v e[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    e[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p + 4 * k * SIDE * 2));
-                __builtin_memcpy(&f[s], e, 16);
-            }
+            for (int k = 0; k < 2; ++k)
+                e[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(p + 4 * k * SIDE * 2));
+            __builtin_memcpy(&f, e, 16);
         }
+        return f;
     }
 };
 
+// Element `e` of binary32 pieces, whose instructions take one of a lane; all of
+// 16-bit ones.
 template <typename X>
-__device__ __forceinline__ float16v multiply(const uint4& a, const uint4& b, float16v acc)
+__device__ __forceinline__ float16v multiply(const uint4& a, const uint4& b, int e, float16v acc)
 {
     if constexpr (sizeof(X) == 4) {
         float4v u, v;
         __builtin_memcpy(&u, &a, 16);
         __builtin_memcpy(&v, &b, 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(u[k], v[k], acc, 0, 0, 0);
-        return acc;
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], v[e], acc, 0, 0, 0);
     } else if constexpr (std::is_same_v<X, __bf16>) {
         bhalf8 u, v;
         __builtin_memcpy(&u, &a, 16);
@@ -406,8 +412,91 @@ struct ProductParams {
 
 template <typename S>
 struct Fragments {
-    uint4 p[S::F], q[S::F];
+    uint4 f[2 * S::F];           // of P, then of Q
 };
+
+// The steps of a tile's sum, in the order of tile.h's, with every instruction in
+// its place: behind each product stand a share of the next depth's reads and,
+// at a step's last depth, of the loads into the buffer that it leaves.  With one
+// wave a SIMD whatever stands in a block of its own leaves the matrix cores idle
+// (the compiler's order: 1,040 TFLOP/s of 8192 x 8192 by 4096 in bfloat16).
+template <typename S, typename X, typename BP, typename BQ, typename RP, typename RQ>
+__device__ __forceinline__ void sum_steps(const BP& bring_p, const BQ& bring_q, const RP& read_p, const RQ& read_q, uint32_t first,
+                                          uint32_t steps, char* (&buffers)[S::BUFFERS], float16v (&acc)[S::F][S::F])
+{
+    constexpr int F = S::F, BUFFERS = S::BUFFERS, LOADS = S::LOADS;
+    constexpr int PRODUCTS = F * F * (sizeof(X) == 4 ? 4 : 1);   // of a depth
+    const uint32_t end = first + steps - 1;
+    Fragments<S> f0, f1;
+    auto read_block = [&](Fragments<S>& f, const char* buffer, int k, uint32_t o) {
+        f.f[k] = k < F ? read_p.read(buffer, k, o) : read_q.read(buffer + S::ROWS, k - F, o);
+    };
+    auto bring = [&](const typename BP::Step& p, const typename BQ::Step& q, int i, char* buffer) {
+        if (i < BP::COUNT)
+            bring_p.bring(p, i, buffer);
+        else
+            bring_q.bring(q, i - BP::COUNT, buffer + S::ROWS);
+    };
+    // the products of a depth; `next` of `from` at depth o is read behind them, and
+    // with LOAD step k comes into `to`
+    auto depth = [&](const Fragments<S>& f, Fragments<S>& next, const char* from, uint32_t o, auto load, uint32_t k, char* to) {
+        constexpr bool LOAD = decltype(load)::value;
+        const auto step_p = bring_p.step(k);
+        const auto step_q = bring_q.step(k);
+        int reads = 0, loads = 0;
+#pragma unroll
+        for (int m = 0; m < PRODUCTS; ++m) {
+            const int s = m / F % F, t = m % F;
+            acc[s][t] = multiply<X>(f.f[s], f.f[F + t], m / (F * F), acc[s][t]);
+            // the reads are done by the middle of the depth
+#pragma unroll
+            for (; reads < 2 * F && reads * PRODUCTS < (m + 1) * 4 * F; ++reads)
+                read_block(next, from, reads, o);
+            if constexpr (LOAD) {
+#pragma unroll
+                for (; loads * PRODUCTS < (m + 1) * LOADS; ++loads)
+                    bring(step_p, step_q, loads, to);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+#pragma unroll
+    for (int b = 0; b < BUFFERS; ++b) {
+        const uint32_t k = min(first + b, end);
+        const auto step_p = bring_p.step(k);
+        const auto step_q = bring_q.step(k);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            bring(step_p, step_q, i, buffers[b]);
+    }
+    landed<(BUFFERS - 1) * LOADS>();
+#pragma unroll
+    for (int k = 0; k < 2 * F; ++k)
+        read_block(f0, buffers[0], k, 0);
+    constexpr std::false_type no{};
+    constexpr std::true_type yes{};
+    // buffer b holds step k and will hold k + BUFFERS; past the end the last step
+    // comes once more and is not used
+    auto work = [&](uint32_t k, int b) {
+        depth(f0, f1, buffers[b], 1, no, 0, nullptr);
+        depth(f1, f0, buffers[b], 2, no, 0, nullptr);
+        depth(f0, f1, buffers[b], 3, no, 0, nullptr);
+        landed<(BUFFERS - 2) * LOADS>();
+        depth(f1, f0, buffers[(b + 1) % BUFFERS], 0, yes, min(k + BUFFERS, end), buffers[b]);
+    };
+    uint32_t k = first;
+    for (; k + BUFFERS <= end + 1; k += BUFFERS) {
+#pragma unroll
+        for (int b = 0; b < BUFFERS; ++b)
+            work(k + b, b);
+    }
+#pragma unroll
+    for (int b = 0; b < BUFFERS - 1; ++b)
+        if (k + b <= end)
+            work(k + b, b);
+    // the loads still under way end before their buffers do
+    landed<0>();
+}
 
 // Workgroups that follow each other go to the eight XCDs in turn: each takes a
 // run of tiles, in columns of 8 tiles of Q, so that what its CUs work on at a time
@@ -453,25 +542,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
         for (int t = 0; t < S::F; ++t)
             acc[s][t] = float16v{};
     const uint32_t first = part * p.part_steps, count = min(p.part_steps, p.steps - first);
-    pipeline<S::LOADS, Fragments<S>>(
-        count, buffers, [](uint32_t, int) {},
-        [&](uint32_t k, char* buffer) {
-            bring_p.bring_step(first + k, buffer);
-            bring_q.bring_step(first + k, buffer + S::ROWS);
-            // the loads stay ahead of the products that hide them
-            __builtin_amdgcn_sched_barrier(0);
-        },
-        [&](Fragments<S>& f, const char* buffer, uint32_t o) {
-            read_p.read(f.p, buffer, o);
-            read_q.read(f.q, buffer + S::ROWS, o);
-        },
-        [&](const Fragments<S>& f, int) {
-#pragma unroll
-            for (int s = 0; s < S::F; ++s)
-#pragma unroll
-                for (int t = 0; t < S::F; ++t)
-                    acc[s][t] = multiply<X>(f.p[s], f.q[t], acc[s][t]);
-        });
+    sum_steps<S, X>(bring_p, bring_q, read_p, read_q, first, count, buffers, acc);
     // out through LDS in binary32, a column of blocks at a time, so that a lane
     // finishes runs of rows, always of the same units
     constexpr uint32_t PITCH = S::F * 32 * 4, PIECES = PITCH / 16;
@@ -776,8 +847,6 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
         const int64_t most = std::max<int64_t>(1, r.steps / 8);
         r.parts = std::max<int64_t>(1, std::min({most, 512 / tiles, int64_t{64}}));
     }
-    if (const char* e = getenv("SQN_SIDE")) r.side = atoi(e);
-    if (const char* e = getenv("SQN_PARTS")) r.parts = std::max<int64_t>(1, std::min<int64_t>(r.steps, atoi(e)));
     r.part_steps = std::max<int64_t>(1, (r.steps + r.parts - 1) / r.parts);
     r.parts = std::max<int64_t>(r.steps ? 1 : 0, (r.steps + r.part_steps - 1) / r.part_steps);
     r.bytes = r.parts > 1 ? aligned(static_cast<size_t>(r.parts) * rows_q * round_up(rows_p, 4) * 4) : 0;
