@@ -499,14 +499,16 @@ __device__ __forceinline__ void sum_steps(const BP& bring_p, const BQ& bring_q, 
 }
 
 // Workgroups that follow each other go to the eight XCDs in turn: each takes a
-// run of tiles, in columns of 8 tiles of Q, so that what its CUs work on at a time
-// shares rows of both factors in the XCD's cache.
-__device__ __forceinline__ void tile_of(uint32_t group, uint32_t tiles_p, uint32_t tiles_q, uint32_t& tp, uint32_t& tq)
+// run of the parts' tiles, in columns of 8 tiles of Q, so that what its CUs work
+// on at a time shares rows of both factors in the XCD's cache.
+__device__ __forceinline__ void tile_of(uint32_t tiles_p, uint32_t tiles_q, uint32_t& part, uint32_t& tp, uint32_t& tq)
 {
     constexpr uint32_t kXcds = 8, kBand = 8;
-    const uint32_t all = tiles_p * tiles_q, each = all / kXcds, more = all % kXcds;
-    const uint32_t xcd = group % kXcds, nth = group / kXcds;
-    const uint32_t t = xcd * each + min(xcd, more) + nth;
+    const uint32_t each = gridDim.x / kXcds, more = gridDim.x % kXcds;
+    const uint32_t xcd = blockIdx.x % kXcds, nth = blockIdx.x / kXcds;
+    const uint32_t all = xcd * each + min(xcd, more) + nth;
+    part = all / (tiles_p * tiles_q);
+    const uint32_t t = all - part * tiles_p * tiles_q;
     const uint32_t band = t / (kBand * tiles_p), in_band = t - band * kBand * tiles_p;
     const uint32_t width = min(kBand, tiles_q - band * kBand);
     tp = in_band / width;
@@ -518,10 +520,8 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
 {
     BUFFERS_IN_LDS(S)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tiles = p.tiles_p * p.tiles_q;
-    const uint32_t part = blockIdx.x / tiles;
-    uint32_t tp, tq;
-    tile_of(blockIdx.x - part * tiles, p.tiles_p, p.tiles_q, tp, tq);
+    uint32_t part, tp, tq;
+    tile_of(p.tiles_p, p.tiles_q, part, tp, tq);
     const uint32_t p0 = tp * S::SIDE, q0 = tq * S::SIDE;
     const Bringer<X, S::SIDE, S::WAVES, PA> bring_p(p.p, p0);
     const Bringer<X, S::SIDE, S::WAVES, QA> bring_q(p.q, q0);
@@ -829,26 +829,44 @@ struct Plan {
 
 int64_t tiles_of(int64_t rows_p, int64_t rows_q, int64_t side) { return (rows_p + side - 1) / side * ((rows_q + side - 1) / side); }
 
-// A larger tile is taken where there are enough of it for most of the CUs; a
-// product of few tiles is split along its sum.
+// Tiles and parts by what they take, in us: the rounds of workgroups on 256 CUs,
+// each the steps of a part and a start and an end, and a launch and the bytes of the
+// parts' sums behind them.  A step's time is the CU's matrix cores' in the largest
+// tiles and for binary32, and what L2 delivers in the smaller ones; two workgroups
+// share a CU without getting through more steps.  (us by side, 64, 128 and 256, of
+// bfloat16: 4096 points of 256 by 256 5, 7 and 20; 65,536 40, 23 and 26; 2048 of 4096
+// by 2048 54, 44 and 87; 8192 of 1024 by 1024 35, 23 and 36; of binary32: 65,536 of
+// 256 by 256 89, 77 and 82; 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and
+// 16, 17 points of 4096 by 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384
+// points 58, 20 and 14.)
 Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
 {
-    Plan r{};
+    constexpr int64_t kSides[3] = {64, 128, 256}, kMostParts = 64, kCus = 256;
+    constexpr double kStep[2][3] = {{0.26, 0.58, 1.32}, {0.51, 1.85, 7.2}}, kEnds[3] = {1.5, 3.0, 18.0};
+    constexpr double kJoin = 3.0, kJoinBytes = 3.5e6;            // a us
+    const int f32 = dtype == SQN_F32 ? 1 : 0;
     const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
-    r.steps = (sum + step - 1) / step;
-    r.parts = 1;
-    if (tiles_of(rows_p, rows_q, 256) >= 200) {
-        r.side = 256;
-    } else if (tiles_of(rows_p, rows_q, 128) >= 200) {
-        r.side = 128;
-    } else {
-        r.side = std::min(rows_p, rows_q) > 64 && r.steps >= 64 ? 128 : 64;
-        const int64_t tiles = std::max<int64_t>(1, tiles_of(rows_p, rows_q, r.side));
-        const int64_t most = std::max<int64_t>(1, r.steps / 8);
-        r.parts = std::max<int64_t>(1, std::min({most, 512 / tiles, int64_t{64}}));
+    const int64_t steps = (sum + step - 1) / step;
+    Plan r{64, steps, std::max<int64_t>(1, steps), steps ? 1 : 0, 0};
+    double least = HUGE_VAL;
+    for (int s = 0; steps && s < 3; ++s) {
+        const int64_t tiles = tiles_of(rows_p, rows_q, kSides[s]);
+        for (int64_t parts = 1; parts <= std::min(kMostParts, steps); parts *= 2) {
+            const int64_t each = (steps + parts - 1) / parts, used = (steps + each - 1) / each;
+            const double sums = used > 1 ? 2.0 * used * 4.0 * rows_q * round_up(rows_p, 4) : 0.0;
+            const double time = static_cast<double>((tiles * used + kCus - 1) / kCus) * (each * kStep[f32][s] + kEnds[s])
+                + (used > 1 ? kJoin + sums / kJoinBytes : 0.0);
+            if (time < least) {
+                least = time;
+                r.side = kSides[s];
+                r.part_steps = each;
+                r.parts = used;
+            }
+            // further parts only add rounds
+            if (tiles * parts >= 2 * kCus)
+                break;
+        }
     }
-    r.part_steps = std::max<int64_t>(1, (r.steps + r.parts - 1) / r.parts);
-    r.parts = std::max<int64_t>(r.steps ? 1 : 0, (r.steps + r.part_steps - 1) / r.part_steps);
     r.bytes = r.parts > 1 ? aligned(static_cast<size_t>(r.parts) * rows_q * round_up(rows_p, 4) * 4) : 0;
     return r;
 }
