@@ -630,6 +630,174 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
     }
 }
 
+// ---- layers of few points
+//
+// For one token's points the weights' bytes are all that takes time.  A
+// workgroup computes 16 units of all points, or 32 or 64 where there are many
+// units (its waves read the points' elements once for each), on the 16 x 16
+// instructions; its waves take the sum's pieces in turn, straight from memory to
+// registers at any alignment, and add up in LDS, in the order of the waves.
+
+constexpr int kFewPoints = 16, kFewWaves = 8;
+
+struct FewParams {
+    const void *x, *w;
+    int64_t x_stride, w_stride;  // elements
+    uint32_t points, cols;
+    Finish f;
+};
+
+// A lane's elements of an instruction's 16 rows: 16 bytes of row lane % 16, those
+// of piece lane / 16 of four.
+template <typename X>
+struct Sixteen {
+    static constexpr uint32_t N = 16 / sizeof(X), ALL = 4 * N;
+
+    static __device__ __forceinline__ uint4 whole(const X* p)
+    {
+        const Run<X, N> r = *reinterpret_cast<const Run<X, N>*>(p);
+        uint4 v;
+        __builtin_memcpy(&v, &r, 16);
+        return v;
+    }
+
+    static __device__ __forceinline__ uint4 ragged(const X* p, uint32_t left)
+    {
+        X e[N];
+#pragma unroll
+        for (uint32_t k = 0; k < N; ++k)
+            e[k] = k < left ? p[k] : X(0.0f);
+        uint4 v;
+        __builtin_memcpy(&v, e, 16);
+        return v;
+    }
+
+    static __device__ __forceinline__ float4v multiply(const uint4& a, const uint4& b, float4v acc)
+    {
+        if constexpr (sizeof(X) == 4) {
+            float4v u, v;
+            __builtin_memcpy(&u, &a, 16);
+            __builtin_memcpy(&v, &b, 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u[k], v[k], acc, 0, 0, 0);
+            return acc;
+        } else if constexpr (std::is_same_v<X, __bf16>) {
+            bhalf8 u, v;
+            __builtin_memcpy(&u, &a, 16);
+            __builtin_memcpy(&v, &b, 16);
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, v, acc, 0, 0, 0);
+        } else {
+            half8 u, v;
+            __builtin_memcpy(&u, &a, 16);
+            __builtin_memcpy(&v, &b, 16);
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(u, v, acc, 0, 0, 0);
+        }
+    }
+};
+
+template <typename X, typename T, int BLOCKS>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewParams p)
+{
+    typedef Sixteen<X> S;
+    constexpr int UNITS = 16 * BLOCKS, V = 4, TOGETHER = 8 / BLOCKS;
+    __shared__ __align__(16) float part[kFewWaves][kFewPoints][UNITS + 4];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const uint32_t unit0 = blockIdx.x * UNITS, mine = lane & 15, at = lane / 16 * S::N;
+    // rows past the ends read the last one, and are not stored
+    const X* x = static_cast<const X*>(p.x) + min(mine, p.points - 1) * p.x_stride + at;
+    const X* w[BLOCKS];
+    float4v acc[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        w[b] = static_cast<const X*>(p.w) + min(unit0 + 16 * b + mine, p.f.units - 1) * p.w_stride + at;
+        acc[b] = float4v{};
+    }
+    // two pieces that follow each other, lines of the rows, are one wave's
+    const uint32_t full = p.cols / S::ALL;
+    uint32_t k = 2 * wave;
+    auto piece = [&](int i) { return k + i / 2 * 2 * waves + i % 2; };
+    for (; piece(TOGETHER - 1) < full; k += TOGETHER * waves) {
+        uint4 of_x[TOGETHER], of_w[TOGETHER][BLOCKS];
+#pragma unroll
+        for (int i = 0; i < TOGETHER; ++i) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+                of_w[i][b] = S::whole(w[b] + piece(i) * S::ALL);
+            of_x[i] = S::whole(x + piece(i) * S::ALL);
+        }
+#pragma unroll
+        for (int i = 0; i < TOGETHER; ++i)
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+                acc[b] = S::multiply(of_w[i][b], of_x[i], acc[b]);
+    }
+    for (; k <= full; k += 2 * waves)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t from = (k + i) * S::ALL;
+            if (k + i < full) {
+                const uint4 of_x = S::whole(x + from);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+                    acc[b] = S::multiply(S::whole(w[b] + from), of_x, acc[b]);
+            } else if (k + i == full && from < p.cols) {
+                const uint32_t left = from + at < p.cols ? p.cols - from - at : 0;
+                const uint4 of_x = S::ragged(x + from, left);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+                    acc[b] = S::multiply(S::ragged(w[b] + from, left), of_x, acc[b]);
+            }
+        }
+    // a lane holds units 4 (lane / 16) .. + 3 of point lane % 16
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+        *reinterpret_cast<float4v*>(&part[wave][mine][16 * b + lane / 16 * 4]) = acc[b];
+    const uint32_t row = threadIdx.x / (UNITS / V), run = threadIdx.x % (UNITS / V) * V;
+    const bool inside = row < p.points && unit0 + run < p.f.units;
+    float bias[V];
+    Raw<T, V> residual;
+    uint64_t key = 0;
+    if (inside) {
+        load_bias<X, V>(p.f, unit0 + run, bias);
+        load_residual<T, V>(p.f, row, unit0 + run, residual);
+        key = p.f.mask.on ? mask_key(p.f.mask) : 0;
+    }
+    __syncthreads();
+    if (!inside)
+        return;
+    float4v total = *reinterpret_cast<const float4v*>(&part[0][row][run]);
+    for (uint32_t i = 1; i < waves; ++i)
+        total += *reinterpret_cast<const float4v*>(&part[i][row][run]);
+    float v[V];
+    __builtin_memcpy(v, &total, 16);
+    finish<X, T, true, V>(p.f, key, row, unit0 + run, bias, residual, v);
+}
+
+template <typename X, typename T>
+void launch_few(const sqn_matrix& x, const sqn_matrix& w, const Finish& f, hipStream_t stream)
+{
+    FewParams p;
+    p.x = x.data;
+    p.w = w.data;
+    p.x_stride = x.row_stride;
+    p.w_stride = w.row_stride;
+    p.points = static_cast<uint32_t>(x.rows);
+    p.cols = static_cast<uint32_t>(x.cols);
+    p.f = f;
+    // a wave for every four pieces of the sum; 64 threads finish each 16 units, so
+    // larger workgroups have as many waves at least
+    const int blocks = f.units >= 64 * 512 ? 4 : f.units >= 32 * 512 ? 2 : 1;
+    const uint32_t waves = std::clamp<uint32_t>((p.cols + 4 * Sixteen<X>::ALL - 1) / (4 * Sixteen<X>::ALL), blocks, kFewWaves);
+    const uint32_t groups = (f.units + 16 * blocks - 1) / (16 * blocks);
+    if (blocks == 4)
+        few_kernel<X, T, 4><<<groups, 64 * waves, 0, stream>>>(p);
+    else if (blocks == 2)
+        few_kernel<X, T, 2><<<groups, 64 * waves, 0, stream>>>(p);
+    else
+        few_kernel<X, T, 1><<<groups, 64 * waves, 0, stream>>>(p);
+}
+
 // ---- factors that do not lie on 16-byte boundaries, copied to where they do
 
 struct PackParams {
@@ -670,11 +838,23 @@ struct SlopeParams {
     const void *grad, *pre;      // pre: null without an activation
     void* dz;                    // [points][pitch] of the factors' type, zeros past the units, or null
     float* sums;                 // [groups down][units] or null
+    void* bias;                  // the sums themselves, where there is one group
+    int32_t bias_dtype;
     int64_t grad_stride, pre_stride;
     uint32_t points, units, pitch, rows, act;     // rows: of a workgroup
     uint32_t across;             // threads along a row: a power of two
     Mask mask;                   // its scale is applied to the products and sums: dz stays in a binary16's range
 };
+
+__device__ __forceinline__ void store_bias(void* out, uint32_t u, float v, int32_t dtype)
+{
+    if (dtype == SQN_F32)
+        static_cast<float*>(out)[u] = v;
+    else if (dtype == SQN_F16)
+        static_cast<_Float16*>(out)[u] = from_f32<_Float16>(v);
+    else
+        static_cast<__bf16*>(out)[u] = from_f32<__bf16>(v);
+}
 
 template <typename X, typename G>
 __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
@@ -689,6 +869,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
     const uint32_t left = unit < p.units ? p.units - unit : 0;
     float sum[V] = {};
     if (unit < p.pitch)
+#pragma unroll 2
         for (uint64_t row = row0 + ty; row < end; row += down) {
             float v[V], z[V];
             load_inside<G, V>(static_cast<const G*>(p.grad) + row * p.grad_stride + unit, left, v);
@@ -704,7 +885,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
             for (int k = 0; k < V; ++k)
                 sum[k] += v[k];
         }
-    if (!p.sums)
+    if (!p.sums && !p.bias)
         return;
 #pragma unroll
     for (int k = 0; k < V; ++k)
@@ -712,10 +893,15 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < p.across * V; c += kThreads) {
         float total = 0.0f;
+#pragma unroll 8
         for (uint32_t k = 0; k < down; ++k)
             total += part[k * p.across + c / V][c % V];
         const uint32_t u = blockIdx.x * p.across * V + c;
-        if (u < p.units)
+        if (u >= p.units)
+            continue;
+        if (p.bias)
+            store_bias(p.bias, u, total * p.mask.scale, p.bias_dtype);
+        else
             p.sums[static_cast<uint64_t>(blockIdx.y) * p.units + u] = total;
     }
 }
@@ -742,13 +928,7 @@ __global__ __launch_bounds__(kSumUnits * kSumSlices) void bias_kernel(const floa
         return;
     for (uint32_t k = 1; k < kSumSlices; ++k)
         total += part[k][tx];
-    total *= scale;
-    if (dtype == SQN_F32)
-        static_cast<float*>(out)[u] = total;
-    else if (dtype == SQN_F16)
-        static_cast<_Float16*>(out)[u] = from_f32<_Float16>(total);
-    else
-        static_cast<__bf16*>(out)[u] = from_f32<__bf16>(total);
+    store_bias(out, u, total * scale, dtype);
 }
 
 // ---- choices
@@ -919,18 +1099,34 @@ void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t 
 template <typename X, typename T>
 void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& f, char* work, hipStream_t stream)
 {
+    if (x.rows <= kFewPoints) {
+        launch_few<X, T>(x, w, f, stream);
+        return;
+    }
     const sqn_matrix a = packed(w, work, stream), b = packed(x, work, stream);
     launch_product<X, T, true, false, false>(along(a), along(b), x.rows, x.cols, f, work, x.dtype, stream);
 }
 
-// Workgroups of slope_kernel down the points, and the rows of one: the sums of
-// at most 512 groups are added up behind it.
-uint32_t slope_rows(int64_t points, int64_t units)
-{
-    const int64_t wide = (units + 255) / 256;
-    const int64_t groups = std::clamp<int64_t>(2048 / wide, 1, 512);
-    return static_cast<uint32_t>(std::max<int64_t>(32, (points + groups - 1) / groups));
-}
+// Workgroups of slope_kernel: `across` threads of one along a row, `rows` of it,
+// `groups` down the points.  Few points are one group, whose sums are the bias's
+// gradient; else some 2048 workgroups, at most 512 groups, whose sums a launch
+// behind it adds up.
+struct SlopePlan {
+    uint32_t across, rows, groups;
+
+    SlopePlan(int64_t points, int64_t units)
+    {
+        const int64_t runs = (units + 7) / 8;
+        const bool few = points <= 256;
+        across = 1;
+        while (across < (few ? 8 : 32) && across < runs)
+            across *= 2;
+        const int64_t wide = (runs + across - 1) / across, down = kThreads / across;
+        const int64_t most = few ? 1 : std::clamp<int64_t>(2048 / wide, 1, 512);
+        rows = static_cast<uint32_t>(std::max((points + most - 1) / most, std::min<int64_t>(points, 4 * down)));
+        groups = rows ? static_cast<uint32_t>((points + rows - 1) / rows) : 0;
+    }
+};
 
 // What a gradient keeps in its workspace, in this order.
 struct GradientScratch {
@@ -943,11 +1139,8 @@ struct GradientScratch {
         own_dz = (for_x || for_w) && (slopes || grad.dtype != x_.dtype || !in_place(grad));
         const int64_t piece = kSlot / static_cast<int64_t>(element_size(x_.dtype));
         dz = own_dz ? aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype)) : 0;
-        sums = 0;
-        if (for_bias && points) {
-            const int64_t rows = slope_rows(points, units);
-            sums = aligned(static_cast<size_t>((points + rows - 1) / rows) * units * 4);
-        }
+        const uint32_t groups = SlopePlan(points, units).groups;
+        sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
         x = for_w ? pack_bytes(x_) : 0;
         w = for_x ? pack_bytes(w_) : 0;
         partial = std::max(for_x ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
@@ -976,8 +1169,8 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         dz.dtype = x.dtype;
         dz.cols = dz.row_stride = round_up(units, Elements<X>::PIECE);
     }
-    uint32_t groups = 0;
-    if (points && (scratch.own_dz || sums)) {
+    const SlopePlan plan(points, units);
+    if (points && (scratch.own_dz || to.bias)) {
         SlopeParams p{};
         p.grad = grad.data;
         p.grad_stride = grad.row_stride;
@@ -988,22 +1181,22 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         p.points = static_cast<uint32_t>(points);
         p.units = static_cast<uint32_t>(units);
         p.pitch = static_cast<uint32_t>(scratch.own_dz ? dz.cols : units);
-        p.rows = slope_rows(points, units);
+        p.rows = plan.rows;
+        p.across = plan.across;
+        if (to.bias && plan.groups == 1) {
+            p.bias = to.bias;
+            p.bias_dtype = to.bias_dtype;
+        }
         p.act = static_cast<uint32_t>(act);
         p.mask = m;
-        const uint32_t runs = (p.pitch + 7) / 8;
-        p.across = 1;
-        while (p.across < 32 && p.across < runs)
-            p.across *= 2;
-        groups = (p.points + p.rows - 1) / p.rows;
-        const dim3 grid((runs + p.across - 1) / p.across, groups);
+        const dim3 grid(((p.pitch + 7) / 8 + p.across - 1) / p.across, plan.groups);
         if (grad.dtype == SQN_F32)
             slope_kernel<X, float><<<grid, kThreads, 0, stream>>>(p);
         else
             slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
     }
-    if (to.bias)
-        bias_kernel<<<static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits), kSumUnits * kSumSlices, 0, stream>>>(sums, groups, static_cast<uint32_t>(units), m.scale,
+    if (to.bias && plan.groups != 1)
+        bias_kernel<<<static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits), kSumUnits * kSumSlices, 0, stream>>>(sums, plan.groups, static_cast<uint32_t>(units), m.scale,
                                                                                        to.bias, to.bias_dtype);
     Finish f{};
     f.scale = m.scale;
@@ -1027,6 +1220,8 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
 
 size_t layer_bytes(const sqn_matrix& x, const sqn_matrix& w)
 {
+    if (x.rows <= kFewPoints)
+        return 0;
     return pack_bytes(x) + pack_bytes(w) + plan_of(w.rows, x.rows, x.cols, x.dtype).bytes;
 }
 

@@ -101,6 +101,8 @@ def _tangent(t: torch.Tensor) -> Optional[torch.Tensor]:
 
 def _no_tangent(what: str, *tensors) -> None:
     """A raw pointer would drop it without a word."""
+    if getattr(forward_ad, "_current_level", 0) < 0:
+        return
     if any(t is not None and _tangent(t) is not None for t in tensors):
         raise RuntimeError(f"{what} has no forward-mode derivative")
 
@@ -353,23 +355,26 @@ def _mask(p: float, seed: int, step: Optional[torch.Tensor], beside: torch.Tenso
     return binding.DropoutMask(p, int(seed) & 0xFFFFFFFFFFFFFFFF, _ptr(step))
 
 
-def _beside(t: Optional[torch.Tensor], shape, dtype, beside: torch.Tensor, name: str) -> None:
-    if t is None:
-        return
+def _beside(t: torch.Tensor, shape, dtype, beside: torch.Tensor, name: str) -> None:
     _on_gpu(t, name, beside)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
 def _wants_gradient(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _dropout(x, p, seed, step, residual, out, stream):
     _on_gpu(x, "x")
     if x.dim() == 0:
         raise ValueError("x must have a dimension")
-    _beside(residual, x.shape, x.dtype, x, "residual")
+    if residual is not None:
+        _beside(residual, x.shape, x.dtype, x, "residual")
     mask = _mask(p, seed, step, x)
     out = _out(out, x.shape, x.dtype, x)
     if out.numel() == 0:
@@ -442,45 +447,51 @@ def _factors(x: torch.Tensor, w: torch.Tensor) -> None:
         raise TypeError(f"x and w must have one dtype, got {x.dtype} and {w.dtype}")
 
 
-def _bias(bias: Optional[torch.Tensor], w: torch.Tensor) -> Optional[torch.Tensor]:
-    if bias is None:
-        return None
+def _bias(bias: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     _on_gpu(bias, "bias", w)
-    if bias.dtype not in (torch.float32, w.dtype) or tuple(bias.shape) != (w.shape[0],):
+    if bias.dtype not in (torch.float32, w.dtype) or bias.dim() != 1 or bias.shape[0] != w.shape[0]:
         raise ValueError(f"bias must be a float32 or {w.dtype} tensor of shape {(w.shape[0],)}, got {bias.dtype} {tuple(bias.shape)}")
     return bias if bias.is_contiguous() else bias.contiguous()
 
 
 def _layer(x, w, bias, activation, residual, p, seed, step, dtype, out, pre, stream):
+    # one token's layer takes less time on the GPU (7 us for 4096 x 4096) than this
+    # call takes to issue, so only what is there is looked at
     _factors(x, w)
-    act = _activation(activation)
-    bias = _bias(bias, w)
+    epilogue = binding.Epilogue()
+    if activation is not None:
+        epilogue.activation = _activation(activation)
     shape = (*x.shape[:-1], w.shape[0])
     if dtype is None:
         dtype = x.dtype if out is None else out.dtype
-    if dtype not in (x.dtype, torch.float32):
+    if dtype != x.dtype and dtype != torch.float32:
         raise TypeError(f"dtype must be float32 or x's {x.dtype}, got {dtype}")
-    _beside(residual, shape, dtype, x, "residual")
+    if bias is not None:
+        bias = _bias(bias, w)
+        epilogue.bias, epilogue.bias_dtype = bias.data_ptr(), _CODES[bias.dtype]
+    if residual is not None:
+        _beside(residual, shape, dtype, x, "residual")
     if pre is not None:
         _out(pre, shape, x.dtype, x, "pre")
-    mask = _mask(p, seed, step, x)
+    if p or step is not None:
+        mask = _mask(p, seed, step, x)
+        epilogue.dropout = ctypes.addressof(mask)
     out = _out(out, shape, dtype, x)
-    if out.numel() == 0:
+    if x.numel() == 0:
         return out
     a, b = _rows(x), _rows(w)
-    more = None if residual is None else _rows(residual)
     source, weights = _matrix(a, "x"), _matrix(b, "w")
-    epilogue = binding.Epilogue(_ptr(bias), 0 if bias is None else _CODES[bias.dtype], act)
-    if p:
-        epilogue.dropout = ctypes.pointer(mask)
-    if more is not None:
-        epilogue.residual = ctypes.pointer(_matrix(more, "residual"))
+    if residual is not None:
+        residual = _rows(residual)
+        of_residual = _matrix(residual, "residual")
+        epilogue.residual = ctypes.addressof(of_residual)
     if pre is not None:
-        epilogue.pre = ctypes.pointer(_matrix(_rows(pre), "pre"))
+        of_pre = _matrix(_rows(pre), "pre")
+        epilogue.pre = ctypes.addressof(of_pre)
     size = lib.sqn_layer_workspace(source, weights)
-    work = _workspace(size, x)
+    work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
     _check(lib.sqn_layer(source, weights, epilogue, _matrix(_rows(out), "out"), _ptr(work), size,
-                         _on(stream, a, b, bias, more, pre, step, out, work)))
+                         _on(stream, a, b, bias, residual, pre, step, out, work)))
     return out
 
 
@@ -523,7 +534,7 @@ def layer(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None,
     epilogue are float32, rounded once.  Differentiable in x, w, bias and
     residual (without `out`, `pre` and `stream`), by layer_gradient, which takes
     what `pre` holds: x w^T + bias in x's dtype.  No forward-mode derivative."""
-    p = _probability(dropout)
+    p = _probability(dropout) if dropout else 0.0
     _no_tangent("layer", x, w, bias, residual)
     if out is None and pre is None and stream is None and _wants_gradient(x, w, bias, residual):
         return _Layer.apply(x, w, bias, residual, step, activation, p, int(seed), dtype)
@@ -539,28 +550,29 @@ def layer_gradient(grad: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre: Op
     is not wanted.  `pre` is what layer wrote there, needed with an activation
     and only then; the residual's gradient is grad.  No gradient passes through
     it."""
-    p = _probability(dropout)
+    p = _probability(dropout) if dropout else 0.0
     _no_tangent("layer_gradient", grad, x, w, pre)
     _factors(x, w)
     act = _activation(activation)
     shape = (*x.shape[:-1], w.shape[0])
     _on_gpu(grad, "grad", x)
-    if tuple(grad.shape) != shape or grad.dtype not in (x.dtype, torch.float32):
+    if grad.shape != shape or (grad.dtype != x.dtype and grad.dtype != torch.float32):
         raise ValueError(f"grad must be a float32 or {x.dtype} tensor of shape {shape}, got {grad.dtype} {tuple(grad.shape)}")
     if (pre is None) != (act == 0):
         raise ValueError("pre goes with an activation, and an activation needs it")
-    _beside(pre, shape, x.dtype, x, "pre")
-    if bias_dtype not in (torch.float32, x.dtype):
+    if pre is not None:
+        _beside(pre, shape, x.dtype, x, "pre")
+    if bias_dtype != torch.float32 and bias_dtype != x.dtype:
         raise TypeError(f"bias_dtype must be float32 or x's {x.dtype}, got {bias_dtype}")
-    mask = _mask(p, seed, step, x)
+    mask = _mask(p, seed, step, x) if p or step is not None else None
     grad_x = _out(None, x.shape, x.dtype, x) if for_x else None
     grad_w = _out(None, w.shape, w.dtype, x) if for_w else None
     grad_bias = _out(None, (w.shape[0],), bias_dtype, x) if for_bias else None
     g, a, b, z = _rows(grad), _rows(x), _rows(w), None if pre is None else _rows(pre)
-    args = (_matrix(g, "grad"), _matrix(a, "x"), _matrix(b, "w"))
-    size = lib.sqn_layer_gradient_workspace(*args, act, mask, for_x, for_w, for_bias)
+    of_g, of_x, of_w = _matrix(g, "grad"), _matrix(a, "x"), _matrix(b, "w")
+    size = lib.sqn_layer_gradient_workspace(of_g, of_x, of_w, act, mask, for_x, for_w, for_bias)
     work = _workspace(size, x)
-    _check(lib.sqn_layer_gradient(*args, None if z is None else _matrix(z, "pre"), act, mask,
+    _check(lib.sqn_layer_gradient(of_g, of_x, of_w, None if z is None else _matrix(z, "pre"), act, mask,
                                   _matrix(_rows(grad_x), "grad_x") if for_x else None,
                                   _matrix(grad_w, "grad_w") if for_w else None, _ptr(grad_bias), _CODES[bias_dtype],
                                   _ptr(work), size, _on(stream, g, a, b, z, step, grad_x, grad_w, grad_bias, work)))

@@ -12,14 +12,12 @@ LAYERS = SETUP + r"""
 def mask(p=0.1, seed=5, step=None):
     return B.DropoutMask(p, seed, step)
 
-def pointer(x):
-    return None if x is None else ctypes.pointer(x)
-
 def epilogue(bias=None, bias_dtype=F32, act=0, drop=None, residual=None, pre=None):
     e = B.Epilogue(bias, bias_dtype, act)
+    e.kept = drop, residual, pre
     for name, value in (("dropout", drop), ("residual", residual), ("pre", pre)):
         if value is not None:
-            setattr(e, name, ctypes.pointer(value))
+            setattr(e, name, ctypes.addressof(value))
     return e
 
 def forward(points, units, cols, dtype=F32, out=None, short=0, shift=0, x=None, w=None, **more):
