@@ -986,6 +986,288 @@ sqn_matrix packed(const sqn_matrix& m, char*& to, hipStream_t stream)
     return c;
 }
 
+// ---- narrow layers of many points
+//
+// Bound by the points' bytes, which move once while the weights stay where they
+// are used: a wave keeps its 32 rows of P (up to four steps) in registers, as
+// fragments, and the workgroups go through the points in slabs that stream into
+// one of four LDS buffers, the next three under way.  Of UB blocks of P the
+// workgroup's waves take one each, SUBS times, with 32 points of the slab each.
+// (Tiles read the points' rows once for every 128 units and wait for their loads a
+// round at a time: 65,536 points of 256 by 256 in binary16 24 us.)
+
+constexpr int kNarrowRows = 256;
+constexpr int64_t kNarrowPoints = 16384;
+
+struct NarrowParams {
+    const void *p, *q;           // the weights, [units][cols] either way; the points' rows
+    int64_t p_stride;            // elements
+    uint64_t q_pitch;            // bytes
+    uint32_t p_lines, p_cols;    // of the weights in memory
+    uint32_t points, valid;      // valid: bytes of a point's row
+    Finish f;                    // units: rows of P
+};
+
+// A piece of 16 bytes at any alignment, of whose elements `left` are there.
+template <typename X>
+__device__ __forceinline__ uint4 piece_of(const X* p, int32_t left)
+{
+    constexpr int N = Elements<X>::PIECE;
+    if (left >= N) {
+        const Run<X, N> r = *reinterpret_cast<const Run<X, N>*>(p);
+        uint4 v;
+        __builtin_memcpy(&v, &r, 16);
+        return v;
+    }
+    X e[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        e[k] = k < left ? p[k] : X(0.0f);
+    uint4 v;
+    __builtin_memcpy(&v, e, 16);
+    return v;
+}
+
+// UB blocks of 32 rows of P, STEPS steps of the sum; a lane brings LOAD bytes at once.
+template <int UB_, int STEPS_, int LOAD_>
+struct Narrow {
+    static constexpr int UB = UB_, STEPS = STEPS_, LOAD = LOAD_;
+    static constexpr int SUBS = UB == 8 ? 1 : UB == 4 || STEPS == 4 ? 2 : 4;
+    static constexpr int WAVES = UB * SUBS, THREADS = 64 * WAVES;     // that multiply; one more brings the points
+    static constexpr int SIDE = 32 * UB, POINTS = 32 * SUBS;
+    static constexpr int BUFFERS = 4;
+    static constexpr int STEP = POINTS * static_cast<int>(kStepBytes), BUFFER = STEPS * STEP;
+    static constexpr int LOADS = BUFFER / (64 * LOAD);                // instructions of a slab
+    static constexpr int PIECES = SIDE * static_cast<int>(kStepBytes) / (static_cast<int>(kSlot) * THREADS);    // of P, a thread and step
+};
+
+template <typename S, typename X, typename T, bool LAYER, bool PA>
+__global__ __launch_bounds__(S::THREADS + 64) void narrow_kernel(NarrowParams p)
+{
+    BUFFERS_IN_LDS(S)
+    constexpr int OWN = 32 * 128;
+    constexpr int SHARED = S::WAVES * OWN > S::SIDE * static_cast<int>(kStepBytes) ? S::WAVES * OWN : S::SIDE * static_cast<int>(kStepBytes);
+    __shared__ __align__(16) char shared[SHARED];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t slabs = (p.points + S::POINTS - 1) / S::POINTS;
+    // of this workgroup: slabs blockIdx.x, + gridDim.x, ...
+    const uint32_t count = (slabs - blockIdx.x + gridDim.x - 1) / gridDim.x;
+
+    if (wave == S::WAVES) {
+        // The wave that brings the points stores nothing, so what it waits for is
+        // the slab alone (where every wave brought a share, a slab waited for the
+        // stores of the one before).
+        constexpr uint32_t OUTSIDE = 0x80000000u, LANES = kStepBytes / S::LOAD;    // of a row's step
+        constexpr uint32_t ROWS = 64 / LANES;                                     // of an instruction
+        const uint32_t byte = lane % LANES * S::LOAD;
+        auto bring_slab = [&](uint32_t nth, char* to) {
+            const uint64_t row0 = (blockIdx.x + static_cast<uint64_t>(nth) * gridDim.x) * S::POINTS;
+            const uint32_t left = nth < count ? p.points - static_cast<uint32_t>(row0) : 0;
+            const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<char*>(static_cast<const char*>(p.q) + row0 * p.q_pitch), 0, OUTSIDE, 0x00020000);
+            // past the last slab and past a row's end nothing is read, and the loads count as ever
+#pragma unroll 8
+            for (uint32_t i = 0; i < S::LOADS; ++i) {
+                const uint32_t step = i * (64 * S::LOAD) / S::STEP, row = i * ROWS % S::POINTS + lane / LANES;
+                const uint32_t at = step * kStepBytes + ((byte / kSlot) ^ (row >> 1 & 7)) * kSlot + byte % kSlot;
+                const uint32_t from = row < left && at < p.valid ? row * static_cast<uint32_t>(p.q_pitch) + at : OUTSIDE;
+                if constexpr (S::LOAD == kSlot)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void*)(to + i * (64 * S::LOAD)), kSlot, from, 0, 0, 0);
+                else
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void*)(to + i * (64 * S::LOAD)), 4, from, 0, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int b = 0; b < S::BUFFERS - 1; ++b)
+            bring_slab(b, buffers[b]);
+        for (int k = 0; k < 2 * S::STEPS; ++k)       // the weights' barriers
+            __builtin_amdgcn_s_barrier();
+        for (uint32_t n = 0; n < count; n += S::BUFFERS)
+#pragma unroll
+            for (int b = 0; b < S::BUFFERS; ++b)
+                if (n + b < count) {
+                    landed<std::min((S::BUFFERS - 2) * S::LOADS, 63)>();
+                    bring_slab(n + b + S::BUFFERS - 1, buffers[(b + S::BUFFERS - 1) % S::BUFFERS]);
+                }
+        // the loads still under way end before their buffers do
+        landed_own<0>();
+        return;
+    }
+
+    const uint32_t block = wave % S::UB, sub = wave / S::UB, half = lane >> 5, mine = lane & 31;
+    // the weights through LDS into the waves that use them, a step at a time
+    uint4 w[S::STEPS * kDepths];
+    {
+        uint4 piece[S::STEPS][S::PIECES];
+        uint32_t to[S::PIECES];
+        const X* rows = static_cast<const X*>(p.p);
+        constexpr uint32_t N = Elements<X>::PIECE, ACROSS = S::SIDE / N;
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) {
+            const uint32_t id = S::THREADS * i + threadIdx.x;
+            const uint32_t line = PA ? id / ACROSS : id / 8, col = PA ? id % ACROSS * N : id % 8 * N;
+            to[i] = PA ? (line * ACROSS + ((id % ACROSS) ^ across_key<X, S::SIDE>(line))) * kSlot
+                       : (line * 8 + ((id % 8) ^ (line >> 1 & 7))) * kSlot;
+            auto of_step = [&](int k, auto load) {
+                const uint32_t l = line + (PA ? k * Elements<X>::STEP : 0), c = col + (PA ? 0 : k * Elements<X>::STEP);
+                return load(rows + l * p.p_stride + c, l < p.p_lines ? static_cast<int32_t>(p.p_cols) - static_cast<int32_t>(c) : 0);
+            };
+            // without a branch all of a thread's loads are under way together
+            if (p.p_cols % N == 0) {
+#pragma unroll
+                for (int k = 0; k < S::STEPS; ++k)
+                    piece[k][i] = of_step(k, [&](const X* from, int32_t left) {
+                        const uint4 v = piece_of<X>(left > 0 ? from : rows, N);
+                        return left > 0 ? v : uint4{0, 0, 0, 0};
+                    });
+            } else {
+#pragma unroll
+                for (int k = 0; k < S::STEPS; ++k)
+                    piece[k][i] = of_step(k, piece_of<X>);
+            }
+        }
+        const Reader<X, S::SIDE, PA, 1> read_p(32 * block);
+#pragma unroll
+        for (int k = 0; k < S::STEPS; ++k) {
+#pragma unroll
+            for (int i = 0; i < S::PIECES; ++i)
+                *reinterpret_cast<uint4*>(shared + to[i]) = piece[k][i];
+            landed<63>();
+#pragma unroll
+            for (int o = 0; o < kDepths; ++o)
+                w[k * kDepths + o] = read_p.read(shared, 0, o);
+            landed<63>();
+        }
+    }
+
+    constexpr int V = 16 / sizeof(T);
+    constexpr uint32_t RUNS = 32 / V, ROUNDS = RUNS / 2;
+    const uint32_t unit = 32 * block + V * (lane % RUNS);
+    float bias[V];
+    if constexpr (LAYER)
+        load_bias<X, V>(p.f, unit, bias);
+    const uint64_t key = LAYER && p.f.mask.on ? mask_key(p.f.mask) : 0;
+    const Reader<X, S::POINTS, false, 1> read_q(32 * sub);
+    char* own = shared + wave * OWN;
+    auto slot = [](uint32_t column, uint32_t piece) { return column * 128 + (piece ^ (column & 7)) * 16; };
+    auto work = [&](uint32_t nth, const char* buffer) {
+        // every wave has read the slab before, and this one has landed
+        landed<63>();
+        // two sums side by side, of every other depth
+        float16v acc[2] = {};
+#pragma unroll
+        for (int k = 0; k < S::STEPS * kDepths; ++k) {
+            const uint4 q = read_q.read(buffer + k / kDepths * S::STEP, 0, k % kDepths);
+#pragma unroll
+            for (int e = 0; e < (sizeof(X) == 4 ? 4 : 1); ++e)
+                acc[(k + e) & 1] = multiply<X>(w[k], q, e, acc[(k + e) & 1]);
+        }
+        acc[0] += acc[1];
+        const uint64_t row0 = (blockIdx.x + static_cast<uint64_t>(nth) * gridDim.x) * S::POINTS + 32 * sub + lane / RUNS;
+        Raw<T, V> residual[ROUNDS];
+        if constexpr (LAYER)
+#pragma unroll
+            for (uint32_t i = 0; i < ROUNDS; ++i)
+                if (row0 + i * (64 / RUNS) < p.points && unit < p.f.units)
+                    load_residual<T, V>(p.f, row0 + i * (64 / RUNS), unit, residual[i]);
+#pragma unroll
+        for (uint32_t g = 0; g < 4; ++g)
+            *reinterpret_cast<float4v*>(own + slot(mine, 2 * g + half))
+                = float4v{acc[0][4 * g], acc[0][4 * g + 1], acc[0][4 * g + 2], acc[0][4 * g + 3]};
+        wave_fence();
+#pragma unroll
+        for (uint32_t i = 0; i < ROUNDS; ++i) {
+            const uint32_t column = i * (64 / RUNS) + lane / RUNS;
+            float v[V];
+#pragma unroll
+            for (int k = 0; k < V / 4; ++k) {
+                const float4v e = *reinterpret_cast<const float4v*>(own + slot(column, V / 4 * (lane % RUNS) + k));
+                __builtin_memcpy(v + 4 * k, &e, 16);
+            }
+            if (row0 + i * (64 / RUNS) < p.points && unit < p.f.units)
+                finish<X, T, LAYER, V>(p.f, key, row0 + i * (64 / RUNS), unit, bias, residual[i], v);
+        }
+        wave_fence();
+    };
+    for (uint32_t n = 0; n < count; n += S::BUFFERS)
+#pragma unroll
+        for (int b = 0; b < S::BUFFERS; ++b)
+            if (n + b < count)
+                work(n + b, buffers[b]);
+}
+
+// Layers whose weights a workgroup's registers hold, of points enough for several
+// slabs a CU.
+bool narrow_of(int64_t units, int64_t sum, int64_t points, int32_t dtype)
+{
+    return units <= kNarrowRows && sum * static_cast<int64_t>(element_size(dtype)) <= 4 * kStepBytes && points >= kNarrowPoints;
+}
+
+// Whether the points' rows can be brought from where they lie: binary32 elements
+// one at a time.
+bool narrow_in_place(const sqn_matrix& q)
+{
+    return in_place(q) || (q.dtype == SQN_F32 && q.row_stride * 4 < (int64_t{1} << 23));
+}
+
+size_t narrow_pack_bytes(const sqn_matrix& q) { return narrow_in_place(q) ? 0 : pack_bytes(q); }
+
+template <typename S, typename X, typename T, bool LAYER, bool PA>
+void launch_narrow_shape(const NarrowParams& p, hipStream_t stream)
+{
+    const uint32_t slabs = (p.points + S::POINTS - 1) / S::POINTS;
+    narrow_kernel<S, X, T, LAYER, PA><<<std::min(slabs, S::WAVES == 8 ? 256u : 512u), S::THREADS + 64, 0, stream>>>(p);
+}
+
+// wide: rows on 16-byte boundaries.
+template <int UB, int STEPS, typename X, typename T, bool LAYER, bool PA>
+void launch_narrow_steps(const NarrowParams& p, bool wide, hipStream_t stream)
+{
+    if constexpr (sizeof(X) == 4) {
+        if (!wide) {
+            launch_narrow_shape<Narrow<UB, STEPS, 4>, X, T, LAYER, PA>(p, stream);
+            return;
+        }
+    }
+    launch_narrow_shape<Narrow<UB, STEPS, 16>, X, T, LAYER, PA>(p, stream);
+}
+
+template <int UB, typename X, typename T, bool LAYER, bool PA>
+void launch_narrow_blocks(const NarrowParams& p, int64_t sum, bool wide, hipStream_t stream)
+{
+    const int64_t steps = (sum * static_cast<int64_t>(sizeof(X)) + kStepBytes - 1) / kStepBytes;
+    if (steps == 1)
+        launch_narrow_steps<UB, 1, X, T, LAYER, PA>(p, wide, stream);
+    else if (steps == 2)
+        launch_narrow_steps<UB, 2, X, T, LAYER, PA>(p, wide, stream);
+    else
+        launch_narrow_steps<UB, 4, X, T, LAYER, PA>(p, wide, stream);
+}
+
+// w [lines][cols]: the units, or, PA, the sum.
+template <typename X, typename T, bool LAYER, bool PA>
+void launch_narrow(const sqn_matrix& w, const sqn_matrix& points, int64_t sum, const Finish& f, char* work, hipStream_t stream)
+{
+    const sqn_matrix q = narrow_in_place(points) ? points : packed(points, work, stream);
+    NarrowParams p;
+    p.p = w.data;
+    p.q = q.data;
+    p.p_stride = w.row_stride;
+    p.q_pitch = static_cast<uint64_t>(q.row_stride) * sizeof(X);
+    p.p_lines = static_cast<uint32_t>(w.rows);
+    p.p_cols = static_cast<uint32_t>(w.cols);
+    p.points = static_cast<uint32_t>(q.rows);
+    p.valid = static_cast<uint32_t>(q.cols * sizeof(X));
+    p.f = f;
+    const bool wide = in_place(q);
+    if (f.units <= 64)
+        launch_narrow_blocks<2, X, T, LAYER, PA>(p, sum, wide, stream);
+    else if (f.units <= 128)
+        launch_narrow_blocks<4, X, T, LAYER, PA>(p, sum, wide, stream);
+    else
+        launch_narrow_blocks<8, X, T, LAYER, PA>(p, sum, wide, stream);
+}
+
 Operand along(const sqn_matrix& m)
 {
     const int64_t size = static_cast<int64_t>(element_size(m.dtype));
@@ -1103,6 +1385,10 @@ void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& 
         launch_few<X, T>(x, w, f, stream);
         return;
     }
+    if (narrow_of(w.rows, x.cols, x.rows, x.dtype)) {
+        launch_narrow<X, T, true, false>(w, x, x.cols, f, work, stream);
+        return;
+    }
     const sqn_matrix a = packed(w, work, stream), b = packed(x, work, stream);
     launch_product<X, T, true, false, false>(along(a), along(b), x.rows, x.cols, f, work, x.dtype, stream);
 }
@@ -1141,9 +1427,10 @@ struct GradientScratch {
         dz = own_dz ? aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype)) : 0;
         const uint32_t groups = SlopePlan(points, units).groups;
         sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
+        const bool narrow = narrow_of(x_.cols, units, points, x_.dtype);
         x = for_w ? pack_bytes(x_) : 0;
-        w = for_x ? pack_bytes(w_) : 0;
-        partial = std::max(for_x ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
+        w = for_x && !narrow ? pack_bytes(w_) : 0;
+        partial = std::max(for_x && !narrow ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
                            for_w ? plan_of(x_.cols, units, points, x_.dtype).bytes : 0);
     }
 
@@ -1202,9 +1489,14 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
     f.scale = m.scale;
     f.units = static_cast<uint32_t>(x.cols);
     if (to.x && points) {
-        const sqn_matrix a = packed(w, work, stream);
         f.out = to.x->data;
         f.out_stride = to.x->row_stride;
+    }
+    if (to.x && narrow_of(x.cols, units, points, x.dtype)) {
+        // dz lies on 16-byte boundaries, or is binary32
+        launch_narrow<X, X, false, true>(w, dz, units, f, work, stream);
+    } else if (to.x && points) {
+        const sqn_matrix a = packed(w, work, stream);
         launch_product<X, X, false, true, false>(across(a), along(dz), points, units, f, work + scratch.x, x.dtype, stream);
     }
     if (to.w) {
@@ -1222,6 +1514,8 @@ size_t layer_bytes(const sqn_matrix& x, const sqn_matrix& w)
 {
     if (x.rows <= kFewPoints)
         return 0;
+    if (narrow_of(w.rows, x.cols, x.rows, x.dtype))
+        return narrow_pack_bytes(x);
     return pack_bytes(x) + pack_bytes(w) + plan_of(w.rows, x.rows, x.cols, x.dtype).bytes;
 }
 

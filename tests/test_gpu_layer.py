@@ -77,6 +77,41 @@ def test_many_tiles(dtype):
         assert ((y.double() - want).abs() <= bound).all(), size
 
 
+def on_gpu(x, w, bias, residual):
+    """The sums in 64 bits on the GPU, and how far they may be off."""
+    x, w = x.double(), w.double()
+    z, off = x @ w.t(), x.abs() @ w.abs().t()
+    if bias is not None:
+        z, off = z + bias.double(), off + bias.double().abs()
+    return z, 2 * U.F32 * (x.shape[1] + 9) * off
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("points", [16384, 16385, 20001])
+@pytest.mark.parametrize("cols,units", [(64, 256), (42, 250), (7, 50), (128, 100), (200, 64), (256, 256), (130, 33), (1, 1)])
+def test_many_points(dtype, points, cols, units):
+    """Narrow layers of many points, every size of registers and slabs."""
+    from paper_2204_02585_amd import learn
+    x, w, bias, residual = inputs(points, cols, units, dtype)
+    pre = torch.empty_like(residual)
+    y = learn.layer(x, w, bias, "relu", residual, pre=pre)
+    z, off = on_gpu(x, w, bias, residual)
+    off_z = off + U.UNIT[dtype] * (z.abs() + off) + U.UNIT[dtype] * U.TINY[dtype]
+    assert ((pre.double() - z).abs() <= off_z).all()
+    want = z.clamp(min=0) + residual.double()
+    off = off + 4 * U.F32 * want.abs()
+    assert ((y.double() - want).abs() <= off + U.UNIT[dtype] * (want.abs() + off) + U.UNIT[dtype] * U.TINY[dtype]).all()
+    # the mask of rows far down
+    y = learn.layer(x, w, dropout=0.5, seed=3, dtype=torch.float32)
+    drop = torch.from_numpy(U.share(points, units, 0.5, 3) == 0).cuda()
+    assert torch.equal(y == 0, drop | (y == 0)) and (y[drop] == 0).all() and (y[~drop] == 0).float().mean() < 0.01
+    # a slice off the boundaries, with NaN around it
+    big = torch.full((points + 1, cols + 9), float("nan"), dtype=dtype, device="cuda")
+    part = big[1:, 3:3 + cols]
+    part.copy_(x)
+    assert torch.equal(learn.layer(part, w, bias), learn.layer(x, w, bias))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_layouts(dtype):
     """Slices off the 16-byte boundaries with NaN around them, transposed and

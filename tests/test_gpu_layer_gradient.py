@@ -64,6 +64,22 @@ def test_many_tiles(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("points,cols,units", [(16384, 256, 64), (20001, 250, 50), (16385, 50, 256), (16400, 100, 128), (16390, 33, 130), (17000, 1, 1)])
+def test_many_points(dtype, points, cols, units):
+    """Narrow layers of many points."""
+    from paper_2204_02585_amd import learn
+    x, w, _, grad = inputs(points, cols, units, dtype)
+    dx, dw, db = learn.layer_gradient(grad, x, w)
+    for got, a, b in ((dx, grad, w.t()), (dw, grad.t(), x.t())):
+        a, b = a.double(), b.double()
+        want = a @ b.t()
+        off = 2 * U.F32 * (a.shape[1] + 8) * (a.abs() @ b.abs().t())
+        assert ((got.double() - want).abs() <= off + U.UNIT[dtype] * (want.abs() + off) + U.UNIT[dtype] * U.TINY[dtype]).all()
+    total = grad.double()
+    assert ((db.double() - total.sum(0)).abs() <= 2 * U.F32 * (points + 8) * total.abs().sum(0)).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_layouts(dtype):
     """Slices off the 16-byte boundaries with NaN around them, broadcast and
     transposed gradients, more dimensions."""
