@@ -597,37 +597,60 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
 }
 
 // The parts of the sums added up, in their order, and finished; zeros of no parts.
+// The threads of a run (a power of two, more where there are many parts of few
+// runs) take every slices-th part, so that their loads are under way together.
 struct PartsParams {
     const float* partial;
     uint64_t rows, runs;         // runs: rows * per_row
     uint32_t parts, pitch, per_row;
+    uint32_t slices;
     Finish f;
 };
 
 template <typename X, typename T, bool LAYER>
-__global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
+__device__ __forceinline__ void parts_share(const PartsParams& p, uint32_t group, uint32_t groups)
 {
     constexpr int V = 4;
+    __shared__ float4v shared[kThreads];
     const uint64_t key = LAYER && p.f.mask.on ? mask_key(p.f.mask) : 0;
-    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.runs;
-         i += static_cast<uint64_t>(gridDim.x) * kThreads) {
-        const uint64_t row = i / p.per_row;
-        const uint32_t unit = static_cast<uint32_t>(i - row * p.per_row) * V;
-        float v[V] = {}, bias[V];
+    const uint32_t width = kThreads / p.slices, tx = threadIdx.x % width, ty = threadIdx.x / width;
+    for (uint64_t first = static_cast<uint64_t>(group) * width; first < p.runs; first += static_cast<uint64_t>(groups) * width) {
+        const uint64_t i = first + tx;
+        const bool inside = i < p.runs;
+        const uint64_t row = inside ? i / p.per_row : 0;
+        const uint32_t unit = inside ? static_cast<uint32_t>(i - row * p.per_row) * V : 0;
+        float bias[V];
         Raw<T, V> residual;
-        if constexpr (LAYER) {
+        if (LAYER && inside && ty == 0) {
             load_bias<X, V>(p.f, unit, bias);
             load_residual<T, V>(p.f, row, unit, residual);
         }
-#pragma unroll 4
-        for (uint32_t k = 0; k < p.parts; ++k) {
-            const float4v e = *reinterpret_cast<const float4v*>(p.partial + (k * p.rows + row) * p.pitch + unit);
-#pragma unroll
-            for (int r = 0; r < V; ++r)
-                v[r] += e[r];
+        float4v total = {};
+        if (inside) {
+#pragma unroll 8
+            for (uint32_t k = ty; k < p.parts; k += p.slices)
+                total += *reinterpret_cast<const float4v*>(p.partial + (k * p.rows + row) * p.pitch + unit);
         }
-        finish<X, T, LAYER, V>(p.f, key, row, unit, bias, residual, v);
+        if (p.slices > 1) {
+            __syncthreads();
+            shared[threadIdx.x] = total;
+            __syncthreads();
+            if (ty == 0)
+                for (uint32_t k = 1; k < p.slices; ++k)
+                    total += shared[k * width + tx];
+        }
+        if (inside && ty == 0) {
+            float v[V];
+            __builtin_memcpy(v, &total, 16);
+            finish<X, T, LAYER, V>(p.f, key, row, unit, bias, residual, v);
+        }
     }
+}
+
+template <typename X, typename T, bool LAYER>
+__global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
+{
+    parts_share<X, T, LAYER>(p, blockIdx.x, gridDim.x);
 }
 
 // ---- layers of few points
@@ -906,29 +929,49 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
     }
 }
 
-// The workgroups' sums added up: 16 units a workgroup, 64 threads each, whose
-// loads are under way together (8 threads each, one load after another, took
-// 17 us of 512 sums).
-constexpr uint32_t kSumUnits = 16, kSumSlices = 64;
+// The sums of slope_kernel's workgroups added up: 4 units a workgroup, 64 threads
+// each, whose loads are under way together (8 threads each, one load after another,
+// took 17 us of 512 sums).
+struct BiasParams {
+    const float* sums;           // [groups][units]
+    void* bias;
+    uint32_t groups, units;
+    int32_t dtype;
+    float scale;
+};
 
-__global__ __launch_bounds__(kSumUnits * kSumSlices) void bias_kernel(const float* sums, uint32_t groups, uint32_t units, float scale,
-                                                                     void* out, int32_t dtype)
+constexpr uint32_t kSumUnits = 4, kSumSlices = kThreads / kSumUnits;
+
+__device__ __forceinline__ void bias_share(const BiasParams& p, uint32_t group)
 {
     __shared__ float part[kSumSlices][kSumUnits + 1];
-    const uint32_t tx = threadIdx.x % kSumUnits, ty = threadIdx.x / kSumUnits, u = blockIdx.x * kSumUnits + tx;
+    const uint32_t tx = threadIdx.x % kSumUnits, ty = threadIdx.x / kSumUnits, u = group * kSumUnits + tx;
     float total = 0.0f;
-    if (u < units) {
+    if (u < p.units) {
 #pragma unroll 8
-        for (uint32_t k = ty; k < groups; k += kSumSlices)
-            total += sums[static_cast<uint64_t>(k) * units + u];
+        for (uint32_t k = ty; k < p.groups; k += kSumSlices)
+            total += p.sums[static_cast<uint64_t>(k) * p.units + u];
     }
     part[ty][tx] = total;
     __syncthreads();
-    if (ty || u >= units)
+    if (ty || u >= p.units)
         return;
+#pragma unroll 8
     for (uint32_t k = 1; k < kSumSlices; ++k)
         total += part[k][tx];
-    store_bias(out, u, total * scale, dtype);
+    store_bias(p.bias, u, total * p.scale, p.dtype);
+}
+
+__global__ __launch_bounds__(kThreads) void bias_kernel(BiasParams p) { bias_share(p, blockIdx.x); }
+
+// The last sums of two gradients in one launch.
+template <typename X>
+__global__ __launch_bounds__(kThreads) void sums_kernel(PartsParams w, BiasParams bias, uint32_t groups_w)
+{
+    if (blockIdx.x < groups_w)
+        parts_share<X, X, false>(w, blockIdx.x, groups_w);
+    else
+        bias_share(bias, blockIdx.x - groups_w);
 }
 
 // ---- choices
@@ -1305,7 +1348,7 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
 {
     constexpr int64_t kSides[3] = {64, 128, 256}, kMostParts = 64, kCus = 256;
     constexpr double kStep[2][3] = {{0.26, 0.58, 1.32}, {0.51, 1.85, 7.2}}, kEnds[3] = {1.5, 3.0, 18.0};
-    constexpr double kJoin = 3.0, kJoinBytes = 3.5e6;            // a us
+    constexpr double kJoin = 4.0, kJoinBytes = 3.5e6;            // a us
     const int f32 = dtype == SQN_F32 ? 1 : 0;
     const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
     const int64_t steps = (sum + step - 1) / step;
@@ -1341,10 +1384,11 @@ void launch_tiles(ProductParams& p, hipStream_t stream)
     tile_kernel<S, X, T, LAYER, PA, QA><<<p.tiles_p * p.tiles_q * p.parts, S::THREADS, 0, stream>>>(p);
 }
 
-// `rows_q`: rows of C.  `partial` holds the plan's bytes.
+// The tiles of a product of `rows_q` rows, and, of several parts or none, what is
+// left to add up.  `partial` holds the plan's bytes.
 template <typename X, typename T, bool LAYER, bool PA, bool QA>
-void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t sum, const Finish& f, char* partial, int32_t dtype,
-                    hipStream_t stream)
+PartsParams launch_tiles_of(const Operand& a, const Operand& b, int64_t rows_q, int64_t sum, const Finish& f, char* partial,
+                            int32_t dtype, hipStream_t stream)
 {
     const Plan plan = plan_of(f.units, rows_q, sum, dtype);
     ProductParams p{};
@@ -1365,8 +1409,6 @@ void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t 
         else
             launch_tiles<Shape<64>, X, T, LAYER, PA, QA>(p, stream);
     }
-    if (plan.parts == 1)
-        return;
     PartsParams j{};
     j.partial = p.partial;
     j.rows = static_cast<uint64_t>(rows_q);
@@ -1375,7 +1417,22 @@ void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t 
     j.per_row = j.pitch / 4;
     j.runs = j.rows * j.per_row;
     j.f = f;
-    parts_kernel<X, T, LAYER><<<groups_of(j.runs), kThreads, 0, stream>>>(j);
+    // up to 16 threads a run, while that leaves all of them busy
+    j.slices = 1;
+    while (2 * j.slices <= std::min(j.parts, 16u) && j.runs * j.slices < 256 * kThreads)
+        j.slices *= 2;
+    return j;
+}
+
+uint32_t groups_of(const PartsParams& j) { return groups_of(j.runs * j.slices); }
+
+template <typename X, typename T, bool LAYER, bool PA, bool QA>
+void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t sum, const Finish& f, char* partial, int32_t dtype,
+                    hipStream_t stream)
+{
+    const PartsParams j = launch_tiles_of<X, T, LAYER, PA, QA>(a, b, rows_q, sum, f, partial, dtype, stream);
+    if (j.parts != 1)
+        parts_kernel<X, T, LAYER><<<groups_of(j), kThreads, 0, stream>>>(j);
 }
 
 template <typename X, typename T>
@@ -1405,7 +1462,7 @@ struct SlopePlan {
         const int64_t runs = (units + 7) / 8;
         const bool few = points <= 256;
         across = 1;
-        while (across < (few ? 8 : 32) && across < runs)
+        while (across < (few ? 4 : 32) && across < runs)
             across *= 2;
         const int64_t wide = (runs + across - 1) / across, down = kThreads / across;
         const int64_t most = few ? 1 : std::clamp<int64_t>(2048 / wide, 1, 512);
@@ -1482,9 +1539,10 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         else
             slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
     }
-    if (to.bias && plan.groups != 1)
-        bias_kernel<<<static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits), kSumUnits * kSumSlices, 0, stream>>>(sums, plan.groups, static_cast<uint32_t>(units), m.scale,
-                                                                                       to.bias, to.bias_dtype);
+    // of one group they have been added up, of none they are zeros
+    const BiasParams bias = {sums, to.bias, plan.groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
+    bool add_bias = to.bias && plan.groups != 1;
+    const uint32_t bias_groups = static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits);
     Finish f{};
     f.scale = m.scale;
     f.units = static_cast<uint32_t>(x.cols);
@@ -1503,8 +1561,16 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         const sqn_matrix a = packed(x, work, stream);
         f.out = to.w->data;
         f.out_stride = to.w->row_stride;
-        launch_product<X, X, false, true, true>(across(a), across(dz), units, points, f, work, x.dtype, stream);
+        const PartsParams j = launch_tiles_of<X, X, false, true, true>(across(a), across(dz), units, points, f, work, x.dtype, stream);
+        if (j.parts != 1 && add_bias) {
+            sums_kernel<X><<<groups_of(j) + bias_groups, kThreads, 0, stream>>>(j, bias, groups_of(j));
+            add_bias = false;
+        } else if (j.parts != 1) {
+            parts_kernel<X, X, false><<<groups_of(j), kThreads, 0, stream>>>(j);
+        }
     }
+    if (add_bias)
+        bias_kernel<<<bias_groups, kThreads, 0, stream>>>(bias);
     return hipGetLastError();
 }
 
