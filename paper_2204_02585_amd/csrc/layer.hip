@@ -1076,16 +1076,17 @@ template <int UB_, int STEPS_, int LOAD_>
 struct Narrow {
     static constexpr int UB = UB_, STEPS = STEPS_, LOAD = LOAD_;
     static constexpr int SUBS = UB == 8 ? 1 : UB == 4 || STEPS == 4 ? 2 : 4;
-    static constexpr int WAVES = UB * SUBS, THREADS = 64 * WAVES;     // that multiply; one more brings the points
+    static constexpr int WAVES = UB * SUBS, THREADS = 64 * WAVES;     // that multiply
+    static constexpr int BRINGERS = LOAD == 4 ? 4 : 1;                // waves that bring the points
     static constexpr int SIDE = 32 * UB, POINTS = 32 * SUBS;
     static constexpr int BUFFERS = 4;
     static constexpr int STEP = POINTS * static_cast<int>(kStepBytes), BUFFER = STEPS * STEP;
-    static constexpr int LOADS = BUFFER / (64 * LOAD);                // instructions of a slab
+    static constexpr int LOADS = BUFFER / (64 * LOAD) / BRINGERS;     // instructions of a slab, of a wave
     static constexpr int PIECES = SIDE * static_cast<int>(kStepBytes) / (static_cast<int>(kSlot) * THREADS);    // of P, a thread and step
 };
 
 template <typename S, typename X, typename T, bool LAYER, bool PA>
-__global__ __launch_bounds__(S::THREADS + 64) void narrow_kernel(NarrowParams p)
+__global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(NarrowParams p)
 {
     BUFFERS_IN_LDS(S)
     constexpr int OWN = 32 * 128;
@@ -1096,8 +1097,8 @@ __global__ __launch_bounds__(S::THREADS + 64) void narrow_kernel(NarrowParams p)
     // of this workgroup: slabs blockIdx.x, + gridDim.x, ...
     const uint32_t count = (slabs - blockIdx.x + gridDim.x - 1) / gridDim.x;
 
-    if (wave == S::WAVES) {
-        // The wave that brings the points stores nothing, so what it waits for is
+    if (wave >= S::WAVES) {
+        // The waves that bring the points store nothing, so what they wait for is
         // the slab alone (where every wave brought a share, a slab waited for the
         // stores of the one before).
         constexpr uint32_t OUTSIDE = 0x80000000u, LANES = kStepBytes / S::LOAD;    // of a row's step
@@ -1110,7 +1111,8 @@ __global__ __launch_bounds__(S::THREADS + 64) void narrow_kernel(NarrowParams p)
                 const_cast<char*>(static_cast<const char*>(p.q) + row0 * p.q_pitch), 0, OUTSIDE, 0x00020000);
             // past the last slab and past a row's end nothing is read, and the loads count as ever
 #pragma unroll 8
-            for (uint32_t i = 0; i < S::LOADS; ++i) {
+            for (uint32_t k = 0; k < S::LOADS; ++k) {
+                const uint32_t i = (wave - S::WAVES) * S::LOADS + k;
                 const uint32_t step = i * (64 * S::LOAD) / S::STEP, row = i * ROWS % S::POINTS + lane / LANES;
                 const uint32_t at = step * kStepBytes + ((byte / kSlot) ^ (row >> 1 & 7)) * kSlot + byte % kSlot;
                 const uint32_t from = row < left && at < p.valid ? row * static_cast<uint32_t>(p.q_pitch) + at : OUTSIDE;
@@ -1259,7 +1261,7 @@ template <typename S, typename X, typename T, bool LAYER, bool PA>
 void launch_narrow_shape(const NarrowParams& p, hipStream_t stream)
 {
     const uint32_t slabs = (p.points + S::POINTS - 1) / S::POINTS;
-    narrow_kernel<S, X, T, LAYER, PA><<<std::min(slabs, S::WAVES == 8 ? 256u : 512u), S::THREADS + 64, 0, stream>>>(p);
+    narrow_kernel<S, X, T, LAYER, PA><<<std::min(slabs, S::WAVES == 8 ? 256u : 512u), S::THREADS + 64 * S::BRINGERS, 0, stream>>>(p);
 }
 
 // wide: rows on 16-byte boundaries.
