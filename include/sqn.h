@@ -542,7 +542,8 @@ typedef struct {
 
 /* A layer: z = x w^T + bias, out = D(act(z)) + residual, [points][units], with
  * x [points][cols] and w [units][cols] of one dtype.  Products and sums in
- * binary32, z included; rounded once to out's dtype (x's or SQN_F32).
+ * binary32, z included; rounded once to out's dtype (x's or SQN_F32).  Sizes,
+ * strides and alignments choose the kernel and with it the order of the sums.
  * points >= 0, units >= 1.
  *   epilogue:  or NULL for none of it;
  *   out:       may be the residual's own memory if the layout is the same;

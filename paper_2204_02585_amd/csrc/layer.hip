@@ -1242,10 +1242,15 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
 }
 
 // Layers whose weights a workgroup's registers hold, of points enough for several
-// slabs a CU.
-bool narrow_of(int64_t units, int64_t sum, int64_t points, int32_t dtype)
+// slabs a CU, where tiles would need copies onto 16-byte boundaries or read the
+// points twice.  (us so and in tiles: 65,536 points of 256 by 256 in binary16 23
+// and 24, the gradient of its points 19 and 25, of 20,000 10 and 9, 64 wide 14 and
+// 12; of 50,001 points of binary32 of 42 by 256 31 and 58.)
+bool narrow_of(const sqn_matrix& w, int64_t units, int64_t sum, int64_t points, bool points_in_place)
 {
-    return units <= kNarrowRows && sum * static_cast<int64_t>(element_size(dtype)) <= 4 * kStepBytes && points >= kNarrowPoints;
+    if (units > kNarrowRows || sum * static_cast<int64_t>(element_size(w.dtype)) > 4 * kStepBytes || points < kNarrowPoints)
+        return false;
+    return !in_place(w) || !points_in_place || (units > kNarrowRows / 2 && points >= 2 * kNarrowPoints);
 }
 
 // Whether the points' rows can be brought from where they lie: binary32 elements
@@ -1444,7 +1449,7 @@ void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& 
         launch_few<X, T>(x, w, f, stream);
         return;
     }
-    if (narrow_of(w.rows, x.cols, x.rows, x.dtype)) {
+    if (narrow_of(w, w.rows, x.cols, x.rows, in_place(x))) {
         launch_narrow<X, T, true, false>(w, x, x.cols, f, work, stream);
         return;
     }
@@ -1486,7 +1491,7 @@ struct GradientScratch {
         dz = own_dz ? aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype)) : 0;
         const uint32_t groups = SlopePlan(points, units).groups;
         sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
-        const bool narrow = narrow_of(x_.cols, units, points, x_.dtype);
+        const bool narrow = narrow_of(w_, x_.cols, units, points, true);
         x = for_w ? pack_bytes(x_) : 0;
         w = for_x && !narrow ? pack_bytes(w_) : 0;
         partial = std::max(for_x && !narrow ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
@@ -1552,8 +1557,7 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         f.out = to.x->data;
         f.out_stride = to.x->row_stride;
     }
-    if (to.x && narrow_of(x.cols, units, points, x.dtype)) {
-        // dz lies on 16-byte boundaries, or is binary32
+    if (to.x && narrow_of(w, x.cols, units, points, true)) {
         launch_narrow<X, X, false, true>(w, dz, units, f, work, stream);
     } else if (to.x && points) {
         const sqn_matrix a = packed(w, work, stream);
@@ -1582,7 +1586,7 @@ size_t layer_bytes(const sqn_matrix& x, const sqn_matrix& w)
 {
     if (x.rows <= kFewPoints)
         return 0;
-    if (narrow_of(w.rows, x.cols, x.rows, x.dtype))
+    if (narrow_of(w, w.rows, x.cols, x.rows, in_place(x)))
         return narrow_pack_bytes(x);
     return pack_bytes(x) + pack_bytes(w) + plan_of(w.rows, x.rows, x.cols, x.dtype).bytes;
 }

@@ -105,11 +105,12 @@ def test_many_points(dtype, points, cols, units):
     y = learn.layer(x, w, dropout=0.5, seed=3, dtype=torch.float32)
     drop = torch.from_numpy(U.share(points, units, 0.5, 3) == 0).cuda()
     assert torch.equal(y == 0, drop | (y == 0)) and (y[drop] == 0).all() and (y[~drop] == 0).float().mean() < 0.01
-    # a slice off the boundaries, with NaN around it
+    # a slice off the boundaries, with NaN around it: another kernel may sum it in another
+    # order, so it is held to the sums' own bound
     big = torch.full((points + 1, cols + 9), float("nan"), dtype=dtype, device="cuda")
     part = big[1:, 3:3 + cols]
     part.copy_(x)
-    assert torch.equal(learn.layer(part, w, bias), learn.layer(x, w, bias))
+    assert ((learn.layer(part, w, bias).double() - z).abs() <= off_z).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
