@@ -1,12 +1,13 @@
 """A plane of learned texels and a small decoder, trained and then held in 4 bits.
 
 A coarse table of features, one row per texel of an n x n plane, is read by
-index; two layers turn a row into a colour.  Training moves the table by its
-lookup gradient and the layers by orthogonalised momentum (Muon); then the
-layers are put into 4-bit blocks and the plane is decoded from them, once for
-all texels and once for a handful of them, as a cursor would ask.
+index; three layers turn a row into a colour, the hidden ones' outputs thinned
+by dropout if asked to.  Training moves the table by its lookup gradient and the
+layers by orthogonalised momentum (Muon); then the layers are put into 4-bit
+blocks and the plane is decoded from them, once for all texels and once for a
+handful of them, as a cursor would ask.
 
-    python -m examples.fit_texels [--side 256] [--steps 200]
+    python -m examples.fit_texels [--side 256] [--steps 200] [--dropout 0.0]
 """
 import argparse
 
@@ -23,8 +24,16 @@ def target(side: int, device) -> torch.Tensor:
     return torch.stack([0.5 + 0.5 * torch.sin(5 * u + 2 * v), 0.25 + 0.5 * inside, 0.5 + 0.4 * torch.cos(4 * v * u)], -1).reshape(-1, 3)
 
 
+def decode(rows: torch.Tensor, layers, dropout: float = 0.0, seed: int = 0) -> torch.Tensor:
+    """Colours of rows [n, features]; a mask of seed `seed` on the last hidden layer."""
+    first, second, head = layers
+    hidden = learn.layer(rows, first, activation="relu")
+    hidden = learn.layer(hidden, second, activation="relu", dropout=dropout, seed=seed)
+    return learn.layer(hidden, head)
+
+
 def fit(side: int = 256, features: int = 32, units: int = 128, points: int = 16384, steps: int = 200,
-        device="cuda", seed: int = 0) -> dict:
+        device="cuda", seed: int = 0, dropout: float = 0.0) -> dict:
     gen = torch.Generator(device="cpu").manual_seed(seed)
 
     def draw(*shape, spread):
@@ -38,13 +47,11 @@ def fit(side: int = 256, features: int = 32, units: int = 128, points: int = 163
     layers = [first, second, head]
     momentum = [torch.zeros_like(w) for w in layers]
 
-    def decode(rows):
-        return torch.relu(torch.relu(rows @ first.t()) @ second.t()) @ head.t()
-
     losses = []
     for step in range(steps):
         ids = torch.randint(0, side * side, (points,), generator=gen).to(device)
-        loss = torch.mean((decode(learn.lookup(table, ids)) - colours[ids]) ** 2)
+        rows = learn.lookup(table, ids)
+        loss = torch.mean((decode(rows, layers, dropout, seed=step) - colours[ids]) ** 2)
         loss.backward()
         rate = 0.02 * (1.0 - step / steps)
         with torch.no_grad():
@@ -61,7 +68,7 @@ def fit(side: int = 256, features: int = 32, units: int = 128, points: int = 163
         losses.append(loss.detach())
 
     with torch.no_grad():
-        exact = decode(table)
+        exact = decode(table, layers)
         q = [learn.quantise(w) for w in layers]
 
         def decode_blocks(rows):
@@ -88,8 +95,9 @@ def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--side", type=int, default=256)
     ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--dropout", type=float, default=0.0)
     args = ap.parse_args()
-    r = fit(side=args.side, steps=args.steps)
+    r = fit(side=args.side, steps=args.steps, dropout=args.dropout)
     print(f"loss {r['first_loss']:.5f} -> {r['last_loss']:.5f} over {args.steps} steps")
     print(f"plane decoded: squared error {r['exact']:.5f} exact, {r['blocks']:.5f} from 4-bit blocks "
           f"({r['bytes_exact']} -> {r['bytes_blocks']} bytes of layers)")

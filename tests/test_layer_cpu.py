@@ -211,3 +211,43 @@ print(json.dumps([of(*c) for c in DATA]))
         parts = 1 << 26
         assert forward <= filled + parts, (p, u, c, t, forward)
         assert backward <= filled + size * p * (u + 7) + 4 * 512 * u + 512 + parts, (p, u, c, t, backward)
+
+
+def test_choice_of_kernels():
+    """Few points take one launch and no scratch, narrow layers of many points one;
+    matrices off the 16-byte boundaries are copied first, save the few and the
+    narrow; products of few tiles are split."""
+    got = fake_hip.run(LAYERS + r"""
+import re
+def names(status):
+    assert status == 0, B.last_error()
+    return [re.search(r"\d+([a-z_]+)_kernel", l.split()[0]).group(1) for l in launches()]
+fake.fake_reset()
+out = {}
+for p, c, u, t in ((1, 4096, 4096, BF16), (16, 33, 5, F32), (17, 4096, 4096, BF16), (17, 64, 64, F32), (2000, 1001, 600, F16), (16384, 42, 250, F32),
+                   (16384, 256, 256, F16), (32768, 256, 256, F16), (32768, 256, 64, F16), (32768, 257, 256, F16), (32768, 43, 256, F16), (16383, 42, 250, F32)):
+    out["f%d_%d_%d" % (p, c, u)] = names(forward(p, u, c, t))
+spaces = [lib.sqn_layer_workspace(mat(p, c, t), mat(u, c, t)) for p, c, u, t in ((16, 4096, 4096, BF16), (32768, 256, 256, F16), (16384, 42, 250, F32))]
+for p, c, u, t in ((100, 2048, 2048, BF16), (50000, 256, 50, F32), (65536, 256, 256, F16), (300, 64, 64, F16), (8192, 4096, 8192, BF16)):
+    out["b%d_%d_%d" % (p, c, u)] = names(backward(p, u, c, t, act=1))
+    out["n%d_%d_%d" % (p, c, u)] = names(backward(p, u, c, t, bias=False))
+out["db"] = names(backward(3000, 64, 64, F32, to_x=False, to_w=False))
+out["none"] = names(backward(0, 64, 64, F32))
+print(json.dumps([out, spaces]))
+""")
+    out, spaces = got
+    assert spaces == [0, 0, 0]
+    assert out["f1_4096_4096"] == out["f16_33_5"] == ["few"]
+    assert out["f17_4096_4096"] == ["tile", "parts"] and out["f17_64_64"] == ["tile"]
+    assert out["f2000_1001_600"] == ["pack", "pack", "tile"]
+    assert out["f16384_42_250"] == out["f32768_256_256"] == ["narrow"]
+    assert out["f16384_256_256"] == out["f32768_256_64"] == ["tile"]
+    assert out["f32768_257_256"] == ["pack", "pack", "tile"] and out["f32768_43_256"] == ["pack", "narrow"]
+    assert out["f16383_42_250"] == ["pack", "pack", "tile"]
+    assert out["b300_64_64"][0] == "slope" and out["n300_64_64"] == ["tile", "tile"]
+    assert out["b65536_256_256"] == ["slope", "narrow", "tile", "sums"] and out["n65536_256_256"] == ["narrow", "tile", "parts"]
+    assert out["b50000_256_50"] == ["slope", "narrow", "tile", "sums"]
+    # the sums of few points are the bias's gradient at once
+    assert "bias" not in out["b100_2048_2048"] and "sums" not in out["b100_2048_2048"]
+    assert out["b8192_4096_8192"] == ["slope", "tile", "tile", "bias"] and out["n8192_4096_8192"] == ["tile", "tile"]
+    assert out["db"] == ["slope", "bias"] and out["none"] == ["parts", "bias"] or out["none"] == ["sums"]
