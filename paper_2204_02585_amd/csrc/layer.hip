@@ -656,9 +656,10 @@ __global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
 // ---- layers of few points
 //
 // For one token's points the weights' bytes are all that takes time.  A
-// workgroup computes 16 units of all points, or 32 or 64 where there are many
-// units (its waves read the points' elements once for each), on the 16 x 16
-// instructions; its waves take the sum's pieces in turn, straight from memory to
+// workgroup computes 16 units of all points, or 64 where there are many units (its
+// waves read the points' elements once for each: 16 points of 4096 by 16,384 in
+// bfloat16 29 us, 43 with 16 units; one of 4096 by 4096 8, 17 with 64), on the
+// 16 x 16 instructions; its waves take the sum's pieces in turn, straight from memory to
 // registers at any alignment, and add up in LDS, in the order of the waves.
 
 constexpr int kFewPoints = 16, kFewWaves = 8;
@@ -810,13 +811,11 @@ void launch_few(const sqn_matrix& x, const sqn_matrix& w, const Finish& f, hipSt
     p.f = f;
     // a wave for every four pieces of the sum; 64 threads finish each 16 units, so
     // larger workgroups have as many waves at least
-    const int blocks = f.units >= 64 * 512 ? 4 : f.units >= 32 * 512 ? 2 : 1;
+    const uint32_t blocks = f.units >= 64 * 256 ? 4 : 1;
     const uint32_t waves = std::clamp<uint32_t>((p.cols + 4 * Sixteen<X>::ALL - 1) / (4 * Sixteen<X>::ALL), blocks, kFewWaves);
     const uint32_t groups = (f.units + 16 * blocks - 1) / (16 * blocks);
     if (blocks == 4)
         few_kernel<X, T, 4><<<groups, 64 * waves, 0, stream>>>(p);
-    else if (blocks == 2)
-        few_kernel<X, T, 2><<<groups, 64 * waves, 0, stream>>>(p);
     else
         few_kernel<X, T, 1><<<groups, 64 * waves, 0, stream>>>(p);
 }
@@ -1049,6 +1048,13 @@ struct NarrowParams {
     uint32_t p_lines, p_cols;    // of the weights in memory
     uint32_t points, valid;      // valid: bytes of a point's row
     Finish f;                    // units: rows of P
+    // with SLOPE, whose points' rows are grad's and become dz's on their way
+    const void* pre;             // or null
+    uint64_t pre_pitch;          // bytes
+    void* dz;                    // [points][dz_pitch elements], or null
+    float* sums;                 // [gridDim.x][sum], or null
+    uint32_t sum, dz_pitch, act;
+    Mask mask;                   // its scale is the finish's
 };
 
 // A piece of 16 bytes at any alignment, of whose elements `left` are there.
@@ -1072,16 +1078,18 @@ __device__ __forceinline__ uint4 piece_of(const X* p, int32_t left)
 }
 
 // UB blocks of 32 rows of P, STEPS steps of the sum; a lane brings LOAD bytes at once.
-template <int UB_, int STEPS_, int LOAD_>
+template <int UB_, int STEPS_, int LOAD_, bool SLOPE_ = false>
 struct Narrow {
     static constexpr int UB = UB_, STEPS = STEPS_, LOAD = LOAD_;
+    static constexpr bool SLOPE = SLOPE_;
     static constexpr int SUBS = UB == 8 ? 1 : UB == 4 || STEPS == 4 ? 2 : 4;
     static constexpr int WAVES = UB * SUBS, THREADS = 64 * WAVES;     // that multiply
     static constexpr int BRINGERS = LOAD == 4 ? 4 : 1;                // waves that bring the points
     static constexpr int SIDE = 32 * UB, POINTS = 32 * SUBS;
     static constexpr int BUFFERS = 4;
-    static constexpr int STEP = POINTS * static_cast<int>(kStepBytes), BUFFER = STEPS * STEP;
-    static constexpr int LOADS = BUFFER / (64 * LOAD) / BRINGERS;     // instructions of a slab, of a wave
+    static constexpr int STEP = POINTS * static_cast<int>(kStepBytes), ROWS = STEPS * STEP;
+    static constexpr int BUFFER = SLOPE ? 2 * ROWS : ROWS;            // grad's rows, and pre's
+    static constexpr int LOADS = ROWS / (64 * LOAD) / BRINGERS;     // instructions of a slab, of a wave
     static constexpr int PIECES = SIDE * static_cast<int>(kStepBytes) / (static_cast<int>(kSlot) * THREADS);    // of P, a thread and step
 };
 
@@ -1104,23 +1112,28 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
         constexpr uint32_t OUTSIDE = 0x80000000u, LANES = kStepBytes / S::LOAD;    // of a row's step
         constexpr uint32_t ROWS = 64 / LANES;                                     // of an instruction
         const uint32_t byte = lane % LANES * S::LOAD;
-        auto bring_slab = [&](uint32_t nth, char* to) {
+        auto bring_rows = [&](const void* q, uint64_t pitch, uint32_t nth, char* to) {
             const uint64_t row0 = (blockIdx.x + static_cast<uint64_t>(nth) * gridDim.x) * S::POINTS;
             const uint32_t left = nth < count ? p.points - static_cast<uint32_t>(row0) : 0;
             const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
-                const_cast<char*>(static_cast<const char*>(p.q) + row0 * p.q_pitch), 0, OUTSIDE, 0x00020000);
+                const_cast<char*>(static_cast<const char*>(q) + row0 * pitch), 0, OUTSIDE, 0x00020000);
             // past the last slab and past a row's end nothing is read, and the loads count as ever
 #pragma unroll 8
             for (uint32_t k = 0; k < S::LOADS; ++k) {
                 const uint32_t i = (wave - S::WAVES) * S::LOADS + k;
                 const uint32_t step = i * (64 * S::LOAD) / S::STEP, row = i * ROWS % S::POINTS + lane / LANES;
                 const uint32_t at = step * kStepBytes + ((byte / kSlot) ^ (row >> 1 & 7)) * kSlot + byte % kSlot;
-                const uint32_t from = row < left && at < p.valid ? row * static_cast<uint32_t>(p.q_pitch) + at : OUTSIDE;
+                const uint32_t from = row < left && at < p.valid ? row * static_cast<uint32_t>(pitch) + at : OUTSIDE;
                 if constexpr (S::LOAD == kSlot)
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void*)(to + i * (64 * S::LOAD)), kSlot, from, 0, 0, 0);
                 else
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_void*)(to + i * (64 * S::LOAD)), 4, from, 0, 0, 0);
             }
+        };
+        auto bring_slab = [&](uint32_t nth, char* to) {
+            bring_rows(p.q, p.q_pitch, nth, to);
+            if (S::SLOPE && p.pre)
+                bring_rows(p.pre, p.pre_pitch, nth, to + S::ROWS);
         };
 #pragma unroll
         for (int b = 0; b < S::BUFFERS - 1; ++b)
@@ -1131,8 +1144,13 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
 #pragma unroll
             for (int b = 0; b < S::BUFFERS; ++b)
                 if (n + b < count) {
-                    landed<std::min((S::BUFFERS - 2) * S::LOADS, 63)>();
+                    if (S::SLOPE && p.pre)
+                        landed<std::min((S::BUFFERS - 2) * 2 * S::LOADS, 63)>();
+                    else
+                        landed<std::min((S::BUFFERS - 2) * S::LOADS, 63)>();
                     bring_slab(n + b + S::BUFFERS - 1, buffers[(b + S::BUFFERS - 1) % S::BUFFERS]);
+                    if constexpr (S::SLOPE)          // dz's barrier
+                        __builtin_amdgcn_s_barrier();
                 }
         // the loads still under way end before their buffers do
         landed_own<0>();
@@ -1195,9 +1213,54 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
     const Reader<X, S::POINTS, false, 1> read_q(32 * sub);
     char* own = shared + wave * OWN;
     auto slot = [](uint32_t column, uint32_t piece) { return column * 128 + (piece ^ (column & 7)) * 16; };
-    auto work = [&](uint32_t nth, const char* buffer) {
+    // With SLOPE a thread takes the same units of rows of every slab, so that their
+    // sums stay with it.
+    constexpr int N = Elements<X>::PIECE;
+    constexpr uint32_t GROUPS = 8 * S::STEPS, DOWN = S::THREADS / GROUPS;
+    const uint32_t of_step = threadIdx.x % GROUPS / 8, piece = threadIdx.x % 8, down = threadIdx.x / GROUPS;
+    const uint32_t of_unit = of_step * Elements<X>::STEP + piece * N;
+    const uint64_t slope_key = S::SLOPE && p.mask.on ? mask_key(p.mask) : 0;
+    float sum[N] = {};
+    auto slope_slab = [&](uint32_t nth, char* buffer) {
+#pragma unroll
+        for (uint32_t row = down; row < S::POINTS; row += DOWN) {
+            char* at = buffer + of_step * S::STEP + row * kStepBytes + (piece ^ (row >> 1 & 7)) * kSlot;
+            const uint64_t point = (blockIdx.x + static_cast<uint64_t>(nth) * gridDim.x) * S::POINTS + row;
+            X e[N];
+            float v[N], z[N];
+            __builtin_memcpy(e, at, 16);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                v[k] = to_f32(e[k]);
+            if (p.mask.on)
+                apply_mask<N>(p.mask, slope_key, point, of_unit, 1.0f, v);
+            if (p.pre) {
+                __builtin_memcpy(e, at + S::ROWS, 16);
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    z[k] = to_f32(e[k]);
+                times_slope<N>(p.act, z, v);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                sum[k] += v[k];
+                e[k] = from_f32<X>(v[k]);
+            }
+            uint4 whole;
+            __builtin_memcpy(&whole, e, 16);
+            *reinterpret_cast<uint4*>(at) = whole;
+            if (p.dz && point < p.points && of_unit < p.dz_pitch)
+                *reinterpret_cast<uint4*>(static_cast<X*>(p.dz) + point * p.dz_pitch + of_unit) = whole;
+        }
+    };
+    auto work = [&](uint32_t nth, char* buffer) {
         // every wave has read the slab before, and this one has landed
         landed<63>();
+        if constexpr (S::SLOPE) {
+            if (down < static_cast<uint32_t>(S::POINTS))
+                slope_slab(nth, buffer);
+            landed<63>();
+        }
         // two sums side by side, of every other depth
         float16v acc[2] = {};
 #pragma unroll
@@ -1239,6 +1302,25 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
         for (int b = 0; b < S::BUFFERS; ++b)
             if (n + b < count)
                 work(n + b, buffers[b]);
+    if constexpr (S::SLOPE) {
+        if (!p.sums)
+            return;
+        // the workgroup's sums, in the order of the rows
+        float(*part)[N] = reinterpret_cast<float(*)[N]>(shared);
+        landed<63>();
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            part[threadIdx.x][k] = sum[k];
+        landed<63>();
+        for (uint32_t u = threadIdx.x; u < p.sum; u += S::THREADS) {
+            const uint32_t group = u / Elements<X>::STEP * 8 + u % Elements<X>::STEP / N;
+            float total = 0.0f;
+#pragma unroll 8
+            for (uint32_t k = 0; k < std::min<uint32_t>(DOWN, S::POINTS); ++k)
+                total += part[k * GROUPS + group][u % N];
+            p.sums[static_cast<uint64_t>(blockIdx.x) * p.sum + u] = total;
+        }
+    }
 }
 
 // Layers whose weights a workgroup's registers hold, of points enough for several
@@ -1262,11 +1344,13 @@ bool narrow_in_place(const sqn_matrix& q)
 
 size_t narrow_pack_bytes(const sqn_matrix& q) { return narrow_in_place(q) ? 0 : pack_bytes(q); }
 
+// The workgroups.
 template <typename S, typename X, typename T, bool LAYER, bool PA>
-void launch_narrow_shape(const NarrowParams& p, hipStream_t stream)
+uint32_t launch_narrow_shape(const NarrowParams& p, hipStream_t stream)
 {
-    const uint32_t slabs = (p.points + S::POINTS - 1) / S::POINTS;
-    narrow_kernel<S, X, T, LAYER, PA><<<std::min(slabs, S::WAVES == 8 ? 256u : 512u), S::THREADS + 64 * S::BRINGERS, 0, stream>>>(p);
+    const uint32_t slabs = (p.points + S::POINTS - 1) / S::POINTS, groups = std::min(slabs, S::WAVES == 8 ? 256u : 512u);
+    narrow_kernel<S, X, T, LAYER, PA><<<groups, S::THREADS + 64 * S::BRINGERS, 0, stream>>>(p);
+    return groups;
 }
 
 // wide: rows on 16-byte boundaries.
@@ -1295,20 +1379,27 @@ void launch_narrow_blocks(const NarrowParams& p, int64_t sum, bool wide, hipStre
 }
 
 // w [lines][cols]: the units, or, PA, the sum.
+NarrowParams narrow_params(const sqn_matrix& w, const sqn_matrix& q, const Finish& f)
+{
+    const int64_t size = static_cast<int64_t>(element_size(q.dtype));
+    NarrowParams p{};
+    p.p = w.data;
+    p.q = q.data;
+    p.p_stride = w.row_stride;
+    p.q_pitch = static_cast<uint64_t>(q.row_stride * size);
+    p.p_lines = static_cast<uint32_t>(w.rows);
+    p.p_cols = static_cast<uint32_t>(w.cols);
+    p.points = static_cast<uint32_t>(q.rows);
+    p.valid = static_cast<uint32_t>(q.cols * size);
+    p.f = f;
+    return p;
+}
+
 template <typename X, typename T, bool LAYER, bool PA>
 void launch_narrow(const sqn_matrix& w, const sqn_matrix& points, int64_t sum, const Finish& f, char* work, hipStream_t stream)
 {
     const sqn_matrix q = narrow_in_place(points) ? points : packed(points, work, stream);
-    NarrowParams p;
-    p.p = w.data;
-    p.q = q.data;
-    p.p_stride = w.row_stride;
-    p.q_pitch = static_cast<uint64_t>(q.row_stride) * sizeof(X);
-    p.p_lines = static_cast<uint32_t>(w.rows);
-    p.p_cols = static_cast<uint32_t>(w.cols);
-    p.points = static_cast<uint32_t>(q.rows);
-    p.valid = static_cast<uint32_t>(q.cols * sizeof(X));
-    p.f = f;
+    const NarrowParams p = narrow_params(w, q, f);
     const bool wide = in_place(q);
     if (f.units <= 64)
         launch_narrow_blocks<2, X, T, LAYER, PA>(p, sum, wide, stream);
@@ -1316,6 +1407,50 @@ void launch_narrow(const sqn_matrix& w, const sqn_matrix& points, int64_t sum, c
         launch_narrow_blocks<4, X, T, LAYER, PA>(p, sum, wide, stream);
     else
         launch_narrow_blocks<8, X, T, LAYER, PA>(p, sum, wide, stream);
+}
+
+// The gradient of the points, and before it dz and the sums of its rows in groups,
+// in one go over grad and pre (apart 65,536 points of 256 by 256 in binary16 took
+// 42 us).
+constexpr uint32_t kSlopedGroups = 256;
+
+bool narrow_sloped(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre)
+{
+    return x.cols > kNarrowRows / 2 && grad.dtype == x.dtype && narrow_of(w, x.cols, w.rows, x.rows, true) && narrow_in_place(grad)
+        && (!pre || narrow_in_place(*pre));
+}
+
+template <int STEPS, typename X>
+uint32_t launch_sloped_steps(const NarrowParams& p, bool wide, hipStream_t stream)
+{
+    if constexpr (sizeof(X) == 4) {
+        if (!wide)
+            return launch_narrow_shape<Narrow<8, STEPS, 4, true>, X, X, false, true>(p, stream);
+    }
+    return launch_narrow_shape<Narrow<8, STEPS, 16, true>, X, X, false, true>(p, stream);
+}
+
+// The groups of sums.
+template <typename X>
+uint32_t launch_sloped(const sqn_matrix& w, const sqn_matrix& grad, const sqn_matrix* pre, int32_t act, const Mask& m, void* dz,
+                       int64_t dz_pitch, float* sums, const Finish& f, hipStream_t stream)
+{
+    NarrowParams p = narrow_params(w, grad, f);
+    p.pre = pre ? pre->data : nullptr;
+    p.pre_pitch = pre ? static_cast<uint64_t>(pre->row_stride) * sizeof(X) : 0;
+    p.dz = dz;
+    p.dz_pitch = static_cast<uint32_t>(dz_pitch);
+    p.sums = sums;
+    p.sum = static_cast<uint32_t>(w.rows);
+    p.act = static_cast<uint32_t>(act);
+    p.mask = m;
+    const bool wide = in_place(grad) && (!pre || in_place(*pre));
+    const int64_t steps = (w.rows * static_cast<int64_t>(sizeof(X)) + kStepBytes - 1) / kStepBytes;
+    if (steps == 1)
+        return launch_sloped_steps<1, X>(p, wide, stream);
+    if (steps == 2)
+        return launch_sloped_steps<2, X>(p, wide, stream);
+    return launch_sloped_steps<4, X>(p, wide, stream);
 }
 
 Operand along(const sqn_matrix& m)
@@ -1459,8 +1594,11 @@ void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& 
 
 // Workgroups of slope_kernel: `across` threads of one along a row, `rows` of it,
 // `groups` down the points.  Few points are one group, whose sums are the bias's
-// gradient; else some 2048 workgroups, at most 512 groups, whose sums a launch
-// behind it adds up.
+// gradient; else some 1024 workgroups, whose sums a launch behind them adds up
+// (65,536 points of 256 units, both launches: 28 us, of 512 workgroups 30, of 2048
+// 31).
+constexpr int64_t kSlopeGroups = 1024;
+
 struct SlopePlan {
     uint32_t across, rows, groups;
 
@@ -1472,7 +1610,7 @@ struct SlopePlan {
         while (across < (few ? 4 : 32) && across < runs)
             across *= 2;
         const int64_t wide = (runs + across - 1) / across, down = kThreads / across;
-        const int64_t most = few ? 1 : std::clamp<int64_t>(2048 / wide, 1, 512);
+        const int64_t most = few ? 1 : std::clamp<int64_t>(kSlopeGroups / wide, 1, kSlopeGroups);
         rows = static_cast<uint32_t>(std::max((points + most - 1) / most, std::min<int64_t>(points, 4 * down)));
         groups = rows ? static_cast<uint32_t>((points + rows - 1) / rows) : 0;
     }
@@ -1489,9 +1627,10 @@ struct GradientScratch {
         own_dz = (for_x || for_w) && (slopes || grad.dtype != x_.dtype || !in_place(grad));
         const int64_t piece = kSlot / static_cast<int64_t>(element_size(x_.dtype));
         dz = own_dz ? aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype)) : 0;
-        const uint32_t groups = SlopePlan(points, units).groups;
-        sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
         const bool narrow = narrow_of(w_, x_.cols, units, points, true);
+        // whether narrow layers' slopes are apart goes by pre's alignment too
+        const uint32_t groups = std::max(SlopePlan(points, units).groups, for_x && narrow ? kSlopedGroups : 0);
+        sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
         x = for_w ? pack_bytes(x_) : 0;
         w = for_x && !narrow ? pack_bytes(w_) : 0;
         partial = std::max(for_x && !narrow ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
@@ -1520,8 +1659,19 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         dz.dtype = x.dtype;
         dz.cols = dz.row_stride = round_up(units, Elements<X>::PIECE);
     }
+    Finish f{};
+    f.scale = m.scale;
+    f.units = static_cast<uint32_t>(x.cols);
+    if (to.x && points) {
+        f.out = to.x->data;
+        f.out_stride = to.x->row_stride;
+    }
     const SlopePlan plan(points, units);
-    if (points && (scratch.own_dz || to.bias)) {
+    uint32_t groups = plan.groups;       // of the bias's sums
+    const bool sloped = to.x && (scratch.own_dz || to.bias) && narrow_sloped(grad, x, w, pre);
+    if (sloped) {
+        groups = launch_sloped<X>(w, grad, pre, act, m, scratch.own_dz && to.w ? dz.data : nullptr, dz.cols, to.bias ? sums : nullptr, f, stream);
+    } else if (points && (scratch.own_dz || to.bias)) {
         SlopeParams p{};
         p.grad = grad.data;
         p.grad_stride = grad.row_stride;
@@ -1547,17 +1697,12 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
             slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
     }
     // of one group they have been added up, of none they are zeros
-    const BiasParams bias = {sums, to.bias, plan.groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
-    bool add_bias = to.bias && plan.groups != 1;
+    const BiasParams bias = {sums, to.bias, groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
+    bool add_bias = to.bias && groups != 1;
     const uint32_t bias_groups = static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits);
-    Finish f{};
-    f.scale = m.scale;
-    f.units = static_cast<uint32_t>(x.cols);
-    if (to.x && points) {
-        f.out = to.x->data;
-        f.out_stride = to.x->row_stride;
-    }
-    if (to.x && narrow_of(w, x.cols, units, points, true)) {
+    if (sloped) {
+        // the points' gradient came with dz
+    } else if (to.x && narrow_of(w, x.cols, units, points, true)) {
         launch_narrow<X, X, false, true>(w, dz, units, f, work, stream);
     } else if (to.x && points) {
         const sqn_matrix a = packed(w, work, stream);

@@ -63,6 +63,19 @@ def _matrix(t: torch.Tensor, name: str) -> Matrix:
     return Matrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, code, 0)
 
 
+def _operand(t: torch.Tensor, name: str):
+    """(_rows(t), _matrix() of it), looked at once: most of a small call is such looks."""
+    if t.dim() != 2 or t.dtype not in _CODES:
+        rows = _rows(t)
+        return rows, _matrix(rows, name)
+    rows, cols = t.shape
+    pitch, step = t.stride()
+    if step != 1 and cols != 1:
+        t = t.contiguous()
+        pitch = cols
+    return t, Matrix(t.data_ptr(), rows, cols, pitch if rows > 1 else cols, _CODES[t.dtype], 0)
+
+
 def _out(out: Optional[torch.Tensor], shape, dtype, beside: torch.Tensor, name: str = "out") -> torch.Tensor:
     """A new tensor beside another, or the caller's, whose rows must lie apart."""
     if out is None:
@@ -379,9 +392,11 @@ def _dropout(x, p, seed, step, residual, out, stream):
     out = _out(out, x.shape, x.dtype, x)
     if out.numel() == 0:
         return out
-    source, more = _rows(x), None if residual is None else _rows(residual)
-    _check(lib.sqn_dropout(_matrix(source, "x"), mask, None if more is None else _matrix(more, "residual"),
-                           _matrix(_rows(out), "out"), _on(stream, source, more, step, out)))
+    source, of_x = _operand(x, "x")
+    of_residual = None
+    if residual is not None:
+        residual, of_residual = _operand(residual, "residual")
+    _check(lib.sqn_dropout(of_x, mask, of_residual, _operand(out, "out")[1], _on(stream, source, residual, step, out)))
     return out
 
 
@@ -479,18 +494,17 @@ def _layer(x, w, bias, activation, residual, p, seed, step, dtype, out, pre, str
     out = _out(out, shape, dtype, x)
     if x.numel() == 0:
         return out
-    a, b = _rows(x), _rows(w)
-    source, weights = _matrix(a, "x"), _matrix(b, "w")
+    a, of_x = _operand(x, "x")
+    b, of_w = _operand(w, "w")
     if residual is not None:
-        residual = _rows(residual)
-        of_residual = _matrix(residual, "residual")
+        residual, of_residual = _operand(residual, "residual")
         epilogue.residual = ctypes.addressof(of_residual)
     if pre is not None:
-        of_pre = _matrix(_rows(pre), "pre")
+        of_pre = _operand(pre, "pre")[1]
         epilogue.pre = ctypes.addressof(of_pre)
-    size = lib.sqn_layer_workspace(source, weights)
-    work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
-    _check(lib.sqn_layer(source, weights, epilogue, _matrix(_rows(out), "out"), _ptr(work), size,
+    size = lib.sqn_layer_workspace(of_x, of_w)
+    work = _workspace(size, x)
+    _check(lib.sqn_layer(of_x, of_w, epilogue, _operand(out, "out")[1], _ptr(work), size,
                          _on(stream, a, b, bias, residual, pre, step, out, work)))
     return out
 
@@ -568,12 +582,15 @@ def layer_gradient(grad: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre: Op
     grad_x = _out(None, x.shape, x.dtype, x) if for_x else None
     grad_w = _out(None, w.shape, w.dtype, x) if for_w else None
     grad_bias = _out(None, (w.shape[0],), bias_dtype, x) if for_bias else None
-    g, a, b, z = _rows(grad), _rows(x), _rows(w), None if pre is None else _rows(pre)
-    of_g, of_x, of_w = _matrix(g, "grad"), _matrix(a, "x"), _matrix(b, "w")
+    g, of_g = _operand(grad, "grad")
+    a, of_x = _operand(x, "x")
+    b, of_w = _operand(w, "w")
+    of_pre = None
+    if pre is not None:
+        pre, of_pre = _operand(pre, "pre")
     size = lib.sqn_layer_gradient_workspace(of_g, of_x, of_w, act, mask, for_x, for_w, for_bias)
     work = _workspace(size, x)
-    _check(lib.sqn_layer_gradient(of_g, of_x, of_w, None if z is None else _matrix(z, "pre"), act, mask,
-                                  _matrix(_rows(grad_x), "grad_x") if for_x else None,
-                                  _matrix(grad_w, "grad_w") if for_w else None, _ptr(grad_bias), _CODES[bias_dtype],
-                                  _ptr(work), size, _on(stream, g, a, b, z, step, grad_x, grad_w, grad_bias, work)))
+    _check(lib.sqn_layer_gradient(of_g, of_x, of_w, of_pre, act, mask, _operand(grad_x, "grad_x")[1] if for_x else None,
+                                  _operand(grad_w, "grad_w")[1] if for_w else None, _ptr(grad_bias), _CODES[bias_dtype],
+                                  _ptr(work), size, _on(stream, g, a, b, pre, step, grad_x, grad_w, grad_bias, work)))
     return grad_x, grad_w, grad_bias

@@ -80,6 +80,55 @@ def test_many_points(dtype, points, cols, units):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("points,cols,units,activation,p", [
+    (32768, 256, 256, "relu", 0.1), (40001, 250, 50, "gelu", 0.5), (32800, 136, 128, "silu", 0.0), (33000, 256, 64, None, 0.25),
+    (32769, 129, 33, "gelu", 0.0), (50001, 256, 8, "relu", 0.9), (32768, 200, 200, "silu", 1.0), (40000, 256, 50, None, 0.0)])
+def test_many_points_with_slopes(dtype, points, cols, units, activation, p):
+    """Narrow layers of many points whose slopes are taken on the way; with the
+    gradient's or the kept values' rows off the boundaries, each wanted alone."""
+    from paper_2204_02585_amd import learn
+    x, w, _, grad = inputs(points, cols, units, dtype)
+    pre = draw((points, units), dtype, torch.Generator().manual_seed(4)) if activation else None
+    share = torch.from_numpy(U.share(points, units, p, 77)).cuda()
+    keep, s = (share > 0).double(), float(share.max()) or 1.0
+    dz, off = keep * grad.double(), torch.zeros((), dtype=torch.float64, device="cuda")
+    if activation:
+        z = pre.double()
+        t = torch.sigmoid(z)
+        slope = {"relu": lambda: (z > 0).double(), "silu": lambda: t * (1 + z * (1 - t)),
+                 "gelu": lambda: torch.special.ndtr(z) + z * torch.exp(-z * z / 2) / (2 * np.pi) ** 0.5}[activation]()
+        off = keep * grad.double().abs() * 32 * U.F32 * (1 + z.abs()) * (activation != "relu")
+        dz = dz * slope
+    half, tiny = U.UNIT[dtype], U.TINY[dtype]
+    rounded = off + half * (dz.abs() + off).clamp(min=tiny)
+    want = []
+    for a, b, o in ((dz, w.t(), rounded), (dz.t(), x.t(), rounded.t())):
+        b = b.double()
+        v, size = a @ b.t(), a.abs() @ b.abs().t()
+        far = s * (2 * U.F32 * (a.shape[1] + 8) * size + o @ b.abs().t()) + 4 * U.F32 * s * v.abs()
+        want.append((s * v, far + half * (s * v.abs() + far).clamp(min=tiny)))
+    db = s * dz.sum(0)
+    want.append((db, s * ((off + torch.zeros_like(dz)).sum(0) + 2 * U.F32 * (points + 8) * dz.abs().sum(0)) + 4 * U.F32 * db.abs()))
+
+    def check_all(g, z, **wanted):
+        for got, (v, bound), name in zip(learn.layer_gradient(g, x, w, z, activation, p, 77, **wanted), want, ("dx", "dw", "db")):
+            if got is not None:
+                bad = ~((got.double() - v).abs() <= bound)
+                assert not bad.any(), (name, wanted, int(bad.sum()), bad.nonzero()[0].tolist())
+
+    check_all(grad, pre)
+    check_all(grad, pre, for_w=False)
+    check_all(grad, pre, for_bias=False)
+    big = torch.full((points, units + 5), float("nan"), dtype=dtype, device="cuda")
+    part = big[:, 3:3 + units]
+    part.copy_(grad)
+    check_all(part, pre)
+    if activation:
+        part.copy_(pre)
+        check_all(grad, part)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_layouts(dtype):
     """Slices off the 16-byte boundaries with NaN around them, broadcast and
     transposed gradients, more dimensions."""
