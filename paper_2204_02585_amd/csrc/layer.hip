@@ -890,23 +890,49 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
     const uint64_t key = p.mask.on ? mask_key(p.mask) : 0;
     const uint32_t left = unit < p.units ? p.units - unit : 0;
     float sum[V] = {};
-    if (unit < p.pitch)
-#pragma unroll 2
-        for (uint64_t row = row0 + ty; row < end; row += down) {
-            float v[V], z[V];
-            load_inside<G, V>(static_cast<const G*>(p.grad) + row * p.grad_stride + unit, left, v);
-            if (p.pre)
-                load_inside<X, V>(static_cast<const X*>(p.pre) + row * p.pre_stride + unit, left, z);
-            if (p.mask.on)
-                apply_mask<V>(p.mask, key, row, unit, 1.0f, v);
-            if (p.pre)
-                times_slope<V>(p.act, z, v);
-            if (p.dz)
-                store_values<X, V>(static_cast<X*>(p.dz) + row * p.pitch + unit, p.pitch - unit, v);
+    // where the run is inside the row there is no branch between its loads and the
+    // next rows'
+    auto rows = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int TOGETHER = WHOLE ? 2 : 1;
+        for (uint64_t row = row0 + ty; row < end; row += TOGETHER * down) {
+            Raw<G, V> of_grad[TOGETHER];
+            Raw<X, V> of_pre[TOGETHER];
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                sum[k] += v[k];
+            for (int i = 0; i < TOGETHER; ++i) {
+                // rows past the end read the last one, and take part in nothing
+                const uint64_t at = std::min(row + i * down, end - 1);
+                of_grad[i].load(static_cast<const G*>(p.grad) + at * p.grad_stride + unit, WHOLE ? V : left);
+                if (p.pre)
+                    of_pre[i].load(static_cast<const X*>(p.pre) + at * p.pre_stride + unit, WHOLE ? V : left);
+            }
+#pragma unroll
+            for (int i = 0; i < TOGETHER; ++i) {
+                const uint64_t at = row + i * down;
+                if (at >= end)
+                    break;
+                float v[V], z[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    v[k] = to_f32(of_grad[i].e[k]);
+                    z[k] = p.pre ? to_f32(of_pre[i].e[k]) : 0.0f;
+                }
+                if (p.mask.on)
+                    apply_mask<V>(p.mask, key, at, unit, 1.0f, v);
+                if (p.pre)
+                    times_slope<V>(p.act, z, v);
+                if (p.dz)
+                    store_values<X, V>(static_cast<X*>(p.dz) + at * p.pitch + unit, WHOLE ? V : p.pitch - unit, v);
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    sum[k] += v[k];
+            }
         }
+    };
+    if (left >= V)
+        rows(std::true_type{});
+    else if (unit < p.pitch)
+        rows(std::false_type{});
     if (!p.sums && !p.bias)
         return;
 #pragma unroll
