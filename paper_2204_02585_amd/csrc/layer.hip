@@ -501,11 +501,12 @@ __device__ __forceinline__ void sum_steps(const BP& bring_p, const BQ& bring_q, 
 // Workgroups that follow each other go to the eight XCDs in turn: each takes a
 // run of the parts' tiles, in columns of 8 tiles of Q, so that what its CUs work
 // on at a time shares rows of both factors in the XCD's cache.
-__device__ __forceinline__ void tile_of(uint32_t tiles_p, uint32_t tiles_q, uint32_t& part, uint32_t& tp, uint32_t& tq)
+__device__ __forceinline__ void tile_of(uint32_t group, uint32_t groups, uint32_t tiles_p, uint32_t tiles_q, uint32_t& part,
+                                        uint32_t& tp, uint32_t& tq)
 {
     constexpr uint32_t kXcds = 8, kBand = 8;
-    const uint32_t each = gridDim.x / kXcds, more = gridDim.x % kXcds;
-    const uint32_t xcd = blockIdx.x % kXcds, nth = blockIdx.x / kXcds;
+    const uint32_t each = groups / kXcds, more = groups % kXcds;
+    const uint32_t xcd = group % kXcds, nth = group / kXcds;
     const uint32_t all = xcd * each + min(xcd, more) + nth;
     part = all / (tiles_p * tiles_q);
     const uint32_t t = all - part * tiles_p * tiles_q;
@@ -516,12 +517,11 @@ __device__ __forceinline__ void tile_of(uint32_t tiles_p, uint32_t tiles_q, uint
 }
 
 template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
-__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductParams p)
+__device__ __forceinline__ void tile_share(const ProductParams& p, uint32_t group, uint32_t groups, char* (&buffers)[S::BUFFERS])
 {
-    BUFFERS_IN_LDS(S)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t part, tp, tq;
-    tile_of(p.tiles_p, p.tiles_q, part, tp, tq);
+    tile_of(group, groups, p.tiles_p, p.tiles_q, part, tp, tq);
     const uint32_t p0 = tp * S::SIDE, q0 = tq * S::SIDE;
     const Bringer<X, S::SIDE, S::WAVES, PA> bring_p(p.p, p0);
     const Bringer<X, S::SIDE, S::WAVES, QA> bring_q(p.q, q0);
@@ -594,6 +594,24 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
         }
         wave_fence();
     }
+}
+
+template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
+__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductParams p)
+{
+    BUFFERS_IN_LDS(S)
+    tile_share<S, X, T, LAYER, PA, QA>(p, blockIdx.x, gridDim.x, buffers);
+}
+
+// Both products of a gradient side by side, the points' first.
+template <typename S, typename X>
+__global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void pair_kernel(ProductParams x, ProductParams w, uint32_t groups_x)
+{
+    BUFFERS_IN_LDS(S)
+    if (blockIdx.x < groups_x)
+        tile_share<S, X, X, false, true, false>(x, blockIdx.x, groups_x, buffers);
+    else
+        tile_share<S, X, X, false, true, true>(w, blockIdx.x - groups_x, gridDim.x - groups_x, buffers);
 }
 
 // The parts of the sums added up, in their order, and finished; zeros of no parts.
@@ -987,16 +1005,17 @@ __device__ __forceinline__ void bias_share(const BiasParams& p, uint32_t group)
     store_bias(p.bias, u, total * p.scale, p.dtype);
 }
 
-__global__ __launch_bounds__(kThreads) void bias_kernel(BiasParams p) { bias_share(p, blockIdx.x); }
-
-// The last sums of two gradients in one launch.
+// What is left of a gradient's sums in one launch: of the points, of the weights and
+// of the bias, each of some workgroups or none.
 template <typename X>
-__global__ __launch_bounds__(kThreads) void sums_kernel(PartsParams w, BiasParams bias, uint32_t groups_w)
+__global__ __launch_bounds__(kThreads) void sums_kernel(PartsParams x, PartsParams w, BiasParams bias, uint32_t groups_x, uint32_t groups_w)
 {
-    if (blockIdx.x < groups_w)
-        parts_share<X, X, false>(w, blockIdx.x, groups_w);
+    if (blockIdx.x < groups_x)
+        parts_share<X, X, false>(x, blockIdx.x, groups_x);
+    else if (blockIdx.x < groups_x + groups_w)
+        parts_share<X, X, false>(w, blockIdx.x - groups_x, groups_w);
     else
-        bias_share(bias, blockIdx.x - groups_w);
+        bias_share(bias, blockIdx.x - groups_x - groups_w);
 }
 
 // ---- choices
@@ -1498,6 +1517,7 @@ struct Plan {
     int64_t side;
     int64_t steps, part_steps, parts;
     size_t bytes;                // of the parts' sums
+    double time, work;           // alone, and of all CUs' time beside others
 };
 
 int64_t tiles_of(int64_t rows_p, int64_t rows_q, int64_t side) { return (rows_p + side - 1) / side * ((rows_q + side - 1) / side); }
@@ -1512,7 +1532,7 @@ int64_t tiles_of(int64_t rows_p, int64_t rows_q, int64_t side) { return (rows_p 
 // 256 by 256 89, 77 and 82; 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and
 // 16, 17 points of 4096 by 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384
 // points 58, 20 and 14.)
-Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
+Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t only = 0)
 {
     constexpr int64_t kSides[3] = {64, 128, 256}, kMostParts = 64, kCus = 256;
     constexpr double kStep[2][3] = {{0.26, 0.58, 1.32}, {0.51, 1.85, 7.2}}, kEnds[3] = {1.5, 3.0, 18.0};
@@ -1520,17 +1540,19 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
     const int f32 = dtype == SQN_F32 ? 1 : 0;
     const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
     const int64_t steps = (sum + step - 1) / step;
-    Plan r{64, steps, std::max<int64_t>(1, steps), steps ? 1 : 0, 0};
-    double least = HUGE_VAL;
+    Plan r{64, steps, std::max<int64_t>(1, steps), steps ? 1 : 0, 0, HUGE_VAL, 0.0};
     for (int s = 0; steps && s < 3; ++s) {
+        if (only && kSides[s] != only)
+            continue;
         const int64_t tiles = tiles_of(rows_p, rows_q, kSides[s]);
         for (int64_t parts = 1; parts <= std::min(kMostParts, steps); parts *= 2) {
             const int64_t each = (steps + parts - 1) / parts, used = (steps + each - 1) / each;
             const double sums = used > 1 ? 2.0 * used * 4.0 * rows_q * round_up(rows_p, 4) : 0.0;
-            const double time = static_cast<double>((tiles * used + kCus - 1) / kCus) * (each * kStep[f32][s] + kEnds[s])
-                + (used > 1 ? kJoin + sums / kJoinBytes : 0.0);
-            if (time < least) {
-                least = time;
+            const double group = each * kStep[f32][s] + kEnds[s], join = used > 1 ? kJoin + sums / kJoinBytes : 0.0;
+            const double time = static_cast<double>((tiles * used + kCus - 1) / kCus) * group + join;
+            if (time < r.time) {
+                r.time = time;
+                r.work = static_cast<double>(tiles * used) / kCus * group + join;
                 r.side = kSides[s];
                 r.part_steps = each;
                 r.parts = used;
@@ -1544,47 +1566,70 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype)
     return r;
 }
 
-template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
-void launch_tiles(ProductParams& p, hipStream_t stream)
-{
-    p.tiles_p = (p.f.units + S::SIDE - 1) / S::SIDE;
-    p.tiles_q = (p.rows + S::SIDE - 1) / S::SIDE;
-    tile_kernel<S, X, T, LAYER, PA, QA><<<p.tiles_p * p.tiles_q * p.parts, S::THREADS, 0, stream>>>(p);
-}
+// Both products of a gradient: in one launch where tiles of one side for both take
+// less than each by itself and a launch between them.  (All of a gradient in bfloat16,
+// so and apart: 1000 points of 512 by 512 17 us and 21, 2048 of 2048 by 2048 49 and 64,
+// 16 of 4096 by 4096 26 and 32.)
+struct GradientPlan {
+    Plan x, w;
+    bool pair;
 
-// The tiles of a product of `rows_q` rows, and, of several parts or none, what is
-// left to add up.  `partial` holds the plan's bytes.
-template <typename X, typename T, bool LAYER, bool PA, bool QA>
-PartsParams launch_tiles_of(const Operand& a, const Operand& b, int64_t rows_q, int64_t sum, const Finish& f, char* partial,
-                            int32_t dtype, hipStream_t stream)
+    GradientPlan(int64_t points, int64_t cols, int64_t units, int32_t dtype)
+        : x(plan_of(cols, points, units, dtype)), w(plan_of(cols, units, points, dtype)), pair(false)
+    {
+        constexpr double kLaunch = 3.0;
+        double least = x.time + w.time + kLaunch;
+        const Plan *best_x = nullptr, *best_w = nullptr;
+        Plan of_x[2], of_w[2];
+        for (int k = 0; points && k < 2; ++k) {
+            of_x[k] = plan_of(cols, points, units, dtype, 64 << k);
+            of_w[k] = plan_of(cols, units, points, dtype, 64 << k);
+            const double time = std::max({of_x[k].time, of_w[k].time, of_x[k].work + of_w[k].work});
+            if (time < least) {
+                least = time;
+                best_x = &of_x[k];
+                best_w = &of_w[k];
+            }
+        }
+        if (best_x) {
+            x = *best_x;
+            w = *best_w;
+            pair = true;
+        }
+    }
+};
+
+// A product of `rows` rows of C; `partial` holds the plan's bytes.
+ProductParams product_of(const Operand& a, const Operand& b, int64_t rows, const Plan& plan, const Finish& f, char* partial)
 {
-    const Plan plan = plan_of(f.units, rows_q, sum, dtype);
     ProductParams p{};
     p.p = a;
     p.q = b;
-    p.rows = static_cast<uint32_t>(rows_q);
+    p.rows = static_cast<uint32_t>(rows);
+    p.tiles_p = static_cast<uint32_t>((f.units + plan.side - 1) / plan.side);
+    p.tiles_q = static_cast<uint32_t>((rows + plan.side - 1) / plan.side);
     p.steps = static_cast<uint32_t>(plan.steps);
     p.part_steps = static_cast<uint32_t>(plan.part_steps);
     p.parts = static_cast<uint32_t>(plan.parts);
     p.partial = reinterpret_cast<float*>(partial);
     p.partial_pitch = static_cast<uint32_t>(round_up(f.units, 4));
     p.f = f;
-    if (plan.parts) {
-        if (plan.side == 256)
-            launch_tiles<Shape<256>, X, T, LAYER, PA, QA>(p, stream);
-        else if (plan.side == 128)
-            launch_tiles<Shape<128>, X, T, LAYER, PA, QA>(p, stream);
-        else
-            launch_tiles<Shape<64>, X, T, LAYER, PA, QA>(p, stream);
-    }
+    return p;
+}
+
+uint32_t groups_of(const ProductParams& p) { return p.tiles_p * p.tiles_q * p.parts; }
+
+// What is left to add up of several parts, or none.
+PartsParams parts_of(const ProductParams& p)
+{
     PartsParams j{};
     j.partial = p.partial;
-    j.rows = static_cast<uint64_t>(rows_q);
+    j.rows = p.rows;
     j.parts = p.parts;
     j.pitch = p.partial_pitch;
     j.per_row = j.pitch / 4;
     j.runs = j.rows * j.per_row;
-    j.f = f;
+    j.f = p.f;
     // up to 16 threads a run, while that leaves all of them busy
     j.slices = 1;
     while (2 * j.slices <= std::min(j.parts, 16u) && j.runs * j.slices < 256 * kThreads)
@@ -1592,15 +1637,30 @@ PartsParams launch_tiles_of(const Operand& a, const Operand& b, int64_t rows_q, 
     return j;
 }
 
-uint32_t groups_of(const PartsParams& j) { return groups_of(j.runs * j.slices); }
+uint32_t groups_of(const PartsParams& j) { return j.parts == 1 ? 0 : groups_of(j.runs * j.slices); }
 
 template <typename X, typename T, bool LAYER, bool PA, bool QA>
-void launch_product(const Operand& a, const Operand& b, int64_t rows_q, int64_t sum, const Finish& f, char* partial, int32_t dtype,
-                    hipStream_t stream)
+void launch_tiles(const ProductParams& p, int64_t side, hipStream_t stream)
 {
-    const PartsParams j = launch_tiles_of<X, T, LAYER, PA, QA>(a, b, rows_q, sum, f, partial, dtype, stream);
-    if (j.parts != 1)
-        parts_kernel<X, T, LAYER><<<groups_of(j), kThreads, 0, stream>>>(j);
+    const uint32_t groups = groups_of(p);
+    if (groups == 0)
+        return;
+    if (side == 256)
+        tile_kernel<Shape<256>, X, T, LAYER, PA, QA><<<groups, Shape<256>::THREADS, 0, stream>>>(p);
+    else if (side == 128)
+        tile_kernel<Shape<128>, X, T, LAYER, PA, QA><<<groups, Shape<128>::THREADS, 0, stream>>>(p);
+    else
+        tile_kernel<Shape<64>, X, T, LAYER, PA, QA><<<groups, Shape<64>::THREADS, 0, stream>>>(p);
+}
+
+template <typename X>
+void launch_pair(const ProductParams& x, const ProductParams& w, int64_t side, hipStream_t stream)
+{
+    const uint32_t of_x = groups_of(x), groups = of_x + groups_of(w);
+    if (side == 128)
+        pair_kernel<Shape<128>, X><<<groups, Shape<128>::THREADS, 0, stream>>>(x, w, of_x);
+    else
+        pair_kernel<Shape<64>, X><<<groups, Shape<64>::THREADS, 0, stream>>>(x, w, of_x);
 }
 
 template <typename X, typename T>
@@ -1615,7 +1675,12 @@ void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& 
         return;
     }
     const sqn_matrix a = packed(w, work, stream), b = packed(x, work, stream);
-    launch_product<X, T, true, false, false>(along(a), along(b), x.rows, x.cols, f, work, x.dtype, stream);
+    const Plan plan = plan_of(f.units, x.rows, x.cols, x.dtype);
+    const ProductParams p = product_of(along(a), along(b), x.rows, plan, f, work);
+    launch_tiles<X, T, true, false, false>(p, plan.side, stream);
+    const PartsParams j = parts_of(p);
+    if (j.parts != 1)
+        parts_kernel<X, T, true><<<groups_of(j), kThreads, 0, stream>>>(j);
 }
 
 // Workgroups of slope_kernel: `across` threads of one along a row, `rows` of it,
@@ -1645,7 +1710,9 @@ struct SlopePlan {
 // What a gradient keeps in its workspace, in this order.
 struct GradientScratch {
     bool own_dz;                 // grad is dz as it lies otherwise
-    size_t dz, sums, x, w, partial;
+    size_t dz, sums, x, w, partial_x, partial_w;
+    bool pair;                   // both products in one launch
+    Plan plan_x, plan_w;
 
     GradientScratch(const sqn_matrix& grad, const sqn_matrix& x_, const sqn_matrix& w_, bool slopes, bool for_x, bool for_w, bool for_bias)
     {
@@ -1659,11 +1726,15 @@ struct GradientScratch {
         sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
         x = for_w ? pack_bytes(x_) : 0;
         w = for_x && !narrow ? pack_bytes(w_) : 0;
-        partial = std::max(for_x && !narrow ? plan_of(x_.cols, points, units, x_.dtype).bytes : 0,
-                           for_w ? plan_of(x_.cols, units, points, x_.dtype).bytes : 0);
+        const GradientPlan plan(points, x_.cols, units, x_.dtype);
+        pair = plan.pair && for_x && for_w && !narrow;
+        plan_x = pair ? plan.x : plan_of(x_.cols, points, units, x_.dtype);
+        plan_w = pair ? plan.w : plan_of(x_.cols, units, points, x_.dtype);
+        partial_x = for_x && !narrow ? plan_x.bytes : 0;
+        partial_w = for_w ? plan_w.bytes : 0;
     }
 
-    size_t bytes() const { return dz + sums + x + w + partial; }
+    size_t bytes() const { return dz + sums + x + w + partial_x + partial_w; }
 };
 
 template <typename X>
@@ -1722,32 +1793,38 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         else
             slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
     }
-    // of one group they have been added up, of none they are zeros
-    const BiasParams bias = {sums, to.bias, groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
-    bool add_bias = to.bias && groups != 1;
-    const uint32_t bias_groups = static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits);
+    ProductParams of_x{}, of_w{};
+    PartsParams left_x{}, left_w{};
+    left_x.parts = left_w.parts = 1;     // nothing
     if (sloped) {
         // the points' gradient came with dz
     } else if (to.x && narrow_of(w, x.cols, units, points, true)) {
         launch_narrow<X, X, false, true>(w, dz, units, f, work, stream);
     } else if (to.x && points) {
         const sqn_matrix a = packed(w, work, stream);
-        launch_product<X, X, false, true, false>(across(a), along(dz), points, units, f, work + scratch.x, x.dtype, stream);
+        of_x = product_of(across(a), along(dz), points, scratch.plan_x, f, work);
+        work += scratch.partial_x;
+        left_x = parts_of(of_x);
+        if (!scratch.pair)
+            launch_tiles<X, X, false, true, false>(of_x, scratch.plan_x.side, stream);
     }
     if (to.w) {
         const sqn_matrix a = packed(x, work, stream);
         f.out = to.w->data;
         f.out_stride = to.w->row_stride;
-        const PartsParams j = launch_tiles_of<X, X, false, true, true>(across(a), across(dz), units, points, f, work, x.dtype, stream);
-        if (j.parts != 1 && add_bias) {
-            sums_kernel<X><<<groups_of(j) + bias_groups, kThreads, 0, stream>>>(j, bias, groups_of(j));
-            add_bias = false;
-        } else if (j.parts != 1) {
-            parts_kernel<X, X, false><<<groups_of(j), kThreads, 0, stream>>>(j);
-        }
+        of_w = product_of(across(a), across(dz), units, scratch.plan_w, f, work);
+        left_w = parts_of(of_w);
+        if (scratch.pair)
+            launch_pair<X>(of_x, of_w, scratch.plan_w.side, stream);
+        else
+            launch_tiles<X, X, false, true, true>(of_w, scratch.plan_w.side, stream);
     }
-    if (add_bias)
-        bias_kernel<<<bias_groups, kThreads, 0, stream>>>(bias);
+    // the bias's sums of one group have been added up, of none they are zeros
+    const BiasParams bias = {sums, to.bias, groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
+    const uint32_t bias_groups = to.bias && groups != 1 ? static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits) : 0;
+    const uint32_t all = groups_of(left_x) + groups_of(left_w) + bias_groups;
+    if (all)
+        sums_kernel<X><<<all, kThreads, 0, stream>>>(left_x, left_w, bias, groups_of(left_x), groups_of(left_w));
     return hipGetLastError();
 }
 

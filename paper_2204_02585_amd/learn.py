@@ -89,6 +89,11 @@ def _out(out: Optional[torch.Tensor], shape, dtype, beside: torch.Tensor, name: 
     return out
 
 
+def _out_like(t: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if type(t) is torch.Tensor and t.is_contiguous() else _out(None, t.shape, t.dtype, t)
+
+
 def _workspace(size: int, beside: torch.Tensor) -> Optional[torch.Tensor]:
     return torch.empty(size, dtype=torch.uint8, device=beside.device) if size else None
 
@@ -389,7 +394,7 @@ def _dropout(x, p, seed, step, residual, out, stream):
     if residual is not None:
         _beside(residual, x.shape, x.dtype, x, "residual")
     mask = _mask(p, seed, step, x)
-    out = _out(out, x.shape, x.dtype, x)
+    out = _out_like(x) if out is None else _out(out, x.shape, x.dtype, x)
     if out.numel() == 0:
         return out
     source, of_x = _operand(x, "x")
@@ -579,8 +584,8 @@ def layer_gradient(grad: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre: Op
     if bias_dtype != torch.float32 and bias_dtype != x.dtype:
         raise TypeError(f"bias_dtype must be float32 or x's {x.dtype}, got {bias_dtype}")
     mask = _mask(p, seed, step, x) if p or step is not None else None
-    grad_x = _out(None, x.shape, x.dtype, x) if for_x else None
-    grad_w = _out(None, w.shape, w.dtype, x) if for_w else None
+    grad_x = _out_like(x) if for_x else None
+    grad_w = _out_like(w) if for_w else None
     grad_bias = _out(None, (w.shape[0],), bias_dtype, x) if for_bias else None
     g, of_g = _operand(grad, "grad")
     a, of_x = _operand(x, "x")
