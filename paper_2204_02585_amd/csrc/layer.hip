@@ -9,7 +9,15 @@
 // it lies in memory: the tiles of tile.h, whose steps bring 128 bytes of the sum
 // of every row, or as many elements of the sum across, and the LDS reads that
 // turn 16-bit elements on their way to the registers.  Nothing is transposed in
-// memory.
+// memory.  Three kernels share the work: tiles; narrow layers of many points, whose
+// bytes are all that counts, with their weights in registers; and layers of few
+// points, with nothing but the weights' bytes.  Which, goes by sizes and alignment
+// (plan_of, layer_plan, GradientPlan, narrow_of, launch_layer_typed).
+//
+// Rounding.  Sums and epilogues are binary32.  dz is rounded to the factors' type
+// for its products (bfloat16: a gradient's error is 2.3e-3 of its norm, 1.7e-3 of it
+// the gradient's own rounding), before the mask's share, which is applied to the
+// sums: so it stays in binary16's range.  The bias's sums take it unrounded.
 #include <math.h>
 #include <algorithm>
 #include <type_traits>
@@ -50,8 +58,9 @@ struct Finish {
 // Phi(-a) = exp(-a^2 / 2) q(a) for a >= 0, and t = 1 / (1 + 0.35 a) takes q to the
 // whole of (0, 1]: a polynomial of degree 9 in t, fitted for the least relative
 // error (3.2e-8; 3.3e-7 with binary32's roundings), so that the values far below
-// zero keep their digits.  20 operations a value with the exponential that the
-// slope shares, where erfcf and expf took 80: of 8192 x 8192 outputs 170 us.
+// zero keep their digits.  22 operations a value, with the exponential that the
+// slope shares (erfcf and expf take some 80: 8192 x 8192 outputs with a mask and z
+// kept took 691 us of a layer, with the loads of the bias that left with them, 545 so).
 __device__ __forceinline__ float normal_share(float z, float& bell)
 {
     const float a = fabsf(z);
@@ -384,9 +393,9 @@ __device__ __forceinline__ float16v multiply(const uint4& a, const uint4& b, int
 // ---- tiles
 
 // A workgroup's tile: SIDE x SIDE of C by 2 x 2 waves.  The wide accumulators of
-// the largest tile (128 x 128 a wave, one wave a SIMD) halve what the products
-// read from LDS: with eight waves of 128 x 64 reads and loads took all of its
-// cycles.
+// the largest tile (128 x 128 a wave, one wave a SIMD) spare LDS: of the 128 bytes a
+// cycle it moves, reads and loads take 96 beside matrix cores that never wait; with
+// eight waves of 128 x 64 they would take all, in tiles of 128 they would take 192.
 template <int SIDE_>
 struct Shape {
     static constexpr int SIDE = SIDE_;
@@ -665,10 +674,10 @@ __device__ __forceinline__ void parts_share(const PartsParams& p, uint32_t group
     }
 }
 
-template <typename X, typename T, bool LAYER>
+template <typename X, typename T>
 __global__ __launch_bounds__(kThreads) void parts_kernel(PartsParams p)
 {
-    parts_share<X, T, LAYER>(p, blockIdx.x, gridDim.x);
+    parts_share<X, T, true>(p, blockIdx.x, gridDim.x);
 }
 
 // ---- layers of few points
@@ -1008,7 +1017,8 @@ __device__ __forceinline__ void bias_share(const BiasParams& p, uint32_t group)
 // What is left of a gradient's sums in one launch: of the points, of the weights and
 // of the bias, each of some workgroups or none.
 template <typename X>
-__global__ __launch_bounds__(kThreads) void sums_kernel(PartsParams x, PartsParams w, BiasParams bias, uint32_t groups_x, uint32_t groups_w)
+__global__ __launch_bounds__(kThreads) void sums_kernel(PartsParams x, PartsParams w, BiasParams bias, uint32_t groups_x,
+                                                        uint32_t groups_w)
 {
     if (blockIdx.x < groups_x)
         parts_share<X, X, false>(x, blockIdx.x, groups_x);
@@ -1135,7 +1145,8 @@ struct Narrow {
     static constexpr int STEP = POINTS * static_cast<int>(kStepBytes), ROWS = STEPS * STEP;
     static constexpr int BUFFER = SLOPE ? 2 * ROWS : ROWS;            // grad's rows, and pre's
     static constexpr int LOADS = ROWS / (64 * LOAD) / BRINGERS;     // instructions of a slab, of a wave
-    static constexpr int PIECES = SIDE * static_cast<int>(kStepBytes) / (static_cast<int>(kSlot) * THREADS);    // of P, a thread and step
+    static constexpr int P_STEP = SIDE * static_cast<int>(kStepBytes);
+    static constexpr int PIECES = P_STEP / (static_cast<int>(kSlot) * THREADS);    // of P, a thread and step
 };
 
 template <typename S, typename X, typename T, bool LAYER, bool PA>
@@ -1143,7 +1154,7 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
 {
     BUFFERS_IN_LDS(S)
     constexpr int OWN = 32 * 128;
-    constexpr int SHARED = S::WAVES * OWN > S::SIDE * static_cast<int>(kStepBytes) ? S::WAVES * OWN : S::SIDE * static_cast<int>(kStepBytes);
+    constexpr int SHARED = std::max(S::WAVES * OWN, S::P_STEP);
     __shared__ __align__(16) char shared[SHARED];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t slabs = (p.points + S::POINTS - 1) / S::POINTS;
@@ -1522,20 +1533,23 @@ struct Plan {
 
 int64_t tiles_of(int64_t rows_p, int64_t rows_q, int64_t side) { return (rows_p + side - 1) / side * ((rows_q + side - 1) / side); }
 
+// A step of tiles of 64, 128 and 256 and a tile's start and end, in us.
+constexpr int64_t kSides[3] = {64, 128, 256}, kCus = 256;
+constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79, 7.2}}, kEnds[3] = {1.5, 3.0, 18.0};
+
 // Tiles and parts by what they take, in us: the rounds of workgroups on 256 CUs,
 // each the steps of a part and a start and an end, and a launch and the bytes of the
 // parts' sums behind them.  A step's time is the CU's matrix cores' in the largest
-// tiles and for binary32, and what L2 delivers in the smaller ones; two workgroups
-// share a CU without getting through more steps.  (us by side, 64, 128 and 256, of
-// bfloat16: 4096 points of 256 by 256 5, 7 and 20; 65,536 40, 23 and 26; 2048 of 4096
-// by 2048 54, 44 and 87; 8192 of 1024 by 1024 35, 23 and 36; of binary32: 65,536 of
-// 256 by 256 89, 77 and 82; 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and
-// 16, 17 points of 4096 by 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384
-// points 58, 20 and 14.)
+// tiles and for binary32, and what L2 and LDS deliver in the smaller ones, of which
+// two workgroups share a CU.  (us by side, 64, 128 and 256, of bfloat16: 4096 points
+// of 256 by 256 5, 7 and 20; 65,536 40, 23 and 26; 2048 of 4096 by 2048 54, 44 and 87;
+// 8192 of 1024 by 1024 35, 23 and 36; of binary32: 65,536 of 256 by 256 89, 77 and 82;
+// 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and 16, 17 points of 4096 by
+// 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384 points 58, 20 and 14.)
 Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t only = 0)
 {
-    constexpr int64_t kSides[3] = {64, 128, 256}, kMostParts = 64, kCus = 256;
-    constexpr double kStep[2][3] = {{0.26, 0.58, 1.32}, {0.51, 1.85, 7.2}}, kEnds[3] = {1.5, 3.0, 18.0};
+    constexpr int64_t kMostParts = 64;
+    constexpr double kAlone = 0.12;      // a step in tiles of 128 takes more without another workgroup beside it
     constexpr double kJoin = 4.0, kJoinBytes = 3.5e6;            // a us
     const int f32 = dtype == SQN_F32 ? 1 : 0;
     const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
@@ -1548,8 +1562,10 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t
         for (int64_t parts = 1; parts <= std::min(kMostParts, steps); parts *= 2) {
             const int64_t each = (steps + parts - 1) / parts, used = (steps + each - 1) / each;
             const double sums = used > 1 ? 2.0 * used * 4.0 * rows_q * round_up(rows_p, 4) : 0.0;
-            const double group = each * kStep[f32][s] + kEnds[s], join = used > 1 ? kJoin + sums / kJoinBytes : 0.0;
-            const double time = static_cast<double>((tiles * used + kCus - 1) / kCus) * group + join;
+            const int64_t rounds = (tiles * used + kCus - 1) / kCus;
+            const double group = each * (kStep[f32][s] + (s == 1 && rounds == 1 ? kAlone : 0.0)) + kEnds[s];
+            const double join = used > 1 ? kJoin + sums / kJoinBytes : 0.0;
+            const double time = rounds * group + join;
             if (time < r.time) {
                 r.time = time;
                 r.work = static_cast<double>(tiles * used) / kCus * group + join;
@@ -1564,6 +1580,28 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t
     }
     r.bytes = r.parts > 1 ? aligned(static_cast<size_t>(r.parts) * rows_q * round_up(rows_p, 4) * 4) : 0;
     return r;
+}
+
+// A layer's tiles: an epilogue that computes or moves more than the sums stands alone
+// in tiles of 256 and beside another tile's products in those of 128.  (8192 by 8192
+// outputs with GELU, a mask and z kept, sums of 1024 elements: 224 and 256 us in tiles
+// of 128 and 256, of 4096 elements 609 and 566.)
+Plan layer_plan(const Finish& f, int64_t rows, int64_t sum, int32_t dtype)
+{
+    Plan plan = plan_of(f.units, rows, sum, dtype);
+    if (plan.side != 256 || plan.parts != 1)
+        return plan;
+    constexpr double kCompute = 9.0, kMove = 11.0, kBeside = 0.2;      // us of a tile of 256; of that in one of 128
+    const double more = kCompute * ((f.act > SQN_ACT_RELU ? 1 : 0) + f.mask.on)
+        + kMove * ((f.pre ? 1 : 0) + (f.residual ? 1 : 0));
+    const int f32 = dtype == SQN_F32 ? 1 : 0;
+    auto time = [&](int s, double ends) {
+        const int64_t rounds = (tiles_of(f.units, rows, kSides[s]) + kCus - 1) / kCus;
+        return rounds * (plan.steps * kStep[f32][s] + kEnds[s] + ends);
+    };
+    if (time(1, kBeside * more) < time(2, more))
+        plan.side = 128;
+    return plan;
 }
 
 // Both products of a gradient: in one launch where tiles of one side for both take
@@ -1675,12 +1713,12 @@ void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& 
         return;
     }
     const sqn_matrix a = packed(w, work, stream), b = packed(x, work, stream);
-    const Plan plan = plan_of(f.units, x.rows, x.cols, x.dtype);
+    const Plan plan = layer_plan(f, x.rows, x.cols, x.dtype);
     const ProductParams p = product_of(along(a), along(b), x.rows, plan, f, work);
     launch_tiles<X, T, true, false, false>(p, plan.side, stream);
     const PartsParams j = parts_of(p);
     if (j.parts != 1)
-        parts_kernel<X, T, true><<<groups_of(j), kThreads, 0, stream>>>(j);
+        parts_kernel<X, T><<<groups_of(j), kThreads, 0, stream>>>(j);
 }
 
 // Workgroups of slope_kernel: `across` threads of one along a row, `rows` of it,
@@ -1767,7 +1805,8 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
     uint32_t groups = plan.groups;       // of the bias's sums
     const bool sloped = to.x && (scratch.own_dz || to.bias) && narrow_sloped(grad, x, w, pre);
     if (sloped) {
-        groups = launch_sloped<X>(w, grad, pre, act, m, scratch.own_dz && to.w ? dz.data : nullptr, dz.cols, to.bias ? sums : nullptr, f, stream);
+        groups = launch_sloped<X>(w, grad, pre, act, m, scratch.own_dz && to.w ? dz.data : nullptr, dz.cols,
+                                  to.bias ? sums : nullptr, f, stream);
     } else if (points && (scratch.own_dz || to.bias)) {
         SlopeParams p{};
         p.grad = grad.data;

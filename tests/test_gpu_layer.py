@@ -152,6 +152,18 @@ def test_layouts(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(3, 500, 300), (17, 4096, 520), (300, 64, 200), (20001, 42, 250), (33000, 64, 200), (2100, 128, 1700)])
+def test_onto_the_residual(dtype, size):
+    """The result in the residual's own memory, whatever the kernel, is what it is
+    elsewhere."""
+    from paper_2204_02585_amd import learn
+    x, w, bias, residual = inputs(*size, dtype)
+    want = learn.layer(x, w, bias, "silu", residual, dropout=0.25, seed=8)
+    assert learn.layer(x, w, bias, "silu", residual, dropout=0.25, seed=8, out=residual) is residual
+    assert torch.equal(residual, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("size", [(2, 100, 40), (40, 100, 40), (40, 4096, 70)])
 def test_not_finite(dtype, size):
     """A NaN or an infinity stays in its row, and products with zeros beside the

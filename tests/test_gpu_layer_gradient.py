@@ -117,6 +117,7 @@ def test_many_points_with_slopes(dtype, points, cols, units, activation, p):
                 assert not bad.any(), (name, wanted, int(bad.sum()), bad.nonzero()[0].tolist())
 
     check_all(grad, pre)
+    check_all(grad.float(), pre)
     check_all(grad, pre, for_w=False)
     check_all(grad, pre, for_bias=False)
     big = torch.full((points, units + 5), float("nan"), dtype=dtype, device="cuda")
