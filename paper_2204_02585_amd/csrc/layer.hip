@@ -130,6 +130,17 @@ __device__ __forceinline__ void times_slope(uint32_t act, const float (&z)[V], f
     }
 }
 
+// The ragged run's address by an offset of zero that the compiler does not know: its
+// accesses were merged with the whole run's where they share one, and a store of 16
+// bytes went out as two of 4 and one of 8, or as two of 2 and one of 12.
+template <typename T>
+__device__ __forceinline__ T* ragged(T* p)
+{
+    uint32_t zero = 0;
+    asm("" : "+v"(zero));
+    return p + zero;
+}
+
 // A run of V elements of which `left` are inside the row.
 template <typename T, int V>
 __device__ __forceinline__ void load_inside(const T* p, uint32_t left, float (&v)[V])
@@ -137,9 +148,10 @@ __device__ __forceinline__ void load_inside(const T* p, uint32_t left, float (&v
     if (left >= V) {
         load_run<T, V>(p, v);
     } else {
+        const T* q = ragged(p);
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            v[k] = k < static_cast<int>(left) ? to_f32(p[k]) : 0.0f;
+            v[k] = k < static_cast<int>(left) ? to_f32(q[k]) : 0.0f;
     }
 }
 
@@ -149,10 +161,11 @@ __device__ __forceinline__ void store_values(T* p, uint32_t left, const float (&
     if (left >= V) {
         store_run<T, V>(p, v);
     } else {
+        T* q = ragged(p);
 #pragma unroll
         for (int k = 0; k < V; ++k)
             if (k < static_cast<int>(left))
-                p[k] = from_f32<T>(v[k]);
+                q[k] = from_f32<T>(v[k]);
     }
 }
 
@@ -165,12 +178,13 @@ struct Raw {
     __device__ __forceinline__ void load(const T* p, uint32_t left)
     {
         if (left >= V) {
-            const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
+                const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
             __builtin_memcpy(e, &r, sizeof(e));
         } else {
+            const T* q = ragged(p);
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                e[k] = k < static_cast<int>(left) ? p[k] : T(0.0f);
+                e[k] = k < static_cast<int>(left) ? q[k] : T(0.0f);
         }
     }
 };
@@ -1123,10 +1137,11 @@ __device__ __forceinline__ uint4 piece_of(const X* p, int32_t left)
         __builtin_memcpy(&v, &r, 16);
         return v;
     }
+    const X* q = ragged(p);
     X e[N];
 #pragma unroll
     for (int k = 0; k < N; ++k)
-        e[k] = k < left ? p[k] : X(0.0f);
+        e[k] = k < left ? q[k] : X(0.0f);
     uint4 v;
     __builtin_memcpy(&v, e, 16);
     return v;
