@@ -1396,14 +1396,20 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
 
 // Layers whose weights a workgroup's registers hold, of points enough for several
 // slabs a CU, where tiles would need copies onto 16-byte boundaries or read the
-// points twice.  (us so and in tiles: 65,536 points of 256 by 256 in binary16 23
-// and 24, the gradient of its points 19 and 25, of 20,000 10 and 9, 64 wide 14 and
-// 12; of 50,001 points of binary32 of 42 by 256 31 and 58.)
+// points twice; of binary16 and bfloat16 also where tiles of 64 and 128 are so many
+// that their starts and ends are most of the time.  (us so and in tiles: 65,536
+// points of 256 by 256 in binary16 19 and 20, the gradient of its points 17 and 18,
+// of 500,000 116 and 154, of 20,000 11 and 10; of 64 by 64 of 65,536 8.0 and 7.7, of
+// 131,072 12 and 13, of 500,000 25 and 46, in binary32 72 and 80; of 128 by 128 of
+// 500,000 42 and 56, in binary32 187 and 176; of 50,001 points of 42 by 256 of
+// binary32 31 and 46.)
 bool narrow_of(const sqn_matrix& w, int64_t units, int64_t sum, int64_t points, bool points_in_place)
 {
     if (units > kNarrowRows || sum * static_cast<int64_t>(element_size(w.dtype)) > 4 * kStepBytes || points < kNarrowPoints)
         return false;
-    return !in_place(w) || !points_in_place || (units > kNarrowRows / 2 && points >= 2 * kNarrowPoints);
+    if (!in_place(w) || !points_in_place)
+        return true;
+    return units > kNarrowRows / 2 ? points >= 2 * kNarrowPoints : w.dtype != SQN_F32 && points >= 8 * kNarrowPoints;
 }
 
 // Whether the points' rows can be brought from where they lie: binary32 elements

@@ -114,6 +114,24 @@ def test_many_points(dtype, points, cols, units):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("points", [131071, 131072, 131103])
+@pytest.mark.parametrize("cols,units", [(64, 64), (128, 100), (256, 8), (8, 128), (40, 40)])
+def test_most_points(dtype, points, cols, units):
+    """Layers of 128 units and fewer, all on the boundaries, of points so many that
+    another kernel takes them, and of one less."""
+    from paper_2204_02585_amd import learn
+    x, w, bias, residual = inputs(points, cols, units, dtype)
+    pre = torch.empty_like(residual)
+    y = learn.layer(x, w, bias, "relu", residual, pre=pre)
+    z, off = on_gpu(x, w, bias, residual)
+    off_z = off + U.UNIT[dtype] * (z.abs() + off) + U.UNIT[dtype] * U.TINY[dtype]
+    assert ((pre.double() - z).abs() <= off_z).all()
+    want = z.clamp(min=0) + residual.double()
+    off = off + 4 * U.F32 * want.abs()
+    assert ((y.double() - want).abs() <= off + U.UNIT[dtype] * (want.abs() + off) + U.UNIT[dtype] * U.TINY[dtype]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_layouts(dtype):
     """Slices off the 16-byte boundaries with NaN around them, transposed and
     broadcast factors, more dimensions, results inside a larger tensor whose rest

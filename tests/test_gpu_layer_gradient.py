@@ -64,7 +64,8 @@ def test_many_tiles(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("points,cols,units", [(16384, 256, 64), (20001, 250, 50), (16385, 50, 256), (16400, 100, 128), (16390, 33, 130), (17000, 1, 1)])
+@pytest.mark.parametrize("points,cols,units", [(16384, 256, 64), (20001, 250, 50), (16385, 50, 256), (16400, 100, 128), (16390, 33, 130), (17000, 1, 1),
+                                               (131071, 64, 64), (131072, 64, 64), (131103, 128, 100), (131073, 40, 256), (140000, 8, 8)])
 def test_many_points(dtype, points, cols, units):
     """Narrow layers of many points."""
     from paper_2204_02585_amd import learn
