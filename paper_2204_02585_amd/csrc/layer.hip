@@ -60,7 +60,7 @@ struct Finish {
 // error (3.2e-8; 3.3e-7 with binary32's roundings), so that the values far below
 // zero keep their digits.  22 operations a value, with the exponential that the
 // slope shares (erfcf and expf take some 80: 8192 x 8192 outputs with a mask and z
-// kept took 691 us of a layer, with the loads of the bias that left with them, 545 so).
+// kept took 691 us of a layer, with the loads of the bias that left with them 545).
 __device__ __forceinline__ float normal_share(float z, float& bell)
 {
     const float a = fabsf(z);
@@ -1105,7 +1105,7 @@ sqn_matrix packed(const sqn_matrix& m, char*& to, hipStream_t stream)
 // one of four LDS buffers, the next three under way.  Of UB blocks of P the
 // workgroup's waves take one each, SUBS times, with 32 points of the slab each.
 // (Tiles read the points' rows once for every 128 units and wait for their loads a
-// round at a time: 65,536 points of 256 by 256 in binary16 24 us.)
+// round at a time: 500,000 points of 256 by 256 in binary16 154 us, 116 so.)
 
 constexpr int kNarrowRows = 256;
 constexpr int64_t kNarrowPoints = 16384;
@@ -1563,8 +1563,8 @@ constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79, 7.2}}, kEnds[3]
 // parts' sums behind them.  A step's time is the CU's matrix cores' in the largest
 // tiles and for binary32, and what L2 and LDS deliver in the smaller ones, of which
 // two workgroups share a CU.  (us by side, 64, 128 and 256, of bfloat16: 4096 points
-// of 256 by 256 5, 7 and 20; 65,536 40, 23 and 26; 2048 of 4096 by 2048 54, 44 and 87;
-// 8192 of 1024 by 1024 35, 23 and 36; of binary32: 65,536 of 256 by 256 89, 77 and 82;
+// of 256 by 256 5, 7 and 19; 65,536 34, 21 and 25; 2048 of 4096 by 2048 54, 44 and 85;
+// 8192 of 1024 by 1024 33, 23 and 36; of binary32: 65,536 of 256 by 256 84, 75 and 80;
 // 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and 16, 17 points of 4096 by
 // 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384 points 58, 20 and 14.)
 Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t only = 0)
@@ -1604,17 +1604,17 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t
 }
 
 // A layer's tiles: an epilogue that computes or moves more than the sums stands alone
-// in tiles of 256 and beside another tile's products in those of 128.  (8192 by 8192
-// outputs with GELU, a mask and z kept, sums of 1024 elements: 224 and 256 us in tiles
-// of 128 and 256, of 4096 elements 609 and 566.)
+// in tiles of 256 and beside another tile's products in those of 128.  (us in tiles of
+// 128 and 256, 8192 by 8192 outputs in bfloat16: sums of 2048 elements with z kept 288
+// and 272, with GELU and a mask 312 and 324, with a residual 319 and 345; with GELU, a
+// mask and z kept, of 1024 211 and 229, of 2048 324 and 330, of 4096 591 and 546.)
 Plan layer_plan(const Finish& f, int64_t rows, int64_t sum, int32_t dtype)
 {
     Plan plan = plan_of(f.units, rows, sum, dtype);
     if (plan.side != 256 || plan.parts != 1)
         return plan;
-    constexpr double kCompute = 9.0, kMove = 11.0, kBeside = 0.2;      // us of a tile of 256; of that in one of 128
-    const double more = kCompute * ((f.act > SQN_ACT_RELU ? 1 : 0) + f.mask.on)
-        + kMove * ((f.pre ? 1 : 0) + (f.residual ? 1 : 0));
+    constexpr double kCompute = 17.0, kKeep = 11.0, kAdd = 33.0, kBeside = 0.2;     // us of a tile of 256; of that in one of 128
+    const double more = kCompute * ((f.act > SQN_ACT_RELU ? 1 : 0) + f.mask.on) + kKeep * (f.pre ? 1 : 0) + kAdd * (f.residual ? 1 : 0);
     const int f32 = dtype == SQN_F32 ? 1 : 0;
     auto time = [&](int s, double ends) {
         const int64_t rounds = (tiles_of(f.units, rows, kSides[s]) + kCus - 1) / kCus;
