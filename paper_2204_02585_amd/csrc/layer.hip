@@ -178,7 +178,7 @@ struct Raw {
     __device__ __forceinline__ void load(const T* p, uint32_t left)
     {
         if (left >= V) {
-                const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
+            const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
             __builtin_memcpy(e, &r, sizeof(e));
         } else {
             const T* q = ragged(p);
