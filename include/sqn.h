@@ -559,9 +559,10 @@ size_t sqn_layer_workspace(const sqn_matrix* x, const sqn_matrix* w);
 /* The gradients of sqn_layer from grad, that of its output:
  *   dz = D(grad) act'(z),  grad_x = dz w,  grad_w = dz^T x,  grad_bias = sum of dz's rows
  * (the residual's is grad itself).  Sums are binary32, in an order that the
- * arguments fix; act'(0) of max(0, z) is 0.  For products of binary16 and
- * bfloat16 factors dz is rounded to x's dtype, before its share 1 / (1 - p);
- * grad_bias sums it unrounded.
+ * arguments fix; act'(0) of max(0, z) is 0.  Beside bfloat16 factors dz is
+ * held to 2^-15 of itself, beside binary16 ones a product with it to 2^-13, in
+ * binary32's range, and exactly where it is grad's own values (of x's dtype,
+ * without an activation or with max(0, z)).
  *   grad:      [points][units] of x's dtype or SQN_F32;
  *   pre:       [points][units] of x's dtype, the z that sqn_layer wrote; NULL
  *              and only then for SQN_ACT_NONE;

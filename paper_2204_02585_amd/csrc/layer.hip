@@ -14,10 +14,11 @@
 // points, with nothing but the weights' bytes.  Which, goes by sizes and alignment
 // (plan_of, layer_plan, GradientPlan, narrow_of, launch_layer_typed).
 //
-// Rounding.  Sums and epilogues are binary32.  dz is rounded to the factors' type
-// for its products (bfloat16: a gradient's error is 2.3e-3 of its norm, 1.7e-3 of it
-// the gradient's own rounding), before the mask's share, which is applied to the
-// sums: so it stays in binary16's range.  The bias's sums take it unrounded.
+// Rounding.  Sums and epilogues are binary32.  Matrix instructions take dz in 16 bits
+// beside 16-bit factors: as it is where it is grad's own values and zeros, else in two
+// parts (terms_of), so that a gradient's error is that of its own rounding.  The mask's
+// share is applied to the sums, before which dz stays in grad's range.  The bias's sums
+// take it in binary32.
 #include <math.h>
 #include <algorithm>
 #include <type_traits>
@@ -247,6 +248,20 @@ struct Operand {
     uint64_t pitch;              // bytes from row to row in memory, a multiple of 16
     uint32_t rows;               // of the factor: along, rows in memory; across, elements of one, in whole 16 bytes
     uint32_t valid;              // of the sum: along, bytes of a row, whole 16; across, rows in memory
+    uint64_t apart;              // bytes from the high parts of the elements to their low ones
+    uint32_t low;                // bit t: term t of the product takes the low parts
+};
+
+// A product of factors in parts: every step of the sum comes once for each term,
+// whose parts the operands name.  Terms of a step follow each other, so that what
+// they share is in the caches.
+struct Terms {
+    uint32_t count, inverse, whole;      // 2^32 / count rounded up, 0 of one; 1 of one
+
+    Terms(uint32_t n = 1) : count(n), inverse(n == 1 ? 0 : n == 2 ? 0x80000000u : 0x55555556u), whole(n == 1) {}
+
+    // the step that step k of all is a term of: exact below 2^31
+    __device__ __forceinline__ uint32_t step(uint32_t k) const { return __umulhi(k, inverse) + k * whole; }
 };
 
 template <typename X>
@@ -267,10 +282,14 @@ __device__ __forceinline__ uint32_t across_key(uint32_t k)
         return SIDE >= 128 ? 4 * (k & 3) : 4 * (k >> 1 & 1);
 }
 
+// Whether a product can have factors in parts.
+template <typename X, bool LAYER>
+constexpr bool kParted = !LAYER && sizeof(X) == 2;
+
 // What a lane brings of a factor's steps, through a buffer descriptor of the
 // tile's rows: pieces past the sum's end lie past the descriptor's, and come as
 // zeros without an access.
-template <typename X, int SIDE, int WAVES, bool ACROSS>
+template <typename X, int SIDE, int WAVES, bool ACROSS, bool PARTED>
 struct Bringer {
     static constexpr int COUNT = SIDE * static_cast<int>(kStepBytes) / (1024 * WAVES);
     static constexpr uint32_t SLOTS = SIDE * sizeof(X) / kSlot;  // of a row across
@@ -280,8 +299,12 @@ struct Bringer {
     uint32_t at[COUNT], place[ACROSS ? COUNT : 1];
     uint32_t valid;
     uint64_t on;                 // bytes from step to step
+    uint64_t apart;              // with PARTED, as the next two
+    uint32_t low;
+    Terms terms;
 
-    __device__ __forceinline__ Bringer(const Operand& o, uint32_t row0)
+    __device__ __forceinline__ Bringer(const Operand& o, uint32_t row0, const Terms& t)
+        : apart(o.apart), low(o.low), terms(t)
     {
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         valid = o.valid;
@@ -317,8 +340,14 @@ struct Bringer {
 
     __device__ __forceinline__ Step step(uint32_t k) const
     {
+        uint64_t part = 0;
+        if constexpr (PARTED) {
+            const uint32_t term = k;
+            k = terms.step(term);
+            part = low >> (term - k * terms.count) & 1 ? apart : 0;
+        }
         // raw bytes, OUTSIDE of them
-        return {__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from + k * on), 0, OUTSIDE, 0x00020000),
+        return {__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from + part + k * on), 0, OUTSIDE, 0x00020000),
                 valid - k * (ACROSS ? Elements<X>::STEP : kStepBytes)};
     }
 
@@ -426,7 +455,8 @@ struct ProductParams {
     Operand p, q;
     uint32_t rows;               // of C
     uint32_t tiles_p, tiles_q;   // of C
-    uint32_t steps, part_steps;  // of the sum, of a part of it
+    uint32_t steps, part_steps;  // of the sum, all terms of it, and of a part of it
+    Terms terms;
     uint32_t parts;              // 1: the sums are finished here
     float* partial;              // [parts][rows][partial_pitch]
     uint32_t partial_pitch;
@@ -443,7 +473,9 @@ struct Fragments {
 // at a step's last depth, of the loads into the buffer that it leaves.  With one
 // wave a SIMD whatever stands in a block of its own leaves the matrix cores idle
 // (the compiler's order: 1,040 TFLOP/s of 8192 x 8192 by 4096 in bfloat16).
-template <typename S, typename X, typename BP, typename BQ, typename RP, typename RQ>
+// (T, the output's type, is here for the host's pass, which has none of the builtins
+// and takes a function whose body it could not read only once.)
+template <typename S, typename X, typename T, typename BP, typename BQ, typename RP, typename RQ>
 __device__ __forceinline__ void sum_steps(const BP& bring_p, const BQ& bring_q, const RP& read_p, const RQ& read_q, uint32_t first,
                                           uint32_t steps, char* (&buffers)[S::BUFFERS], float16v (&acc)[S::F][S::F])
 {
@@ -546,8 +578,8 @@ __device__ __forceinline__ void tile_share(const ProductParams& p, uint32_t grou
     uint32_t part, tp, tq;
     tile_of(group, groups, p.tiles_p, p.tiles_q, part, tp, tq);
     const uint32_t p0 = tp * S::SIDE, q0 = tq * S::SIDE;
-    const Bringer<X, S::SIDE, S::WAVES, PA> bring_p(p.p, p0);
-    const Bringer<X, S::SIDE, S::WAVES, QA> bring_q(p.q, q0);
+    const Bringer<X, S::SIDE, S::WAVES, PA, kParted<X, LAYER>> bring_p(p.p, p0, p.terms);
+    const Bringer<X, S::SIDE, S::WAVES, QA, kParted<X, LAYER>> bring_q(p.q, q0, p.terms);
     const uint32_t wave_p = (wave & 1) * (S::SIDE / 2), wave_q = (wave >> 1) * (S::SIDE / 2);
     const Reader<X, S::SIDE, PA, S::F> read_p(wave_p);
     const Reader<X, S::SIDE, QA, S::F> read_q(wave_q);
@@ -565,7 +597,7 @@ __device__ __forceinline__ void tile_share(const ProductParams& p, uint32_t grou
         for (int t = 0; t < S::F; ++t)
             acc[s][t] = float16v{};
     const uint32_t first = part * p.part_steps, count = min(p.part_steps, p.steps - first);
-    sum_steps<S, X>(bring_p, bring_q, read_p, read_q, first, count, buffers, acc);
+    sum_steps<S, X, T>(bring_p, bring_q, read_p, read_q, first, count, buffers, acc);
     // out through LDS in binary32, a column of blocks at a time, so that a lane
     // finishes runs of rows, always of the same units
     constexpr uint32_t PITCH = S::F * 32 * 4, PIECES = PITCH / 16;
@@ -627,14 +659,14 @@ __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductPa
 }
 
 // Both products of a gradient side by side, the points' first.
-template <typename S, typename X>
+template <typename S, typename X, typename T>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void pair_kernel(ProductParams x, ProductParams w, uint32_t groups_x)
 {
     BUFFERS_IN_LDS(S)
     if (blockIdx.x < groups_x)
-        tile_share<S, X, X, false, true, false>(x, blockIdx.x, groups_x, buffers);
+        tile_share<S, X, T, false, true, false>(x, blockIdx.x, groups_x, buffers);
     else
-        tile_share<S, X, X, false, true, true>(w, blockIdx.x - groups_x, gridDim.x - groups_x, buffers);
+        tile_share<S, X, T, false, true, true>(w, blockIdx.x - groups_x, gridDim.x - groups_x, buffers);
 }
 
 // The parts of the sums added up, in their order, and finished; zeros of no parts.
@@ -895,11 +927,49 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackParams p)
     }
 }
 
+// ---- factors in two parts of 16 bits
+
+// v as the sum of two values of bfloat16, to 2^-15 of itself, and a binary16 exactly.
+// Unless v is 0 both have its sign and are not 0 (the high part is the last value
+// before v), and both are v where it is not finite: so their products with an
+// infinite factor, or of an infinite v, are what v's own is.
+__device__ __forceinline__ void two_parts(float v, __bf16& high, __bf16& low)
+{
+    const uint32_t bits = __float_as_uint(v);
+    const bool finite = fabsf(v) < HUGE_VALF;
+    const float h = finite && v != 0.0f ? __uint_as_float((bits - 1) & 0xffff0000u) : v;
+    high = from_f32<__bf16>(h);
+    low = from_f32<__bf16>(finite ? v - h : v);
+}
+
+// A matrix of binary16 as two of bfloat16, `apart` bytes from each other.
+__global__ __launch_bounds__(kThreads) void part_kernel(PackParams p, uint64_t apart)
+{
+    constexpr int N = 8;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x; i < p.pieces;
+         i += static_cast<uint64_t>(gridDim.x) * kThreads) {
+        const uint64_t row = p.pieces >> 32 ? i / p.per_row : static_cast<uint32_t>(i) / p.per_row;
+        const uint32_t col = static_cast<uint32_t>(i - row * p.per_row) * N;
+        float v[N];
+        load_inside<_Float16, N>(static_cast<const _Float16*>(p.from) + row * p.stride + col, p.cols - col, v);
+        __bf16 high[N], low[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            two_parts(v[k], high[k], low[k]);
+        uint4 piece;
+        __builtin_memcpy(&piece, high, 16);
+        *reinterpret_cast<uint4*>(p.to + i * 16) = piece;
+        __builtin_memcpy(&piece, low, 16);
+        *reinterpret_cast<uint4*>(p.to + apart + i * 16) = piece;
+    }
+}
+
 // ---- the gradient before a layer's activation, and its sums
 
 struct SlopeParams {
     const void *grad, *pre;      // pre: null without an activation
-    void* dz;                    // [points][pitch] of the factors' type, zeros past the units, or null
+    void* dz;                    // [points][pitch] of the products' type, zeros past the units, or null
+    uint64_t apart;              // bytes to its low parts
     float* sums;                 // [groups down][units] or null
     void* bias;                  // the sums themselves, where there is one group
     int32_t bias_dtype;
@@ -919,10 +989,12 @@ __device__ __forceinline__ void store_bias(void* out, uint32_t u, float v, int32
         static_cast<__bf16*>(out)[u] = from_f32<__bf16>(v);
 }
 
-template <typename X, typename G>
+// PARTED: dz in two parts of bfloat16.
+template <typename X, typename G, bool PARTED>
 __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
 {
     constexpr int V = 8;
+    typedef std::conditional_t<PARTED, __bf16, X> D;
     __shared__ float part[kThreads][V + 1];
     const uint32_t tx = threadIdx.x & (p.across - 1), ty = threadIdx.x / p.across, down = kThreads / p.across;
     const uint32_t unit = (blockIdx.x * p.across + tx) * V;
@@ -962,8 +1034,24 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeParams p)
                     apply_mask<V>(p.mask, key, at, unit, 1.0f, v);
                 if (p.pre)
                     times_slope<V>(p.act, z, v);
-                if (p.dz)
-                    store_values<X, V>(static_cast<X*>(p.dz) + at * p.pitch + unit, WHOLE ? V : p.pitch - unit, v);
+                if (p.dz) {
+                    D* to = static_cast<D*>(p.dz) + at * p.pitch + unit;
+                    const uint32_t room = WHOLE ? V : p.pitch - unit;
+                    if constexpr (PARTED) {
+                        float high[V], low[V];
+#pragma unroll
+                        for (int k = 0; k < V; ++k) {
+                            D h, l;
+                            two_parts(v[k], h, l);
+                            high[k] = to_f32(h);
+                            low[k] = to_f32(l);
+                        }
+                        store_values<D, V>(to, room, high);
+                        store_values<D, V>(to + p.apart / sizeof(D), room, low);
+                    } else {
+                        store_values<D, V>(to, room, v);
+                    }
+                }
 #pragma unroll
                 for (int k = 0; k < V; ++k)
                     sum[k] += v[k];
@@ -1121,8 +1209,10 @@ struct NarrowParams {
     const void* pre;             // or null
     uint64_t pre_pitch;          // bytes
     void* dz;                    // [points][dz_pitch elements], or null
+    uint64_t dz_apart;           // bytes to its low parts
     float* sums;                 // [gridDim.x][sum], or null
     uint32_t sum, dz_pitch, act;
+    uint32_t parted;             // bfloat16 with pre: dz's low parts, where pre's rows were, multiply too
     Mask mask;                   // its scale is the finish's
 };
 
@@ -1317,11 +1407,26 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
                 sum[k] += v[k];
                 e[k] = from_f32<X>(v[k]);
             }
+            X low[N];
+            if constexpr (std::is_same_v<X, __bf16>)
+                if (p.parted)
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        two_parts(v[k], e[k], low[k]);
             uint4 whole;
             __builtin_memcpy(&whole, e, 16);
             *reinterpret_cast<uint4*>(at) = whole;
-            if (p.dz && point < p.points && of_unit < p.dz_pitch)
-                *reinterpret_cast<uint4*>(static_cast<X*>(p.dz) + point * p.dz_pitch + of_unit) = whole;
+            char* to = p.dz && point < p.points && of_unit < p.dz_pitch
+                ? reinterpret_cast<char*>(static_cast<X*>(p.dz) + point * p.dz_pitch + of_unit) : nullptr;
+            if (to)
+                *reinterpret_cast<uint4*>(to) = whole;
+            if constexpr (std::is_same_v<X, __bf16>)
+                if (p.parted) {
+                    __builtin_memcpy(&whole, low, 16);
+                    *reinterpret_cast<uint4*>(at + S::ROWS) = whole;
+                    if (to)
+                        *reinterpret_cast<uint4*>(to + p.dz_apart) = whole;
+                }
         }
     };
     auto work = [&](uint32_t nth, char* buffer) {
@@ -1341,6 +1446,15 @@ __global__ __launch_bounds__(S::THREADS + 64 * S::BRINGERS) void narrow_kernel(N
             for (int e = 0; e < (sizeof(X) == 4 ? 4 : 1); ++e)
                 acc[(k + e) & 1] = multiply<X>(w[k], q, e, acc[(k + e) & 1]);
         }
+        // (one loop for both, as a function of the rows, spilled registers)
+        if constexpr (S::SLOPE && std::is_same_v<X, __bf16>)
+            if (p.parted) {
+#pragma unroll
+                for (int k = 0; k < S::STEPS * kDepths; ++k) {
+                    const uint4 q = read_q.read(buffer + S::ROWS + k / kDepths * S::STEP, 0, k % kDepths);
+                    acc[k & 1] = multiply<X>(w[k], q, 0, acc[k & 1]);
+                }
+            }
         acc[0] += acc[1];
         const uint64_t row0 = (blockIdx.x + static_cast<uint64_t>(nth) * gridDim.x) * S::POINTS + 32 * sub + lane / RUNS;
         Raw<T, V> residual[ROUNDS];
@@ -1510,13 +1624,15 @@ uint32_t launch_sloped_steps(const NarrowParams& p, bool wide, hipStream_t strea
 // The groups of sums.
 template <typename X>
 uint32_t launch_sloped(const sqn_matrix& w, const sqn_matrix& grad, const sqn_matrix* pre, int32_t act, const Mask& m, void* dz,
-                       int64_t dz_pitch, float* sums, const Finish& f, hipStream_t stream)
+                       int64_t dz_pitch, uint64_t dz_apart, bool parted, float* sums, const Finish& f, hipStream_t stream)
 {
     NarrowParams p = narrow_params(w, grad, f);
     p.pre = pre ? pre->data : nullptr;
     p.pre_pitch = pre ? static_cast<uint64_t>(pre->row_stride) * sizeof(X) : 0;
     p.dz = dz;
     p.dz_pitch = static_cast<uint32_t>(dz_pitch);
+    p.dz_apart = dz_apart;
+    p.parted = parted ? 1 : 0;
     p.sums = sums;
     p.sum = static_cast<uint32_t>(w.rows);
     p.act = static_cast<uint32_t>(act);
@@ -1534,14 +1650,14 @@ Operand along(const sqn_matrix& m)
 {
     const int64_t size = static_cast<int64_t>(element_size(m.dtype));
     return {static_cast<const char*>(m.data), static_cast<uint64_t>(m.row_stride * size), static_cast<uint32_t>(m.rows),
-            static_cast<uint32_t>(m.cols * size)};
+            static_cast<uint32_t>(m.cols * size), 0, 0};
 }
 
 Operand across(const sqn_matrix& m)
 {
     const int64_t size = static_cast<int64_t>(element_size(m.dtype));
     return {static_cast<const char*>(m.data), static_cast<uint64_t>(m.row_stride * size), static_cast<uint32_t>(m.cols),
-            static_cast<uint32_t>(m.rows)};
+            static_cast<uint32_t>(m.rows), 0, 0};
 }
 
 // Tiles and parts of a product's sum.
@@ -1567,14 +1683,14 @@ constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79, 7.2}}, kEnds[3]
 // 8192 of 1024 by 1024 33, 23 and 36; of binary32: 65,536 of 256 by 256 84, 75 and 80;
 // 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and 16, 17 points of 4096 by
 // 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384 points 58, 20 and 14.)
-Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t only = 0)
+Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t terms = 1, int64_t only = 0)
 {
     constexpr int64_t kMostParts = 64;
     constexpr double kAlone = 0.12;      // a step in tiles of 128 takes more without another workgroup beside it
     constexpr double kJoin = 4.0, kJoinBytes = 3.5e6;            // a us
     const int f32 = dtype == SQN_F32 ? 1 : 0;
     const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
-    const int64_t steps = (sum + step - 1) / step;
+    const int64_t steps = (sum + step - 1) / step * terms;
     Plan r{64, steps, std::max<int64_t>(1, steps), steps ? 1 : 0, 0, HUGE_VAL, 0.0};
     for (int s = 0; steps && s < 3; ++s) {
         if (only && kSides[s] != only)
@@ -1633,16 +1749,16 @@ struct GradientPlan {
     Plan x, w;
     bool pair;
 
-    GradientPlan(int64_t points, int64_t cols, int64_t units, int32_t dtype)
-        : x(plan_of(cols, points, units, dtype)), w(plan_of(cols, units, points, dtype)), pair(false)
+    GradientPlan(int64_t points, int64_t cols, int64_t units, int32_t dtype, int64_t terms)
+        : x(plan_of(cols, points, units, dtype, terms)), w(plan_of(cols, units, points, dtype, terms)), pair(false)
     {
         constexpr double kLaunch = 3.0;
         double least = x.time + w.time + kLaunch;
         const Plan *best_x = nullptr, *best_w = nullptr;
         Plan of_x[2], of_w[2];
         for (int k = 0; points && k < 2; ++k) {
-            of_x[k] = plan_of(cols, points, units, dtype, 64 << k);
-            of_w[k] = plan_of(cols, units, points, dtype, 64 << k);
+            of_x[k] = plan_of(cols, points, units, dtype, terms, 64 << k);
+            of_w[k] = plan_of(cols, units, points, dtype, terms, 64 << k);
             const double time = std::max({of_x[k].time, of_w[k].time, of_x[k].work + of_w[k].work});
             if (time < least) {
                 least = time;
@@ -1659,7 +1775,8 @@ struct GradientPlan {
 };
 
 // A product of `rows` rows of C; `partial` holds the plan's bytes.
-ProductParams product_of(const Operand& a, const Operand& b, int64_t rows, const Plan& plan, const Finish& f, char* partial)
+ProductParams product_of(const Operand& a, const Operand& b, int64_t rows, const Plan& plan, const Finish& f, char* partial,
+                         uint32_t terms = 1)
 {
     ProductParams p{};
     p.p = a;
@@ -1670,6 +1787,7 @@ ProductParams product_of(const Operand& a, const Operand& b, int64_t rows, const
     p.steps = static_cast<uint32_t>(plan.steps);
     p.part_steps = static_cast<uint32_t>(plan.part_steps);
     p.parts = static_cast<uint32_t>(plan.parts);
+    p.terms = Terms(terms);
     p.partial = reinterpret_cast<float*>(partial);
     p.partial_pitch = static_cast<uint32_t>(round_up(f.units, 4));
     p.f = f;
@@ -1712,14 +1830,14 @@ void launch_tiles(const ProductParams& p, int64_t side, hipStream_t stream)
         tile_kernel<Shape<64>, X, T, LAYER, PA, QA><<<groups, Shape<64>::THREADS, 0, stream>>>(p);
 }
 
-template <typename X>
+template <typename X, typename T>
 void launch_pair(const ProductParams& x, const ProductParams& w, int64_t side, hipStream_t stream)
 {
     const uint32_t of_x = groups_of(x), groups = of_x + groups_of(w);
     if (side == 128)
-        pair_kernel<Shape<128>, X><<<groups, Shape<128>::THREADS, 0, stream>>>(x, w, of_x);
+        pair_kernel<Shape<128>, X, T><<<groups, Shape<128>::THREADS, 0, stream>>>(x, w, of_x);
     else
-        pair_kernel<Shape<64>, X><<<groups, Shape<64>::THREADS, 0, stream>>>(x, w, of_x);
+        pair_kernel<Shape<64>, X, T><<<groups, Shape<64>::THREADS, 0, stream>>>(x, w, of_x);
 }
 
 template <typename X, typename T>
@@ -1766,42 +1884,125 @@ struct SlopePlan {
     }
 };
 
+// Terms of a gradient's products.  dz = D(grad) act'(z) is as good as the factors'
+// type for one where it is grad's own values and zeros; else 16 bits would lose digits
+// of binary32 that the sums keep (bfloat16: 2.3e-3 of a gradient's norm for its own
+// rounding's 1.7e-3), and binary16 values out of its range.  It is held in two parts
+// of bfloat16 then, to 2^-15 of itself and in binary32's range.  Against bfloat16
+// factors that makes two terms; against binary16 ones, two parts of bfloat16
+// themselves, three: low by low, 2^-14 of a product at most, is left out.
+constexpr uint32_t kLowOfDz = 2, kLowOfFactor = 4;       // the terms that take them: dz's second, the factor's third
+
+uint32_t terms_of(int32_t act, int32_t grad_dtype, int32_t dtype)
+{
+    if (dtype == SQN_F32 || (act <= SQN_ACT_RELU && grad_dtype == dtype))
+        return 1;
+    return dtype == SQN_BF16 ? 2 : 3;
+}
+
+// The other factor of a product in `terms`: as it lies, packed or in parts.
+size_t factor_bytes(const sqn_matrix& m, uint32_t terms)
+{
+    return terms == 3 ? 2 * aligned(static_cast<size_t>(m.rows) * packed_cols(m) * 2) : pack_bytes(m);
+}
+
+Operand factor_across(const sqn_matrix& m, uint32_t terms, char*& to, hipStream_t stream)
+{
+    if (terms != 3)
+        return across(packed(m, to, stream));
+    sqn_matrix c = m;
+    c.data = to;
+    c.dtype = SQN_BF16;
+    c.cols = c.row_stride = packed_cols(m);
+    Operand o = across(c);
+    o.apart = factor_bytes(m, terms) / 2;
+    o.low = kLowOfFactor;
+    to += factor_bytes(m, terms);
+    if (m.rows == 0)
+        return o;
+    PackParams p;
+    p.from = m.data;
+    p.to = static_cast<char*>(c.data);
+    p.stride = m.row_stride;
+    p.cols = static_cast<uint32_t>(m.cols);
+    p.per_row = static_cast<uint32_t>(c.cols / 8);
+    p.pieces = static_cast<uint64_t>(m.rows) * p.per_row;
+    part_kernel<<<groups_of(p.pieces), kThreads, 0, stream>>>(p, o.apart);
+    return o;
+}
+
 // What a gradient keeps in its workspace, in this order.
 struct GradientScratch {
+    uint32_t terms;
     bool own_dz;                 // grad is dz as it lies otherwise
+    bool narrow;                 // the points' gradient of a narrow layer
     size_t dz, sums, x, w, partial_x, partial_w;
+    size_t dz_apart;             // bytes of dz to its low parts
     bool pair;                   // both products in one launch
     Plan plan_x, plan_w;
 
-    GradientScratch(const sqn_matrix& grad, const sqn_matrix& x_, const sqn_matrix& w_, bool slopes, bool for_x, bool for_w, bool for_bias)
+    GradientScratch(const sqn_matrix& grad, const sqn_matrix& x_, const sqn_matrix& w_, int32_t act, bool masked, bool for_x, bool for_w,
+                    bool for_bias)
     {
         const int64_t points = x_.rows, units = w_.rows;
-        own_dz = (for_x || for_w) && (slopes || grad.dtype != x_.dtype || !in_place(grad));
+        terms = terms_of(act, grad.dtype, x_.dtype);
+        own_dz = (for_x || for_w) && (act != SQN_ACT_NONE || masked || grad.dtype != x_.dtype || !in_place(grad));
         const int64_t piece = kSlot / static_cast<int64_t>(element_size(x_.dtype));
-        dz = own_dz ? aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype)) : 0;
-        const bool narrow = narrow_of(w_, x_.cols, units, points, true);
-        // whether narrow layers' slopes are apart goes by pre's alignment too
-        const uint32_t groups = std::max(SlopePlan(points, units).groups, for_x && narrow ? kSlopedGroups : 0);
+        dz_apart = aligned(static_cast<size_t>(points) * round_up(units, piece) * element_size(x_.dtype));
+        dz = own_dz ? (terms > 1 ? 2 : 1) * dz_apart : 0;
+        // dz in parts is multiplied in narrow kernels where it is made, and whether that
+        // is so goes by pre's alignment too: there is room for either way
+        narrow = for_x && terms < 3 && narrow_of(w_, x_.cols, units, points, true);
+        const bool tiles = for_x && (!narrow || terms == 2);
+        const uint32_t groups = std::max(SlopePlan(points, units).groups, narrow ? kSlopedGroups : 0);
         sums = for_bias && groups > 1 ? aligned(static_cast<size_t>(groups) * units * 4) : 0;
-        x = for_w ? pack_bytes(x_) : 0;
-        w = for_x && !narrow ? pack_bytes(w_) : 0;
-        const GradientPlan plan(points, x_.cols, units, x_.dtype);
+        x = for_w ? factor_bytes(x_, terms) : 0;
+        w = tiles ? factor_bytes(w_, terms) : 0;
+        const GradientPlan plan(points, x_.cols, units, x_.dtype, terms);
         pair = plan.pair && for_x && for_w && !narrow;
-        plan_x = pair ? plan.x : plan_of(x_.cols, points, units, x_.dtype);
-        plan_w = pair ? plan.w : plan_of(x_.cols, units, points, x_.dtype);
-        partial_x = for_x && !narrow ? plan_x.bytes : 0;
+        plan_x = pair ? plan.x : plan_of(x_.cols, points, units, x_.dtype, terms);
+        plan_w = pair ? plan.w : plan_of(x_.cols, units, points, x_.dtype, terms);
+        partial_x = tiles ? plan_x.bytes : 0;
         partial_w = for_w ? plan_w.bytes : 0;
     }
 
     size_t bytes() const { return dz + sums + x + w + partial_x + partial_w; }
 };
 
+// The products of a gradient that tiles compute, from factors of type X.
+template <typename X, typename T>
+void launch_products(const ProductParams* of_x, const ProductParams* of_w, const GradientScratch& scratch, hipStream_t stream)
+{
+    if (of_x && of_w && scratch.pair) {
+        launch_pair<X, T>(*of_x, *of_w, scratch.plan_w.side, stream);
+        return;
+    }
+    if (of_x)
+        launch_tiles<X, T, false, true, false>(*of_x, scratch.plan_x.side, stream);
+    if (of_w)
+        launch_tiles<X, T, false, true, true>(*of_w, scratch.plan_w.side, stream);
+}
+
+template <typename X>
+void launch_slopes(const SlopeParams& p, bool grad_f32, bool parted, const dim3& grid, hipStream_t stream)
+{
+    if constexpr (sizeof(X) == 4)
+        slope_kernel<X, X, false><<<grid, kThreads, 0, stream>>>(p);
+    else if (grad_f32)
+        slope_kernel<X, float, true><<<grid, kThreads, 0, stream>>>(p);
+    else if (parted)
+        slope_kernel<X, X, true><<<grid, kThreads, 0, stream>>>(p);
+    else
+        slope_kernel<X, X, false><<<grid, kThreads, 0, stream>>>(p);
+}
+
 template <typename X>
 hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre,
                                  int32_t act, const sqn_dropout_mask* mask, const LayerGradients& to, void* workspace,
                                  hipStream_t stream)
 {
-    const GradientScratch scratch(grad, x, w, pre || (mask && mask->p != 0.0), to.x, to.w, to.bias);
+    const GradientScratch scratch(grad, x, w, act, mask && mask->p != 0.0, to.x, to.w, to.bias);
+    const uint32_t terms = scratch.terms;
     char* work = static_cast<char*>(workspace);
     const int64_t points = x.rows, units = w.rows;
     const Mask m = mask_of(mask, units);
@@ -1812,7 +2013,7 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
     work += scratch.sums;
     if (scratch.own_dz) {
         dz.data = dz_at;
-        dz.dtype = x.dtype;
+        dz.dtype = terms == 3 ? SQN_BF16 : x.dtype;
         dz.cols = dz.row_stride = round_up(units, Elements<X>::PIECE);
     }
     Finish f{};
@@ -1824,10 +2025,10 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
     }
     const SlopePlan plan(points, units);
     uint32_t groups = plan.groups;       // of the bias's sums
-    const bool sloped = to.x && (scratch.own_dz || to.bias) && narrow_sloped(grad, x, w, pre);
+    const bool sloped = scratch.narrow && (scratch.own_dz || to.bias) && narrow_sloped(grad, x, w, pre);
     if (sloped) {
-        groups = launch_sloped<X>(w, grad, pre, act, m, scratch.own_dz && to.w ? dz.data : nullptr, dz.cols,
-                                  to.bias ? sums : nullptr, f, stream);
+        groups = launch_sloped<X>(w, grad, pre, act, m, scratch.own_dz && to.w ? dz.data : nullptr, dz.cols, scratch.dz_apart,
+                                  terms == 2, to.bias ? sums : nullptr, f, stream);
     } else if (points && (scratch.own_dz || to.bias)) {
         SlopeParams p{};
         p.grad = grad.data;
@@ -1835,6 +2036,7 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         p.pre = pre ? pre->data : nullptr;
         p.pre_stride = pre ? pre->row_stride : 0;
         p.dz = scratch.own_dz ? dz.data : nullptr;
+        p.apart = scratch.dz_apart;
         p.sums = sums;
         p.points = static_cast<uint32_t>(points);
         p.units = static_cast<uint32_t>(units);
@@ -1848,36 +2050,43 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         p.act = static_cast<uint32_t>(act);
         p.mask = m;
         const dim3 grid(((p.pitch + 7) / 8 + p.across - 1) / p.across, plan.groups);
-        if (grad.dtype == SQN_F32)
-            slope_kernel<X, float><<<grid, kThreads, 0, stream>>>(p);
-        else
-            slope_kernel<X, X><<<grid, kThreads, 0, stream>>>(p);
+        launch_slopes<X>(p, grad.dtype == SQN_F32, terms > 1, grid, stream);
     }
+    auto parted = [&](Operand o) {
+        o.apart = scratch.dz_apart;
+        o.low = terms > 1 ? kLowOfDz : 0;
+        return o;
+    };
     ProductParams of_x{}, of_w{};
     PartsParams left_x{}, left_w{};
     left_x.parts = left_w.parts = 1;     // nothing
+    bool tiles_x = false;
     if (sloped) {
         // the points' gradient came with dz
-    } else if (to.x && narrow_of(w, x.cols, units, points, true)) {
+    } else if (scratch.narrow && terms == 1) {
         launch_narrow<X, X, false, true>(w, dz, units, f, work, stream);
     } else if (to.x && points) {
-        const sqn_matrix a = packed(w, work, stream);
-        of_x = product_of(across(a), along(dz), points, scratch.plan_x, f, work);
+        tiles_x = true;
+        const Operand a = factor_across(w, terms, work, stream);
+        of_x = product_of(a, parted(along(dz)), points, scratch.plan_x, f, work, terms);
         work += scratch.partial_x;
         left_x = parts_of(of_x);
-        if (!scratch.pair)
-            launch_tiles<X, X, false, true, false>(of_x, scratch.plan_x.side, stream);
     }
     if (to.w) {
-        const sqn_matrix a = packed(x, work, stream);
+        const Operand a = factor_across(x, terms, work, stream);
         f.out = to.w->data;
         f.out_stride = to.w->row_stride;
-        of_w = product_of(across(a), across(dz), units, scratch.plan_w, f, work);
+        of_w = product_of(a, parted(across(dz)), units, scratch.plan_w, f, work, terms);
         left_w = parts_of(of_w);
-        if (scratch.pair)
-            launch_pair<X>(of_x, of_w, scratch.plan_w.side, stream);
+    }
+    const ProductParams *const dx = tiles_x ? &of_x : nullptr, *const dw = to.w ? &of_w : nullptr;
+    if constexpr (std::is_same_v<X, _Float16>) {
+        if (terms > 1)
+            launch_products<__bf16, X>(dx, dw, scratch, stream);
         else
-            launch_tiles<X, X, false, true, true>(of_w, scratch.plan_w.side, stream);
+            launch_products<X, X>(dx, dw, scratch, stream);
+    } else {
+        launch_products<X, X>(dx, dw, scratch, stream);
     }
     // the bias's sums of one group have been added up, of none they are zeros
     const BiasParams bias = {sums, to.bias, groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
@@ -1932,10 +2141,10 @@ hipError_t launch_layer(const sqn_matrix& x, const sqn_matrix& w, const sqn_epil
     return hipGetLastError();
 }
 
-size_t layer_gradient_bytes(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, bool slopes, bool for_x, bool for_w,
-                            bool for_bias)
+size_t layer_gradient_bytes(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, int32_t act, bool masked, bool for_x,
+                            bool for_w, bool for_bias)
 {
-    return GradientScratch(grad, x, w, slopes, for_x, for_w, for_bias).bytes();
+    return GradientScratch(grad, x, w, act, masked, for_x, for_w, for_bias).bytes();
 }
 
 hipError_t launch_layer_gradient(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre,

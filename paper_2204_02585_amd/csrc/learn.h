@@ -57,9 +57,8 @@ struct LayerGradients {
     void* bias;
     int32_t bias_dtype;
 };
-// slopes: an activation or a mask stands between grad and dz.
-size_t layer_gradient_bytes(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, bool slopes, bool for_x, bool for_w,
-                            bool for_bias);
+size_t layer_gradient_bytes(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, int32_t act, bool masked, bool for_x,
+                            bool for_w, bool for_bias);
 hipError_t launch_layer_gradient(const sqn_matrix& grad, const sqn_matrix& x, const sqn_matrix& w, const sqn_matrix* pre,
                                  int32_t activation, const sqn_dropout_mask* mask, const LayerGradients& to, void* workspace,
                                  hipStream_t stream);

@@ -355,10 +355,7 @@ bool plain_factors(const sqn_matrix* x, const sqn_matrix* w)
     return plain_sizes(x) && plain_sizes(w) && w->rows >= 1 && w->rows <= kMaxCols && w->cols == x->cols && w->dtype == x->dtype;
 }
 
-bool has_slopes(int32_t activation, const sqn_dropout_mask* mask)
-{
-    return activation != SQN_ACT_NONE || (mask && mask->p != 0.0);
-}
+bool masks(const sqn_dropout_mask* mask) { return mask && mask->p != 0.0; }
 
 sqn_status launched(hipError_t e, const char* what)
 {
@@ -615,7 +612,7 @@ size_t sqn_layer_gradient_workspace(const sqn_matrix* grad, const sqn_matrix* x,
 {
     if (!plain_sizes(grad) || !plain_factors(x, w))
         return 0;
-    return sqn::layer_gradient_bytes(*grad, *x, *w, has_slopes(activation, mask), for_x != 0, for_w != 0, for_bias != 0);
+    return sqn::layer_gradient_bytes(*grad, *x, *w, activation, masks(mask), for_x != 0, for_w != 0, for_bias != 0);
 }
 
 sqn_status sqn_layer_gradient(const sqn_matrix* grad, const sqn_matrix* x, const sqn_matrix* w, const sqn_matrix* pre,
@@ -654,7 +651,7 @@ sqn_status sqn_layer_gradient(const sqn_matrix* grad, const sqn_matrix* x, const
     if (!grad_x && !grad_w && !grad_bias)
         return SQN_OK;
     if ((s = check_workspace(workspace, workspace_bytes,
-                             sqn::layer_gradient_bytes(*grad, *x, *w, has_slopes(activation, mask), grad_x != nullptr,
+                             sqn::layer_gradient_bytes(*grad, *x, *w, activation, masks(mask), grad_x != nullptr,
                                                        grad_w != nullptr, grad_bias != nullptr))) != SQN_OK)
         return s;
     const sqn::LayerGradients to = {grad_x, grad_w, grad_bias, bias_dtype};

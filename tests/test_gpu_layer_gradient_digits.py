@@ -1,0 +1,212 @@
+"""How many digits a layer's gradients keep: dz = D(grad) act'(z) is not held in
+fewer than the sums need, whatever the factors' type, nor in a smaller range."""
+import numpy as np
+import pytest
+import torch
+
+from tests import layer_util as U
+from tests.test_gpu_layer import draw, inputs
+
+pytestmark = pytest.mark.gpu
+
+HALVES = [torch.float16, torch.bfloat16]
+# what dz in two parts, and a product's term left out, may be off by, relative to a
+# term: the low part is at most a step of bfloat16, 2^-7, and rounded by half a step of
+# itself, 2^-8; low by low, 2^-7 twice, is left out where the other factor has two parts
+PARTS = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -15, torch.float16: 2.0 ** -15 + 2.0 ** -14}
+
+
+def slope(z, name):
+    s = torch.sigmoid(z)
+    return {None: lambda: torch.ones_like(z), "relu": lambda: (z > 0).double(), "silu": lambda: s * (1 + z * (1 - s)),
+            "gelu": lambda: torch.special.ndtr(z) + z * torch.exp(-z * z / 2) / (2 * np.pi) ** 0.5}[name]()
+
+
+def want_of(grad, x, w, pre, activation, p, seed):
+    """((dx, bound), (dw, bound), (db, bound)) in 64 bits on the GPU."""
+    share = torch.from_numpy(U.share(*grad.shape, p, seed)).cuda()
+    keep, s = (share > 0).double(), float(share.max()) or 1.0
+    dz = keep * grad.double()
+    off = torch.zeros_like(dz)
+    if activation:
+        z = pre.double()
+        if activation != "relu":
+            off = dz.abs() * 32 * U.F32 * (1 + z.abs())
+        dz = dz * slope(z, activation)
+    split = activation in ("gelu", "silu") or grad.dtype != x.dtype
+    parted = off + (PARTS[x.dtype] if split else 0.0) * (dz.abs() + off)
+    half, tiny = U.UNIT[x.dtype], U.TINY[x.dtype]
+    out = []
+    for a, b, o in ((dz, w.t(), parted), (dz.t(), x.t(), parted.t())):
+        b = b.double().contiguous()
+        a, o = a.contiguous(), o.contiguous()
+        v, size = a @ b.t().contiguous(), a.abs() @ b.abs().t().contiguous()
+        # three terms at most, each of the sum's length
+        far = s * (2 * U.F32 * (3 * a.shape[1] + 8) * 1.01 * size + o @ b.abs().t().contiguous()) + 4 * U.F32 * s * v.abs()
+        out.append((s * v, far + half * (s * v.abs() + far).clamp(min=tiny)))
+    db = s * dz.sum(0)
+    out.append((db, s * (off.sum(0) + 2 * U.F32 * (len(dz) + 8) * dz.abs().sum(0)) + 4 * U.F32 * db.abs()))
+    return out
+
+
+def check(got, want, what=""):
+    for g, (v, bound), name in zip(got, want, ("dx", "dw", "db")):
+        if g is not None:
+            far = (g.double() - v).abs()
+            if g.dtype == torch.float16:
+                # from half a step above its largest value, 65504, on binary16 rounds to infinity
+                far[g.isinf() & (v.abs() + bound >= 65520) & (g.sign() == v.sign())] = 0.0
+            bad = ~(far <= bound)
+            assert not bad.any(), (name, what, int(bad.sum()), bad.nonzero()[0].tolist())
+
+
+#       one token, few points, tiles alone and in one launch, ragged; narrow layers whose slopes are taken on
+#       the way, of up to 128 columns, and of steps of 1, 2 and 4
+SIZES = [(1, 64, 64), (17, 40, 24), (100, 256, 300), (300, 200, 129), (257, 513, 31), (1500, 72, 200), (2000, 64, 8), (16, 130, 1000),
+         (32768, 256, 32), (33001, 136, 128), (40000, 200, 250), (32769, 129, 33), (131072, 64, 64), (16384, 250, 56)]
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("activation", ["gelu", "silu"])
+def test_slopes(dtype, size, activation):
+    """Gradients through an activation are as near to the formula as their own
+    rounding and binary32 sums allow."""
+    from paper_2204_02585_amd import learn
+    x, w, _, grad = inputs(*size, dtype)
+    pre = draw(grad.shape, dtype, torch.Generator().manual_seed(9))
+    for p in (0.0, 0.3):
+        want = want_of(grad, x, w, pre, activation, p, 5)
+        check(learn.layer_gradient(grad, x, w, pre, activation, p, 5), want, p)
+        check(learn.layer_gradient(grad, x, w, pre, activation, p, 5, for_w=False, for_bias=False), want, "dx")
+        check(learn.layer_gradient(grad, x, w, pre, activation, p, 5, for_x=False), want, "dw, db")
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("activation", [None, "relu", "gelu"])
+def test_binary32_gradients(dtype, size, activation):
+    """A gradient that comes in binary32, as a layer's with a binary32 result does,
+    keeps its digits."""
+    from paper_2204_02585_amd import learn
+    x, w, _, _ = inputs(*size, dtype)
+    grad = draw((size[0], size[2]), torch.float32, torch.Generator().manual_seed(8))
+    pre = draw(grad.shape, dtype, torch.Generator().manual_seed(9)) if activation else None
+    check(learn.layer_gradient(grad, x, w, pre, activation, 0.3, 5), want_of(grad, x, w, pre, activation, 0.3, 5))
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("activation", [None, "gelu"])
+@pytest.mark.parametrize("cols,units", [(64, 50), (256, 50), (72, 1)])
+def test_small_binary32_gradients(dtype, activation, cols, units):
+    """The gradient of a mean over many points, far below binary16's smallest value,
+    whose sums over the points are well inside its range; and one far above."""
+    from paper_2204_02585_amd import learn
+    x, w, _, _ = inputs(50000, cols, units, dtype)
+    gen = torch.Generator().manual_seed(8)
+    pre = draw((50000, units), dtype, gen) if activation else None
+    # signs that agree: sums are some thousand times a term
+    x = x.abs()
+    grad = 1e-8 * draw((50000, units), torch.float32, gen).abs()
+    dx, dw, db = learn.layer_gradient(grad, x, w, pre, activation)
+    assert (dw > 0).all() and (db > 0).all()
+    check((dx, dw, db), want_of(grad, x, w, pre, activation, 0.0, 0))
+    grad = 1e7 * draw((50000, units), torch.float32, gen)
+    small = x * 2.0 ** -14, w * 2.0 ** -14
+    got = learn.layer_gradient(grad, *small, pre, activation)
+    # a sum over the points is some sqrt(50000) 1e7 2^-14 = 1.4e5: infinite in binary16 where it is above 65504
+    assert torch.isfinite(got[0]).all() and torch.isfinite(got[2]).all()
+    check(got, want_of(grad, *small, pre, activation, 0.0, 0))
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+def test_autograd_in_binary32(dtype):
+    """A head whose result is binary32, under a mean over many points."""
+    from paper_2204_02585_amd import learn
+    x, w, bias, _ = inputs(40000, 128, 24, dtype)
+    w, bias = w.requires_grad_(), bias.requires_grad_()
+    y = learn.layer(x, w, bias, dtype=torch.float32)
+    (y * y).mean().backward()
+    grad = 2.0 / y.numel() * y.detach()
+    want = want_of(grad, x, w.detach(), None, None, 0.0, 0)
+    # the mean's own backward pass rounds each gradient a few times
+    size = grad.double().abs()
+    far = (0.0, 4 * U.F32 * (size.t().contiguous() @ x.double().abs()), 4 * U.F32 * size.sum(0))
+    check((None, w.grad, bias.grad), [(v, bound + f) for (v, bound), f in zip(want, far)])
+
+
+def test_steep_slopes():
+    """GELU's slope is 1.13 at its most: gradients near binary16's largest value do
+    not become infinite on their way."""
+    from paper_2204_02585_amd import learn
+    x, w, _, grad = inputs(40, 32, 24, torch.float16)
+    grad = torch.full_like(grad, 65504.0)
+    pre = torch.full_like(grad, 1.4)
+    x, w = x * 2.0 ** -9, w * 2.0 ** -9
+    got = learn.layer_gradient(grad, x, w, pre, "gelu")
+    assert all(torch.isfinite(t).all() for t in got)
+    check(got, want_of(grad, x, w, pre, "gelu", 0.0, 0))
+
+
+def same_kind(got, want):
+    """Infinities of one sign and NaN in the same places."""
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    assert torch.equal(got.sign()[want.isinf()].double(), want.sign()[want.isinf()])
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("points", [40, 33000])
+def test_infinities(dtype, points):
+    """Infinite factors and gradients give the infinities that the formula gives, also
+    beside values of few digits, whose parts are not zeros."""
+    from paper_2204_02585_amd import learn
+    inf = float("inf")
+    x, w, _, grad = inputs(points, 136, 24, dtype)
+    grad = 1.0 + grad.abs()
+    # zero and one, at which the slopes have few digits: half, and that of one
+    pre = (torch.arange(24, device="cuda") % 2).to(dtype).expand(points, 24).contiguous()
+    grad[:, :8] = 1.0
+    dz = grad.double() * slope(pre.double(), "silu")
+
+    def check_kinds(grad, x, w, dz):
+        dx, dw, _ = learn.layer_gradient(grad, x, w, pre, "silu")
+        same_kind(dx, dz @ w.double())
+        same_kind(dw, dz.t().contiguous() @ x.double())
+
+    w2 = w.clone()
+    w2[4, 7], w2[9, 8] = inf, -inf
+    check_kinds(grad, x, w2, dz)
+    x2 = x.clone()
+    x2[2, 11], x2[5, 12] = inf, -inf
+    check_kinds(grad, x2, w, dz)
+    grad2, dz2 = grad.clone(), dz.clone()
+    grad2[3, 5] = dz2[3, 5] = inf
+    # factors of few digits, their own parts
+    few = torch.where(w.abs() < 0.1, 0.125, -0.5).to(dtype)
+    check_kinds(grad2, x, few, dz2)
+    check_kinds(grad2, 0.25 * (x > 0).to(dtype) + 0.25, w, dz2)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("points", [40, 33000])
+def test_not_finite(dtype, points):
+    """An infinite or missing gradient makes its own point's and unit's gradients not
+    finite, and no others."""
+    from paper_2204_02585_amd import learn
+    for bad in (float("inf"), float("nan")):
+        x, w, _, grad = inputs(points, 136, 24, dtype)
+        pre = draw(grad.shape, dtype, torch.Generator().manual_seed(9))
+        clean = learn.layer_gradient(grad, x, w, pre, "silu")
+        grad[3, 5] = bad
+        dx, dw, db = learn.layer_gradient(grad, x, w, pre, "silu")
+        assert not torch.isfinite(dx[3]).any() and not torch.isfinite(dw[5]).any() and not torch.isfinite(db[5])
+        points_left, units_left = torch.arange(points) != 3, torch.arange(24) != 5
+        assert torch.equal(dx[points_left], clean[0][points_left]) and torch.equal(dw[units_left], clean[1][units_left])
+        assert torch.equal(db[units_left], clean[2][units_left])
+        # in dropped places nothing is left of them
+        share = U.share(points, 24, 0.5, 3)
+        row, unit = (int(k) for k in np.argwhere(share == 0)[7])
+        x, w, _, grad = inputs(points, 136, 24, dtype)
+        clean = learn.layer_gradient(grad, x, w, pre, "silu", 0.5, 3)
+        grad[row, unit] = bad
+        assert all(torch.equal(a, b) for a, b in zip(learn.layer_gradient(grad, x, w, pre, "silu", 0.5, 3), clean))
