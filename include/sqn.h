@@ -520,7 +520,7 @@ typedef struct {
  * the same mask and no residual it is its own gradient.
  *   residual: x's rows, cols and dtype, or NULL;
  *   out:      x's rows, cols and dtype; may be x's or the residual's own memory
- *             if the layout is the same.
+ *             if the layout is the same, and shares none with them otherwise.
  * Errors: SQN_ERR_INVALID_ARG, SQN_ERR_DEVICE. */
 sqn_status sqn_dropout(const sqn_matrix* x, const sqn_dropout_mask* mask, const sqn_matrix* residual, const sqn_matrix* out,
                        void* stream);
@@ -537,7 +537,8 @@ typedef struct {
     const sqn_dropout_mask* dropout;    /* host, or NULL                                */
     const sqn_matrix* residual;         /* [points][units] of out's dtype, or NULL      */
     const sqn_matrix* pre;              /* out: z, [points][units] of x's dtype, as     */
-                                        /* sqn_layer_gradient takes it, or NULL         */
+                                        /* sqn_layer_gradient takes it, or NULL; memory */
+                                        /* of its own, not out's or the residual's      */
 } sqn_epilogue;
 
 /* A layer: z = x w^T + bias, out = D(act(z)) + residual, [points][units], with
@@ -546,7 +547,8 @@ typedef struct {
  * strides and alignments choose the kernel and with it the order of the sums.
  * points >= 0, units >= 1.
  *   epilogue:  or NULL for none of it;
- *   out:       may be the residual's own memory if the layout is the same;
+ *   out:       may be the residual's own memory if the layout is the same, and
+ *              shares none with the inputs otherwise;
  *   workspace: sqn_layer_workspace(x, w) bytes, for these sizes, strides and
  *              alignments (copies of factors that do not lie on 16-byte
  *              boundaries, sums in parts).
@@ -569,7 +571,8 @@ size_t sqn_layer_workspace(const sqn_matrix* x, const sqn_matrix* w);
  *   mask:      the layer's, or NULL;
  *   grad_x:    [points][cols] of x's dtype, or NULL;
  *   grad_w:    [units][cols] of w's dtype, or NULL;
- *   grad_bias: device, [units] of bias_dtype (SQN_F32 or x's), or NULL;
+ *   grad_bias: device, [units] of bias_dtype (SQN_F32 or x's), or NULL; each
+ *              of the three has memory of its own;
  *   workspace: sqn_layer_gradient_workspace bytes for the same arguments.
  * Errors: those of sqn_layer (tiles of grad_x and grad_w). */
 sqn_status sqn_layer_gradient(const sqn_matrix* grad, const sqn_matrix* x, const sqn_matrix* w, const sqn_matrix* pre,

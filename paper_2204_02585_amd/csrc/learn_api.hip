@@ -299,6 +299,54 @@ sqn_status check_like(const sqn_matrix* x, int64_t rows, int64_t cols, int32_t d
     return SQN_OK;
 }
 
+// Rows of bytes in memory: of one row where they follow each other without a gap.
+struct Extent {
+    int64_t at;
+    int64_t rows, width, pitch;
+
+    explicit Extent(const sqn_matrix& m)
+        : at(static_cast<int64_t>(reinterpret_cast<intptr_t>(m.data))), rows(m.rows), width(m.cols * size(m)), pitch(m.row_stride * size(m))
+    {
+        if (rows > 1 && pitch <= width) {
+            width += (rows - 1) * pitch;
+            rows = 1;
+        }
+    }
+
+    static int64_t size(const sqn_matrix& m) { return static_cast<int64_t>(element_size(m.dtype)); }
+};
+
+// Whether two matrices have bytes in common; matrices in rows of different pitch,
+// with gaps in both, are taken to have none.
+bool share_memory(const Extent& a, const Extent& b)
+{
+    if (a.rows == 0 || b.rows == 0 || (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch))
+        return false;
+    const int64_t apart = b.at - a.at, pitch = a.rows > 1 ? a.pitch : b.rows > 1 ? b.pitch : 0;
+    if (pitch == 0)
+        return apart < a.width && -apart < b.width;
+    // row i of a meets row j of b where k = i - j has  apart - a.width < k pitch < apart + b.width
+    auto floor = [pitch](int64_t v) { return v / pitch - (v % pitch < 0 ? 1 : 0); };
+    const int64_t least = floor(apart - a.width) + 1, most = floor(apart + b.width - 1);
+    return least <= most && least < a.rows && most > -b.rows;
+}
+
+// `out` has memory of its own beside x; or, where `same`, x's, element by element.
+sqn_status check_apart(const sqn_matrix* out, const char* what, const sqn_matrix* x, const char* other, bool same = false)
+{
+    if (!out || !x || !share_memory(Extent(*out), Extent(*x)))
+        return SQN_OK;
+    if (same && out->data == x->data && out->dtype == x->dtype && (out->rows == 1 || out->row_stride == x->row_stride))
+        return SQN_OK;
+    return fail(SQN_ERR_INVALID_ARG, "%s (%p) overlaps %s (%p)", what, out->data, other, x->data);
+}
+
+// A bias or its gradient as a matrix of one row.
+sqn_matrix row_of(const void* bias, int64_t units, int32_t dtype)
+{
+    return {const_cast<void*>(bias), bias ? 1 : 0, units, units, dtype, 0};
+}
+
 sqn_status check_bias(const void* bias, int32_t dtype, int64_t units, int32_t x_dtype, const char* what)
 {
     if (!bias)
@@ -562,6 +610,10 @@ sqn_status sqn_dropout(const sqn_matrix* x, const sqn_dropout_mask* mask, const 
         return s;
     if ((s = check_like(out, x->rows, x->cols, x->dtype, true, "out")) != SQN_OK)
         return s;
+    if ((s = check_apart(out, "out", x, "x", true)) != SQN_OK)
+        return s;
+    if ((s = check_apart(out, "out", residual, "residual", true)) != SQN_OK)
+        return s;
     if (x->rows == 0)
         return SQN_OK;
     return launched(sqn::launch_dropout(*x, *mask, residual, *out, static_cast<hipStream_t>(stream)), "dropout");
@@ -599,6 +651,19 @@ sqn_status sqn_layer(const sqn_matrix* x, const sqn_matrix* w, const sqn_epilogu
     if (e.residual && (s = check_like(e.residual, x->rows, w->rows, out->dtype, false, "residual")) != SQN_OK)
         return s;
     if (e.pre && (s = check_like(e.pre, x->rows, w->rows, x->dtype, true, "pre")) != SQN_OK)
+        return s;
+    const sqn_matrix bias = row_of(e.bias, w->rows, e.bias_dtype);
+    const struct {
+        const sqn_matrix* out;
+        const char* what;
+        const sqn_matrix* in;
+        const char* other;
+    } pairs[] = {{out, "out", x, "x"}, {out, "out", w, "w"}, {out, "out", &bias, "bias"}, {e.pre, "pre", x, "x"}, {e.pre, "pre", w, "w"},
+                 {e.pre, "pre", &bias, "bias"}, {e.pre, "pre", e.residual, "residual"}, {e.pre, "pre", out, "out"}};
+    for (const auto& p : pairs)
+        if ((s = check_apart(p.out, p.what, p.in, p.other)) != SQN_OK)
+            return s;
+    if ((s = check_apart(out, "out", e.residual, "residual", true)) != SQN_OK)
         return s;
     if (x->rows == 0)
         return SQN_OK;
@@ -650,6 +715,23 @@ sqn_status sqn_layer_gradient(const sqn_matrix* grad, const sqn_matrix* x, const
         return s;
     if (!grad_x && !grad_w && !grad_bias)
         return SQN_OK;
+    const sqn_matrix bias = row_of(grad_bias, w->rows, bias_dtype);
+    const struct {
+        const sqn_matrix* out;
+        const char* what;
+    } outs[] = {{grad_x, "grad_x"}, {grad_w, "grad_w"}, {&bias, "grad_bias"}};
+    const struct {
+        const sqn_matrix* in;
+        const char* what;
+    } ins[] = {{grad, "grad"}, {x, "x"}, {w, "w"}, {pre, "pre"}};
+    for (int k = 0; k < 3; ++k) {
+        for (const auto& in : ins)
+            if ((s = check_apart(outs[k].out, outs[k].what, in.in, in.what)) != SQN_OK)
+                return s;
+        for (int j = 0; j < k; ++j)
+            if ((s = check_apart(outs[k].out, outs[k].what, outs[j].out, outs[j].what)) != SQN_OK)
+                return s;
+    }
     if ((s = check_workspace(workspace, workspace_bytes,
                              sqn::layer_gradient_bytes(*grad, *x, *w, activation, masks(mask), grad_x != nullptr,
                                                        grad_w != nullptr, grad_bias != nullptr))) != SQN_OK)

@@ -552,7 +552,9 @@ def layer(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None,
     is the mask of `dropout`(..., p=dropout, seed=seed, step=step).  Sums and the
     epilogue are float32, rounded once.  Differentiable in x, w, bias and
     residual (without `out`, `pre` and `stream`), by layer_gradient, which takes
-    what `pre` holds: x w^T + bias in x's dtype.  No forward-mode derivative."""
+    what `pre` holds: x w^T + bias in x's dtype.  `out` may be the residual; else
+    `out` and `pre` share no memory with each other and the inputs.  No
+    forward-mode derivative."""
     p = _probability(dropout) if dropout else 0.0
     _no_tangent("layer", x, w, bias, residual)
     if out is None and pre is None and stream is None and _wants_gradient(x, w, bias, residual):
