@@ -1714,9 +1714,9 @@ struct Plan {
 
 int64_t tiles_of(int64_t rows_p, int64_t rows_q, int64_t side) { return (rows_p + side - 1) / side * ((rows_q + side - 1) / side); }
 
-// A step of tiles of 64, 128 and 256 and a tile's start and end, in us.
+// A step of tiles of 64, 128 and 256 (of 16 bits) and a tile's start and end, in us.
 constexpr int64_t kSides[3] = {64, 128, 256}, kCus = 256;
-constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79, 7.2}}, kEnds[3] = {1.5, 3.0, 18.0};
+constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79}}, kEnds[3] = {1.5, 3.0, 18.0};
 
 // Tiles and parts by what they take, in us: the rounds of workgroups on 256 CUs,
 // each the steps of a part and a start and an end, and a launch and the bytes of the
@@ -1724,8 +1724,9 @@ constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79, 7.2}}, kEnds[3]
 // tiles and for binary32, and what L2 and LDS deliver in the smaller ones, of which
 // two workgroups share a CU.  (us by side, 64, 128 and 256, of bfloat16: 4096 points
 // of 256 by 256 5, 7 and 19; 65,536 34, 21 and 25; 2048 of 4096 by 2048 54, 44 and 85;
-// 8192 of 1024 by 1024 33, 23 and 36; of binary32: 65,536 of 256 by 256 84, 75 and 80;
-// 1024 of 4096 by 1024 72, 237 and 919.  By parts, 1, 4 and 16, 17 points of 4096 by
+// 8192 of 1024 by 1024 33, 23 and 36; of binary32: 65,536 of 256 by 256 84, 75 and 80,
+// 1024 of 4096 by 1024 72, 237 and 919: four tiles of 128 never take more than one of
+// 256, whose reads its matrix instructions outweigh.  By parts, 1, 4 and 16, 17 points of 4096 by
 // 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384 points 58, 20 and 14.)
 Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t terms = 1, int64_t only = 0)
 {
@@ -1736,7 +1737,7 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t
     const int64_t step = kStepBytes / static_cast<int64_t>(element_size(dtype));
     const int64_t steps = (sum + step - 1) / step * terms;
     Plan r{64, steps, std::max<int64_t>(1, steps), steps ? 1 : 0, 0, HUGE_VAL, 0.0};
-    for (int s = 0; steps && s < 3; ++s) {
+    for (int s = 0; steps && s < (f32 ? 2 : 3); ++s) {
         if (only && kSides[s] != only)
             continue;
         const int64_t tiles = tiles_of(rows_p, rows_q, kSides[s]);
@@ -1775,10 +1776,9 @@ Plan layer_plan(const Finish& f, int64_t rows, int64_t sum, int32_t dtype)
         return plan;
     constexpr double kCompute = 17.0, kKeep = 11.0, kAdd = 33.0, kBeside = 0.2;     // us of a tile of 256; of that in one of 128
     const double more = kCompute * ((f.act > SQN_ACT_RELU ? 1 : 0) + f.mask.on) + kKeep * (f.pre ? 1 : 0) + kAdd * (f.residual ? 1 : 0);
-    const int f32 = dtype == SQN_F32 ? 1 : 0;
     auto time = [&](int s, double ends) {
         const int64_t rounds = (tiles_of(f.units, rows, kSides[s]) + kCus - 1) / kCus;
-        return rounds * (plan.steps * kStep[f32][s] + kEnds[s] + ends);
+        return rounds * (plan.steps * kStep[0][s] + kEnds[s] + ends);
     };
     if (time(1, kBeside * more) < time(2, more))
         plan.side = 128;
@@ -1866,9 +1866,12 @@ void launch_tiles(const ProductParams& p, int64_t side, hipStream_t stream)
     const uint32_t groups = groups_of(p);
     if (groups == 0)
         return;
-    if (side == 256)
-        tile_kernel<Shape<256>, X, T, LAYER, PA, QA><<<groups, Shape<256>::THREADS, 0, stream>>>(p);
-    else if (side == 128)
+    if constexpr (sizeof(X) == 2)
+        if (side == 256) {
+            tile_kernel<Shape<256>, X, T, LAYER, PA, QA><<<groups, Shape<256>::THREADS, 0, stream>>>(p);
+            return;
+        }
+    if (side == 128)
         tile_kernel<Shape<128>, X, T, LAYER, PA, QA><<<groups, Shape<128>::THREADS, 0, stream>>>(p);
     else
         tile_kernel<Shape<64>, X, T, LAYER, PA, QA><<<groups, Shape<64>::THREADS, 0, stream>>>(p);

@@ -1,8 +1,14 @@
 """Sizes that take tiles of 256, as the choice of kernels has them now: the GPU
 tests of those kernels (tests/test_gpu_layer_widest.py) reach them by these sizes."""
+import os
 import re
+import subprocess
 
+import pytest
+
+from paper_2204_02585_amd import build
 from tests import fake_hip
+from tests.test_build_guard import LLVM, device_code_objects
 from tests.test_layer_cpu import LAYERS
 
 # points, cols, units, ragged at every end; with all of an epilogue, and with what leaves the residual out
@@ -35,3 +41,18 @@ print(json.dumps(out))
     for case, count, names in got:
         tiles = [n for n in names if re.search(r"\d+(tile|pair)_kernel", n)]
         assert len(tiles) == count and all("ShapeILi256E" in n for n in tiles), (case, tiles)
+
+
+@pytest.mark.skipif(not os.path.exists(f"{LLVM}/llvm-readelf"), reason="ROCm llvm tools missing")
+def test_binary32_has_none(tmp_path):
+    """Tiles of 256 are built for factors of 16 bits only: hardly a size chose them in
+    binary32, where four tiles of 128 take no longer than one."""
+    names = set()
+    for k, (_, blob) in enumerate(device_code_objects(build.LIB_PATH, str(tmp_path))):
+        if b"tile_kernel" in blob:
+            path = tmp_path / f"object{k}.o"
+            path.write_bytes(blob)
+            symbols = subprocess.run([f"{LLVM}/llvm-readelf", "--symbols", "--wide", str(path)], check=True, capture_output=True, text=True).stdout
+            names.update(re.findall(r"\S*tile_kernelINS0_5ShapeILi256E\S*", symbols))
+    assert any("ShapeILi256EEEDF16_" in n for n in names)
+    assert not any("ShapeILi256EEEf" in n for n in names), sorted(names)
