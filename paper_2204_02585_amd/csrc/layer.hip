@@ -326,13 +326,11 @@ __device__ __forceinline__ uint32_t across_key(uint32_t k)
         return SIDE >= 128 ? 4 * (k & 3) : 4 * (k >> 1 & 1);
 }
 
-// Whether a product can have factors in parts.
-template <typename X, bool LAYER>
-constexpr bool kParted = !LAYER && sizeof(X) == 2;
-
 // What a lane brings of a factor's steps, through a buffer descriptor of the
 // tile's rows: pieces past the sum's end lie past the descriptor's, and come as
-// zeros without an access.
+// zeros without an access.  PARTED: of a product in terms, whose few scalar operations
+// a step took tiles of 64 a tenth of their time (65,536 points of 256 by 256 in
+// binary16, dw 21.5 us for 19.3).
 template <typename X, int SIDE, int WAVES, bool ACROSS, bool PARTED>
 struct Bringer {
     static constexpr int COUNT = SIDE * static_cast<int>(kStepBytes) / (1024 * WAVES);
@@ -615,15 +613,15 @@ __device__ __forceinline__ void tile_of(uint32_t group, uint32_t groups, uint32_
     tq = band * kBand + in_band - tp * width;
 }
 
-template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
+template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA, bool PARTED>
 __device__ __forceinline__ void tile_share(const ProductParams& p, uint32_t group, uint32_t groups, char* (&buffers)[S::BUFFERS])
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t part, tp, tq;
     tile_of(group, groups, p.tiles_p, p.tiles_q, part, tp, tq);
     const uint32_t p0 = tp * S::SIDE, q0 = tq * S::SIDE;
-    const Bringer<X, S::SIDE, S::WAVES, PA, kParted<X, LAYER>> bring_p(p.p, p0, p.terms);
-    const Bringer<X, S::SIDE, S::WAVES, QA, kParted<X, LAYER>> bring_q(p.q, q0, p.terms);
+    const Bringer<X, S::SIDE, S::WAVES, PA, PARTED> bring_p(p.p, p0, p.terms);
+    const Bringer<X, S::SIDE, S::WAVES, QA, PARTED> bring_q(p.q, q0, p.terms);
     const uint32_t wave_p = (wave & 1) * (S::SIDE / 2), wave_q = (wave >> 1) * (S::SIDE / 2);
     const Reader<X, S::SIDE, PA, S::F> read_p(wave_p);
     const Reader<X, S::SIDE, QA, S::F> read_q(wave_q);
@@ -695,22 +693,22 @@ __device__ __forceinline__ void tile_share(const ProductParams& p, uint32_t grou
     }
 }
 
-template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA>
+template <typename S, typename X, typename T, bool LAYER, bool PA, bool QA, bool PARTED>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void tile_kernel(ProductParams p)
 {
     BUFFERS_IN_LDS(S)
-    tile_share<S, X, T, LAYER, PA, QA>(p, blockIdx.x, gridDim.x, buffers);
+    tile_share<S, X, T, LAYER, PA, QA, PARTED>(p, blockIdx.x, gridDim.x, buffers);
 }
 
 // Both products of a gradient side by side, the points' first.
-template <typename S, typename X, typename T>
+template <typename S, typename X, typename T, bool PARTED>
 __global__ __launch_bounds__(S::THREADS, S::PER_SIMD) void pair_kernel(ProductParams x, ProductParams w, uint32_t groups_x)
 {
     BUFFERS_IN_LDS(S)
     if (blockIdx.x < groups_x)
-        tile_share<S, X, T, false, true, false>(x, blockIdx.x, groups_x, buffers);
+        tile_share<S, X, T, false, true, false, PARTED>(x, blockIdx.x, groups_x, buffers);
     else
-        tile_share<S, X, T, false, true, true>(w, blockIdx.x - groups_x, gridDim.x - groups_x, buffers);
+        tile_share<S, X, T, false, true, true, PARTED>(w, blockIdx.x - groups_x, gridDim.x - groups_x, buffers);
 }
 
 // The parts of the sums added up, in their order, and finished; zeros of no parts.
@@ -1766,9 +1764,10 @@ Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t
 
 // A layer's tiles: an epilogue that computes or moves more than the sums stands alone
 // in tiles of 256 and beside another tile's products in those of 128.  (us in tiles of
-// 128 and 256, 8192 by 8192 outputs in bfloat16: sums of 2048 elements with z kept 288
-// and 272, with GELU and a mask 312 and 324, with a residual 319 and 345; with GELU, a
-// mask and z kept, of 1024 211 and 229, of 2048 324 and 330, of 4096 591 and 546.)
+// 128 and 256, 8192 by 8192 outputs in bfloat16: sums of 2048 elements with z kept 318
+// and 276, with GELU and a mask 304 and 318, with a residual 338 and 357; with GELU, a
+// mask and z kept, of 1024 227 and 238, of 2048 353 and 340 (on another card 324 and
+// 330), of 4096 595 and 547.)
 Plan layer_plan(const Finish& f, int64_t rows, int64_t sum, int32_t dtype)
 {
     Plan plan = plan_of(f.units, rows, sum, dtype);
@@ -1786,9 +1785,10 @@ Plan layer_plan(const Finish& f, int64_t rows, int64_t sum, int32_t dtype)
 }
 
 // Both products of a gradient: in one launch where tiles of one side for both take
-// less than each by itself and a launch between them.  (All of a gradient in bfloat16,
-// so and apart: 1000 points of 512 by 512 17 us and 21, 2048 of 2048 by 2048 49 and 64,
-// 16 of 4096 by 4096 26 and 32.)
+// less than each by itself and a launch between them.  (All of a gradient in bfloat16 in
+// a graph, so and apart: 1000 points of 512 by 512 13 us and 17, 2048 of 2048 by 2048 47
+// and 59, 16 of 4096 by 4096 26 and 28; with SiLU, whose dz has two parts, 21 and 28, 83
+// and 98, 32 and 32.)
 struct GradientPlan {
     Plan x, w;
     bool pair;
@@ -1860,7 +1860,7 @@ PartsParams parts_of(const ProductParams& p)
 
 uint32_t groups_of(const PartsParams& j) { return j.parts == 1 ? 0 : groups_of(j.runs * j.slices); }
 
-template <typename X, typename T, bool LAYER, bool PA, bool QA>
+template <typename X, typename T, bool LAYER, bool PA, bool QA, bool PARTED>
 void launch_tiles(const ProductParams& p, int64_t side, hipStream_t stream)
 {
     const uint32_t groups = groups_of(p);
@@ -1868,23 +1868,23 @@ void launch_tiles(const ProductParams& p, int64_t side, hipStream_t stream)
         return;
     if constexpr (sizeof(X) == 2)
         if (side == 256) {
-            tile_kernel<Shape<256>, X, T, LAYER, PA, QA><<<groups, Shape<256>::THREADS, 0, stream>>>(p);
+            tile_kernel<Shape<256>, X, T, LAYER, PA, QA, PARTED><<<groups, Shape<256>::THREADS, 0, stream>>>(p);
             return;
         }
     if (side == 128)
-        tile_kernel<Shape<128>, X, T, LAYER, PA, QA><<<groups, Shape<128>::THREADS, 0, stream>>>(p);
+        tile_kernel<Shape<128>, X, T, LAYER, PA, QA, PARTED><<<groups, Shape<128>::THREADS, 0, stream>>>(p);
     else
-        tile_kernel<Shape<64>, X, T, LAYER, PA, QA><<<groups, Shape<64>::THREADS, 0, stream>>>(p);
+        tile_kernel<Shape<64>, X, T, LAYER, PA, QA, PARTED><<<groups, Shape<64>::THREADS, 0, stream>>>(p);
 }
 
-template <typename X, typename T>
+template <typename X, typename T, bool PARTED>
 void launch_pair(const ProductParams& x, const ProductParams& w, int64_t side, hipStream_t stream)
 {
     const uint32_t of_x = groups_of(x), groups = of_x + groups_of(w);
     if (side == 128)
-        pair_kernel<Shape<128>, X, T><<<groups, Shape<128>::THREADS, 0, stream>>>(x, w, of_x);
+        pair_kernel<Shape<128>, X, T, PARTED><<<groups, Shape<128>::THREADS, 0, stream>>>(x, w, of_x);
     else
-        pair_kernel<Shape<64>, X, T><<<groups, Shape<64>::THREADS, 0, stream>>>(x, w, of_x);
+        pair_kernel<Shape<64>, X, T, PARTED><<<groups, Shape<64>::THREADS, 0, stream>>>(x, w, of_x);
 }
 
 template <typename X, typename T>
@@ -1901,7 +1901,7 @@ void launch_layer_typed(const sqn_matrix& x, const sqn_matrix& w, const Finish& 
     const sqn_matrix a = packed(w, work, stream), b = packed(x, work, stream);
     const Plan plan = layer_plan(f, x.rows, x.cols, x.dtype);
     const ProductParams p = product_of(along(a), along(b), x.rows, plan, f, work);
-    launch_tiles<X, T, true, false, false>(p, plan.side, stream);
+    launch_tiles<X, T, true, false, false, false>(p, plan.side, stream);
     const PartsParams j = parts_of(p);
     if (j.parts != 1)
         parts_kernel<X, T><<<groups_of(j), kThreads, 0, stream>>>(j);
@@ -2017,17 +2017,17 @@ struct GradientScratch {
 };
 
 // The products of a gradient that tiles compute, from factors of type X.
-template <typename X, typename T>
+template <typename X, typename T, bool PARTED>
 void launch_products(const ProductParams* of_x, const ProductParams* of_w, const GradientScratch& scratch, hipStream_t stream)
 {
     if (of_x && of_w && scratch.pair) {
-        launch_pair<X, T>(*of_x, *of_w, scratch.plan_w.side, stream);
+        launch_pair<X, T, PARTED>(*of_x, *of_w, scratch.plan_w.side, stream);
         return;
     }
     if (of_x)
-        launch_tiles<X, T, false, true, false>(*of_x, scratch.plan_x.side, stream);
+        launch_tiles<X, T, false, true, false, PARTED>(*of_x, scratch.plan_x.side, stream);
     if (of_w)
-        launch_tiles<X, T, false, true, true>(*of_w, scratch.plan_w.side, stream);
+        launch_tiles<X, T, false, true, true, PARTED>(*of_w, scratch.plan_w.side, stream);
 }
 
 template <typename X>
@@ -2127,14 +2127,10 @@ hipError_t launch_gradient_typed(const sqn_matrix& grad, const sqn_matrix& x, co
         left_w = parts_of(of_w);
     }
     const ProductParams *const dx = tiles_x ? &of_x : nullptr, *const dw = to.w ? &of_w : nullptr;
-    if constexpr (std::is_same_v<X, _Float16>) {
-        if (terms > 1)
-            launch_products<__bf16, X>(dx, dw, scratch, stream);
-        else
-            launch_products<X, X>(dx, dw, scratch, stream);
-    } else {
-        launch_products<X, X>(dx, dw, scratch, stream);
-    }
+    if (terms == 1)
+        launch_products<X, X, false>(dx, dw, scratch, stream);
+    else if constexpr (sizeof(X) == 2)
+        launch_products<__bf16, X, true>(dx, dw, scratch, stream);
     // the bias's sums of one group have been added up, of none they are zeros
     const BiasParams bias = {sums, to.bias, groups, static_cast<uint32_t>(units), to.bias_dtype, m.scale};
     const uint32_t bias_groups = to.bias && groups != 1 ? static_cast<uint32_t>((units + kSumUnits - 1) / kSumUnits) : 0;
