@@ -1018,7 +1018,7 @@ struct SlopeParams {
     int64_t grad_stride, pre_stride;
     uint32_t points, units, pitch, rows, act;     // rows: of a workgroup
     uint32_t across;             // threads along a row: a power of two
-    Mask mask;                   // its scale is applied to the products and sums: dz stays in a binary16's range
+    Mask mask;                   // its scale is applied to the products and sums: dz stays in grad's range
 };
 
 __device__ __forceinline__ void store_bias(void* out, uint32_t u, float v, int32_t dtype)
@@ -1724,8 +1724,8 @@ constexpr double kStep[2][3] = {{0.26, 0.46, 1.45}, {0.51, 1.79}}, kEnds[3] = {1
 // of 256 by 256 5, 7 and 19; 65,536 34, 21 and 25; 2048 of 4096 by 2048 54, 44 and 85;
 // 8192 of 1024 by 1024 33, 23 and 36; of binary32: 65,536 of 256 by 256 84, 75 and 80,
 // 1024 of 4096 by 1024 72, 237 and 919: four tiles of 128 never take more than one of
-// 256, whose reads its matrix instructions outweigh.  By parts, 1, 4 and 16, 17 points of 4096 by
-// 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384 points 58, 20 and 14.)
+// 256, whose reads its matrix instructions outweigh.  By parts, 1, 4 and 16, 17 points
+// of 4096 by 4096 16, 10 and 15; a gradient's 256 x 256 over 16,384 points 58, 20 and 14.)
 Plan plan_of(int64_t rows_p, int64_t rows_q, int64_t sum, int32_t dtype, int64_t terms = 1, int64_t only = 0)
 {
     constexpr int64_t kMostParts = 64;

@@ -210,3 +210,61 @@ def test_not_finite(dtype, points):
         clean = learn.layer_gradient(grad, x, w, pre, "silu", 0.5, 3)
         grad[row, unit] = bad
         assert all(torch.equal(a, b) for a, b in zip(learn.layer_gradient(grad, x, w, pre, "silu", 0.5, 3), clean))
+
+
+@pytest.mark.parametrize("dtype,points,cols,units", [(torch.bfloat16, (1 << 21) + 40, 16, 1024), (torch.float16, (1 << 21) + 40, 16, 1024),
+                                                     (torch.bfloat16, (1 << 23) + 40, 200, 256)])
+def test_far_parts(dtype, points, cols, units):
+    """dz of 2^31 elements and more, its low parts 4 GB on and further: the last rows'
+    gradients, in tiles and where slopes are taken on the way."""
+    from paper_2204_02585_amd import learn
+    gen = torch.Generator().manual_seed(7)
+    last = [draw((70, n), dtype, gen) for n in (cols, units, units)]
+    x, grad, pre = (torch.zeros((points, t.shape[1]), dtype=dtype, device="cuda") for t in last)
+    for whole, end in zip((x, grad, pre), last):
+        whole[-70:] = end
+    w = draw((units, cols), dtype, gen, units ** -0.5)
+    dx, dw, db = learn.layer_gradient(grad, x, w, pre, "silu")
+    assert not dx[:-70].any()
+    want = want_of(last[1], last[0], w, last[2], "silu", 0.0, 0)
+    # the sums run over zeros too, three terms of each row
+    size = (last[1].double().abs().t().contiguous() @ last[0].double().abs(), last[1].double().abs().sum(0))
+    far = [2 * U.F32 * (3 * points + 8) * 1.2 * v for v in size]
+    check((dx[-70:], dw, db), [want[0], (want[1][0], want[1][1] + far[0]), (want[2][0], want[2][1] + far[1])])
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("points,cols,units", [(3, 200, 40), (300, 136, 72), (33000, 136, 64)])
+def test_parts_in_a_graph(dtype, points, cols, units):
+    """Captured, and replayed on other values between eager work: the same bits."""
+    from paper_2204_02585_amd import learn
+
+    def values(seed):
+        gen = torch.Generator().manual_seed(seed)
+        return [draw((points, units), torch.float32, gen), draw((points, units), dtype, gen), draw((points, cols), dtype, gen),
+                draw((units, cols), dtype, gen), draw((points, units), dtype, gen)]
+
+    state = values(0)
+
+    def run():
+        wide, grad, x, w, pre = state
+        return (*learn.layer_gradient(wide, x, w, pre, "gelu", 0.2, 3), *learn.layer_gradient(grad, x, w, pre, "silu"),
+                *learn.layer_gradient(wide, x, w))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for k in range(1, 4):
+        for to, v in zip(state, values(k)):
+            to.copy_(v)
+        want = run()
+        torch.cuda.synchronize()
+        for t in got:
+            t.zero_()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
